@@ -1,0 +1,158 @@
+// The 1x1 projection of rows in 8 bits (e4m3): y[n, o] = x_scale[n] w_scale[o] sum_c x8[n, c] w8[o, c].
+//
+// What 8 bits save here is memory; the products run on the fp16 matrix instructions, at the rate that 16x16x32 has for e4m3 as well.  The e4m3
+// form was measured first: its sums keep some 14 bits of their terms' magnitudes (errors of 2^-14.5 of sum |x w| at 16 channels), where fp16
+// operands, which hold every e4m3 value, leave exact products and fp32 sums.  A lane's 16 bytes of a row make two operands, the low and the
+// high eight contraction slots, so both sides are read 16 bytes a lane in memory order.
+#include "msla_device.h"
+#include "msla_sequence_kernels.h"
+
+namespace msla {
+namespace {
+
+constexpr int kTileK = 128;         // bytes of the contraction a stage
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// sixteen e4m3 values as two operands of fp16 (which has every e4m3 value)
+struct Pair { f16x8 v[2]; };
+__device__ __forceinline__ Pair widen(u32x4 b) {
+    Pair p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const f16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b[j], 1.0f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b[j], 1.0f, true);
+        p.v[j / 2][4 * (j % 2)] = lo[0];
+        p.v[j / 2][4 * (j % 2) + 1] = lo[1];
+        p.v[j / 2][4 * (j % 2) + 2] = hi[0];
+        p.v[j / 2][4 * (j % 2) + 3] = hi[1];
+    }
+    return p;
+}
+
+__device__ __forceinline__ f32x4 mma8(f32x4 c, const Pair& a, const Pair& b) {
+    c = Traits<_Float16>::mma_vec(c, a.v[0], b.v[0]);
+    return Traits<_Float16>::mma_vec(c, a.v[1], b.v[1]);
+}
+
+template <class T>
+__device__ __forceinline__ void store8(T* p, const f32x4& a, const f32x4& b) {
+    if constexpr (sizeof(T) == 2) {
+        typename Traits<T>::Vec v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            v[r] = Traits<T>::from_f32(a[r]);
+            v[4 + r] = Traits<T>::from_f32(b[r]);
+        }
+        *(typename Traits<T>::Vec*)p = v;
+    } else {
+        *(f32x4*)p = a;
+        *(f32x4*)(p + 4) = b;
+    }
+}
+
+// A workgroup has 128 rows x 128 outputs, a wave 64 x 64.  Tiles lie in LDS as rows of 128 bytes whose 16-byte pieces are XORed with the
+// row's number modulo 8, which gives the eight rows that a read serves together all banks.  Outputs are the rows of the matrix
+// instructions, dealt to pairs of blocks so that a lane ends up with eight neighbours of a row of y.
+template <class T>
+__global__ void __launch_bounds__(256, 2) linear_quantized_kernel(const unsigned char* x8, const float* x_scale, const unsigned char* w8,
+                                                                  const float* w_scale, T* y, int64_t rows, int c_in, int c_out, int tiles_o) {
+    constexpr int kM = 128, kN = 128, kPieces = (kM + kN) * kTileK / 16 / 256;
+    __shared__ __align__(16) char lds[2][(kM + kN) * kTileK];
+    const int64_t n0 = (int64_t)(blockIdx.x / tiles_o) * kM;
+    const int o0 = blockIdx.x % tiles_o * kN;
+    const int wave = threadIdx.x >> 6, lane = lane_id(), x = lane & 15, q = lane >> 4;
+    const int wn = wave / 2 * 64, wo = wave % 2 * 64;
+    u32x4 hold[kPieces];
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int p = threadIdx.x + i * 256, row = p / 8, c = k0 + p % 8 * 16;
+            hold[i] = u32x4{0, 0, 0, 0};
+            if (row < kM) {
+                if (n0 + row < rows && c < c_in) hold[i] = *(const u32x4*)(x8 + (n0 + row) * c_in + c);
+            } else {
+                if (o0 + row - kM < c_out && c < c_in) hold[i] = *(const u32x4*)(w8 + (int64_t)(o0 + row - kM) * c_in + c);
+            }
+        }
+    };
+    auto park = [&](char* at) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int p = threadIdx.x + i * 256, row = p / 8;
+            *(u32x4*)(at + row * kTileK + ((p % 8) ^ (row & 7)) * 16) = hold[i];
+        }
+    };
+    f32x4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    const int stages = (c_in + kTileK - 1) / kTileK;
+    load(0);
+    for (int s = 0; s < stages; ++s) {
+        char* at = lds[s & 1];
+        park(at);
+        __syncthreads();
+        if (s + 1 < stages) load((s + 1) * kTileK);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            Pair a[4], b[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int ro = kM + wo + 32 * (i / 2) + 8 * (x >> 2) + 4 * (i & 1) + (x & 3), rn = wn + 16 * i + x;
+                a[i] = widen(*(const u32x4*)(at + ro * kTileK + ((4 * h + q) ^ (ro & 7)) * 16));
+                b[i] = widen(*(const u32x4*)(at + rn * kTileK + ((4 * h + q) ^ (rn & 7)) * 16));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = mma8(acc[i][j], a[i], b[j]);
+        }
+        // (one barrier a stage: the buffer that the next stage fills was last read before this stage's barrier)
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t n = n0 + wn + 16 * j + x;
+        if (n >= rows) continue;
+        const float sx = x_scale[n];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int o = o0 + wo + 32 * p + 8 * q;
+            if (o >= c_out) continue;
+            f32x4 lo = acc[2 * p][j], hi = acc[2 * p + 1][j];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                lo[r] *= sx * w_scale[o + r];
+                hi[r] *= sx * w_scale[o + 4 + r];
+            }
+            store8<T>(y + n * c_out + o, lo, hi);
+        }
+    }
+}
+
+template <class T>
+hipError_t linear_of(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows, int c_in, int c_out,
+                     hipStream_t stream) {
+    const int tiles_o = (c_out + 127) / 128;
+    const int64_t blocks = (rows + 127) / 128 * tiles_o;
+    if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((linear_quantized_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, stream, (const unsigned char*)x8, x_scale,
+                       (const unsigned char*)w8, w_scale, (T*)y, rows, c_in, c_out, tiles_o);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int linear_quantized_splits(int64_t, int, int) { return 1; }
+
+hipError_t launch_linear_quantized(int dt, const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, float*, int,
+                                   int64_t rows, int c_in, int c_out, hipStream_t stream) {
+    switch (dt) {
+        case 0: return linear_of<float>(x8, x_scale, w8, w_scale, y, rows, c_in, c_out, stream);
+        case 1: return linear_of<_Float16>(x8, x_scale, w8, w_scale, y, rows, c_in, c_out, stream);
+        case 2: return linear_of<__bf16>(x8, x_scale, w8, w_scale, y, rows, c_in, c_out, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace msla

@@ -1,0 +1,360 @@
+// Root-mean-square norm of rows with the residual's addition, its gradient, and rows into 8 bits (e4m3 with a scale a row).
+//
+// Bound by memory: a row is read once, stays in registers as fp32 through the sum of its squares (and, into 8 bits, its largest
+// magnitude), and is written once.  16 bytes a lane and access, whatever the row's alignment; a ragged end goes by elements.  LPR lanes
+// share a row: few for short rows, so that a wave holds several, a whole workgroup for long ones.
+#include "msla_device.h"
+#include "msla_sequence_kernels.h"
+
+namespace msla {
+namespace {
+
+constexpr float kTop8 = 448.0f;     // the largest e4m3 value
+
+template <class T>
+__device__ __forceinline__ void load_row(const T* p, int at, int channels, float (&f)[Traits<T>::kVec]) {
+    constexpr int kVec = Traits<T>::kVec;
+    if (at + kVec <= channels) {
+        typename Traits<T>::Vec v;
+        __builtin_memcpy(&v, __builtin_assume_aligned(p + at, sizeof(T)), 16);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) f[e] = Traits<T>::to_f32(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) f[e] = at + e < channels ? Traits<T>::to_f32(p[at + e]) : 0.0f;
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void store_row(T* p, int at, int channels, const float (&f)[Traits<T>::kVec]) {
+    constexpr int kVec = Traits<T>::kVec;
+    typename Traits<T>::Vec v;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) v[e] = Traits<T>::from_f32(f[e]);
+    if (at + kVec <= channels) {
+        __builtin_memcpy(__builtin_assume_aligned(p + at, sizeof(T)), &v, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+            if (at + e < channels) p[at + e] = v[e];
+    }
+}
+
+template <int VEC>
+__device__ __forceinline__ void store_row8(unsigned char* p, int at, int channels, const float (&f)[VEC]) {
+    unsigned w[VEC / 4];
+#pragma unroll
+    for (int e = 0; e < VEC / 4; ++e) {
+        int v = 0;
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * e], f[4 * e + 1], v, false);
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * e + 2], f[4 * e + 3], v, true);
+        w[e] = (unsigned)v;
+    }
+    if (at + VEC <= channels) {
+        __builtin_memcpy(__builtin_assume_aligned(p + at, 1), w, VEC);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (at + e < channels) p[at + e] = (unsigned char)(w[e / 4] >> (8 * (e % 4)));
+    }
+}
+
+// over the LPR lanes of a row; `room`: a float a wave
+template <int LPR, class F>
+__device__ __forceinline__ float over_row(float v, float* room, F&& join) {
+    constexpr int kIn = LPR < 64 ? LPR : 64;
+#pragma unroll
+    for (int d = 1; d < kIn; d *= 2) v = join(v, __shfl_xor(v, d));
+    if constexpr (LPR > 64) {
+        constexpr int kWaves = LPR / 64;
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();                // (the room's last readers are through)
+        if ((threadIdx.x & 63) == 0) room[wave] = v;
+        __syncthreads();
+        v = room[0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) v = join(v, room[w]);
+    }
+    return v;
+}
+
+template <class T, int LPR, int PER, bool EIGHT, bool PLAIN>
+__global__ void __launch_bounds__(LPR > 256 ? LPR : 256) norm_kernel(const T* x, const T* residual, const T* weight, void* y, float* scale, T* sum,
+                                                                     int64_t rows, int channels, float eps) {
+    constexpr int kVec = Traits<T>::kVec, kThreads = LPR > 256 ? LPR : 256, kRows = kThreads / LPR;
+    __shared__ float room[kThreads / 64];
+    const int lane = threadIdx.x % LPR;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR;
+    const bool live = row < rows;
+    const int64_t base = (live ? row : 0) * channels;
+    float r[PER][kVec];
+    float squares = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int at = (lane + i * LPR) * kVec;
+        if (live && at < channels) {
+            load_row<T>(x + base, at, channels, r[i]);
+            if (residual != nullptr) {
+                float f[kVec];
+                load_row<T>(residual + base, at, channels, f);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) r[i][e] += f[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) r[i][e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) squares = fmaf(r[i][e], r[i][e], squares);
+    }
+    if constexpr (!PLAIN) {
+        if (sum != nullptr) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int at = (lane + i * LPR) * kVec;
+                if (live && at < channels) store_row<T>(sum + base, at, channels, r[i]);
+            }
+        }
+        squares = over_row<LPR>(squares, room, [](float a, float b) { return a + b; });
+        const float rstd = 1.0f / sqrtf(squares / (float)channels + eps);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = (lane + i * LPR) * kVec;
+            if (at >= channels) continue;
+            float w[kVec];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) w[e] = 1.0f;
+            if (weight != nullptr) load_row<T>(weight, at, channels, w);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) r[i][e] *= rstd * w[e];
+        }
+    }
+    if constexpr (EIGHT) {
+        float top = 0.0f;
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                top = fmaxf(top, fabsf(r[i][e]));
+                odd |= r[i][e] != r[i][e];
+            }
+        if (odd) top = __builtin_nanf("");
+        // (a NaN anywhere makes the row's scale one: fmaxf would drop it)
+        top = over_row<LPR>(top, room, [](float a, float b) { return a != a || b != b ? __builtin_nanf("") : fmaxf(a, b); });
+        // (rows so small that 448 / top has no fp32 value are lifted first; a row of zeros stays one)
+        const float s = top / kTop8, lift = top < 1e-30f ? 0x1p64f : 1.0f, by = top == 0.0f ? 0.0f : kTop8 / (top * lift);
+        if (live && lane == 0) scale[row] = s;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = (lane + i * LPR) * kVec;
+            if (!live || at >= channels) continue;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                const float v = r[i][e] * lift * by;
+                r[i][e] = v > kTop8 ? kTop8 : (v < -kTop8 ? -kTop8 : v);
+            }
+            store_row8<kVec>((unsigned char*)y + base, at, channels, r[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = (lane + i * LPR) * kVec;
+            if (live && at < channels) store_row<T>((T*)y + base, at, channels, r[i]);
+        }
+    }
+}
+
+// A workgroup walks over rows; a lane has the same channels of each, so it sums their part of d_weight in registers.
+template <class T, int LPR, int PER>
+__global__ void __launch_bounds__(LPR > 256 ? LPR : 256) norm_backward_kernel(const T* sum, const T* weight, const T* d_y, const T* d_sum, T* d_r,
+                                                                              float* partials, int64_t rows, int channels, float eps) {
+    constexpr int kVec = Traits<T>::kVec, kThreads = LPR > 256 ? LPR : 256, kRows = kThreads / LPR;
+    __shared__ float room[2][kThreads / 64];
+    __shared__ float groups[kRows > 1 ? kThreads * PER * kVec : 1];
+    const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
+    float w[PER][kVec], dw[PER][kVec];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int at = (lane + i * LPR) * kVec;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            w[i][e] = 1.0f;
+            dw[i][e] = 0.0f;
+        }
+        if (weight != nullptr && at < channels) load_row<T>(weight, at, channels, w[i]);
+    }
+    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < rows; row0 += (int64_t)gridDim.x * kRows) {
+        const bool live = row0 + group < rows;
+        const int64_t base = (live ? row0 + group : 0) * channels;
+        float r[PER][kVec], g[PER][kVec];
+        float squares = 0.0f, along = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = (lane + i * LPR) * kVec;
+            if (live && at < channels) {
+                load_row<T>(sum + base, at, channels, r[i]);
+                load_row<T>(d_y + base, at, channels, g[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) r[i][e] = g[i][e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                squares = fmaf(r[i][e], r[i][e], squares);
+                along = fmaf(r[i][e] * w[i][e], g[i][e], along);
+            }
+        }
+        squares = over_row<LPR>(squares, room[0], [](float a, float b) { return a + b; });
+        along = over_row<LPR>(along, room[1], [](float a, float b) { return a + b; });
+        const float rstd = 1.0f / sqrtf(squares / (float)channels + eps);
+        const float back = along * rstd * rstd / (float)channels;       // of r, in units of rstd
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = (lane + i * LPR) * kVec;
+            if (!live || at >= channels) continue;
+            float d[kVec], past[kVec];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                dw[i][e] = fmaf(g[i][e], r[i][e] * rstd, dw[i][e]);
+                d[e] = rstd * (w[i][e] * g[i][e] - r[i][e] * back);
+            }
+            if (d_sum != nullptr) {
+                load_row<T>(d_sum + base, at, channels, past);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) d[e] += past[e];
+            }
+            store_row<T>(d_r + base, at, channels, d);
+        }
+    }
+    if (partials == nullptr) return;
+    float* out = partials + (int64_t)blockIdx.x * channels;
+    if constexpr (kRows > 1) {
+        constexpr int kWidth = LPR * PER * kVec;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) groups[group * kWidth + (lane + i * LPR) * kVec + e] = dw[i][e];
+        __syncthreads();
+        for (int c = threadIdx.x; c < channels; c += kThreads) {
+            float s = 0.0f;
+#pragma unroll 4
+            for (int k = 0; k < kRows; ++k) s += groups[k * kWidth + c];
+            out[c] = s;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = (lane + i * LPR) * kVec;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (at + e < channels) out[at + e] = dw[i][e];
+        }
+    }
+}
+
+// d_weight = the sum of the workgroups' parts, in an order of its own: 32 channels a workgroup, eight runs of parts, then those.
+__global__ void __launch_bounds__(256) norm_weight_kernel(const float* partials, float* d_weight, int blocks, int channels) {
+    __shared__ float room[8][33];
+    const int c = blockIdx.x * 32 + threadIdx.x % 32, run = threadIdx.x / 32;
+    float s = 0.0f;
+    if (c < channels) {
+#pragma unroll 8
+        for (int b = run; b < blocks; b += 8) s += partials[(int64_t)b * channels + c];
+    }
+    room[run][threadIdx.x % 32] = s;
+    __syncthreads();
+    if (run == 0 && c < channels) {
+#pragma unroll
+        for (int k = 1; k < 8; ++k) s += room[k][threadIdx.x];
+        d_weight[c] = s;
+    }
+}
+
+// Lanes of a row: the fewest that leave each at most two 16-byte pieces, so that short rows share a wave and long ones have a
+// workgroup; 1024 lanes with up to eight pieces take the longest (32768 fp32 channels).
+struct Lanes { int lpr, per; };
+Lanes lanes_for(int channels, int elem) {
+    const int pieces = (channels * elem + 15) / 16;
+    for (int lpr : {4, 16, 64, 256})
+        if (pieces <= lpr) return {lpr, 1};
+        else if (pieces <= 2 * lpr) return {lpr, 2};
+    return {1024, pieces <= 2048 ? 2 : (pieces <= 4096 ? 4 : 8)};
+}
+
+template <class F>
+hipError_t with_lanes(Lanes l, F&& f) {
+    using std::integral_constant;
+    auto per2 = [&](auto lpr) { return l.per == 1 ? f(lpr, integral_constant<int, 1>{}) : f(lpr, integral_constant<int, 2>{}); };
+    switch (l.lpr) {
+        case 4: return per2(integral_constant<int, 4>{});
+        case 16: return per2(integral_constant<int, 16>{});
+        case 64: return per2(integral_constant<int, 64>{});
+        case 256: return per2(integral_constant<int, 256>{});
+    }
+    if (l.per == 2) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    if (l.per == 4) return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+    return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+}
+
+template <class T>
+hipError_t norm_of(const NormCall& c, hipStream_t stream) {
+    return with_lanes(lanes_for(c.channels, sizeof(T)), [&](auto lpr, auto per) {
+        constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value, kThreads = kLpr > 256 ? kLpr : 256, kRows = kThreads / kLpr;
+        const int64_t blocks = (c.rows + kRows - 1) / kRows;
+        if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
+        const dim3 grid((unsigned)blocks), threads(kThreads);
+        const T *x = (const T*)c.x, *res = (const T*)c.residual, *w = (const T*)c.weight;
+        if (c.plain) hipLaunchKernelGGL((norm_kernel<T, kLpr, kPer, true, true>), grid, threads, 0, stream, x, res, w, c.y, c.scale, (T*)c.sum, c.rows, c.channels, c.eps);
+        else if (c.scale) hipLaunchKernelGGL((norm_kernel<T, kLpr, kPer, true, false>), grid, threads, 0, stream, x, res, w, c.y, c.scale, (T*)c.sum, c.rows, c.channels, c.eps);
+        else hipLaunchKernelGGL((norm_kernel<T, kLpr, kPer, false, false>), grid, threads, 0, stream, x, res, w, c.y, c.scale, (T*)c.sum, c.rows, c.channels, c.eps);
+        return hipGetLastError();
+    });
+}
+
+template <class T>
+hipError_t norm_backward_of(const void* sum, const void* weight, const void* d_y, const void* d_sum, void* d_r, float* d_weight, float* partials,
+                            int64_t rows, int channels, float eps, hipStream_t stream) {
+    const int blocks = norm_backward_blocks(rows, channels, sizeof(T));
+    // (no rows: nothing but a d_weight of zeros)
+    hipError_t e = blocks == 0 ? hipSuccess : with_lanes(lanes_for(channels, sizeof(T)), [&](auto lpr, auto per) {
+        constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value, kThreads = kLpr > 256 ? kLpr : 256;
+        hipLaunchKernelGGL((norm_backward_kernel<T, kLpr, kPer>), dim3(blocks), dim3(kThreads), 0, stream, (const T*)sum, (const T*)weight,
+                           (const T*)d_y, (const T*)d_sum, (T*)d_r, d_weight ? partials : nullptr, rows, channels, eps);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess || d_weight == nullptr) return e;
+    hipLaunchKernelGGL(norm_weight_kernel, dim3((channels + 31) / 32), dim3(256), 0, stream, partials, d_weight, blocks, channels);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Workgroups of the backward pass: enough for every compute unit four times over, few enough that their parts of d_weight are little.
+int norm_backward_blocks(int64_t rows, int channels, int elem) {
+    const Lanes l = lanes_for(channels, elem);
+    const int per_block = (l.lpr > 256 ? l.lpr : 256) / l.lpr;
+    const int64_t all = (rows + per_block - 1) / per_block;
+    return (int)(all < 1024 ? all : 1024);
+}
+
+hipError_t launch_norm(int dt, const NormCall& c, hipStream_t stream) {
+    switch (dt) {
+        case 0: return norm_of<float>(c, stream);
+        case 1: return norm_of<_Float16>(c, stream);
+        case 2: return norm_of<__bf16>(c, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_norm_backward(int dt, const void* sum, const void* weight, const void* d_y, const void* d_sum, void* d_r, float* d_weight,
+                                float* partials, int64_t rows, int channels, float eps, hipStream_t stream) {
+    switch (dt) {
+        case 0: return norm_backward_of<float>(sum, weight, d_y, d_sum, d_r, d_weight, partials, rows, channels, eps, stream);
+        case 1: return norm_backward_of<_Float16>(sum, weight, d_y, d_sum, d_r, d_weight, partials, rows, channels, eps, stream);
+        case 2: return norm_backward_of<__bf16>(sum, weight, d_y, d_sum, d_r, d_weight, partials, rows, channels, eps, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace msla

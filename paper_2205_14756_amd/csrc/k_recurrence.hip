@@ -1,0 +1,794 @@
+// The gated linear recurrence: S_i = a_i S_{i-1} + k_i v_i^T, o_i = scale q_i^T S_i, a_i = exp(log_gate_i).
+//
+// In chunks of 64 tokens, with F the running sum of the gates' logarithms inside a chunk and S the state before it,
+//     o_i = scale ( sum_{j <= i} e^{F_i - F_j} (q_i . k_j) v_j  +  e^{F_i} q_i^T S ),       S <- e^{F_end} S + sum_j e^{F_end - F_j} k_j v_j^T,
+// all of it 16x16 matrix instructions; no exponent is above 0 where no gate is.
+//
+// The gradient is the same scan three times.  With dS the gradient that arrives at a state:
+//     dq_i = scale ( sum_{j <= i} e^{..} (do_i . v_j) k_j + e^{F_i} do_i^T S^T )        the scan with (do; v, k) for (q; k, v)
+//     dk_j = scale   sum_{i >= j} e^{..} (v_j . do_i) q_i + e^{..} v_j^T dS^T           the scan from the end with (v; do, q)
+//     dv_j = scale   sum_{i >= j} e^{..} (k_j . q_i) do_i + e^{..} k_j^T dS             the scan from the end with (k; q, do)
+// From the end means: rows of a chunk in the opposite order, running sums that leave a row's own gate out.  And
+//     d log_gate_t = sum_{i >= t} (q_i . dq_i - k_i . dk_i) + <dS_end, S_end>           over the tokens up to any later border "end",
+// because what flows over the border before t is what leaves the tokens before it and reaches t or later ones.
+//
+// Long sequences are cut into segments, so that the GPU is full: a first pass sums each segment's own contribution to the state, a
+// second joins them in order (a few numbers a state), and the scan starts every segment from its state.  Where a segment holds a whole
+// sequence the first two are not launched.
+#include "recurrence_tile.h"
+#include "msla_sequence_kernels.h"
+
+namespace msla {
+namespace rec {
+
+struct SweepArgs {
+    Heads a, b, c;                  // (q; k, v) and its permutations
+    void* out;
+    long out_ts, out_hs;
+    Heads m;                        // like out: masks it where m.relu is set, and dots[token, head, slice] = m . out
+    float* dots;
+    const void* gate;
+    long gate_ts;
+    const float* start;             // states that segments start from [slot, heads_kv, d, d] (NULL: `first`)
+    const float* first;             // ... that sequences start from [sequence, heads_kv, d, d] (NULL: zero)
+    float* last;                    // ... that sequences end with (NULL: not wanted)
+    int rs, cs;                     // strides of a state's rows (channels of a) and columns (channels of out)
+    Layout layout;
+    int heads, ga, gb, reverse;     // state heads; heads of a and of (b, c) to each
+    float score_scale, in_scale, weight_scale;
+};
+
+struct StateArgs {
+    Heads b, c;
+    const void* gate;
+    long gate_ts;
+    float* own;                     // [slot, heads_kv, d, d]: row channel of b, column channel of c
+    float* decay;                   // [slot, heads_kv]
+    int rs, cs;
+    Layout layout;
+    int heads, gb, reverse;
+    float weight_scale;
+};
+
+// bounds on a tile's magnitudes from what the waves left in LDS (fp16 alone)
+__device__ __forceinline__ float tile_top(const unsigned* top) { return half_bits(max(max(top[0], top[3]), max(top[6], top[9]))); }
+
+__device__ __forceinline__ void leave_top(unsigned* top, unsigned mine) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) mine = max(mine, (unsigned)__shfl_xor((int)mine, d));
+    if (lane_id() == 0) top[(threadIdx.x >> 6) * 3] = mine;
+}
+
+// The state's part of a wave: rows are all channels of the key, columns the wave's 32 output channels.
+template <class T, int D>
+struct State {
+    typedef Tile<T, D> Ti;
+    f32x4 s[Ti::kBlocks][2];
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int b = 0; b < Ti::kBlocks; ++b)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) s[b][n] = f32x4{0, 0, 0, 0};
+    }
+    // element (row, col) at p + row * rs + col * cs; channels that are padding read as zero and are not written
+    __device__ __forceinline__ void read(const float* p, int slice, int rs, int cs) {
+        const int x = lane_id() & 15, q = lane_id() >> 4;
+#pragma unroll
+        for (int b = 0; b < Ti::kBlocks; ++b)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = Ti::channel(b, 4 * q + r), col = slice + Ti::channel(n, x);
+                    s[b][n][r] = D >= 32 || (row < D && col < D) ? p[(long)row * rs + (long)col * cs] : 0.0f;
+                }
+    }
+    __device__ __forceinline__ void write(float* p, int slice, int rs, int cs, float unit) const {
+        const int x = lane_id() & 15, q = lane_id() >> 4;
+#pragma unroll
+        for (int b = 0; b < Ti::kBlocks; ++b)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = Ti::channel(b, 4 * q + r), col = slice + Ti::channel(n, x);
+                    if (D >= 32 || (row < D && col < D)) p[(long)row * rs + (long)col * cs] = s[b][n][r] * unit;
+                }
+    }
+    __device__ __forceinline__ void scale(float f) {
+#pragma unroll
+        for (int b = 0; b < Ti::kBlocks; ++b)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[b][n][r] *= f;
+    }
+    __device__ __forceinline__ float top() const {
+        float t = 0.0f;
+#pragma unroll
+        for (int b = 0; b < Ti::kBlocks; ++b)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) t = fmaxf(t, fabsf(s[b][n][r]));
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) t = fmaxf(t, __shfl_xor(t, d));
+        return t;
+    }
+    // columns n of step b's channels as an operand, in parts
+    __device__ __forceinline__ void operand(int b, int n, float f, typename Ti::Vec (&part)[kParts<T>]) const {
+        float v[Ti::kVec];
+#pragma unroll
+        for (int e = 0; e < Ti::kVec; ++e) v[e] = s[b * Ti::kJoin + e / 4][n][e % 4] * f;
+        Ti::template split<kParts<T>>(v, part);
+    }
+    // += sum_j b_j (w_j c_j)^T over the chunk; vt: the wave's columns of c over tokens
+    __device__ __forceinline__ void add(char* tb, const typename Ti::Vec (&vt)[Ti::kTokenSteps][2], const float* weight, float unit) {
+        const int x = lane_id() & 15, q = lane_id() >> 4;
+#pragma unroll
+        for (int st = 0; st < Ti::kTokenSteps; ++st) {
+            float w[Ti::kVec];
+#pragma unroll
+            for (int j = 0; j < Ti::kJoin; ++j) {
+                const f32x4 f = *(const f32x4*)(weight + st * Ti::kStep + 16 * j + 4 * q);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[4 * j + r] = f[r] * unit;
+            }
+            typename Ti::Vec part[2][kStateParts<T>];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                float v[Ti::kVec];
+#pragma unroll
+                for (int e = 0; e < Ti::kVec; ++e) v[e] = Ti::Tr::to_f32(vt[st][n][e]) * w[e];
+                Ti::template split<kStateParts<T>>(v, part[n]);
+            }
+#pragma unroll
+            for (int b = 0; b < Ti::kBlocks; ++b) {
+                const typename Ti::Vec kt = Ti::token_operand(tb, b, st, x, q);
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int p = 0; p < kStateParts<T>; ++p) s[b][n] = Ti::Tr::mma_vec(s[b][n], kt, part[n][p]);
+            }
+        }
+    }
+};
+
+template <class T>
+__device__ __forceinline__ float gate_of(const void* gate, long ts, const Segment& s, int reverse, long u, int head, int heads) {
+    if (gate == nullptr || u >= s.hi - s.lo || head >= heads) return 0.0f;
+    const long t = reverse ? s.hi - 1 - u : s.lo + u;
+    return (float)((const T*)gate)[t * ts + head];
+}
+
+// What a segment adds to the state, and the product of its gates.
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_state_kernel(StateArgs p) {
+    typedef Tile<T, D> Ti;
+    extern __shared__ __align__(16) char lds[];
+    char* tb = lds;
+    char* tc = tb + Ti::kBytes;
+    Gates* gates = (Gates*)(tc + Ti::kBytes);
+    unsigned* tops = (unsigned*)(gates + Ti::kHeads);           // [2][4 waves][3]
+
+    const Segment seg = find_segment(p.layout, blockIdx.x);
+    if (!seg.live || seg.index == (p.reverse ? 0 : seg.count - 1)) return;     // nothing comes after it
+    const int wave = threadIdx.x >> 6, lane = lane_id(), x = lane & 15, q = lane >> 4;
+    const int head0 = blockIdx.y * Ti::kHeads, mine = wave / Ti::kWavesPerHead, head = head0 + mine;
+    const int slice = wave % Ti::kWavesPerHead * kSlice;
+    const long len = seg.hi - seg.lo;
+    const int chunks = (int)((len + kChunk - 1) / kChunk), steps = chunks * p.gb;
+
+    Ti::clear(tb);
+    Ti::clear(tc);
+    State<T, D> state;
+    state.clear();
+    float exponent = 0.0f, unit = 1.0f;
+    typename Ti::Regs rb, rc;
+    float g = 0.0f;
+    Ti::load(rb, p.b, seg, p.reverse, 0, head0, p.heads, p.gb, 0);
+    Ti::load(rc, p.c, seg, p.reverse, 0, head0, p.heads, p.gb, 0);
+    g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+    __syncthreads();
+    for (int it = 0; it < steps; ++it) {
+        const int sub = it % p.gb;
+        unsigned* top = tops + (it & 1) * 12;
+        Ti::store(rb, tb, p.b.relu);
+        const unsigned mc = Ti::store(rc, tc, p.c.relu);
+        if constexpr (Ti::kNormalise) leave_top(top + 2, mc);
+        if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, g, p.reverse, 1.0f, p.weight_scale, Ti::kNormalise);
+        __syncthreads();
+        if (it + 1 < steps) {
+            const long first = (long)((it + 1) / p.gb) * kChunk;
+            const int next = (it + 1) % p.gb;
+            Ti::load(rb, p.b, seg, p.reverse, first, head0, p.heads, p.gb, next);
+            Ti::load(rc, p.c, seg, p.reverse, first, head0, p.heads, p.gb, next);
+            if (next == 0) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, first + lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+        }
+        const Gates& gt = gates[mine];
+        float fresh = unit, factor = 1.0f;
+        if constexpr (Ti::kNormalise) {
+            const float bound = tile_top(top + 2) * fabsf(p.weight_scale) * gt.grow;
+            if (bound > 0.0f) fresh = normaliser(bound);
+            factor = fresh / unit;
+            unit = fresh;
+        }
+        if (sub == 0) {
+            factor *= gt.total;
+            exponent += gt.exponent;
+        }
+        if (sub == 0 || Ti::kNormalise) state.scale(factor);
+        typename Ti::Vec vt[Ti::kTokenSteps][2];
+#pragma unroll
+        for (int st = 0; st < Ti::kTokenSteps; ++st)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) vt[st][n] = Ti::token_operand(tc + mine * Ti::kHeadBytes, slice / 16 + n, st, x, q);
+        state.add(tb + mine * Ti::kHeadBytes, vt, gt.weight, unit);
+        __syncthreads();
+    }
+    if (head >= p.heads) return;
+    const long at = (long)seg.slot * p.heads + head;
+    state.write(p.own + at * (D * D), slice, p.rs, p.cs, 1.0f / unit);
+    if (lane == 0 && slice == 0) p.decay[at] = __builtin_amdgcn_exp2f(exponent);
+}
+
+// own[slot] (what a segment adds) becomes the state that the segment starts from, in the order of the scan.  Eight segments are read
+// ahead: their loads hang on nothing.
+__global__ void __launch_bounds__(kThreads) recurrence_join_kernel(float* own, const float* decay, const float* first, Layout layout, int heads,
+                                                                   int size, int reverse) {
+    const int b = blockIdx.x / heads, h = blockIdx.x % heads;
+    const int e = (blockIdx.y * kThreads + threadIdx.x) * 4;
+    if (e >= size) return;
+    const long slot0 = first_slot(layout, b);
+    const long from = sequence_start(layout, b), to = max(from, sequence_start(layout, b + 1));
+    const int count = (int)min(max(1L, (to - from + layout.segment - 1) / layout.segment), layout.slots - slot0);
+    f32x4 run = {0, 0, 0, 0};
+    if (first != nullptr) run = *(const f32x4*)(first + ((long)b * heads + h) * size + e);
+    for (int i0 = 0; i0 < count; i0 += 8) {
+        f32x4 add[8];
+        float keep[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            add[i] = f32x4{0, 0, 0, 0};
+            keep[i] = 0.0f;
+            const int k = i0 + i;
+            if (k + 1 < count) {            // (nothing was summed for the last one)
+                const long at = (slot0 + (reverse ? count - 1 - k : k)) * heads + h;
+                add[i] = *(const f32x4*)(own + at * size + e);
+                keep[i] = decay[at];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int k = i0 + i;
+            if (k >= count) break;
+            const long at = (slot0 + (reverse ? count - 1 - k : k)) * heads + h;
+            *(f32x4*)(own + at * size + e) = run;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) run[r] = fmaf(keep[i], run[r], add[i][r]);
+        }
+    }
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_sweep_kernel(SweepArgs p) {
+    typedef Tile<T, D> Ti;
+    typedef typename Ti::Vec Vec;
+    typedef typename Ti::Tr Tr;
+    constexpr int kVec = Ti::kVec;
+    extern __shared__ __align__(16) char lds[];
+    char* ta = lds;
+    char* tb = ta + Ti::kBytes;
+    char* tc = tb + Ti::kBytes;
+    Gates* gates = (Gates*)(tc + Ti::kBytes);
+    unsigned* tops = (unsigned*)(gates + Ti::kHeads);
+
+    const Segment seg = find_segment(p.layout, blockIdx.x);
+    if (!seg.live) return;
+    const int wave = threadIdx.x >> 6, lane = lane_id(), x = lane & 15, q = lane >> 4;
+    const int head0 = blockIdx.y * Ti::kHeads, mine = wave / Ti::kWavesPerHead, head = head0 + mine;
+    const int slice = wave % Ti::kWavesPerHead * kSlice;
+    const bool live = head < p.heads;
+    const long len = seg.hi - seg.lo;
+    const int chunks = (int)((len + kChunk - 1) / kChunk), group = max(p.ga, p.gb), steps = chunks * group;
+
+    Ti::clear(ta);
+    Ti::clear(tb);
+    Ti::clear(tc);
+    State<T, D> state;
+    if (live && p.start != nullptr) state.read(p.start + ((long)seg.slot * p.heads + head) * (D * D), slice, p.rs, p.cs);
+    else if (live && p.first != nullptr) state.read(p.first + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs, p.cs);
+    else state.clear();
+    float unit = 1.0f, bound_s = 0.0f, at = 0.0f, bt = 0.0f, ct = 0.0f;
+    if constexpr (Ti::kNormalise) bound_s = state.top();
+
+    typename Ti::Regs ra, rb, rc;
+    Ti::load(ra, p.a, seg, p.reverse, 0, head0, p.heads, p.ga, 0);
+    Ti::load(rb, p.b, seg, p.reverse, 0, head0, p.heads, p.gb, 0);
+    Ti::load(rc, p.c, seg, p.reverse, 0, head0, p.heads, p.gb, 0);
+    float g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+    f32x4 o[4][2];
+    __syncthreads();
+    for (int it = 0; it < steps; ++it) {
+        const int sub = it % group;
+        const bool new_a = sub == 0 || p.ga > 1, new_b = sub == 0 || p.gb > 1;      // (one of ga, gb is 1)
+        const bool begins = new_a, ends = p.gb == 1 || sub == group - 1;            // of an output's sum
+        const bool feeds = p.ga == 1 || sub == group - 1;                           // the state
+        const long first = (long)(it / group) * kChunk;
+        unsigned* top = tops + (it & 1) * 12;
+        unsigned ma = 0, mb = 0, mc = 0;
+        if (new_a) ma = Ti::store(ra, ta, p.a.relu);
+        if (new_b) {
+            mb = Ti::store(rb, tb, p.b.relu);
+            mc = Ti::store(rc, tc, p.c.relu);
+        }
+        if constexpr (Ti::kNormalise) {
+            leave_top(top, ma);
+            leave_top(top + 1, mb);
+            leave_top(top + 2, mc);
+        }
+        if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, g, p.reverse, p.in_scale, p.weight_scale, Ti::kNormalise);
+        __syncthreads();
+        if (it + 1 < steps) {
+            const long then = (long)((it + 1) / group) * kChunk;
+            const int next = (it + 1) % group;
+            if (next == 0 || p.ga > 1) Ti::load(ra, p.a, seg, p.reverse, then, head0, p.heads, p.ga, p.ga > 1 ? next : 0);
+            if (next == 0 || p.gb > 1) {
+                Ti::load(rb, p.b, seg, p.reverse, then, head0, p.heads, p.gb, p.gb > 1 ? next : 0);
+                Ti::load(rc, p.c, seg, p.reverse, then, head0, p.heads, p.gb, p.gb > 1 ? next : 0);
+            }
+            if (next == 0) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, then + lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+        }
+        const Gates& gt = gates[mine];
+        const char* ha = ta + mine * Ti::kHeadBytes;
+        char* hb = tb + mine * Ti::kHeadBytes;
+        char* hc = tc + mine * Ti::kHeadBytes;
+        if constexpr (Ti::kNormalise) {
+            if (new_a) at = tile_top(top);
+            if (new_b) {
+                bt = tile_top(top + 1);
+                ct = tile_top(top + 2);
+            }
+        }
+        // what the rows take from the state
+        if (begins) {
+            float fs = 1.0f;
+            if constexpr (Ti::kNormalise) fs = normaliser(bound_s * unit);
+#pragma unroll
+            for (int rb_ = 0; rb_ < 4; ++rb_) o[rb_][0] = o[rb_][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < Ti::kSteps; ++s) {
+                Vec part[2][kParts<T>];
+#pragma unroll
+                for (int n = 0; n < 2; ++n) state.operand(s, n, fs, part[n]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const Vec va = Ti::row_operand(ha, 16 * i + x, s, q);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int k = 0; k < kParts<T>; ++k) o[i][n] = Tr::mma_vec(o[i][n], part[n][k], va);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float f = gt.in[16 * i + x] / (fs * unit);
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[i][n][r] *= f;
+            }
+        }
+        // what they take from the chunk's own rows
+        Vec vt[Ti::kTokenSteps][2];
+#pragma unroll
+        for (int st = 0; st < Ti::kTokenSteps; ++st)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) vt[st][n] = Ti::token_operand(hc, slice / 16 + n, st, x, q);
+        float fp = 1.0f;
+        if constexpr (Ti::kNormalise) {
+            fp = normaliser(fabsf(p.score_scale) * (float)Ti::kPad * at * bt * gt.grow);
+            if (fp != 1.0f) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[i][n][r] *= fp;
+            }
+        }
+        static_for<0, 4>([&](auto i_) {
+            constexpr int i = decltype(i_)::value;
+            Vec va[Ti::kSteps];
+#pragma unroll
+            for (int s = 0; s < Ti::kSteps; ++s) va[s] = Ti::row_operand(ha, 16 * i + x, s, q);
+            const float fi = gt.hi[16 * i + x], li = gt.lo[16 * i + x], sc = p.score_scale * fp;
+            static_for<0, i / Ti::kJoin + 1>([&](auto st_) {
+                constexpr int st = decltype(st_)::value;
+                float w[kVec];
+                static_for<0, Ti::kJoin>([&](auto j_) {
+                    constexpr int half = decltype(j_)::value, j = st * Ti::kJoin + half;
+                    if constexpr (j <= i) {
+                        f32x4 d = {0, 0, 0, 0};
+#pragma unroll
+                        for (int s = 0; s < Ti::kSteps; ++s) d = Tr::mma_vec(d, Ti::row_operand(hb, 16 * j + x, s, q), va[s]);
+                        const f32x4 fj = *(const f32x4*)(gt.hi + 16 * j + 4 * q), lj = *(const f32x4*)(gt.lo + 16 * j + 4 * q);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float e = __builtin_amdgcn_exp2f((fi - fj[r]) + (li - lj[r]));
+                            const bool sees = j < i || 4 * q + r <= x;
+                            w[4 * half + r] = sees ? d[r] * e * sc : 0.0f;
+                        }
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) w[4 * half + r] = 0.0f;
+                    }
+                });
+                Vec part[kParts<T>];
+                Ti::template split<kParts<T>>(w, part);
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int k = 0; k < kParts<T>; ++k) o[i][n] = Tr::mma_vec(o[i][n], vt[st][n], part[k]);
+            });
+        });
+        if constexpr (Ti::kNormalise) {
+            if (fp != 1.0f) {
+                const float back = 1.0f / fp;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[i][n][r] *= back;
+            }
+        }
+        // the state behind the chunk
+        if (feeds) {
+            float factor = 1.0f;
+            if constexpr (Ti::kNormalise) {
+                const float bound = ct * fabsf(p.weight_scale) * gt.grow;
+                const float fresh = bound > 0.0f ? normaliser(bound) : unit;
+                factor = fresh / unit;
+                unit = fresh;
+                bound_s = (new_b && sub > 0 && p.gb > 1 ? bound_s : bound_s * gt.total) + (float)kChunk * bt * bound;
+            }
+            const bool decays = p.gb == 1 || sub == 0;
+            if (decays) factor *= gt.total;
+            if (decays || Ti::kNormalise) state.scale(factor);
+            state.add(hb, vt, gt.weight, unit);
+        }
+        if (ends && live) {
+            const int ho = head * p.ga + (p.ga > 1 ? sub : 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const long u = first + 16 * i + x;
+                const bool row = u < len;
+                const long t = row ? Ti::token(seg, p.reverse, u) : 0;
+                float dot = 0.0f;
+#pragma unroll
+                for (int v = 0; v < 8 / kVec; ++v) {            // 16 bytes at a time
+                    const int ch = slice + (kVec == 8 ? 8 * q : 16 * v + 4 * q);
+                    if (!row || (D < 32 && ch >= D)) continue;
+                    float w[kVec];
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) w[e] = kVec == 8 ? o[i][e / 4][e % 4] : o[i][v][e];
+                    if (p.m.p != nullptr) {
+                        const Vec mv = *(const Vec*)((const T*)p.m.p + t * p.m.ts + (long)ho * p.m.hs + ch);
+#pragma unroll
+                        for (int e = 0; e < kVec; ++e) {
+                            const float me = Tr::to_f32(mv[e]);
+                            if (p.m.relu && !(me > 0.0f)) w[e] = 0.0f;
+                            dot = fmaf(me, w[e], dot);
+                        }
+                    }
+                    Vec r;
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) r[e] = Tr::from_f32(w[e]);
+                    *(Vec*)((T*)p.out + t * p.out_ts + (long)ho * p.out_hs + ch) = r;
+                }
+                if (p.dots != nullptr) {
+                    dot += __shfl_xor(dot, 16);
+                    dot += __shfl_xor(dot, 32);
+                    if (q == 0 && row) p.dots[(t * (p.heads * p.ga) + ho) * Ti::kWavesPerHead + wave % Ti::kWavesPerHead] = dot;
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (live && p.last != nullptr && seg.index == (p.reverse ? 0 : seg.count - 1))
+        state.write(p.last + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs, p.cs, 1.0f / unit);
+}
+
+// d log_gate of a segment's tokens and one head: from the segment's end, x_t = q_t . dq_t - k_t . dk_t summed up, on top of
+// <dS, S> at that end.
+template <class T>
+__global__ void __launch_bounds__(kThreads) recurrence_gate_kernel(const float* q_dots, const float* k_dots, int slices, const float* starts,
+                                                                   const float* d_starts, const float* last, const float* d_last, T* d_gate,
+                                                                   long d_gate_ts, Layout layout, int heads, int group, int size) {
+    __shared__ double part[kThreads / 64];
+    const Segment seg = find_segment(layout, blockIdx.x);
+    if (!seg.live) return;
+    const int h = blockIdx.y, wave = threadIdx.x >> 6, lane = lane_id();
+    const bool at_end = seg.index == seg.count - 1;
+    const float* s = at_end ? last : starts;
+    const float* ds = at_end ? d_last : d_starts;
+    double sum = 0.0;
+    if (s != nullptr && ds != nullptr) {
+        const float* sp = s + ((at_end ? (long)seg.sequence : (long)seg.slot + 1) * heads + h) * size;
+        const float* dp = ds + ((at_end ? (long)seg.sequence : (long)seg.slot) * heads + h) * size;
+        for (int e = threadIdx.x * 4; e < size; e += kThreads * 4) {
+            const f32x4 a = *(const f32x4*)(sp + e), b = *(const f32x4*)(dp + e);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += (double)a[r] * (double)b[r];
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    double above = part[0] + part[1] + part[2] + part[3];
+    const long len = seg.hi - seg.lo;
+    for (long u0 = 0; u0 < len; u0 += kThreads) {           // rows from the end
+        const long u = u0 + threadIdx.x, t = seg.hi - 1 - u;
+        double x = 0.0;
+        if (u < len) {
+            for (int g = 0; g < group; ++g)
+                for (int k = 0; k < slices; ++k) x += (double)q_dots[((t * heads + h) * group + g) * slices + k];
+            for (int k = 0; k < slices; ++k) x -= (double)k_dots[(t * heads + h) * slices + k];
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const double up = __shfl_up(x, d);
+            if (lane >= d) x += up;
+        }
+        __syncthreads();
+        if (lane == 63) part[wave] = x;
+        __syncthreads();
+        double before = above;
+        for (int w = 0; w < wave; ++w) before += part[w];
+        if (u < len) d_gate[t * d_gate_ts + h] = (T)(float)(before + x);
+        above += part[0] + part[1] + part[2] + part[3];
+    }
+}
+
+struct StepArgs {
+    Heads q, k, v;
+    const void* gate;
+    long gate_ts;
+    const float* state;
+    float* fresh;
+    void* out;
+    long out_ts, out_hs;
+    long units;                     // sequences * heads
+    int heads, group;
+    float scale;
+};
+
+// One token a sequence: the state is read once and written once, which is what there is to do.  A workgroup has 32 columns of a
+// state (16 for heads of 16): eight lanes a row of them, 16 bytes each, so a thread holds d/32 rows; heads of 16 go four to a workgroup.
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads) recurrence_step_kernel(StepArgs p) {
+    typedef Traits<T> Tr;
+    constexpr int kCols = D < 32 ? D : 32, kLanes = kCols / 4, kGroups = kThreads / kLanes;
+    constexpr int kUnits = D < kGroups ? kGroups / D : 1;           // states of a workgroup
+    constexpr int kRowLanes = kGroups / kUnits, kRows = D / kRowLanes;
+    constexpr int kSlices = D / kCols;
+    __shared__ float part[4][kCols];
+    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+    const long unit = (long)(blockIdx.x / kSlices) * kUnits + group / kRowLanes;
+    const int row0 = group % kRowLanes, col = blockIdx.x % kSlices * kCols + lane * 4;
+    const bool live = unit < p.units;
+    const long b = live ? unit / p.heads : 0;
+    const int h = live ? (int)(unit % p.heads) : 0;
+    f32x4 s[kRows];
+    const float* from = p.state == nullptr ? nullptr : p.state + (b * p.heads + h) * (D * D) + col;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        s[i] = f32x4{0, 0, 0, 0};
+        if (live && from != nullptr) s[i] = *(const f32x4*)(from + (row0 + i * kRowLanes) * D);
+    }
+    const T* kp = (const T*)p.k.p + b * p.k.ts + h * p.k.hs;
+    const f32x4 v = frag_to_f32<T>(load_frag<T>((const T*)p.v.p + b * p.v.ts + h * p.v.hs + col));
+    float keep = 1.0f;
+    if (p.gate != nullptr) {
+        const float g = (float)((const T*)p.gate)[b * p.gate_ts + h];
+        keep = expf(g);
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        float k = Tr::to_f32(kp[row0 + i * kRowLanes]);
+        if (p.k.relu) k = k > 0.0f ? k : 0.0f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[i][r] = fmaf(k, v[r], keep * s[i][r]);
+        if (live) *(f32x4*)(p.fresh + (b * p.heads + h) * (D * D) + (row0 + i * kRowLanes) * D + col) = s[i];
+    }
+    for (int g = 0; g < p.group; ++g) {
+        const T* qp = (const T*)p.q.p + b * p.q.ts + (h * p.group + g) * p.q.hs;
+        f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            float q = Tr::to_f32(qp[row0 + i * kRowLanes]);
+            if (p.q.relu) q = q > 0.0f ? q : 0.0f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = fmaf(q, s[i][r], o[r]);
+        }
+#pragma unroll
+        for (int d = kLanes; d < 64; d *= 2)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] += __shfl_xor(o[r], d);
+        T* out = (T*)p.out + b * p.out_ts + (h * p.group + g) * p.out_hs + col;
+        if constexpr (kRowLanes * kLanes <= 64) {
+            if (live && row0 == 0) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] *= p.scale;
+                store_frag<T>(out, frag_from_f32<T>(o));
+            }
+        } else {
+            const int wave = threadIdx.x >> 6;
+            if ((threadIdx.x & 63) < kLanes) *(f32x4*)&part[wave][lane * 4] = o;
+            __syncthreads();
+            if (threadIdx.x < kLanes && live) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] = ((part[0][lane * 4 + r] + part[1][lane * 4 + r]) + (part[2][lane * 4 + r] + part[3][lane * 4 + r])) * p.scale;
+                store_frag<T>(out, frag_from_f32<T>(o));
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+template <class T, int D>
+constexpr int tile_lds(int tiles) { return tiles * Tile<T, D>::kBytes + Tile<T, D>::kHeads * (int)sizeof(Gates) + 2 * 12 * 4; }
+
+// LDS above the 64 KB that a kernel may ask for by itself is granted once a kernel and device
+template <class K>
+hipError_t allow_lds(K kernel, int bytes, unsigned long long* done) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (bytes <= 65536 || (__atomic_load_n(done, __ATOMIC_ACQUIRE) & bit)) return hipSuccess;
+    e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) __atomic_fetch_or(done, bit, __ATOMIC_RELEASE);
+    return e;
+}
+
+template <class T, int D>
+hipError_t launch_state(const StateArgs& a, hipStream_t stream) {
+    static unsigned long long done = 0;
+    constexpr int bytes = tile_lds<T, D>(2);
+    hipError_t e = allow_lds(&recurrence_state_kernel<T, D>, bytes, &done);
+    if (e != hipSuccess) return e;
+    const dim3 grid(a.layout.slots, (a.heads + Tile<T, D>::kHeads - 1) / Tile<T, D>::kHeads);
+    hipLaunchKernelGGL((recurrence_state_kernel<T, D>), grid, dim3(kThreads), bytes, stream, a);
+    return hipGetLastError();
+}
+
+template <class T, int D>
+hipError_t launch_sweep(const SweepArgs& a, hipStream_t stream) {
+    static unsigned long long done = 0;
+    constexpr int bytes = tile_lds<T, D>(3);
+    hipError_t e = allow_lds(&recurrence_sweep_kernel<T, D>, bytes, &done);
+    if (e != hipSuccess) return e;
+    const dim3 grid(a.layout.slots, (a.heads + Tile<T, D>::kHeads - 1) / Tile<T, D>::kHeads);
+    hipLaunchKernelGGL((recurrence_sweep_kernel<T, D>), grid, dim3(kThreads), bytes, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_join(float* own, const float* decay, const float* first, const Layout& l, int heads, int size, int reverse, hipStream_t stream) {
+    const dim3 grid(l.sequences * heads, (size / 4 + kThreads - 1) / kThreads);
+    hipLaunchKernelGGL(recurrence_join_kernel, grid, dim3(kThreads), 0, stream, own, decay, first, l, heads, size, reverse);
+    return hipGetLastError();
+}
+
+Heads heads_of(const RecurrenceRows& r, int relu) { return Heads{r.p, r.ts, r.hs, relu}; }
+
+Layout layout_of(const RecurrenceCall& c) {
+    return Layout{c.offsets, c.sequences, c.tokens, c.plan.segment, c.plan.slots};
+}
+
+#define MSLA_TRY(x)                         \
+    do {                                    \
+        const hipError_t e_ = (x);          \
+        if (e_ != hipSuccess) return e_;    \
+    } while (0)
+
+template <class T, int D>
+hipError_t forward_of(const RecurrenceCall& c, hipStream_t stream) {
+    const Layout l = layout_of(c);
+    const Heads q = heads_of(c.q, c.rectify), k = heads_of(c.k, c.rectify), v = heads_of(c.v, 0);
+    const float* start = nullptr;
+    if (c.plan.cut) {
+        float* own = (float*)c.ws;
+        float* decay = (float*)(c.ws + c.plan.decay_at);
+        MSLA_TRY((launch_state<T, D>(StateArgs{k, v, c.gate, c.gate_ts, own, decay, D, 1, l, c.heads_kv, 1, 0, 1.0f}, stream)));
+        MSLA_TRY(launch_join(own, decay, c.initial, l, c.heads_kv, D * D, 0, stream));
+        start = own;
+    }
+    return launch_sweep<T, D>(SweepArgs{q, k, v, c.out.p, c.out.ts, c.out.hs, Heads{nullptr, 0, 0, 0}, nullptr, c.gate, c.gate_ts, start,
+                                        c.initial, c.final_state, D, 1, l, c.heads_kv, c.heads_q / c.heads_kv, 1, 0, c.scale, c.scale, 1.0f},
+                              stream);
+}
+
+template <class T, int D>
+hipError_t backward_of(const RecurrenceCall& c, hipStream_t stream) {
+    const Layout l = layout_of(c);
+    const int group = c.heads_q / c.heads_kv;
+    const Heads q = heads_of(c.q, c.rectify), k = heads_of(c.k, c.rectify), v = heads_of(c.v, 0), d_o = heads_of(c.d_out, 0);
+    const Heads no = {nullptr, 0, 0, 0};
+    float* s_own = nullptr;
+    float* d_own = nullptr;
+    if (c.plan.cut) {
+        s_own = (float*)c.ws;
+        d_own = (float*)(c.ws + c.plan.d_states_at);
+        float* decay = (float*)(c.ws + c.plan.decay_at);
+        float* d_decay = (float*)(c.ws + c.plan.d_decay_at);
+        MSLA_TRY((launch_state<T, D>(StateArgs{k, v, c.gate, c.gate_ts, s_own, decay, D, 1, l, c.heads_kv, 1, 0, 1.0f}, stream)));
+        MSLA_TRY((launch_state<T, D>(StateArgs{q, d_o, c.gate, c.gate_ts, d_own, d_decay, D, 1, l, c.heads_kv, group, 1, c.scale}, stream)));
+        MSLA_TRY(launch_join(s_own, decay, c.initial, l, c.heads_kv, D * D, 0, stream));
+        MSLA_TRY(launch_join(d_own, d_decay, c.d_final, l, c.heads_kv, D * D, 1, stream));
+    }
+    float* q_dots = c.d_gate ? (float*)(c.ws + c.plan.dots_at) : nullptr;
+    float* k_dots = c.d_gate ? q_dots + c.tokens * c.heads_q * Tile<T, D>::kWavesPerHead : nullptr;
+    float* last = c.d_gate && c.d_final ? (float*)(c.ws + c.plan.last_at) : nullptr;
+    const Heads mq = c.d_gate || c.rectify ? q : no, mk = c.d_gate || c.rectify ? k : no;
+    MSLA_TRY((launch_sweep<T, D>(SweepArgs{d_o, v, k, c.d_q.p, c.d_q.ts, c.d_q.hs, mq, q_dots, c.gate, c.gate_ts, s_own, c.initial, last, 1, D, l,
+                                           c.heads_kv, group, 1, 0, c.scale, c.scale, 1.0f}, stream)));
+    MSLA_TRY((launch_sweep<T, D>(SweepArgs{v, d_o, q, c.d_k.p, c.d_k.ts, c.d_k.hs, mk, k_dots, c.gate, c.gate_ts, d_own, c.d_final, nullptr, 1, D,
+                                           l, c.heads_kv, 1, group, 1, c.scale, 1.0f, c.scale}, stream)));
+    MSLA_TRY((launch_sweep<T, D>(SweepArgs{k, q, d_o, c.d_v.p, c.d_v.ts, c.d_v.hs, no, nullptr, c.gate, c.gate_ts, d_own, c.d_final, c.d_initial, D,
+                                           1, l, c.heads_kv, 1, group, 1, c.scale, 1.0f, c.scale}, stream)));
+    if (c.d_gate) {
+        hipLaunchKernelGGL((recurrence_gate_kernel<T>), dim3(l.slots, c.heads_kv), dim3(kThreads), 0, stream, q_dots, k_dots,
+                           Tile<T, D>::kWavesPerHead, s_own, d_own, last, c.d_final, (T*)c.d_gate, c.d_gate_ts, l, c.heads_kv, group, D * D);
+        MSLA_TRY(hipGetLastError());
+    }
+    return hipSuccess;
+}
+
+template <class T, int D>
+hipError_t step_of(const RecurrenceCall& c, hipStream_t stream) {
+    constexpr int kCols = D < 32 ? D : 32, kGroups = kThreads / (kCols / 4), kUnits = D < kGroups ? kGroups / D : 1;
+    const long units = (long)c.sequences * c.heads_kv;
+    const long blocks = (units + kUnits - 1) / kUnits * (D / kCols);
+    hipLaunchKernelGGL((recurrence_step_kernel<T, D>), dim3((unsigned)blocks), dim3(kThreads), 0, stream,
+                       StepArgs{heads_of(c.q, c.rectify), heads_of(c.k, c.rectify), heads_of(c.v, 0), c.gate, c.gate_ts, c.initial,
+                                c.final_state, c.out.p, c.out.ts, c.out.hs, units, c.heads_kv, c.heads_q / c.heads_kv, c.scale});
+    return hipGetLastError();
+}
+
+template <class T, int D>
+hipError_t run_of(const RecurrenceCall& c, hipStream_t stream) {
+    switch (c.what) {
+        case 0: return forward_of<T, D>(c, stream);
+        case 1: return backward_of<T, D>(c, stream);
+        default: return step_of<T, D>(c, stream);
+    }
+}
+
+template <class T>
+hipError_t run_for(const RecurrenceCall& c, hipStream_t stream) {
+    switch (c.head_dim) {
+        case 16: return run_of<T, 16>(c, stream);
+        case 32: return run_of<T, 32>(c, stream);
+        case 64: return run_of<T, 64>(c, stream);
+        case 128: return run_of<T, 128>(c, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace rec
+
+hipError_t launch_recurrence(int dt, const RecurrenceCall& c, hipStream_t stream) {
+    switch (dt) {
+        case 0: return rec::run_for<float>(c, stream);
+        case 1: return rec::run_for<_Float16>(c, stream);
+        case 2: return rec::run_for<__bf16>(c, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace msla

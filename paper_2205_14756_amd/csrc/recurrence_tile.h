@@ -1,0 +1,258 @@
+// What the kernels of the gated recurrence (k_recurrence.hip) share: where segments lie, how a chunk of 64 tokens enters LDS, the
+// chunk's running gates, and operands of the matrix instructions out of both.
+//
+// A workgroup has four waves and walks over the chunks of one segment.  A wave owns 32 output channels of one head, so a
+// workgroup holds 128 / d heads (four of 32 and of 16; heads of 16 are padded to 32 with zeros in LDS only).
+//
+// Which register holds what is chosen so that nothing is ever transposed: a result D of a 16x16 matrix instruction (lane (x, q): rows
+// 4q + r, column x) is at once the next one's operand (lane (x, q): the contraction slots that q owns, of row or column x).
+//   - scores come as b a^T, so lane (x, q) has query x and keys 4q + r of each block of 16: an operand over the keys;
+//   - the state's rows (channels of the key) are dealt to the blocks so that two of them hold 8 neighbouring channels a lane, in the order
+//     in which a row of queries is read from LDS 16 bytes a lane; its columns (output channels) likewise, which makes a lane's
+//     results 8 neighbours of an output row;
+//   - operands over tokens out of token-major tiles are gathered by ds_read_b64_tr_b16 (4x16 blocks, any address a lane).
+#pragma once
+#include "msla_device.h"
+
+namespace msla {
+namespace rec {
+
+constexpr int kChunk = 64;
+constexpr int kThreads = 256;
+constexpr int kSlice = 32;          // output channels of a wave
+
+struct Heads {
+    const void* p;
+    long ts, hs;                    // strides of a token and a head, in elements
+    int relu;
+};
+
+struct Layout {
+    const int* offsets;
+    int sequences;
+    long tokens;
+    int segment;                    // tokens of a segment, a multiple of kChunk
+    int slots;                      // segments of all sequences have distinct numbers below this
+};
+
+__device__ __forceinline__ long sequence_start(const Layout& l, int b) {
+    if (l.offsets == nullptr) return l.tokens / l.sequences * b;
+    const long at = l.offsets[b];
+    return at < 0 ? 0 : (at > l.tokens ? l.tokens : at);
+}
+
+// Segment numbers: sequence b's begin at start(b) / segment + b, which leaves room for all of them (and for one where it is
+// empty), so a workgroup finds its own without anyone counting lengths first.
+__device__ __forceinline__ long first_slot(const Layout& l, int b) { return sequence_start(l, b) / l.segment + b; }
+
+struct Segment {
+    int sequence, index, count, slot;
+    long lo, hi;                    // its tokens
+    bool live;
+};
+
+__device__ __forceinline__ Segment find_segment(const Layout& l, int slot) {
+    int lo = 0, hi = l.sequences - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (first_slot(l, mid) <= slot) lo = mid;
+        else hi = mid - 1;
+    }
+    Segment s;
+    s.sequence = lo;
+    s.slot = slot;
+    const long from = sequence_start(l, lo), to = max(from, sequence_start(l, lo + 1));
+    s.index = slot - (int)first_slot(l, lo);
+    s.count = max(1, (int)((to - from + l.segment - 1) / l.segment));
+    s.live = s.index >= 0 && s.index < s.count;
+    s.lo = from + (long)s.index * l.segment;
+    s.hi = min(to, s.lo + l.segment);
+    return s;
+}
+
+template <class T, int D>
+struct Tile {
+    typedef Traits<T> Tr;
+    typedef typename Tr::Vec Vec;
+    static constexpr int kVec = Tr::kVec;
+    static constexpr int kPad = D < 32 ? 32 : D;                // channels in LDS
+    static constexpr int kWavesPerHead = kPad / kSlice;
+    static constexpr int kHeads = 4 / kWavesPerHead;            // heads of a workgroup
+    // rows 32 bytes apart modulo 128: the eight rows that a 16-byte read serves together, and the four of a gather, hit banks of their own
+    static constexpr int kPitch = kPad * (int)sizeof(T) + 32;
+    static constexpr int kHeadBytes = kChunk * kPitch;
+    static constexpr int kBytes = kHeads * kHeadBytes;
+    static constexpr int kStep = 4 * kVec;                      // contraction of one matrix step (fp32: four instructions)
+    static constexpr int kSteps = kPad / kStep;                 // ... over channels
+    static constexpr int kTokenSteps = kChunk / kStep;          // ... over tokens
+    static constexpr int kBlocks = kPad / 16;                   // blocks of 16 key channels
+    static constexpr int kJoin = kVec / 4;                      // results that make one operand
+    static constexpr int kPerRow = kHeads * (D / kVec);         // 16-byte pieces of a tile's row
+    static constexpr int kPieces = (kChunk * kPerRow + kThreads - 1) / kThreads;
+    static constexpr bool kNormalise = std::is_same<T, _Float16>::value;
+
+    struct Regs { u32x4 v[kPieces]; };
+
+    // channel of row (or column) m of block `blk`: see the top of the file
+    static __device__ __forceinline__ int channel(int blk, int m) {
+        return sizeof(T) == 2 ? 32 * (blk >> 1) + 8 * (m >> 2) + 4 * (blk & 1) + (m & 3) : 16 * blk + m;
+    }
+
+    // row u of the segment's chunk `first` .. : token lo + u, or from the segment's end
+    static __device__ __forceinline__ long token(const Segment& s, int reverse, long u) { return reverse ? s.hi - 1 - u : s.lo + u; }
+
+    static __device__ __forceinline__ void load(Regs& r, const Heads& h, const Segment& s, int reverse, long first, int head0, int heads, int per,
+                                                int g) {
+        const long len = s.hi - s.lo;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int p = threadIdx.x + i * kThreads;
+            const int row = p / kPerRow, in = p % kPerRow;
+            const int hl = in / (D / kVec), ch = in % (D / kVec) * kVec;
+            r.v[i] = u32x4{0, 0, 0, 0};
+            if (row < kChunk && first + row < len && head0 + hl < heads)
+                r.v[i] = *(const u32x4*)((const T*)h.p + token(s, reverse, first + row) * h.ts + ((long)(head0 + hl) * per + g) * h.hs + ch);
+        }
+    }
+
+    // into LDS, rectified where asked; returns the largest bit pattern of a finite magnitude (fp16 alone; a value that is not finite may
+    // not spoil the other heads' normalisers)
+    static __device__ __forceinline__ unsigned store(const Regs& r, char* tile, int relu) {
+        typedef short i16x8 __attribute__((ext_vector_type(8)));
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        unsigned top = 0;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int p = threadIdx.x + i * kThreads;
+            const int row = p / kPerRow, in = p % kPerRow;
+            const int hl = in / (D / kVec), ch = in % (D / kVec) * kVec;
+            u32x4 v = r.v[i];
+            if constexpr (sizeof(T) == 2) {
+                const short f = relu ? 0 : -32768;
+                v = __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(i16x8, v), i16x8{f, f, f, f, f, f, f, f}));
+            } else {
+                const int f = relu ? 0 : (int)0x80000000;
+                v = __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(i32x4, v), i32x4{f, f, f, f}));
+            }
+            if constexpr (kNormalise) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned lo = v[j] & 0x7fffu, hi = (v[j] >> 16) & 0x7fffu;
+                    top = max(top, max(lo < 0x7c00u ? lo : 0u, hi < 0x7c00u ? hi : 0u));
+                }
+            }
+            if (row < kChunk) *(u32x4*)(tile + hl * kHeadBytes + row * kPitch + ch * (int)sizeof(T)) = v;
+        }
+        return top;
+    }
+
+    // the padding channels of a head of 16: zero once, never written again
+    static __device__ __forceinline__ void clear(char* tile) {
+        if constexpr (kPad != D)
+            for (int i = threadIdx.x * 16; i < kBytes; i += kThreads * 16) *(u32x4*)(tile + i) = u32x4{0, 0, 0, 0};
+    }
+
+    // operand over channels: row `row`, channels of step s
+    static __device__ __forceinline__ Vec row_operand(const char* tile, int row, int s, int q) {
+        return *(const Vec*)(tile + row * kPitch + (s * kStep + kVec * q) * (int)sizeof(T));
+    }
+
+    // operand over tokens: column channel(blk, x), token slots of step s (16-bit: 32s + 4q + r and 16 further on; fp32: 16s + 4q + r)
+    static __device__ __forceinline__ Vec token_operand(char* tile, int blk, int s, int x, int q) {
+        if constexpr (sizeof(T) == 2) {
+            typedef __attribute__((address_space(3))) i16x4* LdsPtr;
+            char* at = tile + (32 * s + 4 * q + (x >> 2)) * kPitch + (32 * (blk >> 1) + 8 * (x & 3) + 4 * (blk & 1)) * 2;
+            const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at);
+            const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + 16 * kPitch));
+            typedef short i16x8 __attribute__((ext_vector_type(8)));
+            return __builtin_bit_cast(Vec, i16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+        } else {
+            Vec v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = *(const float*)(tile + (16 * s + 4 * q + r) * kPitch + (16 * blk + x) * 4);
+            return v;
+        }
+    }
+
+    // v in PARTS parts of the storage type, each what the ones before left
+    template <int PARTS>
+    static __device__ __forceinline__ void split(const float (&v)[kVec], Vec (&part)[PARTS]) {
+        float rest[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            rest[e] = v[e];
+            // (a product behind v[e] has to be rounded to fp32 here: folded into the conversion to fp16 it rounds once, where the
+            // difference below sees it rounded twice, and one value in some thousands lost its second part)
+            if constexpr (PARTS > 1) asm("" : "+v"(rest[e]));
+        }
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) part[p][e] = Tr::from_f32(rest[e]);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (p + 1 < PARTS) rest[e] -= Tr::to_f32(part[p][e]);
+        }
+    }
+};
+
+// Parts of an operand that is not an input.  Scores and the state on its way into an output: two (bf16 2^-17, fp16 2^-23 of the value),
+// below the output's rounding, and small enough that their sums over a segment give the gates' gradient.  What is added to the state,
+// which is handed out in fp32: three in bf16 (2^-25).
+template <class T> constexpr int kParts = sizeof(T) == 4 ? 1 : 2;
+template <class T> constexpr int kStateParts = std::is_same<T, __bf16>::value ? 3 : kParts<T>;
+
+// A chunk's running gates, in LDS: exponents (base 2) from the chunk's start to each row, as a float and what it leaves out of the
+// double that they are summed in, so that differences stay exact behind a gate that forgets everything.
+struct Gates {
+    float hi[kChunk], lo[kChunk];
+    float in[kChunk];               // the state's factor in this row's output
+    float weight[kChunk];           // this row's factor in the state behind the chunk
+    float total, grow, exponent, pad;       // the state's own factor; how far gates above 0 let a weight grow; log2 of total
+};
+
+constexpr double kLog2e = 1.4426950408889634;
+
+// by one wave; `g`: this lane's row's gate (0 where there is no row)
+__device__ __forceinline__ void run_gates(Gates* out, float g, int reverse, float in_scale, float weight_scale, bool want_grow) {
+    const int lane = lane_id();
+    double own = (double)g * kLog2e;
+    if (own < -150.0) own = -150.0;         // 2^-150 is 0 in fp32; a NaN stays one
+    double sum = own;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const double up = __shfl_up(sum, d);
+        if (lane >= d) sum += up;
+    }
+    const double total = __shfl(sum, 63);
+    const double here = reverse ? sum - own : sum;
+    const float hi = (float)here;
+    out->hi[lane] = hi;
+    out->lo[lane] = (float)(here - (double)hi);
+    out->in[lane] = __builtin_amdgcn_exp2f(hi) * fmaf(out->lo[lane], 0.693147182f, 1.0f) * in_scale;
+    out->weight[lane] = __builtin_amdgcn_exp2f((float)(total - here)) * weight_scale;
+    float grow = own > 0.0 ? (float)own : 0.0f;
+    if (want_grow) {
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) grow += __shfl_xor(grow, d);
+    }
+    if (lane == 0) {
+        out->total = __builtin_amdgcn_exp2f((float)total);
+        out->grow = __builtin_amdgcn_exp2f(grow);
+        out->exponent = (float)total;
+    }
+}
+
+// a power of two that takes values up to `bound` to at most 2^15 (fp16's range); 1 where there is no such bound
+__device__ __forceinline__ float normaliser(float bound) {
+    if (!(bound > 0.0f) || !(bound < 3e38f)) return 1.0f;
+    int e = (int)(__builtin_bit_cast(unsigned, bound) >> 23) - 126;      // bound < 2^e
+    e = 15 - e;
+    e = e < -100 ? -100 : (e > 100 ? 100 : e);
+    return __builtin_bit_cast(float, (unsigned)(e + 127) << 23);
+}
+
+__device__ __forceinline__ float half_bits(unsigned b) { return (float)__builtin_bit_cast(_Float16, (unsigned short)b); }
+
+}  // namespace rec
+}  // namespace msla

@@ -1,0 +1,353 @@
+"""Thin ctypes binding of the sequence operators of libmsla.so (the C ABI of include/msla_sequence.h).
+
+The linear attention of Eq. (3) as a running state over a sequence, the root-mean-square norm with the residual's addition, and
+the projection of rows in 8 bits.  Like ``msla``: argument marshalling only, no CPU fallback, tensors on the current GPU, work on
+its current stream unless one is given.  Buffers that are not passed in are allocated here with torch.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+
+from . import msla as _msla
+from .msla import MSLA_OK, MslaError, _DTYPES, _ptr, _stream
+
+EXPORTS = ("msla_recurrence_workspace_bytes", "msla_recurrence_forward", "msla_recurrence_backward", "msla_recurrence_step",
+           "msla_norm_forward", "msla_norm_quantized", "msla_norm_backward_workspace_bytes", "msla_norm_backward", "msla_quantize_rows",
+           "msla_linear_quantized_workspace_bytes", "msla_linear_quantized")
+
+HEAD_DIMS = (16, 32, 64, 128)
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Shape(ctypes.Structure):
+    _fields_ = [("sequences", ctypes.c_int), ("tokens", ctypes.c_int64), ("offsets", ctypes.c_void_p), ("heads_q", ctypes.c_int),
+                ("heads_kv", ctypes.c_int), ("head_dim", ctypes.c_int), ("scale", ctypes.c_float), ("rectify", ctypes.c_int)]
+
+
+_ready = None
+
+
+def _lib():
+    global _ready
+    if _ready is None:
+        lib = _msla.load_library()
+        vp, i, i64, f, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+        shape, size = ctypes.POINTER(_Shape), ctypes.POINTER(sz)
+        lib.msla_recurrence_workspace_bytes.argtypes = [shape, i, i, size]
+        lib.msla_recurrence_forward.argtypes = [shape, _Heads, _Heads, _Heads, vp, i64, vp, _Heads, vp, vp, sz, i, vp]
+        lib.msla_recurrence_backward.argtypes = [shape, _Heads, _Heads, _Heads, vp, i64, vp, _Heads, vp, _Heads, _Heads, _Heads, vp, i64, vp,
+                                                 vp, sz, i, vp]
+        lib.msla_recurrence_step.argtypes = [shape, _Heads, _Heads, _Heads, vp, i64, vp, _Heads, vp, i, vp]
+        lib.msla_norm_forward.argtypes = [vp, vp, vp, vp, vp, i64, i, f, i, vp]
+        lib.msla_norm_quantized.argtypes = [vp, vp, vp, vp, vp, vp, i64, i, f, i, vp]
+        lib.msla_norm_backward_workspace_bytes.argtypes = [i64, i, i, size]
+        lib.msla_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, i64, i, f, i, vp]
+        lib.msla_quantize_rows.argtypes = [vp, vp, vp, i64, i, i, vp]
+        lib.msla_linear_quantized_workspace_bytes.argtypes = [i64, i, i, size]
+        lib.msla_linear_quantized.argtypes = [vp, vp, vp, vp, vp, vp, sz, i64, i, i, i, vp]
+        for name in EXPORTS:
+            getattr(lib, name).restype = i
+        _ready = lib
+    return _ready
+
+
+def _check(status, where):
+    if status != MSLA_OK:
+        raise MslaError(status, where)
+
+
+def _need(condition, what):
+    if not condition:
+        raise ValueError("msla: " + what)
+
+
+def _on_gpu(*tensors):
+    """All on the current device (whose stream the work goes to)."""
+    here = None
+    for t in tensors:
+        if t is not None:
+            _need(t.is_cuda, "tensors must live in GPU memory")
+            if here is None:
+                here = torch.cuda.current_device()
+            _need(t.get_device() == here, "tensors must live on the current device")
+
+
+def _plain(t, name, shape, dtype):
+    if t is not None:
+        _need(t.is_contiguous(), f"{name} must be contiguous")
+        _need(tuple(t.shape) == tuple(shape), f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+        _need(t.dtype == dtype, f"{name} must be {dtype}, not {t.dtype}")
+
+
+def _rows(t, name, like=None):
+    """A [..., heads, head_dim] tensor as rows of tokens: (data, token stride, head stride), tokens in order."""
+    _need(t.dim() >= 3, f"{name} must be [..., heads, head_dim]")
+    _need(t.stride(-1) == 1 or t.shape[-1] == 1, f"{name}'s channels must lie next to each other")
+    tokens, step = 1, t.stride(-3)
+    for size, stride in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
+        _need(size == 1 or tokens == 1 or stride == step * tokens, f"{name}'s tokens must lie at equal distances")
+        if tokens == 1 and size != 1:
+            step = stride
+        tokens *= size
+    if like is not None:
+        _need(tuple(t.shape) == tuple(like), f"{name} must have the shape {tuple(like)}, not {tuple(t.shape)}")
+    # (the stride of an axis of length one says nothing, and torch leaves anything there)
+    return _Heads(t.data_ptr(), step if tokens > 1 else 0, t.stride(-2) if t.shape[-2] > 1 else 0), tokens
+
+
+def _gate(t, tokens, heads, dtype, name):
+    if t is None:
+        return None, 0
+    _need(t.dtype == dtype, f"{name} must be {dtype}, not {t.dtype}")
+    _need(t.numel() == tokens * heads and t.shape[-1] == heads, f"{name} must be [..., heads_kv]")
+    flat = t if t.dim() == 2 else t.view(-1, heads)
+    _need(heads == 1 or flat.stride(1) == 1, f"{name}'s heads must lie next to each other")
+    return flat.data_ptr(), flat.stride(0) if tokens > 1 else heads
+
+
+class _Call:
+    """The arguments that forward, backward and step share, checked."""
+
+    def __init__(self, q, k, v, log_gate, sequences, offsets, scale, rectify):
+        _need(q.dtype in _DTYPES, f"{q.dtype} is not a storage type")
+        _need(q.dtype == k.dtype == v.dtype, "q, k and v must have one type")
+        self.dtype = q.dtype
+        self.q, self.tokens = _rows(q, "q")
+        self.k, tokens_k = _rows(k, "k")
+        _need(tokens_k == self.tokens, "q and k must have the same tokens")
+        self.v, _ = _rows(v, "v", k.shape)
+        self.heads_q, self.head_dim = q.shape[-2:]
+        self.heads_kv = k.shape[-2]
+        _need(k.shape[-1] == self.head_dim, "q and k must have the same head_dim")
+        if offsets is not None:
+            _need(offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.is_contiguous() and offsets.numel() >= 2,
+                  "offsets must be int32 [sequences + 1]")
+            _need(sequences is None or sequences == offsets.numel() - 1, "offsets must be int32 [sequences + 1]")
+            sequences = offsets.numel() - 1
+        elif sequences is None:
+            sequences = q.shape[0] if q.dim() == 4 else 1
+        self.sequences = int(sequences)
+        self.gate, self.gate_stride = _gate(log_gate, self.tokens, self.heads_kv, q.dtype, "log_gate")
+        scale = self.head_dim ** -0.5 if scale is None else float(scale)
+        self.shape = _Shape(self.sequences, self.tokens, _ptr(offsets), self.heads_q, self.heads_kv, self.head_dim, scale, int(bool(rectify)))
+        self.dt = _DTYPES[q.dtype]
+        self.state_shape = (self.sequences, self.heads_kv, self.head_dim, self.head_dim)
+
+    def workspace(self, given, backward, device):
+        size = ctypes.c_size_t(0)
+        _check(_lib().msla_recurrence_workspace_bytes(ctypes.byref(self.shape), backward, self.dt, ctypes.byref(size)),
+               "msla_recurrence_workspace_bytes")
+        if given is None:
+            given = torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None
+        else:
+            _need(given.is_contiguous() and given.dtype == torch.uint8, "the workspace must be contiguous bytes")
+        return given
+
+
+def msla_recurrence_workspace_bytes(sequences, tokens, heads_q, heads_kv, head_dim, dtype, packed=False, backward=False) -> int:
+    """Bytes that msla_recurrence_forward (or _backward) needs; packed: with offsets."""
+    shape = _Shape(sequences, tokens, 4 if packed else None, heads_q, heads_kv, head_dim, 1.0, 0)
+    size = ctypes.c_size_t(0)
+    _check(_lib().msla_recurrence_workspace_bytes(ctypes.byref(shape), int(backward), _DTYPES[dtype], ctypes.byref(size)),
+           "msla_recurrence_workspace_bytes")
+    return int(size.value)
+
+
+def msla_recurrence_forward(q, k, v, log_gate=None, sequences: Optional[int] = None, offsets=None, initial_state=None, scale=None,
+                            rectify=False, out=None, final_state=None, workspace=None, stream=None):
+    """S_i = exp(log_gate_i) S_{i-1} + k_i v_i^T, out_i = scale q_i^T S_i over every sequence and head.
+
+    q [..., heads_q, d], k and v [..., heads_kv, d], any strides over tokens and heads (so parts of a projected map will do); log_gate
+    [..., heads_kv] in the same type.  The tokens are those of ``sequences`` equally long sequences (by default q.shape[0] of a
+    four-dimensional q, else one), or of sequences packed behind each other that start at ``offsets`` (int32, on the GPU, one more than
+    sequences).  scale: d ** -0.5 by default; rectify: max(., 0) of q and k.  Returns (out, final_state [sequences, heads_kv, d, d] fp32);
+    rows that belong to no sequence are left as they are in a given ``out``."""
+    _on_gpu(q, k, v, log_gate, offsets, initial_state, out, final_state, workspace)
+    c = _Call(q, k, v, log_gate, sequences, offsets, scale, rectify)
+    _plain(initial_state, "initial_state", c.state_shape, torch.float32)
+    _plain(final_state, "final_state", c.state_shape, torch.float32)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _need(out.dtype == q.dtype, "out must have q's type")
+    o, _ = _rows(out, "out", q.shape)
+    if final_state is None:
+        final_state = torch.empty(c.state_shape, dtype=torch.float32, device=q.device)
+    ws = c.workspace(workspace, 0, q.device)
+    _check(_lib().msla_recurrence_forward(ctypes.byref(c.shape), c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(initial_state), o,
+                                          _ptr(final_state), _ptr(ws), 0 if ws is None else ws.numel(), c.dt, _stream(stream)),
+           "msla_recurrence_forward")
+    return out, final_state
+
+
+def msla_recurrence_backward(q, k, v, d_out, log_gate=None, sequences: Optional[int] = None, offsets=None, initial_state=None,
+                             d_final_state=None, scale=None, rectify=False, d_q=None, d_k=None, d_v=None, d_log_gate=None,
+                             d_initial_state=None, workspace=None, stream=None):
+    """The gradient of msla_recurrence_forward: (d_q, d_k, d_v, d_log_gate, d_initial_state), the last two None where log_gate or
+    initial_state is."""
+    _on_gpu(q, k, v, d_out, log_gate, offsets, initial_state, d_final_state, d_q, d_k, d_v, d_log_gate, d_initial_state, workspace)
+    c = _Call(q, k, v, log_gate, sequences, offsets, scale, rectify)
+    _plain(initial_state, "initial_state", c.state_shape, torch.float32)
+    _plain(d_final_state, "d_final_state", c.state_shape, torch.float32)
+    _plain(d_initial_state, "d_initial_state", c.state_shape, torch.float32)
+    _need(d_out.dtype == q.dtype, "d_out must have q's type")
+    do, _ = _rows(d_out, "d_out", q.shape)
+    grads = []
+    for t, like, name in ((d_q, q, "d_q"), (d_k, k, "d_k"), (d_v, v, "d_v")):
+        if t is None:
+            t = torch.empty(like.shape, dtype=q.dtype, device=q.device)
+        _need(t.dtype == q.dtype, f"{name} must have q's type")
+        grads.append((t, _rows(t, name, like.shape)[0]))
+    _need(log_gate is not None or d_log_gate is None, "d_log_gate needs a log_gate")
+    if d_log_gate is None and log_gate is not None:
+        d_log_gate = torch.empty(log_gate.shape, dtype=q.dtype, device=q.device)
+    dg, dg_stride = _gate(d_log_gate, c.tokens, c.heads_kv, q.dtype, "d_log_gate")
+    if d_initial_state is None and initial_state is not None:
+        d_initial_state = torch.empty(c.state_shape, dtype=torch.float32, device=q.device)
+    ws = c.workspace(workspace, 1, q.device)
+    _check(_lib().msla_recurrence_backward(ctypes.byref(c.shape), c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(initial_state), do,
+                                           _ptr(d_final_state), grads[0][1], grads[1][1], grads[2][1], dg, dg_stride,
+                                           _ptr(d_initial_state), _ptr(ws), 0 if ws is None else ws.numel(), c.dt, _stream(stream)),
+           "msla_recurrence_backward")
+    return grads[0][0], grads[1][0], grads[2][0], d_log_gate, d_initial_state
+
+
+def msla_recurrence_step(q, k, v, state, log_gate=None, scale=None, rectify=False, out=None, new_state=None, stream=None):
+    """One token for each of q.shape[0] sequences: q [sequences, heads_q, d], k and v [sequences, heads_kv, d], state [sequences,
+    heads_kv, d, d] fp32.  The state is updated in place unless new_state is given.  Returns (out, new_state)."""
+    if new_state is None:
+        new_state = state
+    _on_gpu(q, k, v, state, log_gate, out, new_state)
+    _need(q.dim() == 3, "q must be [sequences, heads_q, head_dim]")
+    c = _Call(q, k, v, log_gate, q.shape[0], None, scale, rectify)
+    _plain(state, "state", c.state_shape, torch.float32)
+    _plain(new_state, "new_state", c.state_shape, torch.float32)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _need(out.dtype == q.dtype, "out must have q's type")
+    o, _ = _rows(out, "out", q.shape)
+    _check(_lib().msla_recurrence_step(ctypes.byref(c.shape), c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(state), o, _ptr(new_state), c.dt,
+                                       _stream(stream)), "msla_recurrence_step")
+    return out, new_state
+
+
+def _norm_arguments(x, weight, residual, total):
+    _on_gpu(x, weight, residual, total)
+    _need(x.dtype in _DTYPES, f"{x.dtype} is not a storage type")
+    _need(x.dim() >= 1 and x.is_contiguous(), "x must be contiguous rows")
+    _plain(weight, "weight", x.shape[-1:], x.dtype)
+    _plain(residual, "residual", x.shape, x.dtype)
+    _plain(total, "sum_out", x.shape, x.dtype)
+    channels = x.shape[-1]
+    return x.numel() // channels if channels else 0, channels
+
+
+def msla_norm_forward(x, weight=None, residual=None, eps=1e-6, out=None, sum_out=None, stream=None):
+    """(y, r): r = x + residual, y = r / sqrt(mean(r^2) + eps) * weight over the last axis.  Without a residual r is x itself and is not
+    written, unless sum_out is given."""
+    rows, channels = _norm_arguments(x, weight, residual, sum_out)
+    _on_gpu(out)
+    _plain(out, "out", x.shape, x.dtype)
+    if out is None:
+        out = torch.empty_like(x)
+    if sum_out is None and residual is not None:
+        sum_out = torch.empty_like(x)
+    _check(_lib().msla_norm_forward(_ptr(x), _ptr(residual), _ptr(weight), _ptr(out), _ptr(sum_out), rows, channels, float(eps),
+                                    _DTYPES[x.dtype], _stream(stream)), "msla_norm_forward")
+    return out, x if sum_out is None else sum_out
+
+
+def _rows8(x, out8, scale):
+    _on_gpu(out8, scale)
+    _plain(out8, "out8", x.shape, torch.float8_e4m3fn)
+    _plain(scale, "scale", x.shape[:-1], torch.float32)
+    if out8 is None:
+        out8 = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    if scale is None:
+        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    return out8, scale
+
+
+def msla_norm_quantized(x, weight=None, residual=None, eps=1e-6, out8=None, scale=None, sum_out=None, stream=None):
+    """(y8, scale, r): msla_norm_forward with y as e4m3 rows, y ~ y8 * scale[..., None]."""
+    rows, channels = _norm_arguments(x, weight, residual, sum_out)
+    out8, scale = _rows8(x, out8, scale)
+    if sum_out is None and residual is not None:
+        sum_out = torch.empty_like(x)
+    _check(_lib().msla_norm_quantized(_ptr(x), _ptr(residual), _ptr(weight), _ptr(out8), _ptr(scale), _ptr(sum_out), rows, channels,
+                                      float(eps), _DTYPES[x.dtype], _stream(stream)), "msla_norm_quantized")
+    return out8, scale, x if sum_out is None else sum_out
+
+
+def msla_quantize_rows(x, out8=None, scale=None, stream=None):
+    """(x8, scale): rows of x as e4m3, x ~ x8 * scale[..., None]."""
+    rows, channels = _norm_arguments(x, None, None, None)
+    out8, scale = _rows8(x, out8, scale)
+    _check(_lib().msla_quantize_rows(_ptr(x), _ptr(out8), _ptr(scale), rows, channels, _DTYPES[x.dtype], _stream(stream)),
+           "msla_quantize_rows")
+    return out8, scale
+
+
+def msla_norm_backward_workspace_bytes(rows, channels, dtype) -> int:
+    size = ctypes.c_size_t(0)
+    _check(_lib().msla_norm_backward_workspace_bytes(rows, channels, _DTYPES[dtype], ctypes.byref(size)),
+           "msla_norm_backward_workspace_bytes")
+    return int(size.value)
+
+
+def msla_norm_backward(r, weight, d_y, d_sum=None, eps=1e-6, d_r=None, d_weight=None, workspace=None, stream=None):
+    """(d_r, d_weight): the gradient of msla_norm_forward at r (what it returned); d_sum: the gradient that reaches r past the norm.
+    d_r is that of x and of residual alike; d_weight is fp32."""
+    rows, channels = _norm_arguments(r, weight, d_y, d_sum)
+    _on_gpu(d_r, d_weight, workspace)
+    _plain(d_r, "d_r", r.shape, r.dtype)
+    _plain(d_weight, "d_weight", (channels,), torch.float32)
+    if d_r is None:
+        d_r = torch.empty_like(r)
+    if d_weight is None:
+        d_weight = torch.empty(channels, dtype=torch.float32, device=r.device)
+    if workspace is None:
+        workspace = torch.empty(msla_norm_backward_workspace_bytes(rows, channels, r.dtype), dtype=torch.uint8, device=r.device)
+    else:
+        _need(workspace.is_contiguous() and workspace.dtype == torch.uint8, "the workspace must be contiguous bytes")
+    _check(_lib().msla_norm_backward(_ptr(r), _ptr(weight), _ptr(d_y), _ptr(d_sum), _ptr(d_r), _ptr(d_weight), _ptr(workspace),
+                                     workspace.numel(), rows, channels, float(eps), _DTYPES[r.dtype], _stream(stream)),
+           "msla_norm_backward")
+    return d_r, d_weight
+
+
+def msla_linear_quantized_workspace_bytes(rows, c_in, c_out) -> int:
+    size = ctypes.c_size_t(0)
+    _check(_lib().msla_linear_quantized_workspace_bytes(rows, c_in, c_out, ctypes.byref(size)), "msla_linear_quantized_workspace_bytes")
+    return int(size.value)
+
+
+def msla_linear_quantized(x8, x_scale, w8, w_scale, dtype=torch.bfloat16, out=None, workspace=None, stream=None):
+    """y[..., o] = x_scale[...] * w_scale[o] * sum_c x8[..., c] * w8[o, c]: x8, w8 e4m3, scales fp32, y in ``dtype`` (out's, if given)."""
+    _on_gpu(x8, x_scale, w8, w_scale, out, workspace)
+    _need(w8.dim() == 2 and x8.dim() >= 1 and x8.shape[-1] == w8.shape[1], "x8 must be [..., c_in] and w8 [c_out, c_in]")
+    c_out, c_in = w8.shape
+    _plain(x8, "x8", x8.shape, torch.float8_e4m3fn)
+    _plain(w8, "w8", w8.shape, torch.float8_e4m3fn)
+    _plain(x_scale, "x_scale", x8.shape[:-1], torch.float32)
+    _plain(w_scale, "w_scale", (c_out,), torch.float32)
+    dtype = dtype if out is None else out.dtype
+    _need(dtype in _DTYPES, f"{dtype} is not a storage type")
+    _plain(out, "out", x8.shape[:-1] + (c_out,), dtype)
+    if out is None:
+        out = torch.empty(x8.shape[:-1] + (c_out,), dtype=dtype, device=x8.device)
+    rows = x8.numel() // c_in if c_in else 0
+    size = msla_linear_quantized_workspace_bytes(rows, c_in, c_out)
+    if workspace is None:
+        workspace = torch.empty(size, dtype=torch.uint8, device=x8.device) if size else None
+    else:
+        _need(workspace.is_contiguous() and workspace.dtype == torch.uint8, "the workspace must be contiguous bytes")
+    _check(_lib().msla_linear_quantized(_ptr(x8), _ptr(x_scale), _ptr(w8), _ptr(w_scale), _ptr(out), _ptr(workspace),
+                                        0 if workspace is None else workspace.numel(), rows, c_in, c_out, _DTYPES[dtype], _stream(stream)),
+           "msla_linear_quantized")
+    return out

@@ -1,0 +1,209 @@
+"""The root-mean-square norm, its 8-bit rows, its gradient, and the projection of 8-bit rows, against fp64.
+
+Tolerances: half a step of the result's type, plus fp32 on the way: a sum of squares is off by at most channels * 2^-24 of itself where it
+is summed in a row, and here in pieces of at most 64 values and a tree above them, so 2^-17 covers it, the square root, the
+reciprocal and two products; gradients have two such sums.  d_weight sums rows in runs of at most rows / 1024 + 1 and then at most 128 runs and 8."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import sequence_oracle as so
+from paper_2205_14756_amd import sequence as seq
+
+pytestmark = pytest.mark.gpu
+
+TDT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+WAY = 2.0 ** -17
+EPS = 1e-5
+
+
+def half_step(dtype):
+    return torch.finfo(TDT[dtype]).eps / 2
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def rnd(seed, dtype, *shape, scale=1.0):
+    return (torch.from_numpy(np.random.default_rng(seed).standard_normal(shape)) * scale).to(TDT[dtype]).cuda()
+
+
+def close(got, want, tol, what):
+    got = f64(got)
+    assert np.isfinite(got).all(), what
+    worst = float(np.max(np.abs(got - want) / tol)) if got.size else 0.0
+    print(f"  {what}: {worst:.3f} of the tolerance", flush=True)
+    assert worst <= 1.0, what
+
+
+SHAPES = [(1, 1), (5, 7), (3, 16), (130, 33), (64, 64), (9, 128), (257, 520), (2, 2051), (7, 4096), (3, 8200), (2, 16385), (1, 32768)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,channels", SHAPES)
+@pytest.mark.parametrize("full", [True, False])
+def test_norm(dtype, rows, channels, full):
+    print(f"norm {dtype} {rows} x {channels} {'with' if full else 'without'} residual and weight", flush=True)
+    x = rnd(1, dtype, rows, channels, scale=3.0)
+    res, w = (rnd(2, dtype, rows, channels), rnd(3, dtype, channels)) if full else (None, None)
+    guard = torch.full((rows + 2, channels), 7.0, dtype=TDT[dtype], device="cuda")
+    y, r = seq.msla_norm_forward(x, w, res, EPS, out=guard[1:-1])
+    want, sums = so.norm(f64(x), None if res is None else f64(res), None if w is None else f64(w), EPS)
+    close(y, want, (half_step(dtype) + WAY) * np.abs(want) + 2.0 ** -24, "y")
+    assert bool((guard[0] == 7.0).all()) and bool((guard[-1] == 7.0).all())
+    if full:
+        close(r, sums, half_step(dtype) * np.abs(sums) + 1e-7 * (np.abs(f64(x)) + np.abs(f64(res))) + 2.0 ** -25, "sum")
+    else:
+        assert r is x
+    # in place: the sum into the residual, y into x
+    x2, res2 = x.clone(), None if res is None else res.clone()
+    y2, r2 = seq.msla_norm_forward(x2, w, res2, EPS, out=x2, sum_out=res2)
+    assert torch.equal(y2, y) and (res is None or torch.equal(res2, r))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,channels", SHAPES)
+def test_norm_into_8_bits(dtype, rows, channels):
+    print(f"norm into 8 bits {dtype} {rows} x {channels}", flush=True)
+    x, res, w = rnd(1, dtype, rows, channels, scale=3.0), rnd(2, dtype, rows, channels), rnd(3, dtype, channels)
+    y8, scale, r = seq.msla_norm_quantized(x, w, res, EPS)
+    want, _ = so.norm(f64(x), f64(res), f64(w), EPS)
+    top = np.abs(want).max(-1)
+    close(scale, top / 448, 2 * WAY * top / 448 + 1e-38, "scale")
+    # half a step of e4m3 (2^-4 of a value, 2^-10 where it is subnormal), and the value's own error
+    unit = top[:, None] / 448
+    close(f64(y8) * f64(scale)[:, None] if False else y8.double() * scale.double()[:, None], want,
+          np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10 * unit) * (1 + 2.0 ** -10) + 4 * WAY * np.abs(want) + 1e-38, "y8 * scale")
+    assert torch.equal(r, seq.msla_norm_forward(x, w, res, EPS)[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_rows_into_8_bits(dtype):
+    x = rnd(4, dtype, 37, 200, scale=2.0)
+    x[3] = 0
+    x[4] = 0
+    x[4, 17] = -5.0                          # one value: it has the largest code
+    if dtype != "f16":
+        x[5] = x[5] * 1e-35                  # 448 over the largest has no fp32 value
+    x[6, 0], x[7, 1] = float("nan"), float("inf")
+    x8, scale = seq.msla_quantize_rows(x)
+    v = f64(x8)
+    fine = [i for i in range(37) if i not in (6, 7)]
+    top = np.abs(f64(x)).max(-1)
+    assert scale[3] == 0 and bool((x8[3].float() == 0).all())
+    assert v[4, 17] == -448 and np.count_nonzero(v[4]) == 1
+    for i in fine:
+        if top[i]:
+            want = f64(x)[i] / top[i] * 448
+            assert (np.abs(v[i] - want) <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10) * (1 + 2.0 ** -10)).all()
+            assert abs(float(scale[i]) - top[i] / 448) <= 2.0 ** -22 * top[i] / 448 + 1e-44
+    assert not bool(torch.isfinite(scale[6])) and not bool(torch.isfinite(scale[7]))
+    # values that e4m3 has come back as they are
+    grid = torch.arange(256, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn).float()
+    grid = grid[torch.isfinite(grid)].to(TDT[dtype])[None].contiguous()
+    g8, s = seq.msla_quantize_rows(grid)
+    assert float(s) == 1.0 and torch.equal(g8.float(), grid.float())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,channels", SHAPES + [(0, 64), (3000, 24), (2100, 300)])
+@pytest.mark.parametrize("full", [True, False])
+def test_norm_backward(dtype, rows, channels, full):
+    print(f"norm backward {dtype} {rows} x {channels}", flush=True)
+    r, dy = rnd(5, dtype, rows, channels, scale=2.0), rnd(6, dtype, rows, channels)
+    w, ds = (rnd(7, dtype, channels), rnd(8, dtype, rows, channels)) if full else (None, None)
+    n = seq.msla_norm_backward_workspace_bytes(rows, channels, TDT[dtype])
+    ws = torch.full((n + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    d_r, d_w = seq.msla_norm_backward(r, w, dy, ds, EPS, workspace=ws[:n])
+    torch.cuda.synchronize()
+    assert bool((ws[n:] == 0xFF).all())
+    want_r, want_w = so.norm_backward(f64(r), None if w is None else f64(w), f64(dy), None if ds is None else f64(ds), EPS)
+    aw = np.ones(channels) if w is None else np.abs(f64(w))
+    size = np.sqrt((f64(r) ** 2).mean(-1, keepdims=True) + EPS)
+    unit = np.abs(f64(r)) / size
+    mag = (np.abs(f64(dy)) * aw + unit * (np.abs(f64(dy)) * aw * unit).mean(-1, keepdims=True)) / size + (0 if ds is None else np.abs(f64(ds)))
+    close(d_r, want_r, half_step(dtype) * np.abs(want_r) + 4 * WAY * mag + 2.0 ** -24, "d_r")
+    close(d_w, want_w, 4 * WAY * (np.abs(f64(dy)) * unit).sum(0) + 1e-30, "d_weight")
+    again = seq.msla_norm_backward(r, w, dy, ds, EPS)
+    assert torch.equal(again[0], d_r) and torch.equal(again[1], d_w)
+    if rows:                                # into the gradient that it came from
+        dy2 = dy.clone()
+        assert torch.equal(seq.msla_norm_backward(r, w, dy2, ds, EPS, d_r=dy2)[0], d_r)
+
+
+def test_norm_gradient_against_differences():
+    r, w, dy, ds = rnd(9, "f32", 5, 70), rnd(10, "f32", 70), rnd(11, "f32", 5, 70), rnd(12, "f32", 5, 70)
+    d_r, d_w = seq.msla_norm_backward(r, w, dy, ds, EPS)
+    value = lambda r, w: float((seq.msla_norm_forward(r, w, None, EPS)[0].double() * dy.double()).sum() + (r.double() * ds.double()).sum())
+    h = 2.0 ** -7
+    for i, (x, g) in enumerate(((r, d_r), (w, d_w))):
+        e = rnd(13 + i, "f32", *x.shape)
+        got = (value(*((x + h * e, w) if i == 0 else (r, x + h * e))) - value(*((x - h * e, w) if i == 0 else (r, x - h * e)))) / (2 * h)
+        want = float((g.double() * e.double()).sum())
+        # h^2 / 6 of the third derivative, which is of the size of the value's own terms
+        assert abs(got - want) <= h * h * float((g.double().abs() * e.double().abs()).sum()) + 1e-3, (got, want)
+
+
+@pytest.mark.parametrize("offset", [1, 3])
+def test_rows_that_start_anywhere(offset):
+    flat = rnd(15, "bf16", offset + 6 * 128)
+    x = flat[offset:].view(6, 128)
+    assert x.data_ptr() % 16
+    assert torch.equal(seq.msla_norm_forward(x)[0], seq.msla_norm_forward(x.clone())[0])
+    out = torch.empty_like(flat)[offset:].view(6, 128)
+    assert torch.equal(seq.msla_norm_forward(x, out=out)[0], seq.msla_norm_forward(x.clone())[0])
+    a, b = seq.msla_norm_backward(x, None, x), seq.msla_norm_backward(x.clone(), None, x.clone())
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,c_in,c_out", [(1, 16, 16), (1, 4096, 4096), (3, 48, 80), (7, 144, 16), (16, 512, 512), (17, 2048, 272), (48, 4096, 1024),
+                                             (64, 8192, 128), (65, 1040, 144), (127, 256, 256), (128, 128, 128), (129, 2064, 160), (300, 640, 400),
+                                             (513, 16, 1040), (1030, 1024, 2048)])
+def test_linear_quantized(dtype, rows, c_in, c_out):
+    print(f"linear quantized {dtype} {rows} x {c_in} -> {c_out}", flush=True)
+    x8, sx = seq.msla_quantize_rows(rnd(20, "f32", rows, c_in))
+    w8, sw = seq.msla_quantize_rows(rnd(21, "f32", c_out, c_in))
+    guard = torch.full((rows + 2, c_out), 7.0, dtype=TDT[dtype], device="cuda")
+    n = seq.msla_linear_quantized_workspace_bytes(rows, c_in, c_out)
+    ws = torch.full((n + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    y = seq.msla_linear_quantized(x8, sx, w8, sw, out=guard[1:-1], workspace=ws[:n])
+    torch.cuda.synchronize()
+    assert bool((ws[n:] == 0xFF).all()) and bool((guard[0] == 7.0).all()) and bool((guard[-1] == 7.0).all())
+    a, b = x8.double(), w8.double()
+    scales = sx.double()[:, None] * sw.double()
+    want, size = f64((a @ b.t()) * scales), f64((a.abs() @ b.abs().t()) * scales)
+    # products of e4m3 values are exact; fp32 sums of c_in of them, in steps of 32 (2^-24 each), and three factors
+    close(y, want, (half_step(dtype) + 2.0 ** -22) * np.abs(want) + (c_in / 32 + 8) * 2.0 ** -24 * size + 2.0 ** -24, "y")
+
+
+def test_linear_quantized_carries_what_is_not_finite_in_its_row():
+    x8, sx = seq.msla_quantize_rows(rnd(22, "f32", 40, 256))
+    w8, sw = seq.msla_quantize_rows(rnd(23, "f32", 64, 256))
+    clean = seq.msla_linear_quantized(x8, sx, w8, sw)
+    bad = x8.view(torch.uint8).clone()
+    bad[7, 3] = 0x7F
+    got = seq.msla_linear_quantized(bad.view(torch.float8_e4m3fn), sx, w8, sw)
+    assert bool(torch.isnan(got[7]).all())
+    rest = [i for i in range(40) if i != 7]
+    assert torch.equal(got[rest], clean[rest])
+
+
+def test_the_binding_refuses():
+    x = rnd(24, "f16", 4, 64)
+    for bad in [lambda: seq.msla_norm_forward(x.double()), lambda: seq.msla_norm_forward(x[:, ::2]), lambda: seq.msla_norm_forward(x, x[0].float()),
+                lambda: seq.msla_norm_forward(x, x[0, :32].contiguous()), lambda: seq.msla_norm_forward(x, None, x[:3]), lambda: seq.msla_norm_forward(x, out=x[:3]),
+                lambda: seq.msla_norm_quantized(x, out8=x), lambda: seq.msla_quantize_rows(x, scale=x[:, 0].float()[:3]),
+                lambda: seq.msla_norm_backward(x, None, x.float()), lambda: seq.msla_norm_backward(x, None, x, d_weight=x[0])]:
+        with pytest.raises(ValueError):
+            bad()
+    x8, s = seq.msla_quantize_rows(x)
+    for bad in [lambda: seq.msla_linear_quantized(x, s, x8, s), lambda: seq.msla_linear_quantized(x8, s[:3], x8, s), lambda: seq.msla_linear_quantized(x8, s, x8, s, dtype=torch.float64),
+                lambda: seq.msla_linear_quantized(x8, s, x8, s, out=x), lambda: seq.msla_linear_quantized(x8[:, :32], s, x8, s)]:
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(seq.MslaError):
+        seq.msla_norm_forward(x, eps=-1.0)
+    with pytest.raises(seq.MslaError):
+        seq.msla_linear_quantized(x8, s, x8, s)         # four outputs: not a multiple of 16
