@@ -23,8 +23,8 @@ namespace rec {
 
 struct SweepArgs {
     Heads a, b, c;                  // (q; k, v) and its permutations
-    void* out;
-    long out_ts, out_hs;
+    char* out;
+    long out_ts, out_hs;            // bytes
     Heads m;                        // like out: masks it where m.relu is set, and dots[token, head, slice] = m . out
     float* dots;
     const void* gate;
@@ -32,7 +32,7 @@ struct SweepArgs {
     const float* start;             // states that segments start from [slot, heads_kv, d, d] (NULL: `first`)
     const float* first;             // ... that sequences start from [sequence, heads_kv, d, d] (NULL: zero)
     float* last;                    // ... that sequences end with (NULL: not wanted)
-    int rs, cs;                     // strides of a state's rows (channels of a) and columns (channels of out)
+    int rs;                         // 1: a state's rows (channels of a) lie next to each other in memory; d: its columns (channels of out)
     Layout layout;
     int heads, ga, gb, reverse;     // state heads; heads of a and of (b, c) to each
     float score_scale, in_scale, weight_scale;
@@ -42,9 +42,9 @@ struct StateArgs {
     Heads b, c;
     const void* gate;
     long gate_ts;
-    float* own;                     // [slot, heads_kv, d, d]: row channel of b, column channel of c
+    float* own;                     // [slot, heads_kv, d, d]
     float* decay;                   // [slot, heads_kv]
-    int rs, cs;
+    int rs;                         // as above, of rows of channels of b and columns of channels of c
     Layout layout;
     int heads, gb, reverse;
     float weight_scale;
@@ -71,30 +71,38 @@ struct State {
 #pragma unroll
             for (int n = 0; n < 2; ++n) s[b][n] = f32x4{0, 0, 0, 0};
     }
-    // element (row, col) at p + row * rs + col * cs; channels that are padding read as zero and are not written
-    __device__ __forceinline__ void read(const float* p, int slice, int rs, int cs) {
+    // In memory a row's or (rs == 1) a column's elements lie next to each other: a lane's four rows are then one access.  Channels that
+    // are padding read as zero and are not written.
+    template <class F>
+    __device__ __forceinline__ void blocks(int slice, F&& f) {
         const int x = lane_id() & 15, q = lane_id() >> 4;
 #pragma unroll
         for (int b = 0; b < Ti::kBlocks; ++b)
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = Ti::channel(b, 4 * q + r), col = slice + Ti::channel(n, x);
-                    s[b][n][r] = D >= 32 || (row < D && col < D) ? p[(long)row * rs + (long)col * cs] : 0.0f;
-                }
+            for (int n = 0; n < 2; ++n) {
+                const int row = Ti::channel(b, 4 * q), col = slice + Ti::channel(n, x);
+                if (D >= 32 || (row < D && col < D)) f(s[b][n], row, col);
+            }
     }
-    __device__ __forceinline__ void write(float* p, int slice, int rs, int cs, float unit) const {
-        const int x = lane_id() & 15, q = lane_id() >> 4;
+    __device__ __forceinline__ void read(const float* p, int slice, int rs) {
+        clear();
+        if (rs == 1)
+            blocks(slice, [&](f32x4& v, int row, int col) { v = *(const f32x4*)(p + (unsigned)(row + col * D)); });
+        else
+            blocks(slice, [&](f32x4& v, int row, int col) {
 #pragma unroll
-        for (int b = 0; b < Ti::kBlocks; ++b)
+                for (int r = 0; r < 4; ++r) v[r] = p[(unsigned)((row + r) * D + col)];
+            });
+    }
+    __device__ __forceinline__ void write(float* p, int slice, int rs, float unit) {
+        scale(unit);
+        if (rs == 1)
+            blocks(slice, [&](f32x4& v, int row, int col) { *(f32x4*)(p + (unsigned)(row + col * D)) = v; });
+        else
+            blocks(slice, [&](f32x4& v, int row, int col) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = Ti::channel(b, 4 * q + r), col = slice + Ti::channel(n, x);
-                    if (D >= 32 || (row < D && col < D)) p[(long)row * rs + (long)col * cs] = s[b][n][r] * unit;
-                }
+                for (int r = 0; r < 4; ++r) p[(unsigned)((row + r) * D + col)] = v[r];
+            });
     }
     __device__ __forceinline__ void scale(float f) {
 #pragma unroll
@@ -174,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
 
     const Segment seg = find_segment(p.layout, blockIdx.x);
     if (!seg.live || seg.index == (p.reverse ? 0 : seg.count - 1)) return;     // nothing comes after it
-    const int wave = threadIdx.x >> 6, lane = lane_id(), x = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), x = lane & 15, q = lane >> 4;
     const int head0 = blockIdx.y * Ti::kHeads, mine = wave / Ti::kWavesPerHead, head = head0 + mine;
     const int slice = wave % Ti::kWavesPerHead * kSlice;
     const long len = seg.hi - seg.lo;
@@ -187,12 +195,22 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
     float exponent = 0.0f, unit = 1.0f;
     typename Ti::Regs rb, rc;
     float g = 0.0f;
-    Ti::load(rb, p.b, seg, p.reverse, 0, head0, p.heads, p.gb, 0);
-    Ti::load(rc, p.c, seg, p.reverse, 0, head0, p.heads, p.gb, 0);
-    g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+    const int heads = p.heads - head0;
+    const unsigned ob = Ti::offset(p.b, p.reverse, p.gb), oc = Ti::offset(p.c, p.reverse, p.gb);
+    auto tile_at = [&](const Heads& h, long u, int sub) {
+        return h.p + Ti::token(seg, p.reverse, u) * h.ts + ((long)head0 * p.gb + sub) * h.hs;
+    };
+    auto fetch = [&](long u, int sub) {
+        const int rows = (int)min(len - u, (long)kChunk);
+        Ti::load(rb, tile_at(p.b, u, sub), ob, p.b, p.reverse, rows, heads);
+        Ti::load(rc, tile_at(p.c, u, sub), oc, p.c, p.reverse, rows, heads);
+        if (sub == 0) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, u + lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+    };
+    fetch(0, 0);
     __syncthreads();
-    for (int it = 0; it < steps; ++it) {
-        const int sub = it % p.gb;
+    int sub = 0, next_sub = 0;
+    long first = 0;
+    for (int it = 0; it < steps; ++it, first += next_sub == 0 ? kChunk : 0, sub = next_sub) {
         unsigned* top = tops + (it & 1) * 12;
         Ti::store(rb, tb, p.b.relu);
         const unsigned mc = Ti::store(rc, tc, p.c.relu);
@@ -200,11 +218,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
         if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, g, p.reverse, 1.0f, p.weight_scale, Ti::kNormalise);
         __syncthreads();
         if (it + 1 < steps) {
-            const long first = (long)((it + 1) / p.gb) * kChunk;
-            const int next = (it + 1) % p.gb;
-            Ti::load(rb, p.b, seg, p.reverse, first, head0, p.heads, p.gb, next);
-            Ti::load(rc, p.c, seg, p.reverse, first, head0, p.heads, p.gb, next);
-            if (next == 0) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, first + lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+            next_sub = sub + 1 == p.gb ? 0 : sub + 1;
+            fetch(first + (next_sub == 0 ? kChunk : 0), next_sub);
         }
         const Gates& gt = gates[mine];
         float fresh = unit, factor = 1.0f;
@@ -229,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
     }
     if (head >= p.heads) return;
     const long at = (long)seg.slot * p.heads + head;
-    state.write(p.own + at * (D * D), slice, p.rs, p.cs, 1.0f / unit);
+    state.write(p.own + at * (D * D), slice, p.rs, 1.0f / unit);
     if (lane == 0 && slice == 0) p.decay[at] = __builtin_amdgcn_exp2f(exponent);
 }
 
@@ -271,7 +286,8 @@ __global__ void __launch_bounds__(kThreads) recurrence_join_kernel(float* own, c
     }
 }
 
-template <class T, int D>
+// MASKED: out is masked and measured against m (p.m, p.dots)
+template <class T, int D, bool MASKED>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_sweep_kernel(SweepArgs p) {
     typedef Tile<T, D> Ti;
     typedef typename Ti::Vec Vec;
@@ -286,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
 
     const Segment seg = find_segment(p.layout, blockIdx.x);
     if (!seg.live) return;
-    const int wave = threadIdx.x >> 6, lane = lane_id(), x = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), x = lane & 15, q = lane >> 4;
     const int head0 = blockIdx.y * Ti::kHeads, mine = wave / Ti::kWavesPerHead, head = head0 + mine;
     const int slice = wave % Ti::kWavesPerHead * kSlice;
     const bool live = head < p.heads;
@@ -297,25 +313,37 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
     Ti::clear(tb);
     Ti::clear(tc);
     State<T, D> state;
-    if (live && p.start != nullptr) state.read(p.start + ((long)seg.slot * p.heads + head) * (D * D), slice, p.rs, p.cs);
-    else if (live && p.first != nullptr) state.read(p.first + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs, p.cs);
+    if (live && p.start != nullptr) state.read(p.start + ((long)seg.slot * p.heads + head) * (D * D), slice, p.rs);
+    else if (live && p.first != nullptr) state.read(p.first + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs);
     else state.clear();
     float unit = 1.0f, bound_s = 0.0f, at = 0.0f, bt = 0.0f, ct = 0.0f;
     if constexpr (Ti::kNormalise) bound_s = state.top();
 
     typename Ti::Regs ra, rb, rc;
-    Ti::load(ra, p.a, seg, p.reverse, 0, head0, p.heads, p.ga, 0);
-    Ti::load(rb, p.b, seg, p.reverse, 0, head0, p.heads, p.gb, 0);
-    Ti::load(rc, p.c, seg, p.reverse, 0, head0, p.heads, p.gb, 0);
-    float g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+    float g = 0.0f;
+    const int heads = p.heads - head0;
+    const unsigned oa = Ti::offset(p.a, p.reverse, p.ga), ob = Ti::offset(p.b, p.reverse, p.gb), oc = Ti::offset(p.c, p.reverse, p.gb);
+    auto tile_at = [&](const Heads& h, long u, int per, int sub) {
+        return h.p + Ti::token(seg, p.reverse, u) * h.ts + ((long)head0 * per + sub) * h.hs;
+    };
+    auto fetch = [&](long u, int sub) {
+        const int rows = (int)min(len - u, (long)kChunk);
+        if (sub == 0 || p.ga > 1) Ti::load(ra, tile_at(p.a, u, p.ga, p.ga > 1 ? sub : 0), oa, p.a, p.reverse, rows, heads);
+        if (sub == 0 || p.gb > 1) {
+            Ti::load(rb, tile_at(p.b, u, p.gb, p.gb > 1 ? sub : 0), ob, p.b, p.reverse, rows, heads);
+            Ti::load(rc, tile_at(p.c, u, p.gb, p.gb > 1 ? sub : 0), oc, p.c, p.reverse, rows, heads);
+        }
+        if (sub == 0) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, u + lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+    };
+    if (steps > 0) fetch(0, 0);
     f32x4 o[4][2];
     __syncthreads();
-    for (int it = 0; it < steps; ++it) {
-        const int sub = it % group;
+    int sub = 0, next_sub = 0;
+    long first = 0;
+    for (int it = 0; it < steps; ++it, first += next_sub == 0 ? kChunk : 0, sub = next_sub) {
         const bool new_a = sub == 0 || p.ga > 1, new_b = sub == 0 || p.gb > 1;      // (one of ga, gb is 1)
         const bool begins = new_a, ends = p.gb == 1 || sub == group - 1;            // of an output's sum
         const bool feeds = p.ga == 1 || sub == group - 1;                           // the state
-        const long first = (long)(it / group) * kChunk;
         unsigned* top = tops + (it & 1) * 12;
         unsigned ma = 0, mb = 0, mc = 0;
         if (new_a) ma = Ti::store(ra, ta, p.a.relu);
@@ -330,15 +358,26 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
         }
         if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, g, p.reverse, p.in_scale, p.weight_scale, Ti::kNormalise);
         __syncthreads();
-        if (it + 1 < steps) {
-            const long then = (long)((it + 1) / group) * kChunk;
-            const int next = (it + 1) % group;
-            if (next == 0 || p.ga > 1) Ti::load(ra, p.a, seg, p.reverse, then, head0, p.heads, p.ga, p.ga > 1 ? next : 0);
-            if (next == 0 || p.gb > 1) {
-                Ti::load(rb, p.b, seg, p.reverse, then, head0, p.heads, p.gb, p.gb > 1 ? next : 0);
-                Ti::load(rc, p.c, seg, p.reverse, then, head0, p.heads, p.gb, p.gb > 1 ? next : 0);
+        // Rows 16i + x of out lie at one offset from an address of the chunk, as they were loaded.  What they are masked with is asked for before
+        // the next tiles: loads return in order.
+        const int rows = (int)min(len - first, (long)kChunk);
+        const long t0 = Ti::token(seg, p.reverse, first), back = p.reverse ? -15 : 0, step = p.reverse ? -16 : 16;
+        const int xr = p.reverse ? 15 - x : x;
+        Vec mv[MASKED ? 4 : 1][8 / kVec];
+        if constexpr (MASKED) {
+            if (ends && live) {
+                const char* mp = p.m.p + (t0 + back) * p.m.ts + (head * p.ga + (p.ga > 1 ? sub : 0)) * p.m.hs + slice * (int)sizeof(T);
+                const unsigned om = (unsigned)xr * (unsigned)p.m.ts + 16 * q;
+#pragma unroll
+                for (int i = 0; i < 4; ++i, mp += step * p.m.ts)
+#pragma unroll
+                    for (int v = 0; v < 8 / kVec; ++v)
+                        if (16 * i + x < rows && (D >= 32 || (kVec == 8 ? 8 * q : 16 * v + 4 * q) < D)) mv[i][v] = *(const Vec*)(mp + om + 64 * v);
             }
-            if (next == 0) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, then + lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+        }
+        if (it + 1 < steps) {
+            next_sub = sub + 1 == group ? 0 : sub + 1;
+            fetch(first + (next_sub == 0 ? kChunk : 0), next_sub);
         }
         const Gates& gt = gates[mine];
         const char* ha = ta + mine * Ti::kHeadBytes;
@@ -370,6 +409,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
 #pragma unroll
                         for (int k = 0; k < kParts<T>; ++k) o[i][n] = Tr::mma_vec(o[i][n], part[n][k], va);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -431,6 +471,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
                     for (int k = 0; k < kParts<T>; ++k) o[i][n] = Tr::mma_vec(o[i][n], vt[st][n], part[k]);
+                __builtin_amdgcn_sched_barrier(0);
             });
         });
         if constexpr (Ti::kNormalise) {
@@ -442,6 +483,43 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
                     for (int n = 0; n < 2; ++n)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) o[i][n][r] *= back;
+            }
+        }
+        if (ends && live) {
+            const int ho = head * p.ga + (p.ga > 1 ? sub : 0);
+            char* out = p.out + (t0 + back) * p.out_ts + ho * p.out_hs + slice * (int)sizeof(T);
+            const unsigned oo = (unsigned)xr * (unsigned)p.out_ts + 16 * q;
+#pragma unroll
+            for (int i = 0; i < 4; ++i, out += step * p.out_ts) {
+                const bool row = 16 * i + x < rows;
+                float dot = 0.0f;
+#pragma unroll
+                for (int v = 0; v < 8 / kVec; ++v) {            // 16 bytes at a time: channels 8q.. (fp32: 16v + 4q..) of the slice
+                    if (!row || (D < 32 && (kVec == 8 ? 8 * q : 16 * v + 4 * q) >= D)) continue;
+                    float w[kVec];
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) w[e] = kVec == 8 ? o[i][e / 4][e % 4] : o[i][v][e];
+                    if constexpr (MASKED) {
+#pragma unroll
+                        for (int e = 0; e < kVec; ++e) {
+                            const float me = Tr::to_f32(mv[i][v][e]);
+                            if (p.m.relu && !(me > 0.0f)) w[e] = 0.0f;
+                            dot = fmaf(me, w[e], dot);
+                        }
+                    }
+                    Vec r;
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) r[e] = Tr::from_f32(w[e]);
+                    *(Vec*)(out + oo + 64 * v) = r;
+                }
+                if constexpr (MASKED) {
+                    if (p.dots != nullptr) {
+                        dot += __shfl_xor(dot, 16);
+                        dot += __shfl_xor(dot, 32);
+                        if (q == 0 && row)
+                            p.dots[((t0 + (p.reverse ? -(16 * i + x) : 16 * i + x)) * (p.heads * p.ga) + ho) * Ti::kWavesPerHead + wave % Ti::kWavesPerHead] = dot;
+                    }
+                }
             }
         }
         // the state behind the chunk
@@ -459,46 +537,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
             if (decays || Ti::kNormalise) state.scale(factor);
             state.add(hb, vt, gt.weight, unit);
         }
-        if (ends && live) {
-            const int ho = head * p.ga + (p.ga > 1 ? sub : 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const long u = first + 16 * i + x;
-                const bool row = u < len;
-                const long t = row ? Ti::token(seg, p.reverse, u) : 0;
-                float dot = 0.0f;
-#pragma unroll
-                for (int v = 0; v < 8 / kVec; ++v) {            // 16 bytes at a time
-                    const int ch = slice + (kVec == 8 ? 8 * q : 16 * v + 4 * q);
-                    if (!row || (D < 32 && ch >= D)) continue;
-                    float w[kVec];
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e) w[e] = kVec == 8 ? o[i][e / 4][e % 4] : o[i][v][e];
-                    if (p.m.p != nullptr) {
-                        const Vec mv = *(const Vec*)((const T*)p.m.p + t * p.m.ts + (long)ho * p.m.hs + ch);
-#pragma unroll
-                        for (int e = 0; e < kVec; ++e) {
-                            const float me = Tr::to_f32(mv[e]);
-                            if (p.m.relu && !(me > 0.0f)) w[e] = 0.0f;
-                            dot = fmaf(me, w[e], dot);
-                        }
-                    }
-                    Vec r;
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e) r[e] = Tr::from_f32(w[e]);
-                    *(Vec*)((T*)p.out + t * p.out_ts + (long)ho * p.out_hs + ch) = r;
-                }
-                if (p.dots != nullptr) {
-                    dot += __shfl_xor(dot, 16);
-                    dot += __shfl_xor(dot, 32);
-                    if (q == 0 && row) p.dots[(t * (p.heads * p.ga) + ho) * Ti::kWavesPerHead + wave % Ti::kWavesPerHead] = dot;
-                }
-            }
-        }
         __syncthreads();
     }
     if (live && p.last != nullptr && seg.index == (p.reverse ? 0 : seg.count - 1))
-        state.write(p.last + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs, p.cs, 1.0f / unit);
+        state.write(p.last + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs, 1.0f / unit);
 }
 
 // d log_gate of a segment's tokens and one head: from the segment's end, x_t = q_t . dq_t - k_t . dk_t summed up, on top of
@@ -559,7 +601,7 @@ struct StepArgs {
     long gate_ts;
     const float* state;
     float* fresh;
-    void* out;
+    char* out;
     long out_ts, out_hs;
     long units;                     // sequences * heads
     int heads, group;
@@ -589,8 +631,8 @@ __global__ void __launch_bounds__(kThreads) recurrence_step_kernel(StepArgs p) {
         s[i] = f32x4{0, 0, 0, 0};
         if (live && from != nullptr) s[i] = *(const f32x4*)(from + (row0 + i * kRowLanes) * D);
     }
-    const T* kp = (const T*)p.k.p + b * p.k.ts + h * p.k.hs;
-    const f32x4 v = frag_to_f32<T>(load_frag<T>((const T*)p.v.p + b * p.v.ts + h * p.v.hs + col));
+    const T* kp = (const T*)(p.k.p + b * p.k.ts + h * p.k.hs);
+    const f32x4 v = frag_to_f32<T>(load_frag<T>((const T*)(p.v.p + b * p.v.ts + h * p.v.hs) + col));
     float keep = 1.0f;
     if (p.gate != nullptr) {
         const float g = (float)((const T*)p.gate)[b * p.gate_ts + h];
@@ -605,7 +647,7 @@ __global__ void __launch_bounds__(kThreads) recurrence_step_kernel(StepArgs p) {
         if (live) *(f32x4*)(p.fresh + (b * p.heads + h) * (D * D) + (row0 + i * kRowLanes) * D + col) = s[i];
     }
     for (int g = 0; g < p.group; ++g) {
-        const T* qp = (const T*)p.q.p + b * p.q.ts + (h * p.group + g) * p.q.hs;
+        const T* qp = (const T*)(p.q.p + b * p.q.ts + (h * p.group + g) * p.q.hs);
         f32x4 o = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
@@ -618,7 +660,7 @@ __global__ void __launch_bounds__(kThreads) recurrence_step_kernel(StepArgs p) {
         for (int d = kLanes; d < 64; d *= 2)
 #pragma unroll
             for (int r = 0; r < 4; ++r) o[r] += __shfl_xor(o[r], d);
-        T* out = (T*)p.out + b * p.out_ts + (h * p.group + g) * p.out_hs + col;
+        T* out = (T*)(p.out + b * p.out_ts + (h * p.group + g) * p.out_hs) + col;
         if constexpr (kRowLanes * kLanes <= 64) {
             if (live && row0 == 0) {
 #pragma unroll
@@ -667,15 +709,20 @@ hipError_t launch_state(const StateArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-template <class T, int D>
-hipError_t launch_sweep(const SweepArgs& a, hipStream_t stream) {
+template <class T, int D, bool MASKED>
+hipError_t launch_sweep_as(const SweepArgs& a, hipStream_t stream) {
     static unsigned long long done = 0;
     constexpr int bytes = tile_lds<T, D>(3);
-    hipError_t e = allow_lds(&recurrence_sweep_kernel<T, D>, bytes, &done);
+    hipError_t e = allow_lds(&recurrence_sweep_kernel<T, D, MASKED>, bytes, &done);
     if (e != hipSuccess) return e;
     const dim3 grid(a.layout.slots, (a.heads + Tile<T, D>::kHeads - 1) / Tile<T, D>::kHeads);
-    hipLaunchKernelGGL((recurrence_sweep_kernel<T, D>), grid, dim3(kThreads), bytes, stream, a);
+    hipLaunchKernelGGL((recurrence_sweep_kernel<T, D, MASKED>), grid, dim3(kThreads), bytes, stream, a);
     return hipGetLastError();
+}
+
+template <class T, int D>
+hipError_t launch_sweep(const SweepArgs& a, hipStream_t stream) {
+    return a.m.p != nullptr ? launch_sweep_as<T, D, true>(a, stream) : launch_sweep_as<T, D, false>(a, stream);
 }
 
 hipError_t launch_join(float* own, const float* decay, const float* first, const Layout& l, int heads, int size, int reverse, hipStream_t stream) {
@@ -684,7 +731,13 @@ hipError_t launch_join(float* own, const float* decay, const float* first, const
     return hipGetLastError();
 }
 
-Heads heads_of(const RecurrenceRows& r, int relu) { return Heads{r.p, r.ts, r.hs, relu}; }
+template <class T>
+Heads heads_of(const RecurrenceRows& r, int relu) {
+    return Heads{(const char*)r.p, r.ts * (long)sizeof(T), r.hs * (long)sizeof(T), relu};
+}
+// ... of an output: pointer and strides
+#define MSLA_OUT(r) (char*)(r).p, (r).ts * (long)sizeof(T), (r).hs * (long)sizeof(T)
+
 
 Layout layout_of(const RecurrenceCall& c) {
     return Layout{c.offsets, c.sequences, c.tokens, c.plan.segment, c.plan.slots};
@@ -699,17 +752,17 @@ Layout layout_of(const RecurrenceCall& c) {
 template <class T, int D>
 hipError_t forward_of(const RecurrenceCall& c, hipStream_t stream) {
     const Layout l = layout_of(c);
-    const Heads q = heads_of(c.q, c.rectify), k = heads_of(c.k, c.rectify), v = heads_of(c.v, 0);
+    const Heads q = heads_of<T>(c.q, c.rectify), k = heads_of<T>(c.k, c.rectify), v = heads_of<T>(c.v, 0);
     const float* start = nullptr;
     if (c.plan.cut) {
         float* own = (float*)c.ws;
         float* decay = (float*)(c.ws + c.plan.decay_at);
-        MSLA_TRY((launch_state<T, D>(StateArgs{k, v, c.gate, c.gate_ts, own, decay, D, 1, l, c.heads_kv, 1, 0, 1.0f}, stream)));
+        MSLA_TRY((launch_state<T, D>(StateArgs{k, v, c.gate, c.gate_ts, own, decay, D, l, c.heads_kv, 1, 0, 1.0f}, stream)));
         MSLA_TRY(launch_join(own, decay, c.initial, l, c.heads_kv, D * D, 0, stream));
         start = own;
     }
-    return launch_sweep<T, D>(SweepArgs{q, k, v, c.out.p, c.out.ts, c.out.hs, Heads{nullptr, 0, 0, 0}, nullptr, c.gate, c.gate_ts, start,
-                                        c.initial, c.final_state, D, 1, l, c.heads_kv, c.heads_q / c.heads_kv, 1, 0, c.scale, c.scale, 1.0f},
+    return launch_sweep<T, D>(SweepArgs{q, k, v, MSLA_OUT(c.out), Heads{nullptr, 0, 0, 0}, nullptr, c.gate, c.gate_ts, start,
+                                        c.initial, c.final_state, D, l, c.heads_kv, c.heads_q / c.heads_kv, 1, 0, c.scale, c.scale, 1.0f},
                               stream);
 }
 
@@ -717,7 +770,7 @@ template <class T, int D>
 hipError_t backward_of(const RecurrenceCall& c, hipStream_t stream) {
     const Layout l = layout_of(c);
     const int group = c.heads_q / c.heads_kv;
-    const Heads q = heads_of(c.q, c.rectify), k = heads_of(c.k, c.rectify), v = heads_of(c.v, 0), d_o = heads_of(c.d_out, 0);
+    const Heads q = heads_of<T>(c.q, c.rectify), k = heads_of<T>(c.k, c.rectify), v = heads_of<T>(c.v, 0), d_o = heads_of<T>(c.d_out, 0);
     const Heads no = {nullptr, 0, 0, 0};
     float* s_own = nullptr;
     float* d_own = nullptr;
@@ -726,8 +779,8 @@ hipError_t backward_of(const RecurrenceCall& c, hipStream_t stream) {
         d_own = (float*)(c.ws + c.plan.d_states_at);
         float* decay = (float*)(c.ws + c.plan.decay_at);
         float* d_decay = (float*)(c.ws + c.plan.d_decay_at);
-        MSLA_TRY((launch_state<T, D>(StateArgs{k, v, c.gate, c.gate_ts, s_own, decay, D, 1, l, c.heads_kv, 1, 0, 1.0f}, stream)));
-        MSLA_TRY((launch_state<T, D>(StateArgs{q, d_o, c.gate, c.gate_ts, d_own, d_decay, D, 1, l, c.heads_kv, group, 1, c.scale}, stream)));
+        MSLA_TRY((launch_state<T, D>(StateArgs{v, k, c.gate, c.gate_ts, s_own, decay, 1, l, c.heads_kv, 1, 0, 1.0f}, stream)));
+        MSLA_TRY((launch_state<T, D>(StateArgs{d_o, q, c.gate, c.gate_ts, d_own, d_decay, 1, l, c.heads_kv, group, 1, c.scale}, stream)));
         MSLA_TRY(launch_join(s_own, decay, c.initial, l, c.heads_kv, D * D, 0, stream));
         MSLA_TRY(launch_join(d_own, d_decay, c.d_final, l, c.heads_kv, D * D, 1, stream));
     }
@@ -735,12 +788,10 @@ hipError_t backward_of(const RecurrenceCall& c, hipStream_t stream) {
     float* k_dots = c.d_gate ? q_dots + c.tokens * c.heads_q * Tile<T, D>::kWavesPerHead : nullptr;
     float* last = c.d_gate && c.d_final ? (float*)(c.ws + c.plan.last_at) : nullptr;
     const Heads mq = c.d_gate || c.rectify ? q : no, mk = c.d_gate || c.rectify ? k : no;
-    MSLA_TRY((launch_sweep<T, D>(SweepArgs{d_o, v, k, c.d_q.p, c.d_q.ts, c.d_q.hs, mq, q_dots, c.gate, c.gate_ts, s_own, c.initial, last, 1, D, l,
+    MSLA_TRY((launch_sweep<T, D>(SweepArgs{d_o, v, k, MSLA_OUT(c.d_q), mq, q_dots, c.gate, c.gate_ts, s_own, c.initial, last, 1, l,
                                            c.heads_kv, group, 1, 0, c.scale, c.scale, 1.0f}, stream)));
-    MSLA_TRY((launch_sweep<T, D>(SweepArgs{v, d_o, q, c.d_k.p, c.d_k.ts, c.d_k.hs, mk, k_dots, c.gate, c.gate_ts, d_own, c.d_final, nullptr, 1, D,
-                                           l, c.heads_kv, 1, group, 1, c.scale, 1.0f, c.scale}, stream)));
-    MSLA_TRY((launch_sweep<T, D>(SweepArgs{k, q, d_o, c.d_v.p, c.d_v.ts, c.d_v.hs, no, nullptr, c.gate, c.gate_ts, d_own, c.d_final, c.d_initial, D,
-                                           1, l, c.heads_kv, 1, group, 1, c.scale, 1.0f, c.scale}, stream)));
+    MSLA_TRY((launch_sweep<T, D>(SweepArgs{v, d_o, q, MSLA_OUT(c.d_k), mk, k_dots, c.gate, c.gate_ts, d_own, c.d_final, nullptr, 1, l, c.heads_kv, 1, group, 1, c.scale, 1.0f, c.scale}, stream)));
+    MSLA_TRY((launch_sweep<T, D>(SweepArgs{k, q, d_o, MSLA_OUT(c.d_v), no, nullptr, c.gate, c.gate_ts, d_own, c.d_final, c.d_initial, D, l, c.heads_kv, 1, group, 1, c.scale, 1.0f, c.scale}, stream)));
     if (c.d_gate) {
         hipLaunchKernelGGL((recurrence_gate_kernel<T>), dim3(l.slots, c.heads_kv), dim3(kThreads), 0, stream, q_dots, k_dots,
                            Tile<T, D>::kWavesPerHead, s_own, d_own, last, c.d_final, (T*)c.d_gate, c.d_gate_ts, l, c.heads_kv, group, D * D);
@@ -755,8 +806,8 @@ hipError_t step_of(const RecurrenceCall& c, hipStream_t stream) {
     const long units = (long)c.sequences * c.heads_kv;
     const long blocks = (units + kUnits - 1) / kUnits * (D / kCols);
     hipLaunchKernelGGL((recurrence_step_kernel<T, D>), dim3((unsigned)blocks), dim3(kThreads), 0, stream,
-                       StepArgs{heads_of(c.q, c.rectify), heads_of(c.k, c.rectify), heads_of(c.v, 0), c.gate, c.gate_ts, c.initial,
-                                c.final_state, c.out.p, c.out.ts, c.out.hs, units, c.heads_kv, c.heads_q / c.heads_kv, c.scale});
+                       StepArgs{heads_of<T>(c.q, c.rectify), heads_of<T>(c.k, c.rectify), heads_of<T>(c.v, 0), c.gate, c.gate_ts, c.initial,
+                                c.final_state, MSLA_OUT(c.out), units, c.heads_kv, c.heads_q / c.heads_kv, c.scale});
     return hipGetLastError();
 }
 

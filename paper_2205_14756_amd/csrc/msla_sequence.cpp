@@ -81,6 +81,14 @@ msla_status plan_of(const msla_recurrence& s, bool backward, RecurrencePlan* pla
     return MSLA_OK;
 }
 
+// Strides that the kernels' 32-bit offsets inside a chunk of 64 tokens cover, in bytes.
+constexpr int64_t kMostTokenStride = (int64_t)1 << 26, kMostHeadStride = (int64_t)1 << 29;
+
+bool wide(const msla_heads& h, msla_dtype dt) {
+    const int64_t e = (int64_t)elem_size(dt);
+    return h.token_stride * e > kMostTokenStride || h.head_stride * e > kMostHeadStride;
+}
+
 // a [tokens, heads, head_dim] operand: 16-byte pieces, no span beyond kMost
 bool fits(const msla_heads& h, const msla_recurrence& s, int heads, msla_dtype dt) {
     if (s.tokens == 0) return true;
@@ -152,6 +160,7 @@ msla_status msla_recurrence_forward(const msla_recurrence* shape, msla_heads q, 
         !apart(out, s, s.heads_q) || !gate_fits(log_gate, gate_stride, s, dt, false) || !aligned(initial_state, 16) ||
         !aligned(final_state, 16) || same(out, q) || same(out, k) || same(out, v))
         return MSLA_ERR_INVALID_ARG;
+    if (wide(q, dt) || wide(k, dt) || wide(v, dt) || wide(out, dt)) return MSLA_ERR_UNSUPPORTED;
     RecurrenceCall c = {};
     st = plan_of(s, false, &c.plan);
     if (st != MSLA_OK) return st;
@@ -184,6 +193,8 @@ msla_status msla_recurrence_backward(const msla_recurrence* shape, msla_heads q,
         for (const msla_heads* i : {&q, &k, &v, &d_out})
             if (same(*o, *i)) return MSLA_ERR_INVALID_ARG;
     if (same(d_q, d_k) || same(d_q, d_v) || same(d_k, d_v)) return MSLA_ERR_INVALID_ARG;
+    for (const msla_heads* h : {&q, &k, &v, &d_out, &d_q, &d_k, &d_v})
+        if (wide(*h, dt)) return MSLA_ERR_UNSUPPORTED;
     RecurrenceCall c = {};
     st = plan_of(s, true, &c.plan);
     if (st != MSLA_OK) return st;
@@ -213,6 +224,7 @@ msla_status msla_recurrence_step(const msla_recurrence* shape, msla_heads q, msl
         !apart(out, s, s.heads_q) || !gate_fits(log_gate, gate_stride, s, dt, false) || !aligned(state, 16) || !aligned(new_state, 16) ||
         same(out, q) || same(out, k) || same(out, v))
         return MSLA_ERR_INVALID_ARG;
+    if (wide(q, dt) || wide(k, dt) || wide(v, dt) || wide(out, dt)) return MSLA_ERR_UNSUPPORTED;
     RecurrenceCall c = {};
     fill(&c, s, q, k, v, log_gate, gate_stride, state);
     c.what = 2;

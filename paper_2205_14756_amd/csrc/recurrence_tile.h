@@ -22,8 +22,8 @@ constexpr int kThreads = 256;
 constexpr int kSlice = 32;          // output channels of a wave
 
 struct Heads {
-    const void* p;
-    long ts, hs;                    // strides of a token and a head, in elements
+    const char* p;
+    long ts, hs;                    // bytes from a token, and a head, to the next (at most 2^26 and 2^29)
     int relu;
 };
 
@@ -88,7 +88,8 @@ struct Tile {
     static constexpr int kBlocks = kPad / 16;                   // blocks of 16 key channels
     static constexpr int kJoin = kVec / 4;                      // results that make one operand
     static constexpr int kPerRow = kHeads * (D / kVec);         // 16-byte pieces of a tile's row
-    static constexpr int kPieces = (kChunk * kPerRow + kThreads - 1) / kThreads;
+    static constexpr int kPieces = kChunk * kPerRow / kThreads;     // of a thread
+    static_assert(kChunk * kPerRow % kThreads == 0 && kThreads % kPerRow == 0, "whole rows a pass");
     static constexpr bool kNormalise = std::is_same<T, _Float16>::value;
 
     struct Regs { u32x4 v[kPieces]; };
@@ -98,50 +99,65 @@ struct Tile {
         return sizeof(T) == 2 ? 32 * (blk >> 1) + 8 * (m >> 2) + 4 * (blk & 1) + (m & 3) : 16 * blk + m;
     }
 
-    // row u of the segment's chunk `first` .. : token lo + u, or from the segment's end
+    static constexpr int kRowStep = kThreads / kPerRow;         // rows between a thread's pieces
+
     static __device__ __forceinline__ long token(const Segment& s, int reverse, long u) { return reverse ? s.hi - 1 - u : s.lo + u; }
 
-    static __device__ __forceinline__ void load(Regs& r, const Heads& h, const Segment& s, int reverse, long first, int head0, int heads, int per,
-                                                int g) {
-        const long len = s.hi - s.lo;
+    // A thread's pieces of a tile: rows row() + i * kRowStep, all at one offset from an address that is the same for all threads, so a
+    // piece costs a scalar addition and the load.  The strides' bounds keep the offset in 32 bits.
+    static __device__ __forceinline__ int row() { return threadIdx.x / kPerRow; }
+    static __device__ __forceinline__ int head_of() { return threadIdx.x % kPerRow / (D / kVec); }
+    static __device__ __forceinline__ unsigned offset(const Heads& h, int reverse, int per) {
+        const unsigned r = reverse ? kRowStep - 1 - row() : row();
+        return r * (unsigned)h.ts + (unsigned)(head_of() * per) * (unsigned)h.hs + threadIdx.x % (D / kVec) * 16u;
+    }
+    // `at`: the address of the chunk's first token (from the end: its last) and of the workgroup's first head
+    static __device__ __forceinline__ void load(Regs& r, const char* at, unsigned off, const Heads& h, int reverse, int rows, int heads) {
+        if (reverse) at -= (kRowStep - 1) * h.ts;
+        const long step = (reverse ? -kRowStep : kRowStep) * h.ts;
+        if (rows >= kChunk && heads >= kHeads) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int p = threadIdx.x + i * kThreads;
-            const int row = p / kPerRow, in = p % kPerRow;
-            const int hl = in / (D / kVec), ch = in % (D / kVec) * kVec;
-            r.v[i] = u32x4{0, 0, 0, 0};
-            if (row < kChunk && first + row < len && head0 + hl < heads)
-                r.v[i] = *(const u32x4*)((const T*)h.p + token(s, reverse, first + row) * h.ts + ((long)(head0 + hl) * per + g) * h.hs + ch);
+            for (int i = 0; i < kPieces; ++i) {
+                r.v[i] = *(const u32x4*)(at + off);
+                at += step;
+            }
+        } else {
+            const bool mine = head_of() < heads;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                r.v[i] = u32x4{0, 0, 0, 0};
+                if (mine && row() + i * kRowStep < rows) r.v[i] = *(const u32x4*)(at + off);
+                at += step;
+            }
         }
     }
 
     // into LDS, rectified where asked; returns the largest bit pattern of a finite magnitude (fp16 alone; a value that is not finite may
     // not spoil the other heads' normalisers)
-    static __device__ __forceinline__ unsigned store(const Regs& r, char* tile, int relu) {
+    static __device__ __forceinline__ unsigned store(Regs& r, char* tile, int relu) {
         typedef short i16x8 __attribute__((ext_vector_type(8)));
         typedef int i32x4 __attribute__((ext_vector_type(4)));
         unsigned top = 0;
+        if (relu) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                if constexpr (sizeof(T) == 2)
+                    r.v[i] = __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(i16x8, r.v[i]), i16x8{0, 0, 0, 0, 0, 0, 0, 0}));
+                else
+                    r.v[i] = __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(i32x4, r.v[i]), i32x4{0, 0, 0, 0}));
+            }
+        }
+        char* at = tile + head_of() * kHeadBytes + row() * kPitch + threadIdx.x % (D / kVec) * 16;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int p = threadIdx.x + i * kThreads;
-            const int row = p / kPerRow, in = p % kPerRow;
-            const int hl = in / (D / kVec), ch = in % (D / kVec) * kVec;
-            u32x4 v = r.v[i];
-            if constexpr (sizeof(T) == 2) {
-                const short f = relu ? 0 : -32768;
-                v = __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(i16x8, v), i16x8{f, f, f, f, f, f, f, f}));
-            } else {
-                const int f = relu ? 0 : (int)0x80000000;
-                v = __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(i32x4, v), i32x4{f, f, f, f}));
-            }
             if constexpr (kNormalise) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const unsigned lo = v[j] & 0x7fffu, hi = (v[j] >> 16) & 0x7fffu;
+                    const unsigned lo = r.v[i][j] & 0x7fffu, hi = (r.v[i][j] >> 16) & 0x7fffu;
                     top = max(top, max(lo < 0x7c00u ? lo : 0u, hi < 0x7c00u ? hi : 0u));
                 }
             }
-            if (row < kChunk) *(u32x4*)(tile + hl * kHeadBytes + row * kPitch + ch * (int)sizeof(T)) = v;
+            *(u32x4*)(at + i * kRowStep * kPitch) = r.v[i];
         }
         return top;
     }
@@ -213,33 +229,49 @@ struct Gates {
 
 constexpr double kLog2e = 1.4426950408889634;
 
+// v of the lane that a data-parallel move takes it from; 0 where it takes none
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double v) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, ROWS, 0xf, false);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+// sum over this lane and those before it
+__device__ __forceinline__ double running_sum(double v) {
+    v += moved<0x111, 0xf>(v);      // row_shr 1, 2, 4, 8: within 16 lanes
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);      // row_bcast 15: the last lane of rows 0 and 2 to rows 1 and 3
+    v += moved<0x143, 0xc>(v);      // row_bcast 31: that of row 1 to rows 2 and 3
+    return v;
+}
+
 // by one wave; `g`: this lane's row's gate (0 where there is no row)
 __device__ __forceinline__ void run_gates(Gates* out, float g, int reverse, float in_scale, float weight_scale, bool want_grow) {
     const int lane = lane_id();
     double own = (double)g * kLog2e;
     if (own < -150.0) own = -150.0;         // 2^-150 is 0 in fp32; a NaN stays one
-    double sum = own;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double up = __shfl_up(sum, d);
-        if (lane >= d) sum += up;
-    }
-    const double total = __shfl(sum, 63);
+    const double sum = running_sum(own);
+    const unsigned long long last = __builtin_bit_cast(unsigned long long, sum);
+    const double total = __builtin_bit_cast(double, (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(last >> 32), 63) << 32 |
+                                                        (unsigned)__builtin_amdgcn_readlane((int)(unsigned)last, 63));
     const double here = reverse ? sum - own : sum;
-    const float hi = (float)here;
+    const float hi = (float)here, lo = (float)(here - (double)hi);
     out->hi[lane] = hi;
-    out->lo[lane] = (float)(here - (double)hi);
-    out->in[lane] = __builtin_amdgcn_exp2f(hi) * fmaf(out->lo[lane], 0.693147182f, 1.0f) * in_scale;
+    out->lo[lane] = lo;
+    out->in[lane] = __builtin_amdgcn_exp2f(hi) * fmaf(lo, 0.693147182f, 1.0f) * in_scale;
     out->weight[lane] = __builtin_amdgcn_exp2f((float)(total - here)) * weight_scale;
-    float grow = own > 0.0 ? (float)own : 0.0f;
-    if (want_grow) {
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) grow += __shfl_xor(grow, d);
-    }
     if (lane == 0) {
         out->total = __builtin_amdgcn_exp2f((float)total);
-        out->grow = __builtin_amdgcn_exp2f(grow);
         out->exponent = (float)total;
+    }
+    if (want_grow) {
+        float grow = own > 0.0 ? (float)own : 0.0f;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) grow += __shfl_xor(grow, d);
+        if (lane == 0) out->grow = __builtin_amdgcn_exp2f(grow);
     }
 }
 
