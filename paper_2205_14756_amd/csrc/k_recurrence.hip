@@ -151,13 +151,18 @@ struct State {
                 for (int e = 0; e < Ti::kVec; ++e) v[e] = Ti::Tr::to_f32(vt[st][n][e]) * w[e];
                 Ti::template split<kStateParts<T>>(v, part[n]);
             }
+            // (the next block's operand is on its way while this one's products run)
+            typename Ti::Vec kt = Ti::token_operand(tb, 0, st, x, q);
 #pragma unroll
             for (int b = 0; b < Ti::kBlocks; ++b) {
-                const typename Ti::Vec kt = Ti::token_operand(tb, b, st, x, q);
+                typename Ti::Vec next = kt;
+                if (b + 1 < Ti::kBlocks) next = Ti::token_operand(tb, b + 1, st, x, q);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int p = 0; p < kStateParts<T>; ++p)
 #pragma unroll
-                    for (int p = 0; p < kStateParts<T>; ++p) s[b][n] = Ti::Tr::mma_vec(s[b][n], kt, part[n][p]);
+                    for (int n = 0; n < 2; ++n) s[b][n] = Ti::Tr::mma_vec(s[b][n], kt, part[n][p]);
+                kt = next;
             }
         }
     }
@@ -299,6 +304,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
     char* tc = tb + Ti::kBytes;
     Gates* gates = (Gates*)(tc + Ti::kBytes);
     unsigned* tops = (unsigned*)(gates + Ti::kHeads);
+    char* scores = (char*)(tops + 24);
 
     const Segment seg = find_segment(p.layout, blockIdx.x);
     if (!seg.live) return;
@@ -312,6 +318,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
     Ti::clear(ta);
     Ti::clear(tb);
     Ti::clear(tc);
+    // (the upper halves of the steps of blocks 0 and 2 are above the diagonal, and stay zero)
+    if constexpr (Ti::kShare)
+        for (int i = threadIdx.x * 16; i < Ti::kScoreBytes; i += kThreads * 16) *(u32x4*)(scores + i) = u32x4{0, 0, 0, 0};
     State<T, D> state;
     if (live && p.start != nullptr) state.read(p.start + ((long)seg.slot * p.heads + head) * (D * D), slice, p.rs);
     else if (live && p.first != nullptr) state.read(p.first + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs);
@@ -358,8 +367,85 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
         }
         if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, g, p.reverse, p.in_scale, p.weight_scale, Ti::kNormalise);
         __syncthreads();
+        const Gates& gt = gates[mine];
+        const char* ha = ta + mine * Ti::kHeadBytes;
+        char* hb = tb + mine * Ti::kHeadBytes;
+        char* hc = tc + mine * Ti::kHeadBytes;
+        if constexpr (Ti::kNormalise) {
+            if (new_a) at = tile_top(top);
+            if (new_b) {
+                bt = tile_top(top + 1);
+                ct = tile_top(top + 2);
+            }
+        }
+        // scores, where the waves of a head share them
+        float fp = 1.0f;
+        if constexpr (Ti::kNormalise) fp = normaliser(fabsf(p.score_scale) * (float)Ti::kPad * at * bt * gt.grow);
+        if constexpr (Ti::kShare) {
+            // blocks 0, 1, .. of the lower triangle's ten, row by row: every fourth is this wave's
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                const int at_ = wave + 4 * k;
+                if (k == 2 && at_ >= 10) break;
+                const int i = at_ >= 6 ? 3 : (at_ >= 3 ? 2 : (at_ >= 1 ? 1 : 0)), j = at_ - i * (i + 1) / 2;
+                f32x4 d = {0, 0, 0, 0};
+#pragma unroll
+                for (int s = 0; s < Ti::kSteps; ++s)
+                    d = Tr::mma_vec(d, Ti::row_operand(hb, 16 * j + x, s, q), Ti::row_operand(ha, 16 * i + x, s, q));
+                const float fi = gt.hi[16 * i + x], li = gt.lo[16 * i + x], sc = p.score_scale * fp;
+                const f32x4 fj = *(const f32x4*)(gt.hi + 16 * j + 4 * q), lj = *(const f32x4*)(gt.lo + 16 * j + 4 * q);
+                float w[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float e = __builtin_amdgcn_exp2f((fi - fj[r]) + (li - lj[r]));
+                    w[r] = j < i || 4 * q + r <= x ? d[r] * e * sc : 0.0f;
+                }
+                char* to = scores + Ti::score_step(i, j / Ti::kJoin) * 1024 + lane * 16 + (Ti::kJoin == 2 ? (j & 1) * 8 : 0);
+                Ti::leave_scores(w, to);
+            }
+        }
+        // what the rows take from the state
+        if (begins) {
+            float fs = 1.0f;
+            if constexpr (Ti::kNormalise) fs = normaliser(bound_s * unit);
+#pragma unroll
+            for (int rb_ = 0; rb_ < 4; ++rb_) o[rb_][0] = o[rb_][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < Ti::kSteps; ++s) {
+                Vec va[4], part[2][kParts<T>];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) va[i] = Ti::row_operand(ha, 16 * i + x, s, q);
+#pragma unroll
+                for (int n = 0; n < 2; ++n) state.operand(s, n, fs, part[n]);
+#pragma unroll
+                for (int k = 0; k < kParts<T>; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) o[i][n] = Tr::mma_vec(o[i][n], part[n][k], va[i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float f = gt.in[16 * i + x] / (fs * unit);
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[i][n][r] *= f;
+            }
+        }
+        if constexpr (Ti::kNormalise) {
+            if (fp != 1.0f) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[i][n][r] *= fp;
+            }
+        }
         // Rows 16i + x of out lie at one offset from an address of the chunk, as they were loaded.  What they are masked with is asked for before
-        // the next tiles: loads return in order.
+        // the next tiles: loads return in order.  (Asked for here, and not at once, the tiles do not hold registers through the part above.)
         const int rows = (int)min(len - first, (long)kChunk);
         const long t0 = Ti::token(seg, p.reverse, first), back = p.reverse ? -15 : 0, step = p.reverse ? -16 : 16;
         const int xr = p.reverse ? 15 - x : x;
@@ -379,66 +465,26 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
             next_sub = sub + 1 == group ? 0 : sub + 1;
             fetch(first + (next_sub == 0 ? kChunk : 0), next_sub);
         }
-        const Gates& gt = gates[mine];
-        const char* ha = ta + mine * Ti::kHeadBytes;
-        char* hb = tb + mine * Ti::kHeadBytes;
-        char* hc = tc + mine * Ti::kHeadBytes;
-        if constexpr (Ti::kNormalise) {
-            if (new_a) at = tile_top(top);
-            if (new_b) {
-                bt = tile_top(top + 1);
-                ct = tile_top(top + 2);
-            }
-        }
-        // what the rows take from the state
-        if (begins) {
-            float fs = 1.0f;
-            if constexpr (Ti::kNormalise) fs = normaliser(bound_s * unit);
-#pragma unroll
-            for (int rb_ = 0; rb_ < 4; ++rb_) o[rb_][0] = o[rb_][1] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int s = 0; s < Ti::kSteps; ++s) {
-                Vec part[2][kParts<T>];
-#pragma unroll
-                for (int n = 0; n < 2; ++n) state.operand(s, n, fs, part[n]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const Vec va = Ti::row_operand(ha, 16 * i + x, s, q);
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int k = 0; k < kParts<T>; ++k) o[i][n] = Tr::mma_vec(o[i][n], part[n][k], va);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float f = gt.in[16 * i + x] / (fs * unit);
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[i][n][r] *= f;
-            }
-        }
+        if constexpr (Ti::kShare) __syncthreads();
         // what they take from the chunk's own rows
         Vec vt[Ti::kTokenSteps][2];
 #pragma unroll
         for (int st = 0; st < Ti::kTokenSteps; ++st)
 #pragma unroll
             for (int n = 0; n < 2; ++n) vt[st][n] = Ti::token_operand(hc, slice / 16 + n, st, x, q);
-        float fp = 1.0f;
-        if constexpr (Ti::kNormalise) {
-            fp = normaliser(fabsf(p.score_scale) * (float)Ti::kPad * at * bt * gt.grow);
-            if (fp != 1.0f) {
+        if constexpr (Ti::kShare) {
+            static_for<0, 4>([&](auto i_) {
+                constexpr int i = decltype(i_)::value;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int st = 0; st <= i / Ti::kJoin; ++st)
 #pragma unroll
-                    for (int n = 0; n < 2; ++n)
+                    for (int k = 0; k < kParts<T>; ++k) {
+                        const Vec part = *(const Vec*)(scores + (k * Ti::kScoreSteps + Ti::score_step(i, st)) * 1024 + lane * 16);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) o[i][n][r] *= fp;
-            }
-        }
-        static_for<0, 4>([&](auto i_) {
+                        for (int n = 0; n < 2; ++n) o[i][n] = Tr::mma_vec(o[i][n], vt[st][n], part);
+                    }
+            });
+        } else static_for<0, 4>([&](auto i_) {
             constexpr int i = decltype(i_)::value;
             Vec va[Ti::kSteps];
 #pragma unroll
@@ -712,7 +758,7 @@ hipError_t launch_state(const StateArgs& a, hipStream_t stream) {
 template <class T, int D, bool MASKED>
 hipError_t launch_sweep_as(const SweepArgs& a, hipStream_t stream) {
     static unsigned long long done = 0;
-    constexpr int bytes = tile_lds<T, D>(3);
+    constexpr int bytes = tile_lds<T, D>(3) + Tile<T, D>::kScoreBytes;
     hipError_t e = allow_lds(&recurrence_sweep_kernel<T, D, MASKED>, bytes, &done);
     if (e != hipSuccess) return e;
     const dim3 grid(a.layout.slots, (a.heads + Tile<T, D>::kHeads - 1) / Tile<T, D>::kHeads);

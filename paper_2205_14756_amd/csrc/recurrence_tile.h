@@ -70,6 +70,12 @@ __device__ __forceinline__ Segment find_segment(const Layout& l, int slot) {
     return s;
 }
 
+// Parts of an operand that is not an input.  Scores and the state on its way into an output: two (bf16 2^-17, fp16 2^-23 of the value),
+// below the output's rounding, and small enough that their sums over a segment give the gates' gradient.  What is added to the state,
+// which is handed out in fp32: three in bf16 (2^-25).
+template <class T> constexpr int kParts = sizeof(T) == 4 ? 1 : 2;
+template <class T> constexpr int kStateParts = std::is_same<T, __bf16>::value ? 3 : kParts<T>;
+
 template <class T, int D>
 struct Tile {
     typedef Traits<T> Tr;
@@ -90,6 +96,12 @@ struct Tile {
     static constexpr int kPerRow = kHeads * (D / kVec);         // 16-byte pieces of a tile's row
     static constexpr int kPieces = kChunk * kPerRow / kThreads;     // of a thread
     static_assert(kChunk * kPerRow % kThreads == 0 && kThreads % kPerRow == 0, "whole rows a pass");
+    // Scores of a head are the same for its waves: where there are four, each computes a quarter of them and leaves its parts in LDS as
+    // operands, 1 KB a matrix step and part; where there are fewer, each has them all in registers.
+    static constexpr bool kShare = kWavesPerHead == 4;
+    static constexpr int kScoreSteps = kJoin == 2 ? 6 : 10;     // steps of the lower triangle's four rows of blocks
+    static constexpr int kScoreBytes = kShare ? kScoreSteps * 1024 * (sizeof(T) == 4 ? 1 : 2) : 0;
+    static __device__ __forceinline__ constexpr int score_step(int i, int st) { return kJoin == 2 ? (i < 2 ? i : 2 * i - 2) + st : i * (i + 1) / 2 + st; }
     static constexpr bool kNormalise = std::is_same<T, _Float16>::value;
 
     struct Regs { u32x4 v[kPieces]; };
@@ -190,6 +202,26 @@ struct Tile {
         }
     }
 
+    // four scores as operands' parts: half a step of them (fp32: a whole one) at `to`
+    static __device__ __forceinline__ void leave_scores(const float (&w)[4], char* to) {
+        float rest[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            rest[r] = w[r];
+            if constexpr (kParts<T> > 1) asm("" : "+v"(rest[r]));
+        }
+#pragma unroll
+        for (int p = 0; p < kParts<T>; ++p) {
+            typename Tr::Frag f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                f[r] = Tr::from_f32(rest[r]);
+                if (p + 1 < kParts<T>) rest[r] -= Tr::to_f32(f[r]);
+            }
+            store_frag<T>(to + p * kScoreSteps * 1024, f);
+        }
+    }
+
     // v in PARTS parts of the storage type, each what the ones before left
     template <int PARTS>
     static __device__ __forceinline__ void split(const float (&v)[kVec], Vec (&part)[PARTS]) {
@@ -211,12 +243,6 @@ struct Tile {
         }
     }
 };
-
-// Parts of an operand that is not an input.  Scores and the state on its way into an output: two (bf16 2^-17, fp16 2^-23 of the value),
-// below the output's rounding, and small enough that their sums over a segment give the gates' gradient.  What is added to the state,
-// which is handed out in fp32: three in bf16 (2^-25).
-template <class T> constexpr int kParts = sizeof(T) == 4 ? 1 : 2;
-template <class T> constexpr int kStateParts = std::is_same<T, __bf16>::value ? 3 : kParts<T>;
 
 // A chunk's running gates, in LDS: exponents (base 2) from the chunk's start to each row, as a float and what it leaves out of the
 // double that they are summed in, so that differences stay exact behind a gate that forgets everything.
