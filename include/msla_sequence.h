@@ -27,7 +27,7 @@ extern "C" {
 #endif
 
 /* [token, head, channel] in the storage type: channels next to each other, strides in elements (multiples of 16 bytes; not
- * negative; a token's at most 64 MiB, a head's at most 512 MiB, else MSLA_ERR_UNSUPPORTED).  So heads may be part of a wider row: the map that msla_linear projects with w_qkv's row order is
+ * negative; a token's at most 32 MiB, a head's at most 512 MiB, else MSLA_ERR_UNSUPPORTED).  So heads may be part of a wider row: the map that msla_linear projects with w_qkv's row order is
  * q = {p, 3*Ct, 3*d}, k = {p + d, ...}, v = {p + 2*d, ...}.  An output's rows must not overlap each other. */
 typedef struct {
     void* data;                 /* read only where the operand is an input */

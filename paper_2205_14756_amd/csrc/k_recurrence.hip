@@ -21,6 +21,8 @@
 namespace msla {
 namespace rec {
 
+constexpr int kThreads = 256;        // of the kernels that have no tiles
+
 struct SweepArgs {
     Heads a, b, c;                  // (q; k, v) and its permutations
     char* out;
@@ -51,7 +53,13 @@ struct StateArgs {
 };
 
 // bounds on a tile's magnitudes from what the waves left in LDS (fp16 alone)
-__device__ __forceinline__ float tile_top(const unsigned* top) { return half_bits(max(max(top[0], top[3]), max(top[6], top[9]))); }
+template <int WAVES>
+__device__ __forceinline__ float tile_top(const unsigned* top) {
+    unsigned t = top[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) t = max(t, top[3 * w]);
+    return half_bits(t);
+}
 
 __device__ __forceinline__ void leave_top(unsigned* top, unsigned mine) {
 #pragma unroll
@@ -59,33 +67,24 @@ __device__ __forceinline__ void leave_top(unsigned* top, unsigned mine) {
     if (lane_id() == 0) top[(threadIdx.x >> 6) * 3] = mine;
 }
 
-// The state's part of a wave: rows are all channels of the key, columns the wave's 32 output channels.
+// The state's part of a wave: rows are all channels of the key, columns the wave's 16 output channels.
 template <class T, int D>
 struct State {
     typedef Tile<T, D> Ti;
-    f32x4 s[Ti::kBlocks][2];
+    f32x4 s[Ti::kBlocks];
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int b = 0; b < Ti::kBlocks; ++b)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) s[b][n] = f32x4{0, 0, 0, 0};
+        for (int b = 0; b < Ti::kBlocks; ++b) s[b] = f32x4{0, 0, 0, 0};
     }
-    // In memory a row's or (rs == 1) a column's elements lie next to each other: a lane's four rows are then one access.  Channels that
-    // are padding read as zero and are not written.
+    // In memory a row's or (rs == 1) a column's elements lie next to each other: a lane's four rows are then one access.
     template <class F>
     __device__ __forceinline__ void blocks(int slice, F&& f) {
         const int x = lane_id() & 15, q = lane_id() >> 4;
 #pragma unroll
-        for (int b = 0; b < Ti::kBlocks; ++b)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const int row = Ti::channel(b, 4 * q), col = slice + Ti::channel(n, x);
-                if (D >= 32 || (row < D && col < D)) f(s[b][n], row, col);
-            }
+        for (int b = 0; b < Ti::kBlocks; ++b) f(s[b], Ti::channel(b, 4 * q), slice + x);
     }
     __device__ __forceinline__ void read(const float* p, int slice, int rs) {
-        clear();
         if (rs == 1)
             blocks(slice, [&](f32x4& v, int row, int col) { v = *(const f32x4*)(p + (unsigned)(row + col * D)); });
         else
@@ -108,82 +107,79 @@ struct State {
 #pragma unroll
         for (int b = 0; b < Ti::kBlocks; ++b)
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[b][n][r] *= f;
+            for (int r = 0; r < 4; ++r) s[b][r] *= f;
     }
     __device__ __forceinline__ float top() const {
         float t = 0.0f;
 #pragma unroll
         for (int b = 0; b < Ti::kBlocks; ++b)
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) t = fmaxf(t, fabsf(s[b][n][r]));
+            for (int r = 0; r < 4; ++r) t = fmaxf(t, fabsf(s[b][r]));
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) t = fmaxf(t, __shfl_xor(t, d));
         return t;
     }
-    // columns n of step b's channels as an operand, in parts
-    __device__ __forceinline__ void operand(int b, int n, float f, typename Ti::Vec (&part)[kParts<T>]) const {
-        float v[Ti::kVec];
+    // step b's channels as an operand, in parts
+    __device__ __forceinline__ void operand(int b, float f, typename Ti::Op (&part)[kParts<T>]) const {
+        float v[Ti::kOp];
 #pragma unroll
-        for (int e = 0; e < Ti::kVec; ++e) v[e] = s[b * Ti::kJoin + e / 4][n][e % 4] * f;
+        for (int e = 0; e < Ti::kOp; ++e) v[e] = s[b * Ti::kJoinOp + e / 4][e % 4] * f;
         Ti::template split<kParts<T>>(v, part);
     }
     // += sum_j b_j (w_j c_j)^T over the chunk; vt: the wave's columns of c over tokens
-    __device__ __forceinline__ void add(char* tb, const typename Ti::Vec (&vt)[Ti::kTokenSteps][2], const float* weight, float unit) {
+    __device__ __forceinline__ void add(char* tb, const typename Ti::Vec (&vt)[Ti::kTokenSteps], const float* weight, float unit) {
         const int x = lane_id() & 15, q = lane_id() >> 4;
 #pragma unroll
         for (int st = 0; st < Ti::kTokenSteps; ++st) {
-            float w[Ti::kVec];
+            __builtin_amdgcn_sched_barrier(0);
+            // (operands are on their way while others' products run)
+            typename Ti::Vec kt = Ti::key_operand(tb, 0, st, x, q);
+            float v[Ti::kVec];
 #pragma unroll
             for (int j = 0; j < Ti::kJoin; ++j) {
-                const f32x4 f = *(const f32x4*)(weight + st * Ti::kStep + 16 * j + 4 * q);
+                const f32x4 f = *(const f32x4*)(weight + st * Ti::kTokenStep + 16 * j + 4 * q);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) w[4 * j + r] = f[r] * unit;
+                for (int r = 0; r < 4; ++r) {
+                    v[4 * j + r] = Ti::Tr::to_f32(vt[st][4 * j + r]) * f[r];
+                    if constexpr (Ti::kNormalise) v[4 * j + r] *= unit;
+                }
             }
-            typename Ti::Vec part[2][kStateParts<T>];
+            typename Ti::Vec part[kStateParts<T>];
+            Ti::template split<kStateParts<T>>(v, part);
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                float v[Ti::kVec];
+            for (int b = 0; b < Ti::kBlocks; b += 2) {
+                typename Ti::Vec more = kt, next = kt;
+                if (b + 1 < Ti::kBlocks) more = Ti::key_operand(tb, b + 1, st, x, q);
+                if (b + 2 < Ti::kBlocks) next = Ti::key_operand(tb, b + 2, st, x, q);
 #pragma unroll
-                for (int e = 0; e < Ti::kVec; ++e) v[e] = Ti::Tr::to_f32(vt[st][n][e]) * w[e];
-                Ti::template split<kStateParts<T>>(v, part[n]);
-            }
-            // (the next block's operand is on its way while this one's products run)
-            typename Ti::Vec kt = Ti::token_operand(tb, 0, st, x, q);
-#pragma unroll
-            for (int b = 0; b < Ti::kBlocks; ++b) {
-                typename Ti::Vec next = kt;
-                if (b + 1 < Ti::kBlocks) next = Ti::token_operand(tb, b + 1, st, x, q);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int p = 0; p < kStateParts<T>; ++p)
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) s[b][n] = Ti::Tr::mma_vec(s[b][n], kt, part[n][p]);
+                for (int p = 0; p < kStateParts<T>; ++p) {
+                    s[b] = Ti::Tr::mma_vec(s[b], kt, part[p]);
+                    if (b + 1 < Ti::kBlocks) s[b + 1] = Ti::Tr::mma_vec(s[b + 1], more, part[p]);
+                }
                 kt = next;
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
 };
 
+// This lane's row's gate, as it stands in memory: what is done with it waits for it, so that is left for when it is needed.
 template <class T>
-__device__ __forceinline__ float gate_of(const void* gate, long ts, const Segment& s, int reverse, long u, int head, int heads) {
-    if (gate == nullptr || u >= s.hi - s.lo || head >= heads) return 0.0f;
-    const long t = reverse ? s.hi - 1 - u : s.lo + u;
-    return (float)((const T*)gate)[t * ts + head];
+__device__ __forceinline__ T gate_of(const void* gate, long ts, const Segment& s, int reverse, long u, int head, int heads) {
+    T g = (T)0.0f;
+    if (gate != nullptr && u < s.hi - s.lo && head < heads) g = ((const T*)gate)[(reverse ? s.hi - 1 - u : s.lo + u) * ts + head];
+    return g;
 }
 
 // What a segment adds to the state, and the product of its gates.
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_state_kernel(StateArgs p) {
+__global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupancy)) recurrence_state_kernel(StateArgs p) {
     typedef Tile<T, D> Ti;
     extern __shared__ __align__(16) char lds[];
     char* tb = lds;
     char* tc = tb + Ti::kBytes;
     Gates* gates = (Gates*)(tc + Ti::kBytes);
-    unsigned* tops = (unsigned*)(gates + Ti::kHeads);           // [2][4 waves][3]
+    unsigned* tops = (unsigned*)(gates + Ti::kHeads);           // [2][waves][3]
 
     const Segment seg = find_segment(p.layout, blockIdx.x);
     if (!seg.live || seg.index == (p.reverse ? 0 : seg.count - 1)) return;     // nothing comes after it
@@ -193,34 +189,36 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
     const long len = seg.hi - seg.lo;
     const int chunks = (int)((len + kChunk - 1) / kChunk), steps = chunks * p.gb;
 
-    Ti::clear(tb);
-    Ti::clear(tc);
     State<T, D> state;
     state.clear();
     float exponent = 0.0f, unit = 1.0f;
     typename Ti::Regs rb, rc;
-    float g = 0.0f;
+    T g = (T)0.0f;
     const int heads = p.heads - head0;
-    const unsigned ob = Ti::offset(p.b, p.reverse, p.gb), oc = Ti::offset(p.c, p.reverse, p.gb);
-    auto tile_at = [&](const Heads& h, long u, int sub) {
-        return h.p + Ti::token(seg, p.reverse, u) * h.ts + ((long)head0 * p.gb + sub) * h.hs;
-    };
-    auto fetch = [&](long u, int sub) {
+    const unsigned ob = Ti::offset(p.b, p.reverse, p.gb, heads), oc = Ti::offset(p.c, p.reverse, p.gb, heads);
+    const long chunk = p.reverse ? -kChunk : kChunk;
+    const char* pb = Ti::start(p.b, seg, p.reverse, head0 * p.gb);
+    const char* pc = Ti::start(p.c, seg, p.reverse, head0 * p.gb);
+    auto fetch = [&](long u, int sub) {         // the tiles of rows u.. and of the sub-th of the heads of (b, c); pb, pc: their first ones'
         const int rows = (int)min(len - u, (long)kChunk);
-        Ti::load(rb, tile_at(p.b, u, sub), ob, p.b, p.reverse, rows, heads);
-        Ti::load(rc, tile_at(p.c, u, sub), oc, p.c, p.reverse, rows, heads);
-        if (sub == 0) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, u + lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+        if (sub == 0 && wave < Ti::kHeads) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, u + lane, head0 + wave, p.heads);
+        Ti::load(rb, pb + sub * p.b.hs, ob, p.b.ts, p.reverse, rows);
+        Ti::load(rc, pc + sub * p.c.hs, oc, p.c.ts, p.reverse, rows);
+        if (sub + 1 == p.gb) {
+            pb += chunk * p.b.ts;
+            pc += chunk * p.c.ts;
+        }
     };
     fetch(0, 0);
     __syncthreads();
     int sub = 0, next_sub = 0;
     long first = 0;
     for (int it = 0; it < steps; ++it, first += next_sub == 0 ? kChunk : 0, sub = next_sub) {
-        unsigned* top = tops + (it & 1) * 12;
+        unsigned* top = tops + (it & 1) * 3 * Ti::kWaves;
         Ti::store(rb, tb, p.b.relu);
         const unsigned mc = Ti::store(rc, tc, p.c.relu);
         if constexpr (Ti::kNormalise) leave_top(top + 2, mc);
-        if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, g, p.reverse, 1.0f, p.weight_scale, Ti::kNormalise);
+        if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, (float)g, p.reverse, 1.0f, p.weight_scale, Ti::kNormalise);
         __syncthreads();
         if (it + 1 < steps) {
             next_sub = sub + 1 == p.gb ? 0 : sub + 1;
@@ -229,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
         const Gates& gt = gates[mine];
         float fresh = unit, factor = 1.0f;
         if constexpr (Ti::kNormalise) {
-            const float bound = tile_top(top + 2) * fabsf(p.weight_scale) * gt.grow;
+            const float bound = tile_top<Ti::kWaves>(top + 2) * fabsf(p.weight_scale) * gt.grow;
             if (bound > 0.0f) fresh = normaliser(bound);
             factor = fresh / unit;
             unit = fresh;
@@ -239,11 +237,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
             exponent += gt.exponent;
         }
         if (sub == 0 || Ti::kNormalise) state.scale(factor);
-        typename Ti::Vec vt[Ti::kTokenSteps][2];
+        typename Ti::Vec vt[Ti::kTokenSteps];
 #pragma unroll
-        for (int st = 0; st < Ti::kTokenSteps; ++st)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) vt[st][n] = Ti::token_operand(tc + mine * Ti::kHeadBytes, slice / 16 + n, st, x, q);
+        for (int st = 0; st < Ti::kTokenSteps; ++st) vt[st] = Ti::value_operand(tc + mine * Ti::kHeadBytes, slice, st, x, q);
         state.add(tb + mine * Ti::kHeadBytes, vt, gt.weight, unit);
         __syncthreads();
     }
@@ -291,20 +287,36 @@ __global__ void __launch_bounds__(kThreads) recurrence_join_kernel(float* own, c
     }
 }
 
-// MASKED: out is masked and measured against m (p.m, p.dots)
-template <class T, int D, bool MASKED>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_sweep_kernel(SweepArgs p) {
+template <class F>
+__device__ __forceinline__ F load_through(BufRsrc r, unsigned off, unsigned scalar) {
+    if constexpr (sizeof(F) == 8) return __builtin_bit_cast(F, __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, (int)scalar, 0));
+    else return __builtin_bit_cast(F, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)scalar, 0));
+}
+// (no scalar offset in a store: see buf_store16_at_as)
+template <class F>
+__device__ __forceinline__ void store_through(BufRsrc r, unsigned off, F v) {
+    if constexpr (sizeof(F) == 8) buf_store8(r, off, __builtin_bit_cast(u32x2, v));
+    else buf_store16(r, off, __builtin_bit_cast(u32x4, v));
+}
+
+// MASKED: out is masked and measured against m (p.m, p.dots).  GROUP: there are several heads of a, or of (b, c), to a state head.
+template <class T, int D, bool MASKED, bool GROUP>
+__global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupancy)) recurrence_sweep_kernel(SweepArgs p) {
     typedef Tile<T, D> Ti;
     typedef typename Ti::Vec Vec;
+    typedef typename Ti::Op Op;
+    typedef typename Ti::Frag Frag;
     typedef typename Ti::Tr Tr;
-    constexpr int kVec = Ti::kVec;
+    constexpr int kThreads = Ti::kThreads;
+    const int ga = GROUP ? p.ga : 1, gb = GROUP ? p.gb : 1, group = max(ga, gb);
     extern __shared__ __align__(16) char lds[];
     char* ta = lds;
     char* tb = ta + Ti::kBytes;
     char* tc = tb + Ti::kBytes;
     Gates* gates = (Gates*)(tc + Ti::kBytes);
-    unsigned* tops = (unsigned*)(gates + Ti::kHeads);
-    char* scores = (char*)(tops + 24);
+    unsigned* tops = (unsigned*)(gates + Ti::kHeads);           // [2][waves][3]
+    float* dots = (float*)(tops + 6 * Ti::kWaves);              // [waves][64]
+    char* scores = (char*)(dots + kChunk * Ti::kWaves);
 
     const Segment seg = find_segment(p.layout, blockIdx.x);
     if (!seg.live) return;
@@ -313,11 +325,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
     const int slice = wave % Ti::kWavesPerHead * kSlice;
     const bool live = head < p.heads;
     const long len = seg.hi - seg.lo;
-    const int chunks = (int)((len + kChunk - 1) / kChunk), group = max(p.ga, p.gb), steps = chunks * group;
+    const int chunks = (int)((len + kChunk - 1) / kChunk), steps = chunks * group;
 
-    Ti::clear(ta);
-    Ti::clear(tb);
-    Ti::clear(tc);
     // (the upper halves of the steps of blocks 0 and 2 are above the diagonal, and stay zero)
     if constexpr (Ti::kShare)
         for (int i = threadIdx.x * 16; i < Ti::kScoreBytes; i += kThreads * 16) *(u32x4*)(scores + i) = u32x4{0, 0, 0, 0};
@@ -329,31 +338,42 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
     if constexpr (Ti::kNormalise) bound_s = state.top();
 
     typename Ti::Regs ra, rb, rc;
-    float g = 0.0f;
+    T g = (T)0.0f;
     const int heads = p.heads - head0;
-    const unsigned oa = Ti::offset(p.a, p.reverse, p.ga), ob = Ti::offset(p.b, p.reverse, p.gb), oc = Ti::offset(p.c, p.reverse, p.gb);
-    auto tile_at = [&](const Heads& h, long u, int per, int sub) {
-        return h.p + Ti::token(seg, p.reverse, u) * h.ts + ((long)head0 * per + sub) * h.hs;
-    };
-    auto fetch = [&](long u, int sub) {
+    const unsigned oa = Ti::offset(p.a, p.reverse, ga, heads), ob = Ti::offset(p.b, p.reverse, gb, heads), oc = Ti::offset(p.c, p.reverse, gb, heads);
+    const long chunk = p.reverse ? -kChunk : kChunk;
+    const char* pa = Ti::start(p.a, seg, p.reverse, head0 * ga);
+    const char* pb = Ti::start(p.b, seg, p.reverse, head0 * gb);
+    const char* pc = Ti::start(p.c, seg, p.reverse, head0 * gb);
+    auto fetch = [&](long u, int sub) {         // the tiles of rows u.. that the sub-th step of a chunk needs anew
         const int rows = (int)min(len - u, (long)kChunk);
-        if (sub == 0 || p.ga > 1) Ti::load(ra, tile_at(p.a, u, p.ga, p.ga > 1 ? sub : 0), oa, p.a, p.reverse, rows, heads);
-        if (sub == 0 || p.gb > 1) {
-            Ti::load(rb, tile_at(p.b, u, p.gb, p.gb > 1 ? sub : 0), ob, p.b, p.reverse, rows, heads);
-            Ti::load(rc, tile_at(p.c, u, p.gb, p.gb > 1 ? sub : 0), oc, p.c, p.reverse, rows, heads);
+        if (sub == 0 && wave < Ti::kHeads) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, u + lane, head0 + wave, p.heads);
+        if (sub == 0 || ga > 1) Ti::load(ra, pa + (ga > 1 ? sub : 0) * p.a.hs, oa, p.a.ts, p.reverse, rows);
+        if (sub == 0 || gb > 1) {
+            Ti::load(rb, pb + (gb > 1 ? sub : 0) * p.b.hs, ob, p.b.ts, p.reverse, rows);
+            Ti::load(rc, pc + (gb > 1 ? sub : 0) * p.c.hs, oc, p.c.ts, p.reverse, rows);
         }
-        if (sub == 0) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, u + lane, head0 + wave, wave < Ti::kHeads ? p.heads : 0);
+        if (sub + 1 == group) {
+            pa += chunk * p.a.ts;
+            pb += chunk * p.b.ts;
+            pc += chunk * p.c.ts;
+        }
     };
+    // rows 16i + x of out (and of what it is masked with) in the same way; a chunk's last 16 rows are its first ones from the end
+    const unsigned xr = p.reverse ? 15 - x : x, xq = 4 * q * (unsigned)sizeof(T);
+    const unsigned oo = xr * (unsigned)p.out_ts + xq, om = MASKED ? xr * (unsigned)p.m.ts + xq : 0;
+    char* po = p.out + (p.reverse ? seg.hi - kChunk : seg.lo) * p.out_ts + (long)head * ga * p.out_hs + slice * (int)sizeof(T);
+    const char* pm = MASKED ? Ti::start(p.m, seg, p.reverse, head * ga) + slice * (int)sizeof(T) : nullptr;
     if (steps > 0) fetch(0, 0);
-    f32x4 o[4][2];
+    f32x4 o[4];
     __syncthreads();
     int sub = 0, next_sub = 0;
     long first = 0;
     for (int it = 0; it < steps; ++it, first += next_sub == 0 ? kChunk : 0, sub = next_sub) {
-        const bool new_a = sub == 0 || p.ga > 1, new_b = sub == 0 || p.gb > 1;      // (one of ga, gb is 1)
-        const bool begins = new_a, ends = p.gb == 1 || sub == group - 1;            // of an output's sum
-        const bool feeds = p.ga == 1 || sub == group - 1;                           // the state
-        unsigned* top = tops + (it & 1) * 12;
+        const bool new_a = sub == 0 || ga > 1, new_b = sub == 0 || gb > 1;      // (one of ga, gb is 1)
+        const bool begins = new_a, ends = gb == 1 || sub == group - 1;            // of an output's sum
+        const bool feeds = ga == 1 || sub == group - 1;                           // the state
+        unsigned* top = tops + (it & 1) * 3 * Ti::kWaves;
         unsigned ma = 0, mb = 0, mc = 0;
         if (new_a) ma = Ti::store(ra, ta, p.a.relu);
         if (new_b) {
@@ -365,209 +385,178 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
             leave_top(top + 1, mb);
             leave_top(top + 2, mc);
         }
-        if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, g, p.reverse, p.in_scale, p.weight_scale, Ti::kNormalise);
+        if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, (float)g, p.reverse, p.in_scale, p.weight_scale, Ti::kNormalise);
         __syncthreads();
         const Gates& gt = gates[mine];
         const char* ha = ta + mine * Ti::kHeadBytes;
         char* hb = tb + mine * Ti::kHeadBytes;
         char* hc = tc + mine * Ti::kHeadBytes;
-        if constexpr (Ti::kNormalise) {
-            if (new_a) at = tile_top(top);
-            if (new_b) {
-                bt = tile_top(top + 1);
-                ct = tile_top(top + 2);
-            }
-        }
-        // scores, where the waves of a head share them
         float fp = 1.0f;
-        if constexpr (Ti::kNormalise) fp = normaliser(fabsf(p.score_scale) * (float)Ti::kPad * at * bt * gt.grow);
+        if constexpr (Ti::kNormalise) {
+            if (new_a) at = tile_top<Ti::kWaves>(top);
+            if (new_b) {
+                bt = tile_top<Ti::kWaves>(top + 1);
+                ct = tile_top<Ti::kWaves>(top + 2);
+            }
+            fp = normaliser(fabsf(p.score_scale) * (float)D * at * bt * gt.grow);
+        }
+        const float score_scale = p.score_scale * fp;
+        // scores of rows 16i + x and keys 16j + 4q + r
+        auto score = [&](int i, int j, const Op (&va)[Ti::kSteps], float (&w)[4]) {
+            f32x4 d = {0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < Ti::kSteps; ++s) d = Ti::mma(d, Ti::row_operand(hb, 16 * j + x, s, q), va[s]);
+            const float fi = gt.hi[16 * i + x], li = gt.lo[16 * i + x];
+            const f32x4 fj = *(const f32x4*)(gt.hi + 16 * j + 4 * q), lj = *(const f32x4*)(gt.lo + 16 * j + 4 * q);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float e = __builtin_amdgcn_exp2f((fi - fj[r]) + (li - lj[r]));
+                w[r] = j < i || 4 * q + r <= x ? d[r] * e * score_scale : 0.0f;
+            }
+        };
         if constexpr (Ti::kShare) {
-            // blocks 0, 1, .. of the lower triangle's ten, row by row: every fourth is this wave's
+            // blocks 0, 1, .. of the lower triangle's ten, row by row, are dealt to the head's waves
 #pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                const int at_ = wave + 4 * k;
-                if (k == 2 && at_ >= 10) break;
-                const int i = at_ >= 6 ? 3 : (at_ >= 3 ? 2 : (at_ >= 1 ? 1 : 0)), j = at_ - i * (i + 1) / 2;
-                f32x4 d = {0, 0, 0, 0};
+            for (int k = 0; k < (10 + Ti::kWavesPerHead - 1) / Ti::kWavesPerHead; ++k) {
+                int n = wave % Ti::kWavesPerHead + Ti::kWavesPerHead * k;
+                asm volatile("" : "+s"(n));     // (its addresses are not worth registers all through the loop)
+                if (n < 10) {
+                    const int i = n >= 6 ? 3 : (n >= 3 ? 2 : (n >= 1 ? 1 : 0)), j = n - i * (i + 1) / 2;
+                    Op va[Ti::kSteps];
 #pragma unroll
-                for (int s = 0; s < Ti::kSteps; ++s)
-                    d = Tr::mma_vec(d, Ti::row_operand(hb, 16 * j + x, s, q), Ti::row_operand(ha, 16 * i + x, s, q));
-                const float fi = gt.hi[16 * i + x], li = gt.lo[16 * i + x], sc = p.score_scale * fp;
-                const f32x4 fj = *(const f32x4*)(gt.hi + 16 * j + 4 * q), lj = *(const f32x4*)(gt.lo + 16 * j + 4 * q);
-                float w[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float e = __builtin_amdgcn_exp2f((fi - fj[r]) + (li - lj[r]));
-                    w[r] = j < i || 4 * q + r <= x ? d[r] * e * sc : 0.0f;
+                    for (int s = 0; s < Ti::kSteps; ++s) va[s] = Ti::row_operand(ha, 16 * i + x, s, q);
+                    float w[4];
+                    score(i, j, va, w);
+                    Ti::leave_scores(w, scores + Ti::score_step(i, j / Ti::kJoin) * 1024 + lane * 16 + (Ti::kJoin == 2 ? (j & 1) * 8 : 0));
                 }
-                char* to = scores + Ti::score_step(i, j / Ti::kJoin) * 1024 + lane * 16 + (Ti::kJoin == 2 ? (j & 1) * 8 : 0);
-                Ti::leave_scores(w, to);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
         // what the rows take from the state
         if (begins) {
             float fs = 1.0f;
             if constexpr (Ti::kNormalise) fs = normaliser(bound_s * unit);
 #pragma unroll
-            for (int rb_ = 0; rb_ < 4; ++rb_) o[rb_][0] = o[rb_][1] = f32x4{0, 0, 0, 0};
+            for (int i = 0; i < 4; ++i) o[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int s = 0; s < Ti::kSteps; ++s) {
-                Vec va[4], part[2][kParts<T>];
+                Op va[4], part[kParts<T>];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) va[i] = Ti::row_operand(ha, 16 * i + x, s, q);
-#pragma unroll
-                for (int n = 0; n < 2; ++n) state.operand(s, n, fs, part[n]);
+                state.operand(s, fs, part);
 #pragma unroll
                 for (int k = 0; k < kParts<T>; ++k)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int n = 0; n < 2; ++n) o[i][n] = Tr::mma_vec(o[i][n], part[n][k], va[i]);
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int i = 0; i < 4; ++i) o[i] = Ti::mma(o[i], part[k], va[i]);
+                __builtin_amdgcn_sched_barrier(0);      // (or all steps' operands are read ahead, into registers that are not there)
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float f = gt.in[16 * i + x] / (fs * unit);
+                float f = gt.in[16 * i + x];
+                if constexpr (Ti::kNormalise) f /= fs * unit;
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[i][n][r] *= f;
+                for (int r = 0; r < 4; ++r) o[i][r] *= f;
             }
         }
-        if constexpr (Ti::kNormalise) {
-            if (fp != 1.0f) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) o[i][n][r] *= fp;
-            }
-        }
-        // Rows 16i + x of out lie at one offset from an address of the chunk, as they were loaded.  What they are masked with is asked for before
-        // the next tiles: loads return in order.  (Asked for here, and not at once, the tiles do not hold registers through the part above.)
+        // What out is masked with is asked for before the next tiles: loads return in order.  (Asked for here, and not at once, the tiles do not
+        // hold registers through the part above.)
         const int rows = (int)min(len - first, (long)kChunk);
-        const long t0 = Ti::token(seg, p.reverse, first), back = p.reverse ? -15 : 0, step = p.reverse ? -16 : 16;
-        const int xr = p.reverse ? 15 - x : x;
-        Vec mv[MASKED ? 4 : 1][8 / kVec];
+        Frag mv[MASKED ? 4 : 1];
         if constexpr (MASKED) {
             if (ends && live) {
-                const char* mp = p.m.p + (t0 + back) * p.m.ts + (head * p.ga + (p.ga > 1 ? sub : 0)) * p.m.hs + slice * (int)sizeof(T);
-                const unsigned om = (unsigned)xr * (unsigned)p.m.ts + 16 * q;
+                const BufRsrc from = whole_rsrc(pm + (ga > 1 ? sub : 0) * p.m.hs);
 #pragma unroll
-                for (int i = 0; i < 4; ++i, mp += step * p.m.ts)
-#pragma unroll
-                    for (int v = 0; v < 8 / kVec; ++v)
-                        if (16 * i + x < rows && (D >= 32 || (kVec == 8 ? 8 * q : 16 * v + 4 * q) < D)) mv[i][v] = *(const Vec*)(mp + om + 64 * v);
+                for (int i = 0; i < 4; ++i)
+                    mv[i] = load_through<Frag>(from, 16 * i + x < rows ? om : kNowhere, (p.reverse ? 3 - i : i) * 16 * (unsigned)p.m.ts);
+                if (sub + 1 == group) pm += chunk * p.m.ts;
             }
         }
         if (it + 1 < steps) {
             next_sub = sub + 1 == group ? 0 : sub + 1;
             fetch(first + (next_sub == 0 ? kChunk : 0), next_sub);
         }
-        if constexpr (Ti::kShare) __syncthreads();
         // what they take from the chunk's own rows
-        Vec vt[Ti::kTokenSteps][2];
+        if constexpr (Ti::kShare) __syncthreads();
+        Vec vt[Ti::kTokenSteps];
 #pragma unroll
-        for (int st = 0; st < Ti::kTokenSteps; ++st)
+        for (int st = 0; st < Ti::kTokenSteps; ++st) vt[st] = Ti::value_operand(hc, slice, st, x, q);
+        if constexpr (Ti::kNormalise) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n) vt[st][n] = Ti::token_operand(hc, slice / 16 + n, st, x, q);
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[i][r] *= fp;
+        }
         if constexpr (Ti::kShare) {
             static_for<0, 4>([&](auto i_) {
                 constexpr int i = decltype(i_)::value;
 #pragma unroll
                 for (int st = 0; st <= i / Ti::kJoin; ++st)
 #pragma unroll
-                    for (int k = 0; k < kParts<T>; ++k) {
-                        const Vec part = *(const Vec*)(scores + (k * Ti::kScoreSteps + Ti::score_step(i, st)) * 1024 + lane * 16);
-#pragma unroll
-                        for (int n = 0; n < 2; ++n) o[i][n] = Tr::mma_vec(o[i][n], vt[st][n], part);
-                    }
-            });
-        } else static_for<0, 4>([&](auto i_) {
-            constexpr int i = decltype(i_)::value;
-            Vec va[Ti::kSteps];
-#pragma unroll
-            for (int s = 0; s < Ti::kSteps; ++s) va[s] = Ti::row_operand(ha, 16 * i + x, s, q);
-            const float fi = gt.hi[16 * i + x], li = gt.lo[16 * i + x], sc = p.score_scale * fp;
-            static_for<0, i / Ti::kJoin + 1>([&](auto st_) {
-                constexpr int st = decltype(st_)::value;
-                float w[kVec];
-                static_for<0, Ti::kJoin>([&](auto j_) {
-                    constexpr int half = decltype(j_)::value, j = st * Ti::kJoin + half;
-                    if constexpr (j <= i) {
-                        f32x4 d = {0, 0, 0, 0};
-#pragma unroll
-                        for (int s = 0; s < Ti::kSteps; ++s) d = Tr::mma_vec(d, Ti::row_operand(hb, 16 * j + x, s, q), va[s]);
-                        const f32x4 fj = *(const f32x4*)(gt.hi + 16 * j + 4 * q), lj = *(const f32x4*)(gt.lo + 16 * j + 4 * q);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const float e = __builtin_amdgcn_exp2f((fi - fj[r]) + (li - lj[r]));
-                            const bool sees = j < i || 4 * q + r <= x;
-                            w[4 * half + r] = sees ? d[r] * e * sc : 0.0f;
-                        }
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) w[4 * half + r] = 0.0f;
-                    }
-                });
-                Vec part[kParts<T>];
-                Ti::template split<kParts<T>>(w, part);
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int k = 0; k < kParts<T>; ++k) o[i][n] = Tr::mma_vec(o[i][n], vt[st][n], part[k]);
+                    for (int k = 0; k < kParts<T>; ++k)
+                        o[i] = Tr::mma_vec(o[i], vt[st], *(const Vec*)(scores + (k * Ti::kScoreSteps + Ti::score_step(i, st)) * 1024 + lane * 16));
                 __builtin_amdgcn_sched_barrier(0);
             });
-        });
+        } else {
+            static_for<0, 4>([&](auto i_) {
+                constexpr int i = decltype(i_)::value;
+                Op va[Ti::kSteps];
+#pragma unroll
+                for (int s = 0; s < Ti::kSteps; ++s) va[s] = Ti::row_operand(ha, 16 * i + x, s, q);
+                static_for<0, i / Ti::kJoin + 1>([&](auto st_) {
+                    constexpr int st = decltype(st_)::value;
+                    float w[kChunk / 16][4];
+                    static_for<0, Ti::kJoin>([&](auto j_) {
+                        constexpr int half = decltype(j_)::value, j = st * Ti::kJoin + half;
+                        if constexpr (j <= i) {
+                            score(i, j, va, w[half]);
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) w[half][r] = 0.0f;
+                        }
+                    });
+                    float flat[Ti::kVec];
+#pragma unroll
+                    for (int e = 0; e < Ti::kVec; ++e) flat[e] = w[e / 4][e % 4];
+                    Vec part[kParts<T>];
+                    Ti::template split<kParts<T>>(flat, part);
+#pragma unroll
+                    for (int k = 0; k < kParts<T>; ++k) o[i] = Tr::mma_vec(o[i], vt[st], part[k]);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
+        }
         if constexpr (Ti::kNormalise) {
-            if (fp != 1.0f) {
-                const float back = 1.0f / fp;
+            const float undo = 1.0f / fp;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) o[i][n][r] *= back;
-            }
+                for (int r = 0; r < 4; ++r) o[i][r] *= undo;
         }
         if (ends && live) {
-            const int ho = head * p.ga + (p.ga > 1 ? sub : 0);
-            char* out = p.out + (t0 + back) * p.out_ts + ho * p.out_hs + slice * (int)sizeof(T);
-            const unsigned oo = (unsigned)xr * (unsigned)p.out_ts + 16 * q;
+            const BufRsrc to = whole_rsrc(po + (ga > 1 ? sub : 0) * p.out_hs);
+            if (sub + 1 == group) po += chunk * p.out_ts;
 #pragma unroll
-            for (int i = 0; i < 4; ++i, out += step * p.out_ts) {
+            for (int i = 0; i < 4; ++i) {
                 const bool row = 16 * i + x < rows;
                 float dot = 0.0f;
-#pragma unroll
-                for (int v = 0; v < 8 / kVec; ++v) {            // 16 bytes at a time: channels 8q.. (fp32: 16v + 4q..) of the slice
-                    if (!row || (D < 32 && (kVec == 8 ? 8 * q : 16 * v + 4 * q) >= D)) continue;
-                    float w[kVec];
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e) w[e] = kVec == 8 ? o[i][e / 4][e % 4] : o[i][v][e];
-                    if constexpr (MASKED) {
-#pragma unroll
-                        for (int e = 0; e < kVec; ++e) {
-                            const float me = Tr::to_f32(mv[i][v][e]);
-                            if (p.m.relu && !(me > 0.0f)) w[e] = 0.0f;
-                            dot = fmaf(me, w[e], dot);
-                        }
-                    }
-                    Vec r;
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e) r[e] = Tr::from_f32(w[e]);
-                    *(Vec*)(out + oo + 64 * v) = r;
-                }
                 if constexpr (MASKED) {
-                    if (p.dots != nullptr) {
-                        dot += __shfl_xor(dot, 16);
-                        dot += __shfl_xor(dot, 32);
-                        if (q == 0 && row)
-                            p.dots[((t0 + (p.reverse ? -(16 * i + x) : 16 * i + x)) * (p.heads * p.ga) + ho) * Ti::kWavesPerHead + wave % Ti::kWavesPerHead] = dot;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float me = Tr::to_f32(mv[i][r]);      // (0 where there is no row)
+                        if (p.m.relu && !(me > 0.0f)) o[i][r] = 0.0f;
+                        dot = fmaf(me, o[i][r], dot);
                     }
+                }
+                store_through(to, row ? oo + (p.reverse ? 3 - i : i) * 16 * (unsigned)p.out_ts : kNowhere, frag_from_f32<T>(o[i]));
+                if constexpr (MASKED) {
+                    dot += __shfl_xor(dot, 16);
+                    dot += __shfl_xor(dot, 32);
+                    if (q == 0) dots[wave * kChunk + 16 * i + x] = dot;
                 }
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
         // the state behind the chunk
         if (feeds) {
             float factor = 1.0f;
@@ -576,14 +565,24 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
                 const float fresh = bound > 0.0f ? normaliser(bound) : unit;
                 factor = fresh / unit;
                 unit = fresh;
-                bound_s = (new_b && sub > 0 && p.gb > 1 ? bound_s : bound_s * gt.total) + (float)kChunk * bt * bound;
+                bound_s = (new_b && sub > 0 && gb > 1 ? bound_s : bound_s * gt.total) + (float)kChunk * bt * bound;
             }
-            const bool decays = p.gb == 1 || sub == 0;
+            const bool decays = gb == 1 || sub == 0;
             if (decays) factor *= gt.total;
             if (decays || Ti::kNormalise) state.scale(factor);
             state.add(hb, vt, gt.weight, unit);
         }
         __syncthreads();
+        if constexpr (MASKED) {
+            // a row's dot product from its head's waves (the next ones are left behind two more barriers, or one that this wave has to reach)
+            if (ends && p.dots != nullptr && wave < Ti::kHeads && lane < rows && head0 + wave < p.heads) {
+                float dot = 0.0f;
+#pragma unroll
+                for (int w = 0; w < Ti::kWavesPerHead; ++w) dot += dots[(wave * Ti::kWavesPerHead + w) * kChunk + lane];
+                const int hd = (head0 + wave) * ga + (ga > 1 ? sub : 0);
+                p.dots[Ti::token(seg, p.reverse, first + lane) * (p.heads * ga) + hd] = dot;
+            }
+        }
     }
     if (live && p.last != nullptr && seg.index == (p.reverse ? 0 : seg.count - 1))
         state.write(p.last + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs, 1.0f / unit);
@@ -592,7 +591,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) recurrence_s
 // d log_gate of a segment's tokens and one head: from the segment's end, x_t = q_t . dq_t - k_t . dk_t summed up, on top of
 // <dS, S> at that end.
 template <class T>
-__global__ void __launch_bounds__(kThreads) recurrence_gate_kernel(const float* q_dots, const float* k_dots, int slices, const float* starts,
+__global__ void __launch_bounds__(kThreads) recurrence_gate_kernel(const float* q_dots, const float* k_dots, const float* starts,
                                                                    const float* d_starts, const float* last, const float* d_last, T* d_gate,
                                                                    long d_gate_ts, Layout layout, int heads, int group, int size) {
     __shared__ double part[kThreads / 64];
@@ -622,9 +621,8 @@ __global__ void __launch_bounds__(kThreads) recurrence_gate_kernel(const float* 
         const long u = u0 + threadIdx.x, t = seg.hi - 1 - u;
         double x = 0.0;
         if (u < len) {
-            for (int g = 0; g < group; ++g)
-                for (int k = 0; k < slices; ++k) x += (double)q_dots[((t * heads + h) * group + g) * slices + k];
-            for (int k = 0; k < slices; ++k) x -= (double)k_dots[(t * heads + h) * slices + k];
+            for (int g = 0; g < group; ++g) x += (double)q_dots[(t * heads + h) * group + g];
+            x -= (double)k_dots[t * heads + h];
         }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -729,7 +727,9 @@ __global__ void __launch_bounds__(kThreads) recurrence_step_kernel(StepArgs p) {
 
 // ------------------------------------------------------------------------------------------------ host side
 template <class T, int D>
-constexpr int tile_lds(int tiles) { return tiles * Tile<T, D>::kBytes + Tile<T, D>::kHeads * (int)sizeof(Gates) + 2 * 12 * 4; }
+constexpr int tile_lds(int tiles) { return tiles * Tile<T, D>::kBytes + Tile<T, D>::kHeads * (int)sizeof(Gates) + 6 * Tile<T, D>::kWaves * 4; }
+template <class T, int D>
+constexpr int sweep_lds() { return tile_lds<T, D>(3) + kChunk * Tile<T, D>::kWaves * 4 + Tile<T, D>::kScoreBytes; }
 
 // LDS above the 64 KB that a kernel may ask for by itself is granted once a kernel and device
 template <class K>
@@ -751,24 +751,26 @@ hipError_t launch_state(const StateArgs& a, hipStream_t stream) {
     hipError_t e = allow_lds(&recurrence_state_kernel<T, D>, bytes, &done);
     if (e != hipSuccess) return e;
     const dim3 grid(a.layout.slots, (a.heads + Tile<T, D>::kHeads - 1) / Tile<T, D>::kHeads);
-    hipLaunchKernelGGL((recurrence_state_kernel<T, D>), grid, dim3(kThreads), bytes, stream, a);
+    hipLaunchKernelGGL((recurrence_state_kernel<T, D>), grid, dim3(Tile<T, D>::kThreads), bytes, stream, a);
     return hipGetLastError();
 }
 
-template <class T, int D, bool MASKED>
+template <class T, int D, bool MASKED, bool GROUP>
 hipError_t launch_sweep_as(const SweepArgs& a, hipStream_t stream) {
     static unsigned long long done = 0;
-    constexpr int bytes = tile_lds<T, D>(3) + Tile<T, D>::kScoreBytes;
-    hipError_t e = allow_lds(&recurrence_sweep_kernel<T, D, MASKED>, bytes, &done);
+    constexpr int bytes = sweep_lds<T, D>();
+    hipError_t e = allow_lds(&recurrence_sweep_kernel<T, D, MASKED, GROUP>, bytes, &done);
     if (e != hipSuccess) return e;
     const dim3 grid(a.layout.slots, (a.heads + Tile<T, D>::kHeads - 1) / Tile<T, D>::kHeads);
-    hipLaunchKernelGGL((recurrence_sweep_kernel<T, D, MASKED>), grid, dim3(kThreads), bytes, stream, a);
+    hipLaunchKernelGGL((recurrence_sweep_kernel<T, D, MASKED, GROUP>), grid, dim3(Tile<T, D>::kThreads), bytes, stream, a);
     return hipGetLastError();
 }
 
 template <class T, int D>
 hipError_t launch_sweep(const SweepArgs& a, hipStream_t stream) {
-    return a.m.p != nullptr ? launch_sweep_as<T, D, true>(a, stream) : launch_sweep_as<T, D, false>(a, stream);
+    const bool group = a.ga > 1 || a.gb > 1;
+    if (a.m.p != nullptr) return group ? launch_sweep_as<T, D, true, true>(a, stream) : launch_sweep_as<T, D, true, false>(a, stream);
+    return group ? launch_sweep_as<T, D, false, true>(a, stream) : launch_sweep_as<T, D, false, false>(a, stream);
 }
 
 hipError_t launch_join(float* own, const float* decay, const float* first, const Layout& l, int heads, int size, int reverse, hipStream_t stream) {
@@ -831,7 +833,7 @@ hipError_t backward_of(const RecurrenceCall& c, hipStream_t stream) {
         MSLA_TRY(launch_join(d_own, d_decay, c.d_final, l, c.heads_kv, D * D, 1, stream));
     }
     float* q_dots = c.d_gate ? (float*)(c.ws + c.plan.dots_at) : nullptr;
-    float* k_dots = c.d_gate ? q_dots + c.tokens * c.heads_q * Tile<T, D>::kWavesPerHead : nullptr;
+    float* k_dots = c.d_gate ? q_dots + c.tokens * c.heads_q : nullptr;
     float* last = c.d_gate && c.d_final ? (float*)(c.ws + c.plan.last_at) : nullptr;
     const Heads mq = c.d_gate || c.rectify ? q : no, mk = c.d_gate || c.rectify ? k : no;
     MSLA_TRY((launch_sweep<T, D>(SweepArgs{d_o, v, k, MSLA_OUT(c.d_q), mq, q_dots, c.gate, c.gate_ts, s_own, c.initial, last, 1, l,
@@ -839,8 +841,7 @@ hipError_t backward_of(const RecurrenceCall& c, hipStream_t stream) {
     MSLA_TRY((launch_sweep<T, D>(SweepArgs{v, d_o, q, MSLA_OUT(c.d_k), mk, k_dots, c.gate, c.gate_ts, d_own, c.d_final, nullptr, 1, l, c.heads_kv, 1, group, 1, c.scale, 1.0f, c.scale}, stream)));
     MSLA_TRY((launch_sweep<T, D>(SweepArgs{k, q, d_o, MSLA_OUT(c.d_v), no, nullptr, c.gate, c.gate_ts, d_own, c.d_final, c.d_initial, D, l, c.heads_kv, 1, group, 1, c.scale, 1.0f, c.scale}, stream)));
     if (c.d_gate) {
-        hipLaunchKernelGGL((recurrence_gate_kernel<T>), dim3(l.slots, c.heads_kv), dim3(kThreads), 0, stream, q_dots, k_dots,
-                           Tile<T, D>::kWavesPerHead, s_own, d_own, last, c.d_final, (T*)c.d_gate, c.d_gate_ts, l, c.heads_kv, group, D * D);
+        hipLaunchKernelGGL((recurrence_gate_kernel<T>), dim3(l.slots, c.heads_kv), dim3(kThreads), 0, stream, q_dots, k_dots, s_own, d_own, last, c.d_final, (T*)c.d_gate, c.d_gate_ts, l, c.heads_kv, group, D * D);
         MSLA_TRY(hipGetLastError());
     }
     return hipSuccess;

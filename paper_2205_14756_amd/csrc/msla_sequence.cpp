@@ -42,7 +42,7 @@ msla_status check_shape(const msla_recurrence* s, msla_dtype dt) {
 
 // Segments are as long as leaves kWantGroups workgroups.  One that spans all tokens keeps every sequence whole.
 msla_status plan_of(const msla_recurrence& s, bool backward, RecurrencePlan* plan) {
-    const int per_group = s.head_dim < 32 ? 4 : 128 / s.head_dim;           // heads of a workgroup
+    const int per_group = s.head_dim >= 64 ? 1 : 64 / s.head_dim;           // heads of a workgroup
     const int64_t groups = (s.heads_kv + per_group - 1) / per_group;
     const int64_t want = (kWantGroups + groups - 1) / groups;
     int64_t segment = ((s.tokens + want - 1) / want + 63) / 64 * 64;
@@ -71,9 +71,8 @@ msla_status plan_of(const msla_recurrence& s, bool backward, RecurrencePlan* pla
         }
     }
     if (backward) {
-        const size_t waves = s.head_dim <= 32 ? 1 : s.head_dim / 32;
         plan->dots_at = at;
-        at += align_up((size_t)s.tokens * (s.heads_q + s.heads_kv) * waves * 4);
+        at += align_up((size_t)s.tokens * (s.heads_q + s.heads_kv) * 4);
         plan->last_at = at;
         at += align_up((size_t)s.sequences * s.heads_kv * state);
     }
@@ -82,7 +81,7 @@ msla_status plan_of(const msla_recurrence& s, bool backward, RecurrencePlan* pla
 }
 
 // Strides that the kernels' 32-bit offsets inside a chunk of 64 tokens cover, in bytes.
-constexpr int64_t kMostTokenStride = (int64_t)1 << 26, kMostHeadStride = (int64_t)1 << 29;
+constexpr int64_t kMostTokenStride = (int64_t)1 << 25, kMostHeadStride = (int64_t)1 << 29;
 
 bool wide(const msla_heads& h, msla_dtype dt) {
     const int64_t e = (int64_t)elem_size(dt);

@@ -1,15 +1,15 @@
 // What the kernels of the gated recurrence (k_recurrence.hip) share: where segments lie, how a chunk of 64 tokens enters LDS, the
 // chunk's running gates, and operands of the matrix instructions out of both.
 //
-// A workgroup has four waves and walks over the chunks of one segment.  A wave owns 32 output channels of one head, so a
-// workgroup holds 128 / d heads (four of 32 and of 16; heads of 16 are padded to 32 with zeros in LDS only).
+// A workgroup walks over the chunks of one segment; a wave owns 16 output channels of one head, so that its part of the state leaves room for
+// three or four waves on a SIMD: this work is a mixture of matrix and vector instructions and LDS latency, and what hides one is another wave.
+// A head of 128 is a workgroup of eight waves; workgroups of four hold one head of 64, two of 32 or four of 16.
 //
 // Which register holds what is chosen so that nothing is ever transposed: a result D of a 16x16 matrix instruction (lane (x, q): rows
 // 4q + r, column x) is at once the next one's operand (lane (x, q): the contraction slots that q owns, of row or column x).
 //   - scores come as b a^T, so lane (x, q) has query x and keys 4q + r of each block of 16: an operand over the keys;
 //   - the state's rows (channels of the key) are dealt to the blocks so that two of them hold 8 neighbouring channels a lane, in the order
-//     in which a row of queries is read from LDS 16 bytes a lane; its columns (output channels) likewise, which makes a lane's
-//     results 8 neighbours of an output row;
+//     in which a row of queries is read from LDS 16 bytes a lane;
 //   - operands over tokens out of token-major tiles are gathered by ds_read_b64_tr_b16 (4x16 blocks, any address a lane).
 #pragma once
 #include "msla_device.h"
@@ -18,12 +18,11 @@ namespace msla {
 namespace rec {
 
 constexpr int kChunk = 64;
-constexpr int kThreads = 256;
-constexpr int kSlice = 32;          // output channels of a wave
+constexpr int kSlice = 16;          // output channels of a wave
 
 struct Heads {
     const char* p;
-    long ts, hs;                    // bytes from a token, and a head, to the next (at most 2^26 and 2^29)
+    long ts, hs;                    // bytes from a token, and a head, to the next (at most 2^25 and 2^29)
     int relu;
 };
 
@@ -45,6 +44,12 @@ __device__ __forceinline__ long sequence_start(const Layout& l, int b) {
 // empty), so a workgroup finds its own without anyone counting lengths first.
 __device__ __forceinline__ long first_slot(const Layout& l, int b) { return sequence_start(l, b) / l.segment + b; }
 
+// (the same in all lanes, and known to be: addresses made of it are scalar)
+__device__ __forceinline__ long uniform(long v) {
+    return (long)((unsigned long)(unsigned)__builtin_amdgcn_readfirstlane((int)((unsigned long)v >> 32)) << 32 |
+                  (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned long)v));
+}
+
 struct Segment {
     int sequence, index, count, slot;
     long lo, hi;                    // its tokens
@@ -59,9 +64,10 @@ __device__ __forceinline__ Segment find_segment(const Layout& l, int slot) {
         else hi = mid - 1;
     }
     Segment s;
+    lo = __builtin_amdgcn_readfirstlane(lo);
     s.sequence = lo;
     s.slot = slot;
-    const long from = sequence_start(l, lo), to = max(from, sequence_start(l, lo + 1));
+    const long from = uniform(sequence_start(l, lo)), to = max(from, uniform(sequence_start(l, lo + 1)));
     s.index = slot - (int)first_slot(l, lo);
     s.count = max(1, (int)((to - from + l.segment - 1) / l.segment));
     s.live = s.index >= 0 && s.index < s.count;
@@ -76,29 +82,44 @@ __device__ __forceinline__ Segment find_segment(const Layout& l, int slot) {
 template <class T> constexpr int kParts = sizeof(T) == 4 ? 1 : 2;
 template <class T> constexpr int kStateParts = std::is_same<T, __bf16>::value ? 3 : kParts<T>;
 
+// A resource over all that a 32-bit offset reaches, and an offset outside of it.
+constexpr unsigned kNowhere = 0xfffffff0u;
+__device__ __forceinline__ BufRsrc whole_rsrc(const char* at) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, (int)kNowhere, 0x00020000);
+}
+
 template <class T, int D>
 struct Tile {
     typedef Traits<T> Tr;
-    typedef typename Tr::Vec Vec;
+    typedef typename Tr::Vec Vec;               // an operand over tokens
+    typedef typename Tr::Frag Frag;
     static constexpr int kVec = Tr::kVec;
-    static constexpr int kPad = D < 32 ? 32 : D;                // channels in LDS
-    static constexpr int kWavesPerHead = kPad / kSlice;
-    static constexpr int kHeads = 4 / kWavesPerHead;            // heads of a workgroup
-    // rows 32 bytes apart modulo 128: the eight rows that a 16-byte read serves together, and the four of a gather, hit banks of their own
-    static constexpr int kPitch = kPad * (int)sizeof(T) + 32;
+    static constexpr int kWaves = D == 128 ? 8 : 4, kThreads = 64 * kWaves;
+    static constexpr int kWavesPerHead = D / kSlice;
+    static constexpr int kHeads = kWaves / kWavesPerHead;       // heads of a workgroup
+    // waves that a SIMD has room for by registers and LDS
+    static constexpr int kOccupancy = sizeof(T) == 4 ? 2 : (D == 64 ? 3 : 4);
+    // an operand over channels: 16 bytes a lane, for heads of 16 in 16 bits 8 (16 channels make one of the smaller matrix instruction's)
+    static constexpr int kOp = D == 16 ? 4 : kVec;
+    typedef typename std::conditional<D == 16, Frag, Vec>::type Op;
+    static constexpr int kStep = 4 * kOp;                       // channels of one matrix step (fp32: four instructions)
+    static constexpr int kSteps = D / kStep;
+    static constexpr int kBlocks = D / 16;                      // blocks of 16 key channels
+    static constexpr int kJoinOp = kOp / 4;                     // results that make one operand over channels
+    static constexpr int kTokenStep = 4 * kVec;                 // ... over tokens
+    static constexpr int kTokenSteps = kChunk / kTokenStep;
+    static constexpr int kJoin = kVec / 4;
+    // rows 32 bytes apart modulo 128 (16 where they are 32 long): the rows that a read serves together, and the four of a gather, spread
+    // over the banks
+    static constexpr int kPitch = D * (int)sizeof(T) + (D * sizeof(T) == 32 ? 16 : 32);
     static constexpr int kHeadBytes = kChunk * kPitch;
     static constexpr int kBytes = kHeads * kHeadBytes;
-    static constexpr int kStep = 4 * kVec;                      // contraction of one matrix step (fp32: four instructions)
-    static constexpr int kSteps = kPad / kStep;                 // ... over channels
-    static constexpr int kTokenSteps = kChunk / kStep;          // ... over tokens
-    static constexpr int kBlocks = kPad / 16;                   // blocks of 16 key channels
-    static constexpr int kJoin = kVec / 4;                      // results that make one operand
     static constexpr int kPerRow = kHeads * (D / kVec);         // 16-byte pieces of a tile's row
     static constexpr int kPieces = kChunk * kPerRow / kThreads;     // of a thread
     static_assert(kChunk * kPerRow % kThreads == 0 && kThreads % kPerRow == 0, "whole rows a pass");
-    // Scores of a head are the same for its waves: where there are four, each computes a quarter of them and leaves its parts in LDS as
-    // operands, 1 KB a matrix step and part; where there are fewer, each has them all in registers.
-    static constexpr bool kShare = kWavesPerHead == 4;
+    // Scores of a head are the same for its waves: where there are four or eight, each computes its share of them and leaves its parts in LDS
+    // as operands, 1 KB a matrix step and part; where there are two (or one), each has them all in registers.
+    static constexpr bool kShare = kWavesPerHead >= 4;
     static constexpr int kScoreSteps = kJoin == 2 ? 6 : 10;     // steps of the lower triangle's four rows of blocks
     static constexpr int kScoreBytes = kShare ? kScoreSteps * 1024 * (sizeof(T) == 4 ? 1 : 2) : 0;
     static __device__ __forceinline__ constexpr int score_step(int i, int st) { return kJoin == 2 ? (i < 2 ? i : 2 * i - 2) + st : i * (i + 1) / 2 + st; }
@@ -106,42 +127,42 @@ struct Tile {
 
     struct Regs { u32x4 v[kPieces]; };
 
-    // channel of row (or column) m of block `blk`: see the top of the file
+    static __device__ __forceinline__ f32x4 mma(f32x4 c, const Op& a, const Op& b) {
+        if constexpr (D == 16) return Tr::mma16(c, a, b);
+        else return Tr::mma_vec(c, a, b);
+    }
+
+    // key channel of row m of block `blk`: see the top of the file
     static __device__ __forceinline__ int channel(int blk, int m) {
-        return sizeof(T) == 2 ? 32 * (blk >> 1) + 8 * (m >> 2) + 4 * (blk & 1) + (m & 3) : 16 * blk + m;
+        return kJoinOp == 2 ? 32 * (blk >> 1) + 8 * (m >> 2) + 4 * (blk & 1) + (m & 3) : 16 * blk + m;
     }
 
     static constexpr int kRowStep = kThreads / kPerRow;         // rows between a thread's pieces
 
     static __device__ __forceinline__ long token(const Segment& s, int reverse, long u) { return reverse ? s.hi - 1 - u : s.lo + u; }
 
-    // A thread's pieces of a tile: rows row() + i * kRowStep, all at one offset from an address that is the same for all threads, so a
-    // piece costs a scalar addition and the load.  The strides' bounds keep the offset in 32 bits.
+    // A thread's pieces of a tile: rows row() + i * kRowStep, through a buffer resource at the tile's lowest address: one 32-bit offset a thread
+    // and tile, a scalar one a piece.  (The strides' bounds keep their sum below 2^32; addresses of 64 bits a lane took twelve registers
+    // and as many vector additions a chunk, and the registers were not there.)
     static __device__ __forceinline__ int row() { return threadIdx.x / kPerRow; }
     static __device__ __forceinline__ int head_of() { return threadIdx.x % kPerRow / (D / kVec); }
-    static __device__ __forceinline__ unsigned offset(const Heads& h, int reverse, int per) {
+    static __device__ __forceinline__ unsigned offset(const Heads& h, int reverse, int per, int heads) {
+        if (head_of() >= heads) return kNowhere;
         const unsigned r = reverse ? kRowStep - 1 - row() : row();
         return r * (unsigned)h.ts + (unsigned)(head_of() * per) * (unsigned)h.hs + threadIdx.x % (D / kVec) * 16u;
     }
-    // `at`: the address of the chunk's first token (from the end: its last) and of the workgroup's first head
-    static __device__ __forceinline__ void load(Regs& r, const char* at, unsigned off, const Heads& h, int reverse, int rows, int heads) {
-        if (reverse) at -= (kRowStep - 1) * h.ts;
-        const long step = (reverse ? -kRowStep : kRowStep) * h.ts;
-        if (rows >= kChunk && heads >= kHeads) {
+    // the lowest address of the segment's first chunk (from the end: of the last tokens' chunk) and of a head
+    static __device__ __forceinline__ const char* start(const Heads& h, const Segment& s, int reverse, int head) {
+        return h.p + (reverse ? s.hi - kChunk : s.lo) * h.ts + head * h.hs;
+    }
+    // (rows above `rows` are not the segment's, heads above `heads` nobody's: zero, and not read, by the resource's range check, which leaves no
+    // branch around a load and nothing to wait for)
+    static __device__ __forceinline__ void load(Regs& r, const char* at, unsigned off, long ts, int reverse, int rows) {
+        const BufRsrc from = whole_rsrc(at);
+        const unsigned step = (unsigned)kRowStep * (unsigned)ts;
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                r.v[i] = *(const u32x4*)(at + off);
-                at += step;
-            }
-        } else {
-            const bool mine = head_of() < heads;
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                r.v[i] = u32x4{0, 0, 0, 0};
-                if (mine && row() + i * kRowStep < rows) r.v[i] = *(const u32x4*)(at + off);
-                at += step;
-            }
-        }
+        for (int i = 0; i < kPieces; ++i)
+            r.v[i] = buf_load16(from, row() + i * kRowStep < rows ? off : kNowhere, (int)((reverse ? kPieces - 1 - i : i) * step));
     }
 
     // into LDS, rectified where asked; returns the largest bit pattern of a finite magnitude (fp16 alone; a value that is not finite may
@@ -174,71 +195,62 @@ struct Tile {
         return top;
     }
 
-    // the padding channels of a head of 16: zero once, never written again
-    static __device__ __forceinline__ void clear(char* tile) {
-        if constexpr (kPad != D)
-            for (int i = threadIdx.x * 16; i < kBytes; i += kThreads * 16) *(u32x4*)(tile + i) = u32x4{0, 0, 0, 0};
-    }
-
     // operand over channels: row `row`, channels of step s
-    static __device__ __forceinline__ Vec row_operand(const char* tile, int row, int s, int q) {
-        return *(const Vec*)(tile + row * kPitch + (s * kStep + kVec * q) * (int)sizeof(T));
+    static __device__ __forceinline__ Op row_operand(const char* tile, int row, int s, int q) {
+        return *(const Op*)(tile + row * kPitch + (s * kStep + kOp * q) * (int)sizeof(T));
     }
 
-    // operand over tokens: column channel(blk, x), token slots of step s (16-bit: 32s + 4q + r and 16 further on; fp32: 16s + 4q + r)
-    static __device__ __forceinline__ Vec token_operand(char* tile, int blk, int s, int x, int q) {
+    // Operand over tokens, token slots of step s (16-bit: 32s + 4q + r and 16 further on; fp32: 16s + 4q + r): column x of the 16 channels
+    // that start at `at` (bytes into a row), four of them every `apart` bytes.
+    static __device__ __forceinline__ Vec gather(char* tile, int at, int apart, int s, int x, int q) {
         if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) i16x4* LdsPtr;
-            char* at = tile + (32 * s + 4 * q + (x >> 2)) * kPitch + (32 * (blk >> 1) + 8 * (x & 3) + 4 * (blk & 1)) * 2;
-            const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at);
-            const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + 16 * kPitch));
+            char* from = tile + (32 * s + 4 * q + (x >> 2)) * kPitch + at + apart * (x & 3);
+            const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)from);
+            const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(from + 16 * kPitch));
             typedef short i16x8 __attribute__((ext_vector_type(8)));
             return __builtin_bit_cast(Vec, i16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
         } else {
             Vec v;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = *(const float*)(tile + (16 * s + 4 * q + r) * kPitch + (16 * blk + x) * 4);
+            for (int r = 0; r < 4; ++r) v[r] = *(const float*)(tile + (16 * s + 4 * q + r) * kPitch + at + x * 4);
             return v;
         }
+    }
+    // ... rows of block `blk` of the state; the wave's own output channels
+    static __device__ __forceinline__ Vec key_operand(char* tile, int blk, int s, int x, int q) {
+        if constexpr (kJoinOp == 2) return gather(tile, 64 * (blk >> 1) + 8 * (blk & 1), 16, s, x, q);
+        else return gather(tile, 16 * blk * (int)sizeof(T), 8, s, x, q);
+    }
+    static __device__ __forceinline__ Vec value_operand(char* tile, int slice, int s, int x, int q) {
+        return gather(tile, slice * (int)sizeof(T), 8, s, x, q);
     }
 
     // four scores as operands' parts: half a step of them (fp32: a whole one) at `to`
     static __device__ __forceinline__ void leave_scores(const float (&w)[4], char* to) {
-        float rest[4];
+        Frag part[kParts<T>];
+        split<kParts<T>>(w, part);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            rest[r] = w[r];
-            if constexpr (kParts<T> > 1) asm("" : "+v"(rest[r]));
-        }
-#pragma unroll
-        for (int p = 0; p < kParts<T>; ++p) {
-            typename Tr::Frag f;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                f[r] = Tr::from_f32(rest[r]);
-                if (p + 1 < kParts<T>) rest[r] -= Tr::to_f32(f[r]);
-            }
-            store_frag<T>(to + p * kScoreSteps * 1024, f);
-        }
+        for (int p = 0; p < kParts<T>; ++p) store_frag<T>(to + p * kScoreSteps * 1024, part[p]);
     }
 
     // v in PARTS parts of the storage type, each what the ones before left
-    template <int PARTS>
-    static __device__ __forceinline__ void split(const float (&v)[kVec], Vec (&part)[PARTS]) {
-        float rest[kVec];
+    template <int PARTS, class V, int N>
+    static __device__ __forceinline__ void split(const float (&v)[N], V (&part)[PARTS]) {
+        float rest[N];
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
+        for (int e = 0; e < N; ++e) {
             rest[e] = v[e];
             // (a product behind v[e] has to be rounded to fp32 here: folded into the conversion to fp16 it rounds once, where the
             // difference below sees it rounded twice, and one value in some thousands lost its second part)
-            if constexpr (PARTS > 1) asm("" : "+v"(rest[e]));
+            if constexpr (kNormalise) asm("" : "+v"(rest[e]));
         }
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) part[p][e] = Tr::from_f32(rest[e]);
+            for (int e = 0; e < N; ++e) part[p][e] = Tr::from_f32(rest[e]);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e)
+            for (int e = 0; e < N; ++e)
                 if (p + 1 < PARTS) rest[e] -= Tr::to_f32(part[p][e]);
         }
     }
