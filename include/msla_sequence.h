@@ -56,7 +56,7 @@ typedef struct {
  * (the numerator of Eq. (3), over the tokens so far; without the division, whose gradient has no bound -- a norm over the head's
  * channels takes its place).
  *   q [tokens, heads_q, head_dim];  k, v [tokens, heads_kv, head_dim];  out like q
- *   log_gate [tokens, heads_kv] in the storage type (aligned to its element), rows gate_stride elements apart, or NULL: nothing is
+ *   log_gate [tokens, heads_kv] in the storage type (aligned to its element), rows gate_stride elements (at most 32 MiB) apart, or NULL: nothing is
  *       forgotten.  At most 0 in earnest; -inf (and anything below -103) forgets all that was.
  *   initial_state, final_state [sequences, heads_kv, head_dim (of k), head_dim (of v)] fp32, either may be NULL; final_state may be
  *       initial_state itself.  A sequence without tokens hands its state on.

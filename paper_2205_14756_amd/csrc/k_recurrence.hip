@@ -128,7 +128,7 @@ struct State {
     }
     // += sum_j b_j (w_j c_j)^T over the chunk; vt: the wave's columns of c over tokens
     __device__ __forceinline__ void add(char* tb, const typename Ti::Vec (&vt)[Ti::kTokenSteps], const float* weight, float unit) {
-        const int x = lane_id() & 15, q = lane_id() >> 4;
+        const int lane = lane_id_again(), x = lane & 15, q = lane >> 4;
 #pragma unroll
         for (int st = 0; st < Ti::kTokenSteps; ++st) {
             __builtin_amdgcn_sched_barrier(0);
@@ -163,12 +163,37 @@ struct State {
     }
 };
 
-// This lane's row's gate, as it stands in memory: what is done with it waits for it, so that is left for when it is needed.
+// A chunk's gates, a lane's row each, as they stand in memory: what is done with them waits for them, so that is left for when they are
+// needed.  Like the tiles: from a lowest address, 0 where there is no row.
 template <class T>
-__device__ __forceinline__ T gate_of(const void* gate, long ts, const Segment& s, int reverse, long u, int head, int heads) {
-    T g = (T)0.0f;
-    if (gate != nullptr && u < s.hi - s.lo && head < heads) g = ((const T*)gate)[(reverse ? s.hi - 1 - u : s.lo + u) * ts + head];
-    return g;
+struct GateRows {
+    const T* at;
+    long ts;
+    int live;
+    __device__ __forceinline__ GateRows(const void* gate, long ts_, const Segment& s, int reverse, int head, int heads) {
+        at = (const T*)gate + (reverse ? s.hi - kChunk : s.lo) * ts_ + head;
+        ts = ts_;
+        live = gate != nullptr && head < heads;
+    }
+    __device__ __forceinline__ T next(int rows, int reverse) {
+        const BufRsrc from = whole_rsrc((const char*)at);
+        const int lane = lane_id_again();
+        const unsigned o = lane < (live ? rows : 0) ? (unsigned)(reverse ? kChunk - 1 - lane : lane) * (unsigned)(ts * (long)sizeof(T)) : kNowhere;
+        at += (reverse ? -kChunk : kChunk) * ts;
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(from, (int)o, 0, 0));
+        else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(from, (int)o, 0, 0));
+    }
+};
+
+// v of a column's four lanes (x, 0..3), summed in all of them
+__device__ __forceinline__ float over_column(float v) {
+    unsigned a = __builtin_bit_cast(unsigned, v);
+    const u32x2 rows = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    unsigned lo = rows[0], hi = rows[1];        // (a vector's element does not bit-cast: see frag_relu_bits)
+    a = __builtin_bit_cast(unsigned, __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi));
+    const u32x2 halves = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+    lo = halves[0], hi = halves[1];
+    return __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
 }
 
 // What a segment adds to the state, and the product of its gates.
@@ -183,7 +208,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
 
     const Segment seg = find_segment(p.layout, blockIdx.x);
     if (!seg.live || seg.index == (p.reverse ? 0 : seg.count - 1)) return;     // nothing comes after it
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), x = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
     const int head0 = blockIdx.y * Ti::kHeads, mine = wave / Ti::kWavesPerHead, head = head0 + mine;
     const int slice = wave % Ti::kWavesPerHead * kSlice;
     const long len = seg.hi - seg.lo;
@@ -193,17 +218,17 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     state.clear();
     float exponent = 0.0f, unit = 1.0f;
     typename Ti::Regs rb, rc;
+    GateRows<T> gate_rows(p.gate, p.gate_ts, seg, p.reverse, head0 + wave, p.heads);
     T g = (T)0.0f;
     const int heads = p.heads - head0;
-    const unsigned ob = Ti::offset(p.b, p.reverse, p.gb, heads), oc = Ti::offset(p.c, p.reverse, p.gb, heads);
     const long chunk = p.reverse ? -kChunk : kChunk;
     const char* pb = Ti::start(p.b, seg, p.reverse, head0 * p.gb);
     const char* pc = Ti::start(p.c, seg, p.reverse, head0 * p.gb);
     auto fetch = [&](long u, int sub) {         // the tiles of rows u.. and of the sub-th of the heads of (b, c); pb, pc: their first ones'
         const int rows = (int)min(len - u, (long)kChunk);
-        if (sub == 0 && wave < Ti::kHeads) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, u + lane, head0 + wave, p.heads);
-        Ti::load(rb, pb + sub * p.b.hs, ob, p.b.ts, p.reverse, rows);
-        Ti::load(rc, pc + sub * p.c.hs, oc, p.c.ts, p.reverse, rows);
+        if (sub == 0 && wave < Ti::kHeads) g = gate_rows.next(rows, p.reverse);
+        Ti::load(rb, pb + sub * p.b.hs, p.b, p.reverse, p.gb, rows, heads, wave);
+        Ti::load(rc, pc + sub * p.c.hs, p.c, p.reverse, p.gb, rows, heads, wave);
         if (sub + 1 == p.gb) {
             pb += chunk * p.b.ts;
             pc += chunk * p.c.ts;
@@ -215,8 +240,8 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     long first = 0;
     for (int it = 0; it < steps; ++it, first += next_sub == 0 ? kChunk : 0, sub = next_sub) {
         unsigned* top = tops + (it & 1) * 3 * Ti::kWaves;
-        Ti::store(rb, tb, p.b.relu);
-        const unsigned mc = Ti::store(rc, tc, p.c.relu);
+        Ti::store(rb, tb, p.b.relu, wave);
+        const unsigned mc = Ti::store(rc, tc, p.c.relu, wave);
         if constexpr (Ti::kNormalise) leave_top(top + 2, mc);
         if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, (float)g, p.reverse, 1.0f, p.weight_scale, Ti::kNormalise);
         __syncthreads();
@@ -237,6 +262,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
             exponent += gt.exponent;
         }
         if (sub == 0 || Ti::kNormalise) state.scale(factor);
+        const int again = lane_id_again(), x = again & 15, q = again >> 4;
         typename Ti::Vec vt[Ti::kTokenSteps];
 #pragma unroll
         for (int st = 0; st < Ti::kTokenSteps; ++st) vt[st] = Ti::value_operand(tc + mine * Ti::kHeadBytes, slice, st, x, q);
@@ -320,7 +346,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
 
     const Segment seg = find_segment(p.layout, blockIdx.x);
     if (!seg.live) return;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), x = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head0 = blockIdx.y * Ti::kHeads, mine = wave / Ti::kWavesPerHead, head = head0 + mine;
     const int slice = wave % Ti::kWavesPerHead * kSlice;
     const bool live = head < p.heads;
@@ -338,20 +364,20 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     if constexpr (Ti::kNormalise) bound_s = state.top();
 
     typename Ti::Regs ra, rb, rc;
+    GateRows<T> gate_rows(p.gate, p.gate_ts, seg, p.reverse, head0 + wave, p.heads);
     T g = (T)0.0f;
     const int heads = p.heads - head0;
-    const unsigned oa = Ti::offset(p.a, p.reverse, ga, heads), ob = Ti::offset(p.b, p.reverse, gb, heads), oc = Ti::offset(p.c, p.reverse, gb, heads);
     const long chunk = p.reverse ? -kChunk : kChunk;
     const char* pa = Ti::start(p.a, seg, p.reverse, head0 * ga);
     const char* pb = Ti::start(p.b, seg, p.reverse, head0 * gb);
     const char* pc = Ti::start(p.c, seg, p.reverse, head0 * gb);
     auto fetch = [&](long u, int sub) {         // the tiles of rows u.. that the sub-th step of a chunk needs anew
         const int rows = (int)min(len - u, (long)kChunk);
-        if (sub == 0 && wave < Ti::kHeads) g = gate_of<T>(p.gate, p.gate_ts, seg, p.reverse, u + lane, head0 + wave, p.heads);
-        if (sub == 0 || ga > 1) Ti::load(ra, pa + (ga > 1 ? sub : 0) * p.a.hs, oa, p.a.ts, p.reverse, rows);
+        if (sub == 0 && wave < Ti::kHeads) g = gate_rows.next(rows, p.reverse);
+        if (sub == 0 || ga > 1) Ti::load(ra, pa + (ga > 1 ? sub : 0) * p.a.hs, p.a, p.reverse, ga, rows, heads, wave);
         if (sub == 0 || gb > 1) {
-            Ti::load(rb, pb + (gb > 1 ? sub : 0) * p.b.hs, ob, p.b.ts, p.reverse, rows);
-            Ti::load(rc, pc + (gb > 1 ? sub : 0) * p.c.hs, oc, p.c.ts, p.reverse, rows);
+            Ti::load(rb, pb + (gb > 1 ? sub : 0) * p.b.hs, p.b, p.reverse, gb, rows, heads, wave);
+            Ti::load(rc, pc + (gb > 1 ? sub : 0) * p.c.hs, p.c, p.reverse, gb, rows, heads, wave);
         }
         if (sub + 1 == group) {
             pa += chunk * p.a.ts;
@@ -360,8 +386,6 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         }
     };
     // rows 16i + x of out (and of what it is masked with) in the same way; a chunk's last 16 rows are its first ones from the end
-    const unsigned xr = p.reverse ? 15 - x : x, xq = 4 * q * (unsigned)sizeof(T);
-    const unsigned oo = xr * (unsigned)p.out_ts + xq, om = MASKED ? xr * (unsigned)p.m.ts + xq : 0;
     char* po = p.out + (p.reverse ? seg.hi - kChunk : seg.lo) * p.out_ts + (long)head * ga * p.out_hs + slice * (int)sizeof(T);
     const char* pm = MASKED ? Ti::start(p.m, seg, p.reverse, head * ga) + slice * (int)sizeof(T) : nullptr;
     if (steps > 0) fetch(0, 0);
@@ -375,10 +399,10 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         const bool feeds = ga == 1 || sub == group - 1;                           // the state
         unsigned* top = tops + (it & 1) * 3 * Ti::kWaves;
         unsigned ma = 0, mb = 0, mc = 0;
-        if (new_a) ma = Ti::store(ra, ta, p.a.relu);
+        if (new_a) ma = Ti::store(ra, ta, p.a.relu, wave);
         if (new_b) {
-            mb = Ti::store(rb, tb, p.b.relu);
-            mc = Ti::store(rc, tc, p.c.relu);
+            mb = Ti::store(rb, tb, p.b.relu, wave);
+            mc = Ti::store(rc, tc, p.c.relu, wave);
         }
         if constexpr (Ti::kNormalise) {
             leave_top(top, ma);
@@ -387,6 +411,8 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         }
         if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, (float)g, p.reverse, p.in_scale, p.weight_scale, Ti::kNormalise);
         __syncthreads();
+        // (a lane's number, and the addresses that are made of it, anew for each part: see Tile::load)
+        int lane = lane_id_again(), x = lane & 15, q = lane >> 4;
         const Gates& gt = gates[mine];
         const char* ha = ta + mine * Ti::kHeadBytes;
         char* hb = tb + mine * Ti::kHeadBytes;
@@ -465,19 +491,17 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         Frag mv[MASKED ? 4 : 1];
         if constexpr (MASKED) {
             if (ends && live) {
+                const unsigned om = (unsigned)(p.reverse ? 15 - x : x) * (unsigned)p.m.ts + 4 * q * (unsigned)sizeof(T);
                 const BufRsrc from = whole_rsrc(pm + (ga > 1 ? sub : 0) * p.m.hs);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    mv[i] = load_through<Frag>(from, 16 * i + x < rows ? om : kNowhere, (p.reverse ? 3 - i : i) * 16 * (unsigned)p.m.ts);
+                    mv[i] = load_through<Frag>(from, x < rows - 16 * i ? om : kNowhere, (p.reverse ? 3 - i : i) * 16 * (unsigned)p.m.ts);
                 if (sub + 1 == group) pm += chunk * p.m.ts;
             }
         }
-        if (it + 1 < steps) {
-            next_sub = sub + 1 == group ? 0 : sub + 1;
-            fetch(first + (next_sub == 0 ? kChunk : 0), next_sub);
-        }
         // what they take from the chunk's own rows
         if constexpr (Ti::kShare) __syncthreads();
+        lane = lane_id_again(), x = lane & 15, q = lane >> 4;
         Vec vt[Ti::kTokenSteps];
 #pragma unroll
         for (int st = 0; st < Ti::kTokenSteps; ++st) vt[st] = Ti::value_operand(hc, slice, st, x, q);
@@ -536,9 +560,11 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         if (ends && live) {
             const BufRsrc to = whole_rsrc(po + (ga > 1 ? sub : 0) * p.out_hs);
             if (sub + 1 == group) po += chunk * p.out_ts;
+            lane = lane_id_again(), x = lane & 15, q = lane >> 4;
+            const unsigned off = (unsigned)(p.reverse ? 15 - x : x) * (unsigned)p.out_ts + 4 * q * (unsigned)sizeof(T);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool row = 16 * i + x < rows;
+                const bool row = x < rows - 16 * i;
                 float dot = 0.0f;
                 if constexpr (MASKED) {
 #pragma unroll
@@ -548,13 +574,16 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
                         dot = fmaf(me, o[i][r], dot);
                     }
                 }
-                store_through(to, row ? oo + (p.reverse ? 3 - i : i) * 16 * (unsigned)p.out_ts : kNowhere, frag_from_f32<T>(o[i]));
+                store_through(to, row ? off + (p.reverse ? 3 - i : i) * 16 * (unsigned)p.out_ts : kNowhere, frag_from_f32<T>(o[i]));
                 if constexpr (MASKED) {
-                    dot += __shfl_xor(dot, 16);
-                    dot += __shfl_xor(dot, 32);
+                    dot = over_column(dot);
                     if (q == 0) dots[wave * kChunk + 16 * i + x] = dot;
                 }
             }
+        }
+        if (it + 1 < steps) {
+            next_sub = sub + 1 == group ? 0 : sub + 1;
+            fetch(first + (next_sub == 0 ? kChunk : 0), next_sub);
         }
         __builtin_amdgcn_sched_barrier(0);
         // the state behind the chunk
@@ -575,6 +604,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         __syncthreads();
         if constexpr (MASKED) {
             // a row's dot product from its head's waves (the next ones are left behind two more barriers, or one that this wave has to reach)
+            lane = lane_id_again();
             if (ends && p.dots != nullptr && wave < Ti::kHeads && lane < rows && head0 + wave < p.heads) {
                 float dot = 0.0f;
 #pragma unroll

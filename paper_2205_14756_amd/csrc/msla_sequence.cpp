@@ -109,7 +109,7 @@ bool apart(const msla_heads& h, const msla_recurrence& s, int heads) {
 
 bool gate_fits(const void* gate, int64_t stride, const msla_recurrence& s, msla_dtype dt, bool written) {
     if (gate == nullptr || s.tokens == 0) return true;
-    if (!aligned(gate, elem_size(dt)) || stride < 0 || stride > kMost / s.tokens) return false;
+    if (!aligned(gate, elem_size(dt)) || stride < 0 || stride * (int64_t)elem_size(dt) > kMostTokenStride) return false;
     return !written || s.tokens == 1 || stride >= s.heads_kv;
 }
 

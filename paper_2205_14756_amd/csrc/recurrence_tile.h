@@ -141,33 +141,35 @@ struct Tile {
 
     static __device__ __forceinline__ long token(const Segment& s, int reverse, long u) { return reverse ? s.hi - 1 - u : s.lo + u; }
 
-    // A thread's pieces of a tile: rows row() + i * kRowStep, through a buffer resource at the tile's lowest address: one 32-bit offset a thread
-    // and tile, a scalar one a piece.  (The strides' bounds keep their sum below 2^32; addresses of 64 bits a lane took twelve registers
-    // and as many vector additions a chunk, and the registers were not there.)
-    static __device__ __forceinline__ int row() { return threadIdx.x / kPerRow; }
-    static __device__ __forceinline__ int head_of() { return threadIdx.x % kPerRow / (D / kVec); }
-    static __device__ __forceinline__ unsigned offset(const Heads& h, int reverse, int per, int heads) {
-        if (head_of() >= heads) return kNowhere;
-        const unsigned r = reverse ? kRowStep - 1 - row() : row();
-        return r * (unsigned)h.ts + (unsigned)(head_of() * per) * (unsigned)h.hs + threadIdx.x % (D / kVec) * 16u;
-    }
+    // A thread's pieces of a tile: rows row(t) + i * kRowStep, through a buffer resource at the tile's lowest address: one 32-bit offset a
+    // thread and tile, a scalar one a piece.  (The strides' bounds keep their sum below 2^32.)  The thread's number t is made anew for each
+    // tile, and the offset of it: kept over the loop, they cost registers that are not there, and what is spilled here is waited for among
+    // the loads in flight.
+    static __device__ __forceinline__ int row(int t) { return t / kPerRow; }
+    static __device__ __forceinline__ int head_of(int t) { return t % kPerRow / (D / kVec); }
+    static __device__ __forceinline__ int thread(int wave) { return 64 * wave + lane_id_again(); }
     // the lowest address of the segment's first chunk (from the end: of the last tokens' chunk) and of a head
     static __device__ __forceinline__ const char* start(const Heads& h, const Segment& s, int reverse, int head) {
         return h.p + (reverse ? s.hi - kChunk : s.lo) * h.ts + head * h.hs;
     }
-    // (rows above `rows` are not the segment's, heads above `heads` nobody's: zero, and not read, by the resource's range check, which leaves no
-    // branch around a load and nothing to wait for)
-    static __device__ __forceinline__ void load(Regs& r, const char* at, unsigned off, long ts, int reverse, int rows) {
+    // Rows above `rows` are not the segment's, heads above `heads` nobody's: zero, and not read, by the resource's range check, which leaves no
+    // branch around a load and nothing to wait for.
+    static __device__ __forceinline__ void load(Regs& r, const char* at, const Heads& h, int reverse, int per, int rows, int heads, int wave) {
+        const int t = thread(wave);
         const BufRsrc from = whole_rsrc(at);
-        const unsigned step = (unsigned)kRowStep * (unsigned)ts;
+        const unsigned step = (unsigned)kRowStep * (unsigned)h.ts;
+        unsigned off = (unsigned)(reverse ? kRowStep - 1 - row(t) : row(t)) * (unsigned)h.ts + (unsigned)(head_of(t) * per) * (unsigned)h.hs +
+                       t % (D / kVec) * 16u;
+        if (kHeads > 1 && head_of(t) >= heads) off = kNowhere;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
-            r.v[i] = buf_load16(from, row() + i * kRowStep < rows ? off : kNowhere, (int)((reverse ? kPieces - 1 - i : i) * step));
+            r.v[i] = buf_load16(from, row(t) < rows - i * kRowStep ? off : kNowhere, (int)((reverse ? kPieces - 1 - i : i) * step));
     }
 
     // into LDS, rectified where asked; returns the largest bit pattern of a finite magnitude (fp16 alone; a value that is not finite may
     // not spoil the other heads' normalisers)
-    static __device__ __forceinline__ unsigned store(Regs& r, char* tile, int relu) {
+    static __device__ __forceinline__ unsigned store(Regs& r, char* tile, int relu, int wave) {
+        const int t = thread(wave);
         typedef short i16x8 __attribute__((ext_vector_type(8)));
         typedef int i32x4 __attribute__((ext_vector_type(4)));
         unsigned top = 0;
@@ -180,7 +182,7 @@ struct Tile {
                     r.v[i] = __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(i32x4, r.v[i]), i32x4{0, 0, 0, 0}));
             }
         }
-        char* at = tile + head_of() * kHeadBytes + row() * kPitch + threadIdx.x % (D / kVec) * 16;
+        char* at = tile + head_of(t) * kHeadBytes + row(t) * kPitch + t % (D / kVec) * 16;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             if constexpr (kNormalise) {
@@ -234,24 +236,43 @@ struct Tile {
         for (int p = 0; p < kParts<T>; ++p) store_frag<T>(to + p * kScoreSteps * 1024, part[p]);
     }
 
-    // v in PARTS parts of the storage type, each what the ones before left
+    // v in PARTS parts of the storage type, each what the ones before left.  Pairs at a time: a rounded pair is one register, and is taken apart
+    // again by a shift and a mask (bf16) instead of being rounded twice.
     template <int PARTS, class V, int N>
     static __device__ __forceinline__ void split(const float (&v)[N], V (&part)[PARTS]) {
-        float rest[N];
+        if constexpr (sizeof(T) == 4) {
+            static_assert(PARTS == 1, "fp32 is whole");
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            rest[e] = v[e];
-            // (a product behind v[e] has to be rounded to fp32 here: folded into the conversion to fp16 it rounds once, where the
-            // difference below sees it rounded twice, and one value in some thousands lost its second part)
-            if constexpr (kNormalise) asm("" : "+v"(rest[e]));
-        }
+            for (int e = 0; e < N; ++e) part[0][e] = v[e];
+        } else {
+            typedef T Pair __attribute__((ext_vector_type(2)));
+            unsigned word[PARTS][N / 2];
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
+            for (int e = 0; e < N; e += 2) {
+                float x = v[e], y = v[e + 1];
+                // (a product behind them has to be rounded to fp32 here: folded into the conversion to fp16 it rounds once, where the
+                // difference below sees it rounded twice, and one value in some thousands lost its second part)
+                if constexpr (kNormalise) asm("" : "+v"(x), "+v"(y));
 #pragma unroll
-            for (int e = 0; e < N; ++e) part[p][e] = Tr::from_f32(rest[e]);
+                for (int p = 0; p < PARTS; ++p) {
+                    const Pair r = {Tr::from_f32(x), Tr::from_f32(y)};
+                    unsigned w = __builtin_bit_cast(unsigned, r);
+                    if (p + 1 < PARTS) {
+                        asm("" : "+v"(w));
+                        if constexpr (kNormalise) {
+                            const Pair back = __builtin_bit_cast(Pair, w);
+                            x -= (float)back[0];
+                            y -= (float)back[1];
+                        } else {
+                            x -= __builtin_bit_cast(float, w << 16);
+                            y -= __builtin_bit_cast(float, w & 0xffff0000u);
+                        }
+                    }
+                    word[p][e / 2] = w;
+                }
+            }
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (p + 1 < PARTS) rest[e] -= Tr::to_f32(part[p][e]);
+            for (int p = 0; p < PARTS; ++p) __builtin_memcpy(&part[p], word[p], sizeof(V));
         }
     }
 };
