@@ -27,7 +27,7 @@ extern "C" {
 #endif
 
 /* [token, head, channel] in the storage type: channels next to each other, strides in elements (multiples of 16 bytes; not
- * negative; a token's at most 32 MiB, a head's at most 512 MiB, else MSLA_ERR_UNSUPPORTED).  So heads may be part of a wider row: the map that msla_linear projects with w_qkv's row order is
+ * negative; a token's below 16 MiB, a head's at most 512 MiB, else MSLA_ERR_UNSUPPORTED).  So heads may be part of a wider row: the map that msla_linear projects with w_qkv's row order is
  * q = {p, 3*Ct, 3*d}, k = {p + d, ...}, v = {p + 2*d, ...}.  An output's rows must not overlap each other. */
 typedef struct {
     void* data;                 /* read only where the operand is an input */
@@ -56,7 +56,7 @@ typedef struct {
  * (the numerator of Eq. (3), over the tokens so far; without the division, whose gradient has no bound -- a norm over the head's
  * channels takes its place).
  *   q [tokens, heads_q, head_dim];  k, v [tokens, heads_kv, head_dim];  out like q
- *   log_gate [tokens, heads_kv] in the storage type (aligned to its element), rows gate_stride elements (at most 32 MiB) apart, or NULL: nothing is
+ *   log_gate [tokens, heads_kv] in the storage type (aligned to its element), rows gate_stride elements (below 16 MiB) apart, or NULL: nothing is
  *       forgotten.  At most 0 in earnest; -inf (and anything below -103) forgets all that was.
  *   initial_state, final_state [sequences, heads_kv, head_dim (of k), head_dim (of v)] fp32, either may be NULL; final_state may be
  *       initial_state itself.  A sequence without tokens hands its state on.

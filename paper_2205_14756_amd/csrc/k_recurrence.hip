@@ -178,7 +178,7 @@ struct GateRows {
     __device__ __forceinline__ T next(int rows, int reverse) {
         const BufRsrc from = whole_rsrc((const char*)at);
         const int lane = lane_id_again();
-        const unsigned o = lane < (live ? rows : 0) ? (unsigned)(reverse ? kChunk - 1 - lane : lane) * (unsigned)(ts * (long)sizeof(T)) : kNowhere;
+        const unsigned o = lane < (live ? rows : 0) ? times(reverse ? kChunk - 1 - lane : lane, ts * (long)sizeof(T)) : kNowhere;
         at += (reverse ? -kChunk : kChunk) * ts;
         if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(from, (int)o, 0, 0));
         else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(from, (int)o, 0, 0));
@@ -220,15 +220,16 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     typename Ti::Regs rb, rc;
     GateRows<T> gate_rows(p.gate, p.gate_ts, seg, p.reverse, head0 + wave, p.heads);
     T g = (T)0.0f;
+    double base = 0.0;              // of the head whose gates this wave sums
     const int heads = p.heads - head0;
     const long chunk = p.reverse ? -kChunk : kChunk;
     const char* pb = Ti::start(p.b, seg, p.reverse, head0 * p.gb);
     const char* pc = Ti::start(p.c, seg, p.reverse, head0 * p.gb);
     auto fetch = [&](long u, int sub) {         // the tiles of rows u.. and of the sub-th of the heads of (b, c); pb, pc: their first ones'
-        const int rows = (int)min(len - u, (long)kChunk);
+        const int rows = (int)min(len - u, (long)kChunk), t = Ti::thread(wave);
         if (sub == 0 && wave < Ti::kHeads) g = gate_rows.next(rows, p.reverse);
-        Ti::load(rb, pb + sub * p.b.hs, p.b, p.reverse, p.gb, rows, heads, wave);
-        Ti::load(rc, pc + sub * p.c.hs, p.c, p.reverse, p.gb, rows, heads, wave);
+        Ti::load(rb, pb + sub * p.b.hs, p.b, p.reverse, p.gb, rows, heads, t);
+        Ti::load(rc, pc + sub * p.c.hs, p.c, p.reverse, p.gb, rows, heads, t);
         if (sub + 1 == p.gb) {
             pb += chunk * p.b.ts;
             pc += chunk * p.c.ts;
@@ -240,10 +241,11 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     long first = 0;
     for (int it = 0; it < steps; ++it, first += next_sub == 0 ? kChunk : 0, sub = next_sub) {
         unsigned* top = tops + (it & 1) * 3 * Ti::kWaves;
-        Ti::store(rb, tb, p.b.relu, wave);
-        const unsigned mc = Ti::store(rc, tc, p.c.relu, wave);
+        const int t = Ti::thread(wave);
+        Ti::store(rb, tb, p.b.relu, t);
+        const unsigned mc = Ti::store(rc, tc, p.c.relu, t);
         if constexpr (Ti::kNormalise) leave_top(top + 2, mc);
-        if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, (float)g, p.reverse, 1.0f, p.weight_scale, Ti::kNormalise);
+        if (sub == 0 && wave < Ti::kHeads) run_gates<!Ti::kNormalise>(gates + wave, (float)g, p.reverse, 1.0f, p.weight_scale, Ti::kNormalise, base);
         __syncthreads();
         if (it + 1 < steps) {
             next_sub = sub + 1 == p.gb ? 0 : sub + 1;
@@ -260,8 +262,9 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         if (sub == 0) {
             factor *= gt.total;
             exponent += gt.exponent;
+            if constexpr (!Ti::kNormalise) unit = gt.unit;
         }
-        if (sub == 0 || Ti::kNormalise) state.scale(factor);
+        if (factor != 1.0f) state.scale(factor);
         const int again = lane_id_again(), x = again & 15, q = again >> 4;
         typename Ti::Vec vt[Ti::kTokenSteps];
 #pragma unroll
@@ -271,7 +274,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     }
     if (head >= p.heads) return;
     const long at = (long)seg.slot * p.heads + head;
-    state.write(p.own + at * (D * D), slice, p.rs, 1.0f / unit);
+    state.write(p.own + at * (D * D), slice, p.rs, Ti::kNormalise ? 1.0f / unit : unit);
     if (lane == 0 && slice == 0) p.decay[at] = __builtin_amdgcn_exp2f(exponent);
 }
 
@@ -366,18 +369,19 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     typename Ti::Regs ra, rb, rc;
     GateRows<T> gate_rows(p.gate, p.gate_ts, seg, p.reverse, head0 + wave, p.heads);
     T g = (T)0.0f;
+    double base = 0.0;              // of the head whose gates this wave sums
     const int heads = p.heads - head0;
     const long chunk = p.reverse ? -kChunk : kChunk;
     const char* pa = Ti::start(p.a, seg, p.reverse, head0 * ga);
     const char* pb = Ti::start(p.b, seg, p.reverse, head0 * gb);
     const char* pc = Ti::start(p.c, seg, p.reverse, head0 * gb);
     auto fetch = [&](long u, int sub) {         // the tiles of rows u.. that the sub-th step of a chunk needs anew
-        const int rows = (int)min(len - u, (long)kChunk);
+        const int rows = (int)min(len - u, (long)kChunk), t = Ti::thread(wave);
         if (sub == 0 && wave < Ti::kHeads) g = gate_rows.next(rows, p.reverse);
-        if (sub == 0 || ga > 1) Ti::load(ra, pa + (ga > 1 ? sub : 0) * p.a.hs, p.a, p.reverse, ga, rows, heads, wave);
+        if (sub == 0 || ga > 1) Ti::load(ra, pa + (ga > 1 ? sub : 0) * p.a.hs, p.a, p.reverse, ga, rows, heads, t);
         if (sub == 0 || gb > 1) {
-            Ti::load(rb, pb + (gb > 1 ? sub : 0) * p.b.hs, p.b, p.reverse, gb, rows, heads, wave);
-            Ti::load(rc, pc + (gb > 1 ? sub : 0) * p.c.hs, p.c, p.reverse, gb, rows, heads, wave);
+            Ti::load(rb, pb + (gb > 1 ? sub : 0) * p.b.hs, p.b, p.reverse, gb, rows, heads, t);
+            Ti::load(rc, pc + (gb > 1 ? sub : 0) * p.c.hs, p.c, p.reverse, gb, rows, heads, t);
         }
         if (sub + 1 == group) {
             pa += chunk * p.a.ts;
@@ -399,17 +403,18 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         const bool feeds = ga == 1 || sub == group - 1;                           // the state
         unsigned* top = tops + (it & 1) * 3 * Ti::kWaves;
         unsigned ma = 0, mb = 0, mc = 0;
-        if (new_a) ma = Ti::store(ra, ta, p.a.relu, wave);
+        const int t = Ti::thread(wave);
+        if (new_a) ma = Ti::store(ra, ta, p.a.relu, t);
         if (new_b) {
-            mb = Ti::store(rb, tb, p.b.relu, wave);
-            mc = Ti::store(rc, tc, p.c.relu, wave);
+            mb = Ti::store(rb, tb, p.b.relu, t);
+            mc = Ti::store(rc, tc, p.c.relu, t);
         }
         if constexpr (Ti::kNormalise) {
             leave_top(top, ma);
             leave_top(top + 1, mb);
             leave_top(top + 2, mc);
         }
-        if (sub == 0 && wave < Ti::kHeads) run_gates(gates + wave, (float)g, p.reverse, p.in_scale, p.weight_scale, Ti::kNormalise);
+        if (sub == 0 && wave < Ti::kHeads) run_gates<!Ti::kNormalise>(gates + wave, (float)g, p.reverse, p.in_scale, p.weight_scale, Ti::kNormalise, base);
         __syncthreads();
         // (a lane's number, and the addresses that are made of it, anew for each part: see Tile::load)
         int lane = lane_id_again(), x = lane & 15, q = lane >> 4;
@@ -491,13 +496,17 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         Frag mv[MASKED ? 4 : 1];
         if constexpr (MASKED) {
             if (ends && live) {
-                const unsigned om = (unsigned)(p.reverse ? 15 - x : x) * (unsigned)p.m.ts + 4 * q * (unsigned)sizeof(T);
+                const unsigned om = times(p.reverse ? 15 - x : x, p.m.ts) + 4 * q * (unsigned)sizeof(T);
                 const BufRsrc from = whole_rsrc(pm + (ga > 1 ? sub : 0) * p.m.hs);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     mv[i] = load_through<Frag>(from, x < rows - 16 * i ? om : kNowhere, (p.reverse ? 3 - i : i) * 16 * (unsigned)p.m.ts);
                 if (sub + 1 == group) pm += chunk * p.m.ts;
             }
+        }
+        if (it + 1 < steps) {
+            next_sub = sub + 1 == group ? 0 : sub + 1;
+            fetch(first + (next_sub == 0 ? kChunk : 0), next_sub);
         }
         // what they take from the chunk's own rows
         if constexpr (Ti::kShare) __syncthreads();
@@ -561,7 +570,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
             const BufRsrc to = whole_rsrc(po + (ga > 1 ? sub : 0) * p.out_hs);
             if (sub + 1 == group) po += chunk * p.out_ts;
             lane = lane_id_again(), x = lane & 15, q = lane >> 4;
-            const unsigned off = (unsigned)(p.reverse ? 15 - x : x) * (unsigned)p.out_ts + 4 * q * (unsigned)sizeof(T);
+            const unsigned off = times(p.reverse ? 15 - x : x, p.out_ts) + 4 * q * (unsigned)sizeof(T);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bool row = x < rows - 16 * i;
@@ -581,10 +590,6 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
                 }
             }
         }
-        if (it + 1 < steps) {
-            next_sub = sub + 1 == group ? 0 : sub + 1;
-            fetch(first + (next_sub == 0 ? kChunk : 0), next_sub);
-        }
         __builtin_amdgcn_sched_barrier(0);
         // the state behind the chunk
         if (feeds) {
@@ -598,7 +603,8 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
             }
             const bool decays = gb == 1 || sub == 0;
             if (decays) factor *= gt.total;
-            if (decays || Ti::kNormalise) state.scale(factor);
+            if constexpr (!Ti::kNormalise) unit = gt.unit;
+            if (factor != 1.0f) state.scale(factor);
             state.add(hb, vt, gt.weight, unit);
         }
         __syncthreads();
@@ -615,7 +621,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         }
     }
     if (live && p.last != nullptr && seg.index == (p.reverse ? 0 : seg.count - 1))
-        state.write(p.last + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs, 1.0f / unit);
+        state.write(p.last + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs, Ti::kNormalise ? 1.0f / unit : unit);
 }
 
 // d log_gate of a segment's tokens and one head: from the segment's end, x_t = q_t . dq_t - k_t . dk_t summed up, on top of

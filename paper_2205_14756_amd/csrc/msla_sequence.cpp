@@ -81,7 +81,7 @@ msla_status plan_of(const msla_recurrence& s, bool backward, RecurrencePlan* pla
 }
 
 // Strides that the kernels' 32-bit offsets inside a chunk of 64 tokens cover, in bytes.
-constexpr int64_t kMostTokenStride = (int64_t)1 << 25, kMostHeadStride = (int64_t)1 << 29;
+constexpr int64_t kMostTokenStride = ((int64_t)1 << 24) - 1, kMostHeadStride = (int64_t)1 << 29;
 
 bool wide(const msla_heads& h, msla_dtype dt) {
     const int64_t e = (int64_t)elem_size(dt);

@@ -22,7 +22,7 @@ constexpr int kSlice = 16;          // output channels of a wave
 
 struct Heads {
     const char* p;
-    long ts, hs;                    // bytes from a token, and a head, to the next (at most 2^25 and 2^29)
+    long ts, hs;                    // bytes from a token, and a head, to the next (below 2^24, and at most 2^29)
     int relu;
 };
 
@@ -87,6 +87,9 @@ constexpr unsigned kNowhere = 0xfffffff0u;
 __device__ __forceinline__ BufRsrc whole_rsrc(const char* at) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, (int)kNowhere, 0x00020000);
 }
+
+// a row's number, below 256, times a token's stride (a product of 24-bit factors issues four times as fast as one of 32)
+__device__ __forceinline__ unsigned times(unsigned row, long ts) { return __umul24(row, (unsigned)ts); }
 
 template <class T, int D>
 struct Tile {
@@ -154,12 +157,11 @@ struct Tile {
     }
     // Rows above `rows` are not the segment's, heads above `heads` nobody's: zero, and not read, by the resource's range check, which leaves no
     // branch around a load and nothing to wait for.
-    static __device__ __forceinline__ void load(Regs& r, const char* at, const Heads& h, int reverse, int per, int rows, int heads, int wave) {
-        const int t = thread(wave);
+    static __device__ __forceinline__ void load(Regs& r, const char* at, const Heads& h, int reverse, int per, int rows, int heads, int t) {
         const BufRsrc from = whole_rsrc(at);
         const unsigned step = (unsigned)kRowStep * (unsigned)h.ts;
-        unsigned off = (unsigned)(reverse ? kRowStep - 1 - row(t) : row(t)) * (unsigned)h.ts + (unsigned)(head_of(t) * per) * (unsigned)h.hs +
-                       t % (D / kVec) * 16u;
+        unsigned off = times((unsigned)(reverse ? kRowStep - 1 - row(t) : row(t)), h.ts) + t % (D / kVec) * 16u;
+        if (kHeads > 1) off += (unsigned)(head_of(t) * per) * (unsigned)h.hs;
         if (kHeads > 1 && head_of(t) >= heads) off = kNowhere;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
@@ -168,8 +170,7 @@ struct Tile {
 
     // into LDS, rectified where asked; returns the largest bit pattern of a finite magnitude (fp16 alone; a value that is not finite may
     // not spoil the other heads' normalisers)
-    static __device__ __forceinline__ unsigned store(Regs& r, char* tile, int relu, int wave) {
-        const int t = thread(wave);
+    static __device__ __forceinline__ unsigned store(Regs& r, char* tile, int relu, int t) {
         typedef short i16x8 __attribute__((ext_vector_type(8)));
         typedef int i32x4 __attribute__((ext_vector_type(4)));
         unsigned top = 0;
@@ -279,12 +280,17 @@ struct Tile {
 
 // A chunk's running gates, in LDS: exponents (base 2) from the chunk's start to each row, as a float and what it leaves out of the
 // double that they are summed in, so that differences stay exact behind a gate that forgets everything.
+//
+// The state is kept as 2^base times what stands in registers: while base stays small, a chunk's gates move base instead of multiplying every
+// element, and the rows' weights make up for it.
 struct Gates {
     float hi[kChunk], lo[kChunk];
     float in[kChunk];               // the state's factor in this row's output
     float weight[kChunk];           // this row's factor in the state behind the chunk
-    float total, grow, exponent, pad;       // the state's own factor; how far gates above 0 let a weight grow; log2 of total
+    float total, grow, exponent, unit;      // what the registers are multiplied by; how far gates above 0 let a weight grow; log2 of the chunk's
+                                            // gates; 2^base behind the chunk
 };
+constexpr float kMostBase = 64.0f;
 
 constexpr double kLog2e = 1.4426950408889634;
 
@@ -307,9 +313,10 @@ __device__ __forceinline__ double running_sum(double v) {
     return v;
 }
 
-// by one wave; `g`: this lane's row's gate (0 where there is no row)
-__device__ __forceinline__ void run_gates(Gates* out, float g, int reverse, float in_scale, float weight_scale, bool want_grow) {
-    const int lane = lane_id();
+// By one wave; `g`: this lane's row's gate (0 where there is no row); base: before the chunk, and then behind it.  LAZY: base may move.
+template <bool LAZY>
+__device__ __forceinline__ void run_gates(Gates* out, float g, int reverse, float in_scale, float weight_scale, bool want_grow, double& base) {
+    const int lane = lane_id_again();
     double own = (double)g * kLog2e;
     if (own < -150.0) own = -150.0;         // 2^-150 is 0 in fp32; a NaN stays one
     const double sum = running_sum(own);
@@ -320,11 +327,19 @@ __device__ __forceinline__ void run_gates(Gates* out, float g, int reverse, floa
     const float hi = (float)here, lo = (float)(here - (double)hi);
     out->hi[lane] = hi;
     out->lo[lane] = lo;
-    out->in[lane] = __builtin_amdgcn_exp2f(hi) * fmaf(lo, 0.693147182f, 1.0f) * in_scale;
-    out->weight[lane] = __builtin_amdgcn_exp2f((float)(total - here)) * weight_scale;
+    const double in = here + base;
+    const float in_hi = (float)in;
+    out->in[lane] = __builtin_amdgcn_exp2f(in_hi) * fmaf((float)(in - (double)in_hi), 0.693147182f, 1.0f) * in_scale;
+    const double moved = base + total;
+    const bool moves = LAZY && moved > -kMostBase && moved < kMostBase;
+    const double weight = moves ? -in : total - here;
+    const float w_hi = (float)weight;
+    out->weight[lane] = __builtin_amdgcn_exp2f(w_hi) * fmaf((float)(weight - (double)w_hi), 0.693147182f, 1.0f) * weight_scale;
+    base = moves ? moved : 0.0;
     if (lane == 0) {
-        out->total = __builtin_amdgcn_exp2f((float)total);
+        out->total = moves ? 1.0f : __builtin_amdgcn_exp2f((float)moved);
         out->exponent = (float)total;
+        out->unit = __builtin_amdgcn_exp2f((float)base);
     }
     if (want_grow) {
         float grow = own > 0.0 ? (float)own : 0.0f;

@@ -389,8 +389,8 @@ def test_the_binding_refuses():
 
 def test_offsets_beyond_the_first_2_gib():
     """Tokens whose bytes lie beyond 2^32 from the operand's start: wide rows of which a head is a small part."""
-    tokens, d = 140, 16
-    wide = 1 << 24                                              # elements from token to token, as far as they may lie apart: 140 * 32 MiB = 4.7 GB
+    tokens, d = 300, 16
+    wide = (1 << 23) - 8                                        # elements from token to token, as far as they may lie apart: 300 * 16 MiB = 5 GB
     big = torch.zeros(tokens * wide, dtype=torch.bfloat16, device="cuda").view(tokens, 1, wide)
     t = make(18, "bf16", tokens, 1, 1, d, [tokens], initial=False)
     big[:, :, :d] = t["k"]
