@@ -204,7 +204,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     char* tb = lds;
     char* tc = tb + Ti::kBytes;
     Gates* gates = (Gates*)(tc + Ti::kBytes);
-    unsigned* tops = (unsigned*)(gates + Ti::kHeads);           // [2][waves][3]
+    unsigned* tops = (unsigned*)(gates + 2 * Ti::kHeads);           // [2][waves][3]
 
     const Segment seg = find_segment(p.layout, blockIdx.x);
     if (!seg.live || seg.index == (p.reverse ? 0 : seg.count - 1)) return;     // nothing comes after it
@@ -218,7 +218,8 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     state.clear();
     float exponent = 0.0f, unit = 1.0f;
     typename Ti::Regs rb, rc;
-    GateRows<T> gate_rows(p.gate, p.gate_ts, seg, p.reverse, head0 + wave, p.heads);
+    const int gate_wave = Ti::kWaves - 1 - wave;        // the last waves have the fewest scores to compute
+    GateRows<T> gate_rows(p.gate, p.gate_ts, seg, p.reverse, head0 + gate_wave, p.heads);
     T g = (T)0.0f;
     double base = 0.0;              // of the head whose gates this wave sums
     const int heads = p.heads - head0;
@@ -227,7 +228,6 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     const char* pc = Ti::start(p.c, seg, p.reverse, head0 * p.gb);
     auto fetch = [&](long u, int sub) {         // the tiles of rows u.. and of the sub-th of the heads of (b, c); pb, pc: their first ones'
         const int rows = (int)min(len - u, (long)kChunk), t = Ti::thread(wave);
-        if (sub == 0 && wave < Ti::kHeads) g = gate_rows.next(rows, p.reverse);
         Ti::load(rb, pb + sub * p.b.hs, p.b, p.reverse, p.gb, rows, heads, t);
         Ti::load(rc, pc + sub * p.c.hs, p.c, p.reverse, p.gb, rows, heads, t);
         if (sub + 1 == p.gb) {
@@ -235,7 +235,16 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
             pc += chunk * p.c.ts;
         }
     };
+    // gates run a chunk ahead of the tiles: they are summed by a wave while the others multiply
+    auto gates_of = [&](long u) {
+        if (gate_wave < Ti::kHeads && u < len) {
+            run_gates<!Ti::kNormalise>(gates + (u / kChunk & 1) * Ti::kHeads + gate_wave, (float)g, p.reverse, 1.0f, p.weight_scale, Ti::kNormalise, base);
+            g = gate_rows.next((int)min(len - u - kChunk, (long)kChunk), p.reverse);
+        }
+    };
+    if (gate_wave < Ti::kHeads) g = gate_rows.next((int)min(len, (long)kChunk), p.reverse);
     fetch(0, 0);
+    gates_of(0);
     __syncthreads();
     int sub = 0, next_sub = 0;
     long first = 0;
@@ -245,13 +254,13 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         Ti::store(rb, tb, p.b.relu, t);
         const unsigned mc = Ti::store(rc, tc, p.c.relu, t);
         if constexpr (Ti::kNormalise) leave_top(top + 2, mc);
-        if (sub == 0 && wave < Ti::kHeads) run_gates<!Ti::kNormalise>(gates + wave, (float)g, p.reverse, 1.0f, p.weight_scale, Ti::kNormalise, base);
         __syncthreads();
         if (it + 1 < steps) {
             next_sub = sub + 1 == p.gb ? 0 : sub + 1;
             fetch(first + (next_sub == 0 ? kChunk : 0), next_sub);
         }
-        const Gates& gt = gates[mine];
+        const Gates& gt = gates[(first / kChunk & 1) * Ti::kHeads + mine];
+        if (sub == 0) gates_of(first + kChunk);
         float fresh = unit, factor = 1.0f;
         if constexpr (Ti::kNormalise) {
             const float bound = tile_top<Ti::kWaves>(top + 2) * fabsf(p.weight_scale) * gt.grow;
@@ -321,13 +330,6 @@ __device__ __forceinline__ F load_through(BufRsrc r, unsigned off, unsigned scal
     if constexpr (sizeof(F) == 8) return __builtin_bit_cast(F, __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, (int)scalar, 0));
     else return __builtin_bit_cast(F, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)scalar, 0));
 }
-// (no scalar offset in a store: see buf_store16_at_as)
-template <class F>
-__device__ __forceinline__ void store_through(BufRsrc r, unsigned off, F v) {
-    if constexpr (sizeof(F) == 8) buf_store8(r, off, __builtin_bit_cast(u32x2, v));
-    else buf_store16(r, off, __builtin_bit_cast(u32x4, v));
-}
-
 // MASKED: out is masked and measured against m (p.m, p.dots).  GROUP: there are several heads of a, or of (b, c), to a state head.
 template <class T, int D, bool MASKED, bool GROUP>
 __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupancy)) recurrence_sweep_kernel(SweepArgs p) {
@@ -343,7 +345,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     char* tb = ta + Ti::kBytes;
     char* tc = tb + Ti::kBytes;
     Gates* gates = (Gates*)(tc + Ti::kBytes);
-    unsigned* tops = (unsigned*)(gates + Ti::kHeads);           // [2][waves][3]
+    unsigned* tops = (unsigned*)(gates + 2 * Ti::kHeads);           // [2][waves][3]
     float* dots = (float*)(tops + 6 * Ti::kWaves);              // [waves][64]
     char* scores = (char*)(dots + kChunk * Ti::kWaves);
 
@@ -367,7 +369,8 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     if constexpr (Ti::kNormalise) bound_s = state.top();
 
     typename Ti::Regs ra, rb, rc;
-    GateRows<T> gate_rows(p.gate, p.gate_ts, seg, p.reverse, head0 + wave, p.heads);
+    const int gate_wave = Ti::kWaves - 1 - wave;        // the last waves have the fewest scores to compute
+    GateRows<T> gate_rows(p.gate, p.gate_ts, seg, p.reverse, head0 + gate_wave, p.heads);
     T g = (T)0.0f;
     double base = 0.0;              // of the head whose gates this wave sums
     const int heads = p.heads - head0;
@@ -377,7 +380,6 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     const char* pc = Ti::start(p.c, seg, p.reverse, head0 * gb);
     auto fetch = [&](long u, int sub) {         // the tiles of rows u.. that the sub-th step of a chunk needs anew
         const int rows = (int)min(len - u, (long)kChunk), t = Ti::thread(wave);
-        if (sub == 0 && wave < Ti::kHeads) g = gate_rows.next(rows, p.reverse);
         if (sub == 0 || ga > 1) Ti::load(ra, pa + (ga > 1 ? sub : 0) * p.a.hs, p.a, p.reverse, ga, rows, heads, t);
         if (sub == 0 || gb > 1) {
             Ti::load(rb, pb + (gb > 1 ? sub : 0) * p.b.hs, p.b, p.reverse, gb, rows, heads, t);
@@ -392,7 +394,16 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     // rows 16i + x of out (and of what it is masked with) in the same way; a chunk's last 16 rows are its first ones from the end
     char* po = p.out + (p.reverse ? seg.hi - kChunk : seg.lo) * p.out_ts + (long)head * ga * p.out_hs + slice * (int)sizeof(T);
     const char* pm = MASKED ? Ti::start(p.m, seg, p.reverse, head * ga) + slice * (int)sizeof(T) : nullptr;
+    // gates run a chunk ahead of the tiles: they are summed by a wave while the others multiply
+    auto gates_of = [&](long u) {
+        if (gate_wave < Ti::kHeads && u < len) {
+            run_gates<!Ti::kNormalise>(gates + (u / kChunk & 1) * Ti::kHeads + gate_wave, (float)g, p.reverse, p.in_scale, p.weight_scale, Ti::kNormalise, base);
+            g = gate_rows.next((int)min(len - u - kChunk, (long)kChunk), p.reverse);
+        }
+    };
+    if (gate_wave < Ti::kHeads) g = gate_rows.next((int)min(len, (long)kChunk), p.reverse);
     if (steps > 0) fetch(0, 0);
+    gates_of(0);
     f32x4 o[4];
     __syncthreads();
     int sub = 0, next_sub = 0;
@@ -414,11 +425,11 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
             leave_top(top + 1, mb);
             leave_top(top + 2, mc);
         }
-        if (sub == 0 && wave < Ti::kHeads) run_gates<!Ti::kNormalise>(gates + wave, (float)g, p.reverse, p.in_scale, p.weight_scale, Ti::kNormalise, base);
         __syncthreads();
         // (a lane's number, and the addresses that are made of it, anew for each part: see Tile::load)
         int lane = lane_id_again(), x = lane & 15, q = lane >> 4;
-        const Gates& gt = gates[mine];
+        const Gates& gt = gates[(first / kChunk & 1) * Ti::kHeads + mine];
+        if (sub == 0) gates_of(first + kChunk);
         const char* ha = ta + mine * Ti::kHeadBytes;
         char* hb = tb + mine * Ti::kHeadBytes;
         char* hc = tc + mine * Ti::kHeadBytes;
@@ -570,23 +581,37 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
             const BufRsrc to = whole_rsrc(po + (ga > 1 ? sub : 0) * p.out_hs);
             if (sub + 1 == group) po += chunk * p.out_ts;
             lane = lane_id_again(), x = lane & 15, q = lane >> 4;
-            const unsigned off = times(p.reverse ? 15 - x : x, p.out_ts) + 4 * q * (unsigned)sizeof(T);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool row = x < rows - 16 * i;
-                float dot = 0.0f;
                 if constexpr (MASKED) {
+                    float dot = 0.0f;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float me = Tr::to_f32(mv[i][r]);      // (0 where there is no row)
                         if (p.m.relu && !(me > 0.0f)) o[i][r] = 0.0f;
                         dot = fmaf(me, o[i][r], dot);
                     }
-                }
-                store_through(to, row ? off + (p.reverse ? 3 - i : i) * 16 * (unsigned)p.out_ts : kNowhere, frag_from_f32<T>(o[i]));
-                if constexpr (MASKED) {
                     dot = over_column(dot);
                     if (q == 0) dots[wave * kChunk + 16 * i + x] = dot;
+                }
+            }
+            if constexpr (sizeof(T) == 2) {
+                // two rows of blocks trade halves between neighbouring groups of 16 lanes: a lane then has 8 channels of one row, 16 bytes
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    const u32x2 a = __builtin_bit_cast(u32x2, frag_from_f32<T>(o[i])), b = __builtin_bit_cast(u32x2, frag_from_f32<T>(o[i + 1]));
+                    const u32x2 s0 = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+                    const u32x2 s1 = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+                    const int row = 16 * (i + (q & 1)) + x;
+                    const unsigned off = times(p.reverse ? kChunk - 1 - row : row, p.out_ts) + 16 * (q >> 1);
+                    buf_store16(to, row < rows ? off : kNowhere, u32x4{s0[0], s1[0], s0[1], s1[1]});
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = 16 * i + x;
+                    const unsigned off = times(p.reverse ? kChunk - 1 - row : row, p.out_ts) + 16 * q;
+                    buf_store16(to, row < rows ? off : kNowhere, __builtin_bit_cast(u32x4, o[i]));
                 }
             }
         }
@@ -763,7 +788,7 @@ __global__ void __launch_bounds__(kThreads) recurrence_step_kernel(StepArgs p) {
 
 // ------------------------------------------------------------------------------------------------ host side
 template <class T, int D>
-constexpr int tile_lds(int tiles) { return tiles * Tile<T, D>::kBytes + Tile<T, D>::kHeads * (int)sizeof(Gates) + 6 * Tile<T, D>::kWaves * 4; }
+constexpr int tile_lds(int tiles) { return tiles * Tile<T, D>::kBytes + 2 * Tile<T, D>::kHeads * (int)sizeof(Gates) + 6 * Tile<T, D>::kWaves * 4; }
 template <class T, int D>
 constexpr int sweep_lds() { return tile_lds<T, D>(3) + kChunk * Tile<T, D>::kWaves * 4 + Tile<T, D>::kScoreBytes; }
 
