@@ -112,11 +112,9 @@ msla_status msla_quantize_rows(const void* x, void* x8, float* scale, int64_t ro
 
 /* y[n, o] = x_scale[n] * w_scale[o] * sum_c x8[n, c] w8[o, c]   (msla_linear of rows that stand in 8 bits)
  *   x8 [rows, c_in], w8 [c_out, c_in] e4m3;  x_scale [rows], w_scale [c_out] fp32 (aligned to 4 bytes);  y [rows, c_out] in dt.
- * c_in, c_out multiples of 16.  fp32 sums.  workspace: for few rows the contraction is split; the query may report 0. */
-msla_status msla_linear_quantized_workspace_bytes(int64_t rows, int c_in, int c_out, size_t* bytes);
-msla_status msla_linear_quantized(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y,
-                                  void* workspace, size_t workspace_bytes, int64_t rows, int c_in, int c_out, msla_dtype dt,
-                                  void* stream);
+ * c_in, c_out multiples of 16.  Products are exact, sums fp32. */
+msla_status msla_linear_quantized(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows, int c_in,
+                                  int c_out, msla_dtype dt, void* stream);
 
 #ifdef __cplusplus
 }

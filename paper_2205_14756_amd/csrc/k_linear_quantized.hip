@@ -130,23 +130,111 @@ __global__ void __launch_bounds__(256, 2) linear_quantized_kernel(const unsigned
     }
 }
 
+// Which of the two: by rounds of their workgroups over the 256 compute units.  A round takes, by measurement at 512 .. 8192 channels, 2.7 ns a
+// channel of the contraction here (64 rows, 16 outputs) and 9.8 ns there (128 rows, 128 outputs, one workgroup to a unit): at 4096 channels 11
+// and 40 us.  4096 -> 4096: 64 rows 12 against 43 us, 192 rows 34 against 43, 256 rows 44 against 43; 8192 -> 512: 512 rows 22 against 81.
+bool rows_kernel_wins(int64_t rows, int c_out) {
+    if (rows <= 48) return true;
+    const int64_t here = ((rows + 63) / 64 * (c_out / 16) + 255) / 256, there = ((rows + 127) / 128 * ((c_out + 127) / 128) + 255) / 256;
+    return here * 27 < there * 98;
+}
+
+// Few rows: the weights are read once and that is what there is to do, so a workgroup has 16 outputs, its eight waves take 128 bytes of the
+// contraction each in turn, and their sums meet in LDS.  Up to 64 rows a workgroup (BLOCKS of 16), which come out of L2.
+template <class T, int BLOCKS>
+__global__ void __launch_bounds__(512) linear_quantized_rows_kernel(const unsigned char* x8, const float* x_scale, const unsigned char* w8,
+                                                                    const float* w_scale, T* y, int64_t rows, int c_in, int c_out) {
+    constexpr int kWaves = 8;
+    __shared__ float sums[kWaves][BLOCKS][16][17];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), x = lane & 15, q = lane >> 4;
+    const int o0 = blockIdx.x * 16;
+    const int64_t n0 = (int64_t)blockIdx.y * (16 * BLOCKS);
+    const unsigned char* wp = w8 + (int64_t)(o0 + x) * c_in + 16 * q;
+    const unsigned char* xp[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) xp[b] = x8 + min(n0 + 16 * b + x, rows - 1) * c_in + 16 * q;     // (rows behind the last: not stored)
+    f32x4 acc[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) acc[b] = f32x4{0, 0, 0, 0};
+    struct Stage { u32x4 w[2], x[BLOCKS][2]; };
+    auto load = [&](Stage& s, int k0) {
+        if (k0 + kTileK <= c_in) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                s.w[h] = *(const u32x4*)(wp + k0 + 64 * h);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) s.x[b][h] = *(const u32x4*)(xp[b] + k0 + 64 * h);
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool in = k0 + 64 * h + 16 * q < c_in;
+                s.w[h] = u32x4{0, 0, 0, 0};
+                if (in) s.w[h] = *(const u32x4*)(wp + k0 + 64 * h);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                    s.x[b][h] = u32x4{0, 0, 0, 0};
+                    if (in) s.x[b][h] = *(const u32x4*)(xp[b] + k0 + 64 * h);
+                }
+            }
+        }
+    };
+    auto multiply = [&](const Stage& s) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const Pair w = widen(s.w[h]);
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) acc[b] = mma8(acc[b], w, widen(s.x[b][h]));
+        }
+    };
+    constexpr int kStride = kWaves * kTileK;
+    Stage s0, s1;
+    int k = wave * kTileK;
+    if (k < c_in) load(s0, k);
+    for (; k < c_in; k += 2 * kStride) {
+        if (k + kStride < c_in) load(s1, k + kStride);
+        multiply(s0);
+        if (k + 2 * kStride < c_in) load(s0, k + 2 * kStride);
+        if (k + kStride < c_in) multiply(s1);
+    }
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][b][x][4 * q + r] = acc[b][r];
+    __syncthreads();
+    for (int e = threadIdx.x; e < BLOCKS * 256; e += 512) {
+        const int n = e / 16, o = e % 16;
+        if (n0 + n >= rows) continue;
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += sums[w][n / 16][n % 16][o];
+        y[(n0 + n) * c_out + o0 + o] = Traits<T>::from_f32(v * (x_scale[n0 + n] * w_scale[o0 + o]));
+    }
+}
+
 template <class T>
 hipError_t linear_of(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows, int c_in, int c_out,
                      hipStream_t stream) {
+    const unsigned char *xp = (const unsigned char*)x8, *wp = (const unsigned char*)w8;
     const int tiles_o = (c_out + 127) / 128;
-    const int64_t blocks = (rows + 127) / 128 * tiles_o;
-    if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((linear_quantized_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, stream, (const unsigned char*)x8, x_scale,
-                       (const unsigned char*)w8, w_scale, (T*)y, rows, c_in, c_out, tiles_o);
+    const int64_t tiles = (rows + 127) / 128 * tiles_o;
+    if (tiles > 0x7fffffffL) return hipErrorInvalidValue;
+    if (rows_kernel_wins(rows, c_out)) {
+        const dim3 threads(512);
+        if (rows <= 16) hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 1>), dim3(c_out / 16, 1), threads, 0, stream, xp, x_scale, wp, w_scale, (T*)y, rows, c_in, c_out);
+        else if (rows <= 32) hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 2>), dim3(c_out / 16, 1), threads, 0, stream, xp, x_scale, wp, w_scale, (T*)y, rows, c_in, c_out);
+        else if (rows <= 48) hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 3>), dim3(c_out / 16, 1), threads, 0, stream, xp, x_scale, wp, w_scale, (T*)y, rows, c_in, c_out);
+        else hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 4>), dim3(c_out / 16, (unsigned)((rows + 63) / 64)), threads, 0, stream, xp, x_scale, wp, w_scale, (T*)y, rows, c_in, c_out);
+    } else {
+        hipLaunchKernelGGL((linear_quantized_kernel<T>), dim3((unsigned)tiles), dim3(256), 0, stream, xp, x_scale, wp, w_scale, (T*)y, rows, c_in, c_out, tiles_o);
+    }
     return hipGetLastError();
 }
 
 }  // namespace
 
-int linear_quantized_splits(int64_t, int, int) { return 1; }
-
-hipError_t launch_linear_quantized(int dt, const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, float*, int,
-                                   int64_t rows, int c_in, int c_out, hipStream_t stream) {
+hipError_t launch_linear_quantized(int dt, const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows,
+                                   int c_in, int c_out, hipStream_t stream) {
     switch (dt) {
         case 0: return linear_of<float>(x8, x_scale, w8, w_scale, y, rows, c_in, c_out, stream);
         case 1: return linear_of<_Float16>(x8, x_scale, w8, w_scale, y, rows, c_in, c_out, stream);

@@ -289,36 +289,14 @@ msla_status msla_norm_backward(const void* sum, const void* weight, const void* 
                                                 (hipStream_t)stream));
 }
 
-static msla_status check_linear(int64_t rows, int c_in, int c_out) {
-    if (rows < 0 || c_in <= 0 || c_out <= 0) return MSLA_ERR_INVALID_ARG;
+msla_status msla_linear_quantized(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows, int c_in,
+                                  int c_out, msla_dtype dt, void* stream) {
+    if (rows < 0 || c_in <= 0 || c_out <= 0 || !known(dt)) return MSLA_ERR_INVALID_ARG;
+    if (!aligned(x8, 16) || !aligned(w8, 16) || !aligned(y, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 4)) return MSLA_ERR_INVALID_ARG;
     if (c_in % 16 != 0 || c_out % 16 != 0 || rows > 0x7fffffffLL) return MSLA_ERR_UNSUPPORTED;
-    return MSLA_OK;
-}
-
-msla_status msla_linear_quantized_workspace_bytes(int64_t rows, int c_in, int c_out, size_t* bytes) {
-    if (bytes == nullptr) return MSLA_ERR_INVALID_ARG;
-    const msla_status st = check_linear(rows, c_in, c_out);
-    if (st != MSLA_OK) return st;
-    const int splits = rows > 0 ? msla::linear_quantized_splits(rows, c_in, c_out) : 1;
-    *bytes = splits > 1 ? align_up((size_t)splits * rows * c_out * 4) : 0;
-    return MSLA_OK;
-}
-
-msla_status msla_linear_quantized(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, void* workspace,
-                                  size_t workspace_bytes, int64_t rows, int c_in, int c_out, msla_dtype dt, void* stream) {
-    const msla_status st = check_linear(rows, c_in, c_out);
-    if (st != MSLA_OK) return st;
-    if (!known(dt) || !aligned(x8, 16) || !aligned(w8, 16) || !aligned(y, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 4))
-        return MSLA_ERR_INVALID_ARG;
     if (rows == 0) return MSLA_OK;
     if (!x8 || !x_scale || !w8 || !w_scale || !y || y == x8 || y == w8) return MSLA_ERR_INVALID_ARG;
-    const int splits = msla::linear_quantized_splits(rows, c_in, c_out);
-    if (splits > 1) {
-        if (workspace == nullptr || !aligned(workspace, 16)) return MSLA_ERR_INVALID_ARG;
-        if (workspace_bytes < (size_t)splits * rows * c_out * 4) return MSLA_ERR_WORKSPACE;
-    }
-    return status_of(msla::launch_linear_quantized((int)dt, x8, x_scale, w8, w_scale, y, (float*)workspace, splits, rows, c_in, c_out,
-                                                   (hipStream_t)stream));
+    return status_of(msla::launch_linear_quantized((int)dt, x8, x_scale, w8, w_scale, y, rows, c_in, c_out, (hipStream_t)stream));
 }
 
 }  // extern "C"

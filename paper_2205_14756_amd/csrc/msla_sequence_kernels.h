@@ -55,8 +55,7 @@ int norm_backward_blocks(int64_t rows, int channels, int elem);
 hipError_t launch_norm_backward(int dt, const void* sum, const void* weight, const void* d_y, const void* d_sum, void* d_r, float* d_weight,
                                 float* partials, int64_t rows, int channels, float eps, hipStream_t stream);
 
-int linear_quantized_splits(int64_t rows, int c_in, int c_out);
-hipError_t launch_linear_quantized(int dt, const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, float* partials,
-                                   int splits, int64_t rows, int c_in, int c_out, hipStream_t stream);
+hipError_t launch_linear_quantized(int dt, const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows,
+                                   int c_in, int c_out, hipStream_t stream);
 
 }  // namespace msla

@@ -16,7 +16,7 @@ from .msla import MSLA_OK, MslaError, _DTYPES, _ptr, _stream
 
 EXPORTS = ("msla_recurrence_workspace_bytes", "msla_recurrence_forward", "msla_recurrence_backward", "msla_recurrence_step",
            "msla_norm_forward", "msla_norm_quantized", "msla_norm_backward_workspace_bytes", "msla_norm_backward", "msla_quantize_rows",
-           "msla_linear_quantized_workspace_bytes", "msla_linear_quantized")
+           "msla_linear_quantized")
 
 HEAD_DIMS = (16, 32, 64, 128)
 
@@ -49,8 +49,7 @@ def _lib():
         lib.msla_norm_backward_workspace_bytes.argtypes = [i64, i, i, size]
         lib.msla_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, i64, i, f, i, vp]
         lib.msla_quantize_rows.argtypes = [vp, vp, vp, i64, i, i, vp]
-        lib.msla_linear_quantized_workspace_bytes.argtypes = [i64, i, i, size]
-        lib.msla_linear_quantized.argtypes = [vp, vp, vp, vp, vp, vp, sz, i64, i, i, i, vp]
+        lib.msla_linear_quantized.argtypes = [vp, vp, vp, vp, vp, i64, i, i, i, vp]
         for name in EXPORTS:
             getattr(lib, name).restype = i
         _ready = lib
@@ -62,99 +61,130 @@ def _check(status, where):
         raise MslaError(status, where)
 
 
-def _need(condition, what):
-    if not condition:
-        raise ValueError("msla: " + what)
+def _refuse(what):
+    raise ValueError("msla: " + what)
+
+
+# Small calls wait for the host (a call on one token is some us on the GPU), so the checks below are made of few attribute reads: contiguous
+# operands, which most are, are recognised by one, and shapes are compared as they come.
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _on_gpu(*tensors):
     """All on the current device (whose stream the work goes to)."""
-    here = None
+    here = -1
     for t in tensors:
         if t is not None:
-            _need(t.is_cuda, "tensors must live in GPU memory")
-            if here is None:
-                here = torch.cuda.current_device()
-            _need(t.get_device() == here, "tensors must live on the current device")
+            at = t.get_device()
+            if at != here or at < 0:
+                if not (at >= 0 and t.is_cuda):
+                    _refuse("tensors must live in GPU memory")
+                if at != _device():
+                    _refuse("tensors must live on the current device")
+                here = at
 
 
 def _plain(t, name, shape, dtype):
-    if t is not None:
-        _need(t.is_contiguous(), f"{name} must be contiguous")
-        _need(tuple(t.shape) == tuple(shape), f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-        _need(t.dtype == dtype, f"{name} must be {dtype}, not {t.dtype}")
+    if t is not None and not (t.shape == shape and t.dtype == dtype and t.is_contiguous()):
+        if not t.is_contiguous():
+            _refuse(f"{name} must be contiguous")
+        if not (tuple(t.shape) == tuple(shape)):
+            _refuse(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+        if not (t.dtype == dtype):
+            _refuse(f"{name} must be {dtype}, not {t.dtype}")
 
 
 def _rows(t, name, like=None):
     """A [..., heads, head_dim] tensor as rows of tokens: (data, token stride, head stride), tokens in order."""
-    _need(t.dim() >= 3, f"{name} must be [..., heads, head_dim]")
-    _need(t.stride(-1) == 1 or t.shape[-1] == 1, f"{name}'s channels must lie next to each other")
-    tokens, step = 1, t.stride(-3)
-    for size, stride in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
-        _need(size == 1 or tokens == 1 or stride == step * tokens, f"{name}'s tokens must lie at equal distances")
+    shape = t.shape
+    if like is not None and shape != like:
+        _refuse(f"{name} must have the shape {tuple(like)}, not {tuple(shape)}")
+    if not (len(shape) >= 3):
+        _refuse(f"{name} must be [..., heads, head_dim]")
+    heads, dim = shape[-2:]
+    if t.is_contiguous():
+        row = heads * dim
+        return _Heads(t.data_ptr(), row, dim), t.numel() // row if row else 0
+    strides = t.stride()
+    if not (strides[-1] == 1 or dim == 1):
+        _refuse(f"{name}'s channels must lie next to each other")
+    tokens, step = 1, strides[-3]
+    for size, stride in zip(shape[-3::-1], strides[-3::-1]):
+        if not (size == 1 or tokens == 1 or stride == step * tokens):
+            _refuse(f"{name}'s tokens must lie at equal distances")
         if tokens == 1 and size != 1:
             step = stride
         tokens *= size
-    if like is not None:
-        _need(tuple(t.shape) == tuple(like), f"{name} must have the shape {tuple(like)}, not {tuple(t.shape)}")
     # (the stride of an axis of length one says nothing, and torch leaves anything there)
-    return _Heads(t.data_ptr(), step if tokens > 1 else 0, t.stride(-2) if t.shape[-2] > 1 else 0), tokens
+    return _Heads(t.data_ptr(), step if tokens > 1 else 0, strides[-2] if heads > 1 else 0), tokens
 
 
 def _gate(t, tokens, heads, dtype, name):
     if t is None:
         return None, 0
-    _need(t.dtype == dtype, f"{name} must be {dtype}, not {t.dtype}")
-    _need(t.numel() == tokens * heads and t.shape[-1] == heads, f"{name} must be [..., heads_kv]")
+    if not (t.dtype == dtype):
+        _refuse(f"{name} must be {dtype}, not {t.dtype}")
+    if not (t.shape[-1] == heads and t.numel() == tokens * heads):
+        _refuse(f"{name} must be [..., heads_kv]")
+    if t.is_contiguous():
+        return t.data_ptr(), heads
     flat = t if t.dim() == 2 else t.view(-1, heads)
-    _need(heads == 1 or flat.stride(1) == 1, f"{name}'s heads must lie next to each other")
+    if not (heads == 1 or flat.stride(1) == 1):
+        _refuse(f"{name}'s heads must lie next to each other")
     return flat.data_ptr(), flat.stride(0) if tokens > 1 else heads
 
 
 class _Call:
     """The arguments that forward, backward and step share, checked."""
+    __slots__ = ("q", "k", "v", "gate", "gate_stride", "tokens", "heads_kv", "shape", "dt", "state_shape")
 
     def __init__(self, q, k, v, log_gate, sequences, offsets, scale, rectify):
-        _need(q.dtype in _DTYPES, f"{q.dtype} is not a storage type")
-        _need(q.dtype == k.dtype == v.dtype, "q, k and v must have one type")
-        self.dtype = q.dtype
-        self.q, self.tokens = _rows(q, "q")
+        dtype = q.dtype
+        self.dt = dt = _DTYPES.get(dtype)
+        if dt is None:
+            _refuse(f"{dtype} is not a storage type")
+        if not (dtype == k.dtype and dtype == v.dtype):
+            _refuse("q, k and v must have one type")
+        kv = k.shape
+        self.q, tokens = _rows(q, "q")
         self.k, tokens_k = _rows(k, "k")
-        _need(tokens_k == self.tokens, "q and k must have the same tokens")
-        self.v, _ = _rows(v, "v", k.shape)
-        self.heads_q, self.head_dim = q.shape[-2:]
-        self.heads_kv = k.shape[-2]
-        _need(k.shape[-1] == self.head_dim, "q and k must have the same head_dim")
+        if not (tokens_k == tokens):
+            _refuse("q and k must have the same tokens")
+        self.v, _ = _rows(v, "v", kv)
+        heads_q, head_dim = q.shape[-2:]
+        heads_kv = kv[-2]
+        if not (kv[-1] == head_dim):
+            _refuse("q and k must have the same head_dim")
         if offsets is not None:
-            _need(offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.is_contiguous() and offsets.numel() >= 2,
-                  "offsets must be int32 [sequences + 1]")
-            _need(sequences is None or sequences == offsets.numel() - 1, "offsets must be int32 [sequences + 1]")
+            if not (offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.is_contiguous() and offsets.numel() >= 2):
+                _refuse("offsets must be int32 [sequences + 1]")
+            if not (sequences is None or sequences == offsets.numel() - 1):
+                _refuse("offsets must be int32 [sequences + 1]")
             sequences = offsets.numel() - 1
+            offsets = offsets.data_ptr()
         elif sequences is None:
             sequences = q.shape[0] if q.dim() == 4 else 1
-        self.sequences = int(sequences)
-        self.gate, self.gate_stride = _gate(log_gate, self.tokens, self.heads_kv, q.dtype, "log_gate")
-        scale = self.head_dim ** -0.5 if scale is None else float(scale)
-        self.shape = _Shape(self.sequences, self.tokens, _ptr(offsets), self.heads_q, self.heads_kv, self.head_dim, scale, int(bool(rectify)))
-        self.dt = _DTYPES[q.dtype]
-        self.state_shape = (self.sequences, self.heads_kv, self.head_dim, self.head_dim)
+        self.gate, self.gate_stride = _gate(log_gate, tokens, heads_kv, dtype, "log_gate")
+        self.tokens, self.heads_kv = tokens, heads_kv
+        self.shape = _Shape(int(sequences), tokens, offsets, heads_q, heads_kv, head_dim, head_dim ** -0.5 if scale is None else scale,
+                            1 if rectify else 0)
+        self.state_shape = (sequences, heads_kv, head_dim, head_dim)
 
     def workspace(self, given, backward, device):
+        if given is not None:
+            if not (given.is_contiguous() and given.dtype == torch.uint8):
+                _refuse("the workspace must be contiguous bytes")
+            return given
         size = ctypes.c_size_t(0)
-        _check(_lib().msla_recurrence_workspace_bytes(ctypes.byref(self.shape), backward, self.dt, ctypes.byref(size)),
-               "msla_recurrence_workspace_bytes")
-        if given is None:
-            given = torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None
-        else:
-            _need(given.is_contiguous() and given.dtype == torch.uint8, "the workspace must be contiguous bytes")
-        return given
+        _check(_lib().msla_recurrence_workspace_bytes(self.shape, backward, self.dt, size), "msla_recurrence_workspace_bytes")
+        return torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None
 
 
 def msla_recurrence_workspace_bytes(sequences, tokens, heads_q, heads_kv, head_dim, dtype, packed=False, backward=False) -> int:
     """Bytes that msla_recurrence_forward (or _backward) needs; packed: with offsets."""
     shape = _Shape(sequences, tokens, 4 if packed else None, heads_q, heads_kv, head_dim, 1.0, 0)
     size = ctypes.c_size_t(0)
-    _check(_lib().msla_recurrence_workspace_bytes(ctypes.byref(shape), int(backward), _DTYPES[dtype], ctypes.byref(size)),
+    _check(_lib().msla_recurrence_workspace_bytes(shape, int(backward), _DTYPES[dtype], size),
            "msla_recurrence_workspace_bytes")
     return int(size.value)
 
@@ -173,13 +203,14 @@ def msla_recurrence_forward(q, k, v, log_gate=None, sequences: Optional[int] = N
     _plain(initial_state, "initial_state", c.state_shape, torch.float32)
     _plain(final_state, "final_state", c.state_shape, torch.float32)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _need(out.dtype == q.dtype, "out must have q's type")
+        out = q.new_empty(q.shape)
+    if not (out.dtype == q.dtype):
+        _refuse("out must have q's type")
     o, _ = _rows(out, "out", q.shape)
     if final_state is None:
         final_state = torch.empty(c.state_shape, dtype=torch.float32, device=q.device)
     ws = c.workspace(workspace, 0, q.device)
-    _check(_lib().msla_recurrence_forward(ctypes.byref(c.shape), c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(initial_state), o,
+    _check(_lib().msla_recurrence_forward(c.shape, c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(initial_state), o,
                                           _ptr(final_state), _ptr(ws), 0 if ws is None else ws.numel(), c.dt, _stream(stream)),
            "msla_recurrence_forward")
     return out, final_state
@@ -195,22 +226,25 @@ def msla_recurrence_backward(q, k, v, d_out, log_gate=None, sequences: Optional[
     _plain(initial_state, "initial_state", c.state_shape, torch.float32)
     _plain(d_final_state, "d_final_state", c.state_shape, torch.float32)
     _plain(d_initial_state, "d_initial_state", c.state_shape, torch.float32)
-    _need(d_out.dtype == q.dtype, "d_out must have q's type")
+    if not (d_out.dtype == q.dtype):
+        _refuse("d_out must have q's type")
     do, _ = _rows(d_out, "d_out", q.shape)
     grads = []
     for t, like, name in ((d_q, q, "d_q"), (d_k, k, "d_k"), (d_v, v, "d_v")):
         if t is None:
             t = torch.empty(like.shape, dtype=q.dtype, device=q.device)
-        _need(t.dtype == q.dtype, f"{name} must have q's type")
+        if not (t.dtype == q.dtype):
+            _refuse(f"{name} must have q's type")
         grads.append((t, _rows(t, name, like.shape)[0]))
-    _need(log_gate is not None or d_log_gate is None, "d_log_gate needs a log_gate")
+    if not (log_gate is not None or d_log_gate is None):
+        _refuse("d_log_gate needs a log_gate")
     if d_log_gate is None and log_gate is not None:
         d_log_gate = torch.empty(log_gate.shape, dtype=q.dtype, device=q.device)
     dg, dg_stride = _gate(d_log_gate, c.tokens, c.heads_kv, q.dtype, "d_log_gate")
     if d_initial_state is None and initial_state is not None:
         d_initial_state = torch.empty(c.state_shape, dtype=torch.float32, device=q.device)
     ws = c.workspace(workspace, 1, q.device)
-    _check(_lib().msla_recurrence_backward(ctypes.byref(c.shape), c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(initial_state), do,
+    _check(_lib().msla_recurrence_backward(c.shape, c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(initial_state), do,
                                            _ptr(d_final_state), grads[0][1], grads[1][1], grads[2][1], dg, dg_stride,
                                            _ptr(d_initial_state), _ptr(ws), 0 if ws is None else ws.numel(), c.dt, _stream(stream)),
            "msla_recurrence_backward")
@@ -223,23 +257,27 @@ def msla_recurrence_step(q, k, v, state, log_gate=None, scale=None, rectify=Fals
     if new_state is None:
         new_state = state
     _on_gpu(q, k, v, state, log_gate, out, new_state)
-    _need(q.dim() == 3, "q must be [sequences, heads_q, head_dim]")
+    if not (q.dim() == 3):
+        _refuse("q must be [sequences, heads_q, head_dim]")
     c = _Call(q, k, v, log_gate, q.shape[0], None, scale, rectify)
     _plain(state, "state", c.state_shape, torch.float32)
     _plain(new_state, "new_state", c.state_shape, torch.float32)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _need(out.dtype == q.dtype, "out must have q's type")
+        out = q.new_empty(q.shape)
+    if not (out.dtype == q.dtype):
+        _refuse("out must have q's type")
     o, _ = _rows(out, "out", q.shape)
-    _check(_lib().msla_recurrence_step(ctypes.byref(c.shape), c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(state), o, _ptr(new_state), c.dt,
+    _check(_lib().msla_recurrence_step(c.shape, c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(state), o, _ptr(new_state), c.dt,
                                        _stream(stream)), "msla_recurrence_step")
     return out, new_state
 
 
 def _norm_arguments(x, weight, residual, total):
     _on_gpu(x, weight, residual, total)
-    _need(x.dtype in _DTYPES, f"{x.dtype} is not a storage type")
-    _need(x.dim() >= 1 and x.is_contiguous(), "x must be contiguous rows")
+    if not (x.dtype in _DTYPES):
+        _refuse(f"{x.dtype} is not a storage type")
+    if not (x.dim() >= 1 and x.is_contiguous()):
+        _refuse("x must be contiguous rows")
     _plain(weight, "weight", x.shape[-1:], x.dtype)
     _plain(residual, "residual", x.shape, x.dtype)
     _plain(total, "sum_out", x.shape, x.dtype)
@@ -267,9 +305,9 @@ def _rows8(x, out8, scale):
     _plain(out8, "out8", x.shape, torch.float8_e4m3fn)
     _plain(scale, "scale", x.shape[:-1], torch.float32)
     if out8 is None:
-        out8 = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+        out8 = x.new_empty(x.shape, dtype=torch.float8_e4m3fn)
     if scale is None:
-        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        scale = x.new_empty(x.shape[:-1], dtype=torch.float32)
     return out8, scale
 
 
@@ -295,7 +333,7 @@ def msla_quantize_rows(x, out8=None, scale=None, stream=None):
 
 def msla_norm_backward_workspace_bytes(rows, channels, dtype) -> int:
     size = ctypes.c_size_t(0)
-    _check(_lib().msla_norm_backward_workspace_bytes(rows, channels, _DTYPES[dtype], ctypes.byref(size)),
+    _check(_lib().msla_norm_backward_workspace_bytes(rows, channels, _DTYPES[dtype], size),
            "msla_norm_backward_workspace_bytes")
     return int(size.value)
 
@@ -314,40 +352,36 @@ def msla_norm_backward(r, weight, d_y, d_sum=None, eps=1e-6, d_r=None, d_weight=
     if workspace is None:
         workspace = torch.empty(msla_norm_backward_workspace_bytes(rows, channels, r.dtype), dtype=torch.uint8, device=r.device)
     else:
-        _need(workspace.is_contiguous() and workspace.dtype == torch.uint8, "the workspace must be contiguous bytes")
+        if not (workspace.is_contiguous() and workspace.dtype == torch.uint8):
+            _refuse("the workspace must be contiguous bytes")
     _check(_lib().msla_norm_backward(_ptr(r), _ptr(weight), _ptr(d_y), _ptr(d_sum), _ptr(d_r), _ptr(d_weight), _ptr(workspace),
                                      workspace.numel(), rows, channels, float(eps), _DTYPES[r.dtype], _stream(stream)),
            "msla_norm_backward")
     return d_r, d_weight
 
 
-def msla_linear_quantized_workspace_bytes(rows, c_in, c_out) -> int:
-    size = ctypes.c_size_t(0)
-    _check(_lib().msla_linear_quantized_workspace_bytes(rows, c_in, c_out, ctypes.byref(size)), "msla_linear_quantized_workspace_bytes")
-    return int(size.value)
-
-
-def msla_linear_quantized(x8, x_scale, w8, w_scale, dtype=torch.bfloat16, out=None, workspace=None, stream=None):
+def msla_linear_quantized(x8, x_scale, w8, w_scale, dtype=torch.bfloat16, out=None, stream=None):
     """y[..., o] = x_scale[...] * w_scale[o] * sum_c x8[..., c] * w8[o, c]: x8, w8 e4m3, scales fp32, y in ``dtype`` (out's, if given)."""
-    _on_gpu(x8, x_scale, w8, w_scale, out, workspace)
-    _need(w8.dim() == 2 and x8.dim() >= 1 and x8.shape[-1] == w8.shape[1], "x8 must be [..., c_in] and w8 [c_out, c_in]")
+    _on_gpu(x8, x_scale, w8, w_scale, out)
+    shape = x8.shape
+    if not (w8.dim() == 2 and len(shape) >= 1 and shape[-1] == w8.shape[1]):
+        _refuse("x8 must be [..., c_in] and w8 [c_out, c_in]")
     c_out, c_in = w8.shape
-    _plain(x8, "x8", x8.shape, torch.float8_e4m3fn)
-    _plain(w8, "w8", w8.shape, torch.float8_e4m3fn)
-    _plain(x_scale, "x_scale", x8.shape[:-1], torch.float32)
+    _plain(x8, "x8", shape, torch.float8_e4m3fn)
+    _plain(w8, "w8", (c_out, c_in), torch.float8_e4m3fn)
+    _plain(x_scale, "x_scale", shape[:-1], torch.float32)
     _plain(w_scale, "w_scale", (c_out,), torch.float32)
-    dtype = dtype if out is None else out.dtype
-    _need(dtype in _DTYPES, f"{dtype} is not a storage type")
-    _plain(out, "out", x8.shape[:-1] + (c_out,), dtype)
+    if out is not None:
+        dtype = out.dtype
+    dt = _DTYPES.get(dtype)
+    if dt is None:
+        _refuse(f"{dtype} is not a storage type")
+    to = shape[:-1] + (c_out,)
     if out is None:
-        out = torch.empty(x8.shape[:-1] + (c_out,), dtype=dtype, device=x8.device)
-    rows = x8.numel() // c_in if c_in else 0
-    size = msla_linear_quantized_workspace_bytes(rows, c_in, c_out)
-    if workspace is None:
-        workspace = torch.empty(size, dtype=torch.uint8, device=x8.device) if size else None
+        out = x8.new_empty(to, dtype=dtype)
     else:
-        _need(workspace.is_contiguous() and workspace.dtype == torch.uint8, "the workspace must be contiguous bytes")
-    _check(_lib().msla_linear_quantized(_ptr(x8), _ptr(x_scale), _ptr(w8), _ptr(w_scale), _ptr(out), _ptr(workspace),
-                                        0 if workspace is None else workspace.numel(), rows, c_in, c_out, _DTYPES[dtype], _stream(stream)),
-           "msla_linear_quantized")
+        _plain(out, "out", to, dtype)
+    rows = x8.numel() // c_in if c_in else 0
+    _check(_lib().msla_linear_quantized(x8.data_ptr(), x_scale.data_ptr(), w8.data_ptr(), w_scale.data_ptr(), out.data_ptr(), rows, c_in, c_out, dt,
+                                        _stream(stream)), "msla_linear_quantized")
     return out

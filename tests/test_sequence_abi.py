@@ -146,16 +146,12 @@ def test_norm_is_refused(lib):
 
 
 def test_linear_quantized_is_refused(lib):
-    f = lambda x=P, sx=2 * P, w=3 * P, sw=4 * P, y=5 * P, rows=4, i=64, o=32, dt=F16, n=1 << 40, ws=P: lib.msla_linear_quantized(
-        x, sx, w, sw, y, ws, n, rows, i, o, dt, None)
+    f = lambda x=P, sx=2 * P, w=3 * P, sw=4 * P, y=5 * P, rows=4, i=64, o=32, dt=F16: lib.msla_linear_quantized(x, sx, w, sw, y, rows, i, o, dt, None)
     for kw in (dict(x=None), dict(sx=None), dict(w=None), dict(sw=None), dict(y=None), dict(rows=-1), dict(i=0), dict(o=0), dict(dt=3), dict(x=P + 8),
                dict(w=P + 8), dict(y=P + 8), dict(sx=P + 2), dict(sw=P + 2), dict(y=P), dict(y=3 * P)):
         assert f(**kw) == INVALID, kw
     assert f(i=40) == f(o=40) == f(rows=1 << 31) == UNSUPPORTED
     assert f(rows=0) == OK
-    size = ctypes.c_size_t(5)
-    assert lib.msla_linear_quantized_workspace_bytes(4, 40, 32, ctypes.byref(size)) == UNSUPPORTED and size.value == 5
-    assert lib.msla_linear_quantized_workspace_bytes(4, 64, 32, None) == INVALID
 
 
 def test_the_binding_refuses_what_is_not_on_the_gpu():
