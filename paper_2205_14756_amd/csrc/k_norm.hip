@@ -1,8 +1,9 @@
 // Root-mean-square norm of rows with the residual's addition, its gradient, and rows into 8 bits (e4m3 with a scale a row).
 //
 // Bound by memory: a row is read once, stays in registers as fp32 through the sum of its squares (and, into 8 bits, its largest
-// magnitude), and is written once.  16 bytes a lane and access, whatever the row's alignment; a ragged end goes by elements.  LPR lanes
-// share a row: few for short rows, so that a wave holds several, a whole workgroup for long ones.
+// magnitude), and is written once.  16 bytes a lane and access, whatever the row's alignment; where the row's length is no multiple of that, the
+// last piece starts early, at the row's end less 16 bytes: what it has in common with the piece before counts once in sums and is stored twice
+// with the same values.  LPR lanes share a row: few for short rows, so that a wave holds several, a whole workgroup for long ones.
 #include "msla_device.h"
 #include "msla_sequence_kernels.h"
 
@@ -11,18 +12,38 @@ namespace {
 
 constexpr float kTop8 = 448.0f;     // the largest e4m3 value
 
+// A lane's i-th piece of a row: its first channel, and how many of its channels the piece before has.
+template <int VEC>
+struct Piece {
+    int at, skip;
+    bool live;
+    __device__ __forceinline__ Piece(int i, int channels) {
+        const int first = i * VEC;
+        live = first < channels;
+        at = max(0, min(first, channels - VEC));
+        skip = first - at;
+    }
+};
+
+// (rows shorter than a piece go by elements)
 template <class T>
-__device__ __forceinline__ void load_row(const T* p, int at, int channels, float (&f)[Traits<T>::kVec]) {
+__device__ __forceinline__ typename Traits<T>::Vec load_raw(const T* p, int at, int channels) {
     constexpr int kVec = Traits<T>::kVec;
-    if (at + kVec <= channels) {
-        typename Traits<T>::Vec v;
+    typename Traits<T>::Vec v;
+    if (channels >= kVec) {
         __builtin_memcpy(&v, __builtin_assume_aligned(p + at, sizeof(T)), 16);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) f[e] = Traits<T>::to_f32(v[e]);
     } else {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) f[e] = at + e < channels ? Traits<T>::to_f32(p[at + e]) : 0.0f;
+        for (int e = 0; e < kVec; ++e) v[e] = e < channels ? p[e] : Traits<T>::from_f32(0.0f);
     }
+    return v;
+}
+
+template <class T>
+__device__ __forceinline__ void load_row(const T* p, int at, int channels, float (&f)[Traits<T>::kVec]) {
+    const typename Traits<T>::Vec v = load_raw<T>(p, at, channels);
+#pragma unroll
+    for (int e = 0; e < Traits<T>::kVec; ++e) f[e] = Traits<T>::to_f32(v[e]);
 }
 
 template <class T>
@@ -31,12 +52,12 @@ __device__ __forceinline__ void store_row(T* p, int at, int channels, const floa
     typename Traits<T>::Vec v;
 #pragma unroll
     for (int e = 0; e < kVec; ++e) v[e] = Traits<T>::from_f32(f[e]);
-    if (at + kVec <= channels) {
+    if (channels >= kVec) {
         __builtin_memcpy(__builtin_assume_aligned(p + at, sizeof(T)), &v, 16);
     } else {
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
-            if (at + e < channels) p[at + e] = v[e];
+            if (e < channels) p[e] = v[e];
     }
 }
 
@@ -50,12 +71,35 @@ __device__ __forceinline__ void store_row8(unsigned char* p, int at, int channel
         v = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * e + 2], f[4 * e + 3], v, true);
         w[e] = (unsigned)v;
     }
-    if (at + VEC <= channels) {
+    if (channels >= VEC) {
         __builtin_memcpy(__builtin_assume_aligned(p + at, 1), w, VEC);
     } else {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-            if (at + e < channels) p[at + e] = (unsigned char)(w[e / 4] >> (8 * (e % 4)));
+            if (e < channels) p[e] = (unsigned char)(w[e / 4] >> (8 * (e % 4)));
+    }
+}
+
+// two sums over the LPR lanes of a row; `room`: two pairs a wave, which take turns, so that one barrier does
+template <int LPR>
+__device__ __forceinline__ void sum_row(float& a, float& b, f32x2* room) {
+    constexpr int kIn = LPR < 64 ? LPR : 64;
+#pragma unroll
+    for (int d = 1; d < kIn; d *= 2) {
+        a += __shfl_xor(a, d);
+        b += __shfl_xor(b, d);
+    }
+    if constexpr (LPR > 64) {
+        constexpr int kWaves = LPR / 64;
+        if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = f32x2{a, b};
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const f32x2 v = room[w];
+            a += v[0];
+            b += v[1];
+        }
     }
 }
 
@@ -91,12 +135,12 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) norm_kernel(const T* x,
     float squares = 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int at = (lane + i * LPR) * kVec;
-        if (live && at < channels) {
-            load_row<T>(x + base, at, channels, r[i]);
+        const Piece<kVec> pc(lane + i * LPR, channels);
+        if (live && pc.live) {
+            load_row<T>(x + base, pc.at, channels, r[i]);
             if (residual != nullptr) {
                 float f[kVec];
-                load_row<T>(residual + base, at, channels, f);
+                load_row<T>(residual + base, pc.at, channels, f);
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) r[i][e] += f[e];
             }
@@ -105,26 +149,27 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) norm_kernel(const T* x,
             for (int e = 0; e < kVec; ++e) r[i][e] = 0.0f;
         }
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) squares = fmaf(r[i][e], r[i][e], squares);
+        for (int e = 0; e < kVec; ++e) squares += e < pc.skip ? 0.0f : r[i][e] * r[i][e];
     }
     if constexpr (!PLAIN) {
+        squares = over_row<LPR>(squares, room, [](float a, float b) { return a + b; });
+        // (only now that the whole row has been read: sum may lie on x or residual, and the last piece shares channels with another lane's)
         if (sum != nullptr) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int at = (lane + i * LPR) * kVec;
-                if (live && at < channels) store_row<T>(sum + base, at, channels, r[i]);
+                const Piece<kVec> pc(lane + i * LPR, channels);
+                if (live && pc.live) store_row<T>(sum + base, pc.at, channels, r[i]);
             }
         }
-        squares = over_row<LPR>(squares, room, [](float a, float b) { return a + b; });
         const float rstd = 1.0f / sqrtf(squares / (float)channels + eps);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int at = (lane + i * LPR) * kVec;
-            if (at >= channels) continue;
+            const Piece<kVec> pc(lane + i * LPR, channels);
+            if (!pc.live) continue;
             float w[kVec];
 #pragma unroll
             for (int e = 0; e < kVec; ++e) w[e] = 1.0f;
-            if (weight != nullptr) load_row<T>(weight, at, channels, w);
+            if (weight != nullptr) load_row<T>(weight, pc.at, channels, w);
 #pragma unroll
             for (int e = 0; e < kVec; ++e) r[i][e] *= rstd * w[e];
         }
@@ -147,94 +192,137 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) norm_kernel(const T* x,
         if (live && lane == 0) scale[row] = s;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int at = (lane + i * LPR) * kVec;
-            if (!live || at >= channels) continue;
+            const Piece<kVec> pc(lane + i * LPR, channels);
+            if (!live || !pc.live) continue;
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
                 const float v = r[i][e] * lift * by;
                 r[i][e] = v > kTop8 ? kTop8 : (v < -kTop8 ? -kTop8 : v);
             }
-            store_row8<kVec>((unsigned char*)y + base, at, channels, r[i]);
+            store_row8<kVec>((unsigned char*)y + base, pc.at, channels, r[i]);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int at = (lane + i * LPR) * kVec;
-            if (live && at < channels) store_row<T>((T*)y + base, at, channels, r[i]);
+            const Piece<kVec> pc(lane + i * LPR, channels);
+            if (live && pc.live) store_row<T>((T*)y + base, pc.at, channels, r[i]);
         }
     }
 }
 
-// A workgroup walks over rows; a lane has the same channels of each, so it sums their part of d_weight in registers.
+// A workgroup walks over rows; a lane has the same channels of each, so it sums their part of d_weight in registers.  The next row is on its way
+// while this one is reduced.
 template <class T, int LPR, int PER>
 __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) norm_backward_kernel(const T* sum, const T* weight, const T* d_y, const T* d_sum, T* d_r,
                                                                               float* partials, int64_t rows, int channels, float eps) {
     constexpr int kVec = Traits<T>::kVec, kThreads = LPR > 256 ? LPR : 256, kRows = kThreads / LPR;
-    __shared__ float room[2][kThreads / 64];
+    typedef typename Traits<T>::Vec Vec;
+    __shared__ f32x2 room[2][kThreads / 64];
     __shared__ float groups[kRows > 1 ? kThreads * PER * kVec : 1];
     const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
-    float w[PER][kVec], dw[PER][kVec];
+    const Vec zero = {};
+    // Rows of up to two pieces a lane stay in registers, and the next one is asked for before this one is reduced; longer ones, and the weight,
+    // are read again (out of L2) for the second pass.
+    constexpr bool kHold = LPR < 1024 ? PER <= 2 : PER == 1;
+    float dw[PER][kVec];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int at = (lane + i * LPR) * kVec;
+    for (int i = 0; i < PER; ++i)
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-            w[i][e] = 1.0f;
-            dw[i][e] = 0.0f;
-        }
-        if (weight != nullptr && at < channels) load_row<T>(weight, at, channels, w[i]);
+        for (int e = 0; e < kVec; ++e) dw[i][e] = 0.0f;
+    auto weight_of = [&](int i) {
+        const Piece<kVec> pc(lane + i * LPR, channels);
+        Vec v;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = Traits<T>::from_f32(1.0f);
+        if (weight != nullptr && pc.live) v = load_raw<T>(weight, pc.at, channels);
+        return v;
+    };
+    Vec kept[kHold ? PER : 1];
+    if constexpr (kHold) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) kept[i] = weight_of(i);
     }
-    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < rows; row0 += (int64_t)gridDim.x * kRows) {
-        const bool live = row0 + group < rows;
-        const int64_t base = (live ? row0 + group : 0) * channels;
-        float r[PER][kVec], g[PER][kVec];
+    struct Row { Vec r[kHold ? PER : 1], g[kHold ? PER : 1], past[kHold ? PER : 1]; };
+    auto read = [&](int64_t row, int i, Vec& r, Vec& g, Vec& past) {
+        const Piece<kVec> pc(lane + i * LPR, channels);
+        r = g = past = zero;
+        if (row < rows && pc.live) {
+            r = load_raw<T>(sum + row * channels, pc.at, channels);
+            g = load_raw<T>(d_y + row * channels, pc.at, channels);
+            if (d_sum != nullptr) past = load_raw<T>(d_sum + row * channels, pc.at, channels);
+        }
+    };
+    auto fetch = [&](Row& to, int64_t row) {
+        if constexpr (kHold) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) read(row, i, to.r[i], to.g[i], to.past[i]);
+        }
+    };
+    auto step = [&](const Row& now, int64_t row, int turn) {
         float squares = 0.0f, along = 0.0f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int at = (lane + i * LPR) * kVec;
-            if (live && at < channels) {
-                load_row<T>(sum + base, at, channels, r[i]);
-                load_row<T>(d_y + base, at, channels, g[i]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < kVec; ++e) r[i][e] = g[i][e] = 0.0f;
-            }
+            const Piece<kVec> pc(lane + i * LPR, channels);
+            Vec r, g, past, w;
+            if constexpr (kHold) r = now.r[i], g = now.g[i], w = kept[i];
+            else read(row, i, r, g, past), w = weight_of(i);
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
-                squares = fmaf(r[i][e], r[i][e], squares);
-                along = fmaf(r[i][e] * w[i][e], g[i][e], along);
+                const float one = e < pc.skip ? 0.0f : Traits<T>::to_f32(r[e]);
+                squares = fmaf(one, one, squares);
+                along = fmaf(one * Traits<T>::to_f32(w[e]), Traits<T>::to_f32(g[e]), along);
             }
         }
-        squares = over_row<LPR>(squares, room[0], [](float a, float b) { return a + b; });
-        along = over_row<LPR>(along, room[1], [](float a, float b) { return a + b; });
+        sum_row<LPR>(squares, along, room[turn]);
         const float rstd = 1.0f / sqrtf(squares / (float)channels + eps);
         const float back = along * rstd * rstd / (float)channels;       // of r, in units of rstd
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int at = (lane + i * LPR) * kVec;
-            if (!live || at >= channels) continue;
-            float d[kVec], past[kVec];
+            const Piece<kVec> pc(lane + i * LPR, channels);
+            Vec r, g, past, w;
+            if constexpr (kHold) r = now.r[i], g = now.g[i], past = now.past[i], w = kept[i];
+            else read(row, i, r, g, past), w = weight_of(i);
+            if (row >= rows || !pc.live) continue;
+            float d[kVec];
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
-                dw[i][e] = fmaf(g[i][e], r[i][e] * rstd, dw[i][e]);
-                d[e] = rstd * (w[i][e] * g[i][e] - r[i][e] * back);
+                const float rf = Traits<T>::to_f32(r[e]), gf = Traits<T>::to_f32(g[e]);
+                dw[i][e] = fmaf(gf, rf * rstd, dw[i][e]);
+                d[e] = fmaf(rstd, Traits<T>::to_f32(w[e]) * gf - rf * back, Traits<T>::to_f32(past[e]));
             }
-            if (d_sum != nullptr) {
-                load_row<T>(d_sum + base, at, channels, past);
+            if (kHold || pc.skip == 0) {
+                store_row<T>(d_r + row * channels, pc.at, channels, d);
+            } else {
+                // (d_r may be d_y, and what the lane before has stored there was read again here: its own channels alone)
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) d[e] += past[e];
+                for (int e = 0; e < kVec; ++e)
+                    if (e >= pc.skip) d_r[row * channels + pc.at + e] = Traits<T>::from_f32(d[e]);
             }
-            store_row<T>(d_r + base, at, channels, d);
         }
+    };
+    int64_t row = (int64_t)blockIdx.x * kRows + group;
+    const int64_t last = rows + group, stride = (int64_t)gridDim.x * kRows;     // (all of a workgroup's rows pass `last` in the same step)
+    Row here, there;
+    fetch(here, row);
+    for (; row < last; row += 2 * stride) {
+        fetch(there, row + stride);
+        step(here, row, 0);
+        if (row + stride >= last) break;
+        fetch(here, row + 2 * stride);
+        step(there, row + stride, 1);
     }
     if (partials == nullptr) return;
     float* out = partials + (int64_t)blockIdx.x * channels;
     if constexpr (kRows > 1) {
+        // (by channel: a piece that starts early leaves out what the one before has)
         constexpr int kWidth = LPR * PER * kVec;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
+        for (int i = 0; i < PER; ++i) {
+            const Piece<kVec> pc(lane + i * LPR, channels);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) groups[group * kWidth + (lane + i * LPR) * kVec + e] = dw[i][e];
+            for (int e = 0; e < kVec; ++e)
+                if (pc.live && e >= pc.skip) groups[group * kWidth + pc.at + e] = dw[i][e];
+        }
         __syncthreads();
         for (int c = threadIdx.x; c < channels; c += kThreads) {
             float s = 0.0f;
@@ -245,28 +333,28 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) norm_backward_kernel(co
     } else {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int at = (lane + i * LPR) * kVec;
+            const Piece<kVec> pc(lane + i * LPR, channels);
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
-                if (at + e < channels) out[at + e] = dw[i][e];
+                if (pc.live && e >= pc.skip) out[pc.at + e] = dw[i][e];
         }
     }
 }
 
-// d_weight = the sum of the workgroups' parts, in an order of its own: 32 channels a workgroup, eight runs of parts, then those.
-__global__ void __launch_bounds__(256) norm_weight_kernel(const float* partials, float* d_weight, int blocks, int channels) {
-    __shared__ float room[8][33];
+// d_weight = the sum of the workgroups' parts, in an order of its own: 32 channels a workgroup, 32 runs of parts, then those.
+__global__ void __launch_bounds__(1024) norm_weight_kernel(const float* partials, float* d_weight, int blocks, int channels) {
+    __shared__ float room[32][33];
     const int c = blockIdx.x * 32 + threadIdx.x % 32, run = threadIdx.x / 32;
     float s = 0.0f;
     if (c < channels) {
 #pragma unroll 8
-        for (int b = run; b < blocks; b += 8) s += partials[(int64_t)b * channels + c];
+        for (int b = run; b < blocks; b += 32) s += partials[(int64_t)b * channels + c];
     }
     room[run][threadIdx.x % 32] = s;
     __syncthreads();
     if (run == 0 && c < channels) {
 #pragma unroll
-        for (int k = 1; k < 8; ++k) s += room[k][threadIdx.x];
+        for (int k = 1; k < 32; ++k) s += room[k][threadIdx.x];
         d_weight[c] = s;
     }
 }
@@ -279,7 +367,7 @@ Lanes lanes_for(int channels, int elem) {
     for (int lpr : {4, 16, 64, 256})
         if (pieces <= lpr) return {lpr, 1};
         else if (pieces <= 2 * lpr) return {lpr, 2};
-    return {1024, pieces <= 2048 ? 2 : (pieces <= 4096 ? 4 : 8)};
+    return {1024, pieces <= 1024 ? 1 : (pieces <= 2048 ? 2 : (pieces <= 4096 ? 4 : 8))};
 }
 
 template <class F>
@@ -292,6 +380,7 @@ hipError_t with_lanes(Lanes l, F&& f) {
         case 64: return per2(integral_constant<int, 64>{});
         case 256: return per2(integral_constant<int, 256>{});
     }
+    if (l.per == 1) return f(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
     if (l.per == 2) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
     if (l.per == 4) return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
     return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
@@ -324,18 +413,18 @@ hipError_t norm_backward_of(const void* sum, const void* weight, const void* d_y
         return hipGetLastError();
     });
     if (e != hipSuccess || d_weight == nullptr) return e;
-    hipLaunchKernelGGL(norm_weight_kernel, dim3((channels + 31) / 32), dim3(256), 0, stream, partials, d_weight, blocks, channels);
+    hipLaunchKernelGGL(norm_weight_kernel, dim3((channels + 31) / 32), dim3(1024), 0, stream, partials, d_weight, blocks, channels);
     return hipGetLastError();
 }
 
 }  // namespace
 
-// Workgroups of the backward pass: enough for every compute unit four times over, few enough that their parts of d_weight are little.
+// Workgroups of the backward pass: what the compute units hold at once, so that their parts of d_weight are few.
 int norm_backward_blocks(int64_t rows, int channels, int elem) {
     const Lanes l = lanes_for(channels, elem);
     const int per_block = (l.lpr > 256 ? l.lpr : 256) / l.lpr;
     const int64_t all = (rows + per_block - 1) / per_block;
-    return (int)(all < 1024 ? all : 1024);
+    return (int)(all < 512 ? all : 512);
 }
 
 hipError_t launch_norm(int dt, const NormCall& c, hipStream_t stream) {
