@@ -25,9 +25,9 @@ msla_status status_of(hipError_t e) { return e == hipSuccess ? MSLA_OK : MSLA_ER
 
 // Workgroups that a scan should have at least: two for each of an MI355X's 256 compute units.
 constexpr int64_t kWantGroups = 512;
-// Tokens below which a segment is not cut further: the pass that sums segments, the one that joins them and their launches cost about what
-// four chunks in a row do.
-constexpr int64_t kLeastSegment = 256;
+// Steps of 64 tokens and a head that a workgroup may take in a row before a sequence is cut at all: the pass that sums segments, the one
+// that joins them and their launches cost about what these do.
+constexpr int64_t kUncutSteps = 3;
 
 msla_status check_shape(const msla_recurrence* s, msla_dtype dt) {
     if (s == nullptr || !known(dt)) return MSLA_ERR_INVALID_ARG;
@@ -45,10 +45,13 @@ msla_status plan_of(const msla_recurrence& s, bool backward, RecurrencePlan* pla
     const int per_group = s.head_dim >= 64 ? 1 : 64 / s.head_dim;           // heads of a workgroup
     const int64_t groups = (s.heads_kv + per_group - 1) / per_group;
     const int64_t want = (kWantGroups + groups - 1) / groups;
-    int64_t segment = ((s.tokens + want - 1) / want + 63) / 64 * 64;
-    if (segment < kLeastSegment) segment = kLeastSegment;
+    int64_t segment = (s.tokens / want + 63) / 64 * 64;
+    const int64_t least = s.head_dim == 128 ? 128 : 64;         // (a state of 128 x 128 is as much traffic as four tiles of 64 tokens)
+    if (segment < least) segment = least;
     const int64_t longest = s.offsets ? s.tokens : s.tokens / s.sequences;
-    plan->cut = longest > segment;
+    // (equal sequences that are workgroups enough for half of the places run whole: cut, they do 1.4 times the work)
+    const bool enough = s.offsets == nullptr && s.sequences * groups * 2 >= kWantGroups;
+    plan->cut = longest > segment && !enough && (longest + 63) / 64 * (s.heads_q / s.heads_kv) > kUncutSteps;
     if (!plan->cut) segment = (s.tokens / 64 + 1) * 64;
     const int64_t slots = s.tokens / segment + s.sequences;
     if (segment > 0x7fffffffLL || slots > 0x7fffffffLL / s.heads_kv) return MSLA_ERR_UNSUPPORTED;
