@@ -126,8 +126,10 @@ struct State {
         for (int e = 0; e < Ti::kOp; ++e) v[e] = s[b * Ti::kJoinOp + e / 4][e % 4] * f;
         Ti::template split<kParts<T>>(v, part);
     }
-    // += sum_j b_j (w_j c_j)^T over the chunk; vt: the wave's columns of c over tokens
-    __device__ __forceinline__ void add(char* tb, const typename Ti::Vec (&vt)[Ti::kTokenSteps], const float* weight, float unit) {
+    // += sum_j b_j (w_j c_j)^T over the chunk; vt: the wave's columns of c over tokens.  ALWAYS or exact: with all of kStateParts (a state that
+    // is handed out), else with those of kParts (one that only goes into outputs, in as many parts).
+    template <bool ALWAYS>
+    __device__ __forceinline__ void add(char* tb, const typename Ti::Vec (&vt)[Ti::kTokenSteps], const float* weight, float unit, bool exact) {
         const int lane = lane_id_again(), x = lane & 15, q = lane >> 4;
 #pragma unroll
         for (int st = 0; st < Ti::kTokenSteps; ++st) {
@@ -152,12 +154,19 @@ struct State {
                 if (b + 1 < Ti::kBlocks) more = Ti::key_operand(tb, b + 1, st, x, q);
                 if (b + 2 < Ti::kBlocks) next = Ti::key_operand(tb, b + 2, st, x, q);
 #pragma unroll
-                for (int p = 0; p < kStateParts<T>; ++p) {
+                for (int p = 0; p < (ALWAYS ? kStateParts<T> : kParts<T>); ++p) {
                     s[b] = Ti::Tr::mma_vec(s[b], kt, part[p]);
                     if (b + 1 < Ti::kBlocks) s[b + 1] = Ti::Tr::mma_vec(s[b + 1], more, part[p]);
                 }
                 kt = next;
                 __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (!ALWAYS && kStateParts<T> > kParts<T>) {
+                if (exact) {
+#pragma unroll
+                    for (int b = 0; b < Ti::kBlocks; ++b)
+                        s[b] = Ti::Tr::mma_vec(s[b], Ti::key_operand(tb, b, st, x, q), part[kParts<T>]);
+                }
             }
         }
     }
@@ -278,7 +287,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         typename Ti::Vec vt[Ti::kTokenSteps];
 #pragma unroll
         for (int st = 0; st < Ti::kTokenSteps; ++st) vt[st] = Ti::value_operand(tc + mine * Ti::kHeadBytes, slice, st, x, q);
-        state.add(tb + mine * Ti::kHeadBytes, vt, gt.weight, unit);
+        state.template add<true>(tb + mine * Ti::kHeadBytes, vt, gt.weight, unit, true);
         __syncthreads();
     }
     if (head >= p.heads) return;
@@ -288,39 +297,59 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
 }
 
 // own[slot] (what a segment adds) becomes the state that the segment starts from, in the order of the scan.  Eight segments are read
-// ahead: their loads hang on nothing.
+// ahead: their loads hang on nothing.  CROSS, with `others` (the same of the scan in the opposite order, joined before): crossing[slot, head, workgroup]
+// becomes the part of <own, others> at the border where a segment starts here and the one before it (in this order) started there, what the
+// gates' gradient is summed up from.
+template <bool CROSS>
 __global__ void __launch_bounds__(kThreads) recurrence_join_kernel(float* own, const float* decay, const float* first, Layout layout, int heads,
-                                                                   int size, int reverse) {
+                                                                   int size, int reverse, const float* others, float* crossing) {
+    constexpr int kAhead = 8;
+    __shared__ float part[kAhead][kThreads / 64];
     const int b = blockIdx.x / heads, h = blockIdx.x % heads;
     const int e = (blockIdx.y * kThreads + threadIdx.x) * 4;
-    if (e >= size) return;
+    const bool mine = e < size;
     const long slot0 = first_slot(layout, b);
     const long from = sequence_start(layout, b), to = max(from, sequence_start(layout, b + 1));
     const int count = (int)min(max(1L, (to - from + layout.segment - 1) / layout.segment), layout.slots - slot0);
     f32x4 run = {0, 0, 0, 0};
-    if (first != nullptr) run = *(const f32x4*)(first + ((long)b * heads + h) * size + e);
-    for (int i0 = 0; i0 < count; i0 += 8) {
-        f32x4 add[8];
-        float keep[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            add[i] = f32x4{0, 0, 0, 0};
+    if (mine && first != nullptr) run = *(const f32x4*)(first + ((long)b * heads + h) * size + e);
+    for (int i0 = 0; i0 < count; i0 += kAhead) {
+        f32x4 add[kAhead], other[kAhead];
+        float keep[kAhead];
+        static_for<0, kAhead>([&](auto i_) {
+            constexpr int i = decltype(i_)::value;
+            add[i] = other[i] = f32x4{0, 0, 0, 0};
             keep[i] = 0.0f;
             const int k = i0 + i;
-            if (k + 1 < count) {            // (nothing was summed for the last one)
+            if (mine && k + 1 < count) {            // (nothing was summed for the last one)
                 const long at = (slot0 + (reverse ? count - 1 - k : k)) * heads + h;
                 add[i] = *(const f32x4*)(own + at * size + e);
                 keep[i] = decay[at];
             }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
+            if (CROSS && mine && k > 0 && k < count)
+                other[i] = *(const f32x4*)(others + ((slot0 + (reverse ? count - k : k - 1)) * heads + h) * size + e);
+        });
+        static_for<0, kAhead>([&](auto i_) {
+            constexpr int i = decltype(i_)::value;
             const int k = i0 + i;
-            if (k >= count) break;
-            const long at = (slot0 + (reverse ? count - 1 - k : k)) * heads + h;
-            *(f32x4*)(own + at * size + e) = run;
+            if (k < count) {
+                const long at = (slot0 + (reverse ? count - 1 - k : k)) * heads + h;
+                if (mine) *(f32x4*)(own + at * size + e) = run;
+                if constexpr (CROSS) {
+                    const float dot = running_sum((run[0] * other[i][0] + run[1] * other[i][1]) + (run[2] * other[i][2] + run[3] * other[i][3]));
+                    if (lane_id() == 63) part[i][threadIdx.x >> 6] = dot;
+                }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) run[r] = fmaf(keep[i], run[r], add[i][r]);
+                for (int r = 0; r < 4; ++r) run[r] = fmaf(keep[i], run[r], add[i][r]);
+            }
+        });
+        if constexpr (CROSS) {
+            __syncthreads();
+            const int k = i0 + (int)threadIdx.x;
+            if (threadIdx.x < kAhead && k < count)
+                crossing[((slot0 + (reverse ? count - 1 - k : k)) * heads + h) * gridDim.y + blockIdx.y] =
+                    (part[threadIdx.x][0] + part[threadIdx.x][1]) + (part[threadIdx.x][2] + part[threadIdx.x][3]);
+            __syncthreads();
         }
     }
 }
@@ -405,6 +434,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     if (steps > 0) fetch(0, 0);
     gates_of(0);
     f32x4 o[4];
+    const bool hands_out = p.last != nullptr && seg.index == (p.reverse ? 0 : seg.count - 1);
     __syncthreads();
     int sub = 0, next_sub = 0;
     long first = 0;
@@ -630,7 +660,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
             if (decays) factor *= gt.total;
             if constexpr (!Ti::kNormalise) unit = gt.unit;
             if (factor != 1.0f) state.scale(factor);
-            state.add(hb, vt, gt.weight, unit);
+            state.template add<false>(hb, vt, gt.weight, unit, hands_out);
         }
         __syncthreads();
         if constexpr (MASKED) {
@@ -645,27 +675,26 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
             }
         }
     }
-    if (live && p.last != nullptr && seg.index == (p.reverse ? 0 : seg.count - 1))
+    if (live && hands_out)
         state.write(p.last + ((long)seg.sequence * p.heads + head) * (D * D), slice, p.rs, Ti::kNormalise ? 1.0f / unit : unit);
 }
 
-// d log_gate of a segment's tokens and one head: from the segment's end, x_t = q_t . dq_t - k_t . dk_t summed up, on top of
-// <dS, S> at that end.
+// d log_gate of a segment's tokens and one head: from the segment's end, x_t = q_t . dq_t - k_t . dk_t summed up, on top of <dS, S> at
+// that end: the parts that the join left, or, at the sequence's end, of what came in and what was handed out there.
 template <class T>
-__global__ void __launch_bounds__(kThreads) recurrence_gate_kernel(const float* q_dots, const float* k_dots, const float* starts,
-                                                                   const float* d_starts, const float* last, const float* d_last, T* d_gate,
-                                                                   long d_gate_ts, Layout layout, int heads, int group, int size) {
+__global__ void __launch_bounds__(kThreads) recurrence_gate_kernel(const float* q_dots, const float* k_dots, const float* crossing, int parts,
+                                                                   const float* last, const float* d_last, T* d_gate, long d_gate_ts, Layout layout,
+                                                                   int heads, int group, int size) {
     __shared__ double part[kThreads / 64];
     const Segment seg = find_segment(layout, blockIdx.x);
     if (!seg.live) return;
     const int h = blockIdx.y, wave = threadIdx.x >> 6, lane = lane_id();
-    const bool at_end = seg.index == seg.count - 1;
-    const float* s = at_end ? last : starts;
-    const float* ds = at_end ? d_last : d_starts;
     double sum = 0.0;
-    if (s != nullptr && ds != nullptr) {
-        const float* sp = s + ((at_end ? (long)seg.sequence : (long)seg.slot + 1) * heads + h) * size;
-        const float* dp = ds + ((at_end ? (long)seg.sequence : (long)seg.slot) * heads + h) * size;
+    if (seg.index < seg.count - 1) {
+        if ((int)threadIdx.x < parts) sum = (double)crossing[((long)seg.slot * heads + h) * parts + threadIdx.x];
+    } else if (last != nullptr && d_last != nullptr) {
+        const float* sp = last + ((long)seg.sequence * heads + h) * size;
+        const float* dp = d_last + ((long)seg.sequence * heads + h) * size;
         for (int e = threadIdx.x * 4; e < size; e += kThreads * 4) {
             const f32x4 a = *(const f32x4*)(sp + e), b = *(const f32x4*)(dp + e);
 #pragma unroll
@@ -834,9 +863,13 @@ hipError_t launch_sweep(const SweepArgs& a, hipStream_t stream) {
     return group ? launch_sweep_as<T, D, false, true>(a, stream) : launch_sweep_as<T, D, false, false>(a, stream);
 }
 
-hipError_t launch_join(float* own, const float* decay, const float* first, const Layout& l, int heads, int size, int reverse, hipStream_t stream) {
-    const dim3 grid(l.sequences * heads, (size / 4 + kThreads - 1) / kThreads);
-    hipLaunchKernelGGL(recurrence_join_kernel, grid, dim3(kThreads), 0, stream, own, decay, first, l, heads, size, reverse);
+int join_groups(int size) { return (size / 4 + kThreads - 1) / kThreads; }
+
+hipError_t launch_join(float* own, const float* decay, const float* first, const Layout& l, int heads, int size, int reverse, const float* others,
+                       float* crossing, hipStream_t stream) {
+    const dim3 grid(l.sequences * heads, join_groups(size));
+    if (others != nullptr) hipLaunchKernelGGL(recurrence_join_kernel<true>, grid, dim3(kThreads), 0, stream, own, decay, first, l, heads, size, reverse, others, crossing);
+    else hipLaunchKernelGGL(recurrence_join_kernel<false>, grid, dim3(kThreads), 0, stream, own, decay, first, l, heads, size, reverse, others, crossing);
     return hipGetLastError();
 }
 
@@ -867,7 +900,7 @@ hipError_t forward_of(const RecurrenceCall& c, hipStream_t stream) {
         float* own = (float*)c.ws;
         float* decay = (float*)(c.ws + c.plan.decay_at);
         MSLA_TRY((launch_state<T, D>(StateArgs{k, v, c.gate, c.gate_ts, own, decay, D, l, c.heads_kv, 1, 0, 1.0f}, stream)));
-        MSLA_TRY(launch_join(own, decay, c.initial, l, c.heads_kv, D * D, 0, stream));
+        MSLA_TRY(launch_join(own, decay, c.initial, l, c.heads_kv, D * D, 0, nullptr, nullptr, stream));
         start = own;
     }
     return launch_sweep<T, D>(SweepArgs{q, k, v, MSLA_OUT(c.out), Heads{nullptr, 0, 0, 0}, nullptr, c.gate, c.gate_ts, start,
@@ -883,6 +916,7 @@ hipError_t backward_of(const RecurrenceCall& c, hipStream_t stream) {
     const Heads no = {nullptr, 0, 0, 0};
     float* s_own = nullptr;
     float* d_own = nullptr;
+    float* crossing = (float*)(c.ws + c.plan.crossing_at);
     if (c.plan.cut) {
         s_own = (float*)c.ws;
         d_own = (float*)(c.ws + c.plan.d_states_at);
@@ -890,8 +924,8 @@ hipError_t backward_of(const RecurrenceCall& c, hipStream_t stream) {
         float* d_decay = (float*)(c.ws + c.plan.d_decay_at);
         MSLA_TRY((launch_state<T, D>(StateArgs{v, k, c.gate, c.gate_ts, s_own, decay, 1, l, c.heads_kv, 1, 0, 1.0f}, stream)));
         MSLA_TRY((launch_state<T, D>(StateArgs{d_o, q, c.gate, c.gate_ts, d_own, d_decay, 1, l, c.heads_kv, group, 1, c.scale}, stream)));
-        MSLA_TRY(launch_join(s_own, decay, c.initial, l, c.heads_kv, D * D, 0, stream));
-        MSLA_TRY(launch_join(d_own, d_decay, c.d_final, l, c.heads_kv, D * D, 1, stream));
+        MSLA_TRY(launch_join(s_own, decay, c.initial, l, c.heads_kv, D * D, 0, nullptr, nullptr, stream));
+        MSLA_TRY(launch_join(d_own, d_decay, c.d_final, l, c.heads_kv, D * D, 1, c.d_gate ? s_own : nullptr, crossing, stream));
     }
     float* q_dots = c.d_gate ? (float*)(c.ws + c.plan.dots_at) : nullptr;
     float* k_dots = c.d_gate ? q_dots + c.tokens * c.heads_q : nullptr;
@@ -902,7 +936,7 @@ hipError_t backward_of(const RecurrenceCall& c, hipStream_t stream) {
     MSLA_TRY((launch_sweep<T, D>(SweepArgs{v, d_o, q, MSLA_OUT(c.d_k), mk, k_dots, c.gate, c.gate_ts, d_own, c.d_final, nullptr, 1, l, c.heads_kv, 1, group, 1, c.scale, 1.0f, c.scale}, stream)));
     MSLA_TRY((launch_sweep<T, D>(SweepArgs{k, q, d_o, MSLA_OUT(c.d_v), no, nullptr, c.gate, c.gate_ts, d_own, c.d_final, c.d_initial, D, l, c.heads_kv, 1, group, 1, c.scale, 1.0f, c.scale}, stream)));
     if (c.d_gate) {
-        hipLaunchKernelGGL((recurrence_gate_kernel<T>), dim3(l.slots, c.heads_kv), dim3(kThreads), 0, stream, q_dots, k_dots, s_own, d_own, last, c.d_final, (T*)c.d_gate, c.d_gate_ts, l, c.heads_kv, group, D * D);
+        hipLaunchKernelGGL((recurrence_gate_kernel<T>), dim3(l.slots, c.heads_kv), dim3(kThreads), 0, stream, q_dots, k_dots, crossing, join_groups(D * D), last, c.d_final, (T*)c.d_gate, c.d_gate_ts, l, c.heads_kv, group, D * D);
         MSLA_TRY(hipGetLastError());
     }
     return hipSuccess;

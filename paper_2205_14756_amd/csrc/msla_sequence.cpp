@@ -71,6 +71,8 @@ msla_status plan_of(const msla_recurrence& s, bool backward, RecurrencePlan* pla
         if (backward) {
             plan->d_decay_at = at;
             at += decays;
+            plan->crossing_at = at;
+            at += decays * 16;          // (at most 16 parts of a state's 128 x 128 numbers)
         }
     }
     if (backward) {

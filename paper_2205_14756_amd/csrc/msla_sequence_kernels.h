@@ -15,7 +15,7 @@ struct RecurrenceRows {
 struct RecurrencePlan {
     int segment = 0, slots = 0;
     bool cut = false;               // more than one segment to a sequence is possible
-    size_t d_states_at = 0, decay_at = 0, d_decay_at = 0, dots_at = 0, last_at = 0, bytes = 0;
+    size_t d_states_at = 0, decay_at = 0, d_decay_at = 0, crossing_at = 0, dots_at = 0, last_at = 0, bytes = 0;
 };
 
 struct RecurrenceCall {

@@ -296,6 +296,10 @@ constexpr double kLog2e = 1.4426950408889634;
 
 // v of the lane that a data-parallel move takes it from; 0 where it takes none
 template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+template <int CTRL, int ROWS>
 __device__ __forceinline__ double moved(double v) {
     const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
     const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, ROWS, 0xf, false);
@@ -303,7 +307,8 @@ __device__ __forceinline__ double moved(double v) {
     return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
 }
 // sum over this lane and those before it
-__device__ __forceinline__ double running_sum(double v) {
+template <class V>
+__device__ __forceinline__ V running_sum(V v) {
     v += moved<0x111, 0xf>(v);      // row_shr 1, 2, 4, 8: within 16 lanes
     v += moved<0x112, 0xf>(v);
     v += moved<0x114, 0xf>(v);
