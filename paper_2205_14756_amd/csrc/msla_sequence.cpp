@@ -26,8 +26,10 @@ msla_status status_of(hipError_t e) { return e == hipSuccess ? MSLA_OK : MSLA_ER
 // Workgroups that a scan should have at least: two for each of an MI355X's 256 compute units.
 constexpr int64_t kWantGroups = 512;
 // Steps of 64 tokens and a head that a workgroup may take in a row before a sequence is cut at all: the pass that sums segments, the one
-// that joins them and their launches cost about what these do.
-constexpr int64_t kUncutSteps = 3;
+// that joins them and their launches cost about what these do.  One sequence, 8 heads of 64 in bf16, us replayed (called one by one), cut against
+// whole: forward, 4 steps 13.7 (22.8) against 14.9 (15.0), 8 steps 14.6 (23.1) against 25.6 (25.8); the gradient, whose three sweeps repay
+// the extra launches sooner, 4 steps 39 (48) against 49 (50).
+constexpr int64_t kUncutSteps = 4, kUncutStepsBackward = 3;
 
 msla_status check_shape(const msla_recurrence* s, msla_dtype dt) {
     if (s == nullptr || !known(dt)) return MSLA_ERR_INVALID_ARG;
@@ -51,7 +53,7 @@ msla_status plan_of(const msla_recurrence& s, bool backward, RecurrencePlan* pla
     const int64_t longest = s.offsets ? s.tokens : s.tokens / s.sequences;
     // (equal sequences that are workgroups enough for half of the places run whole: cut, they do 1.4 times the work)
     const bool enough = s.offsets == nullptr && s.sequences * groups * 2 >= kWantGroups;
-    plan->cut = longest > segment && !enough && (longest + 63) / 64 * (s.heads_q / s.heads_kv) > kUncutSteps;
+    plan->cut = longest > segment && !enough && (longest + 63) / 64 * (s.heads_q / s.heads_kv) > (backward ? kUncutStepsBackward : kUncutSteps);
     if (!plan->cut) segment = (s.tokens / 64 + 1) * 64;
     const int64_t slots = s.tokens / segment + s.sequences;
     if (segment > 0x7fffffffLL || slots > 0x7fffffffLL / s.heads_kv) return MSLA_ERR_UNSUPPORTED;
