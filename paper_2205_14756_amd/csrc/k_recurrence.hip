@@ -62,9 +62,8 @@ __device__ __forceinline__ float tile_top(const unsigned* top) {
 }
 
 __device__ __forceinline__ void leave_top(unsigned* top, unsigned mine) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) mine = max(mine, (unsigned)__shfl_xor((int)mine, d));
-    if (lane_id() == 0) top[(threadIdx.x >> 6) * 3] = mine;
+    mine = running_max(mine);
+    if (lane_id() == 63) top[(threadIdx.x >> 6) * 3] = mine;
 }
 
 // The state's part of a wave: rows are all channels of the key, columns the wave's 16 output channels.
@@ -361,7 +360,7 @@ __device__ __forceinline__ F load_through(BufRsrc r, unsigned off, unsigned scal
 }
 // MASKED: out is masked and measured against m (p.m, p.dots).  GROUP: there are several heads of a, or of (b, c), to a state head.
 template <class T, int D, bool MASKED, bool GROUP>
-__global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupancy)) recurrence_sweep_kernel(SweepArgs p) {
+__global__ void __launch_bounds__((Tile<T, D>::kThreads), (MASKED && Tile<T, D>::kWide16 ? 2 : Tile<T, D>::kOccupancy)) recurrence_sweep_kernel(SweepArgs p) {
     typedef Tile<T, D> Ti;
     typedef typename Ti::Vec Vec;
     typedef typename Ti::Op Op;
@@ -523,13 +522,19 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
                     for (int i = 0; i < 4; ++i) o[i] = Ti::mma(o[i], part[k], va[i]);
                 __builtin_amdgcn_sched_barrier(0);      // (or all steps' operands are read ahead, into registers that are not there)
             }
+            const float all = Ti::kNormalise ? fp / (fs * unit) : 1.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float f = gt.in[16 * i + x];
-                if constexpr (Ti::kNormalise) f /= fs * unit;
+                if constexpr (Ti::kNormalise) f *= all;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[i][r] *= f;
             }
+        } else if constexpr (Ti::kNormalise) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[i][r] *= fp;
         }
         // What out is masked with is asked for before the next tiles: loads return in order.  (Asked for here, and not at once, the tiles do not
         // hold registers through the part above.)
@@ -555,12 +560,6 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         Vec vt[Ti::kTokenSteps];
 #pragma unroll
         for (int st = 0; st < Ti::kTokenSteps; ++st) vt[st] = Ti::value_operand(hc, slice, st, x, q);
-        if constexpr (Ti::kNormalise) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o[i][r] *= fp;
-        }
         if constexpr (Ti::kShare) {
             static_for<0, 4>([&](auto i_) {
                 constexpr int i = decltype(i_)::value;

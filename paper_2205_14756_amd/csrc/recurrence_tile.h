@@ -102,6 +102,8 @@ struct Tile {
     static constexpr int kHeads = kWaves / kWavesPerHead;       // heads of a workgroup
     // waves that a SIMD has room for by registers and LDS
     static constexpr int kOccupancy = sizeof(T) == 4 ? 2 : (D == 64 ? 3 : 4);
+    // heads of 128 in fp16, whose normalisers need registers of their own
+    static constexpr bool kWide16 = D == 128 && std::is_same<T, _Float16>::value;
     // an operand over channels: 16 bytes a lane, for heads of 16 in 16 bits 8 (16 channels make one of the smaller matrix instruction's)
     static constexpr int kOp = D == 16 ? 4 : kVec;
     typedef typename std::conditional<D == 16, Frag, Vec>::type Op;
@@ -282,7 +284,8 @@ struct Tile {
 // double that they are summed in, so that differences stay exact behind a gate that forgets everything.
 //
 // The state is kept as 2^base times what stands in registers: while base stays small, a chunk's gates move base instead of multiplying every
-// element, and the rows' weights make up for it.
+// element, and the rows' weights make up for it.  |base| < 16 leaves fp32's range to the state but for that factor, and mild gates reach it
+// once in several chunks.
 struct Gates {
     float hi[kChunk], lo[kChunk];
     float in[kChunk];               // the state's factor in this row's output
@@ -290,7 +293,7 @@ struct Gates {
     float total, grow, exponent, unit;      // what the registers are multiplied by; how far gates above 0 let a weight grow; log2 of the chunk's
                                             // gates; 2^base behind the chunk
 };
-constexpr float kMostBase = 64.0f;
+constexpr float kMostBase = 16.0f;
 
 constexpr double kLog2e = 1.4426950408889634;
 
@@ -306,6 +309,10 @@ __device__ __forceinline__ double moved(double v) {
     const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, ROWS, 0xf, false);
     return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned moved(unsigned v) {
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
 // sum over this lane and those before it
 template <class V>
 __device__ __forceinline__ V running_sum(V v) {
@@ -315,6 +322,17 @@ __device__ __forceinline__ V running_sum(V v) {
     v += moved<0x118, 0xf>(v);
     v += moved<0x142, 0xa>(v);      // row_bcast 15: the last lane of rows 0 and 2 to rows 1 and 3
     v += moved<0x143, 0xc>(v);      // row_bcast 31: that of row 1 to rows 2 and 3
+    return v;
+}
+
+// the largest of this lane and those before it
+__device__ __forceinline__ unsigned running_max(unsigned v) {
+    v = max(v, moved<0x111, 0xf>(v));
+    v = max(v, moved<0x112, 0xf>(v));
+    v = max(v, moved<0x114, 0xf>(v));
+    v = max(v, moved<0x118, 0xf>(v));
+    v = max(v, moved<0x142, 0xa>(v));
+    v = max(v, moved<0x143, 0xc>(v));
     return v;
 }
 
@@ -347,10 +365,8 @@ __device__ __forceinline__ void run_gates(Gates* out, float g, int reverse, floa
         out->unit = __builtin_amdgcn_exp2f((float)base);
     }
     if (want_grow) {
-        float grow = own > 0.0 ? (float)own : 0.0f;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) grow += __shfl_xor(grow, d);
-        if (lane == 0) out->grow = __builtin_amdgcn_exp2f(grow);
+        const float grow = running_sum(own > 0.0 ? (float)own : 0.0f);
+        if (lane == 63) out->grow = __builtin_amdgcn_exp2f(grow);
     }
 }
 

@@ -73,7 +73,7 @@ def test_norm_into_8_bits(dtype, rows, channels):
     close(scale, top / 448, 2 * WAY * top / 448 + 1e-38, "scale")
     # half a step of e4m3 (2^-4 of a value, 2^-10 where it is subnormal), and the value's own error
     unit = top[:, None] / 448
-    close(f64(y8) * f64(scale)[:, None] if False else y8.double() * scale.double()[:, None], want,
+    close(y8.double() * scale.double()[:, None], want,
           np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10 * unit) * (1 + 2.0 ** -10) + 4 * WAY * np.abs(want) + 1e-38, "y8 * scale")
     assert torch.equal(r, seq.msla_norm_forward(x, w, res, EPS)[1])
 

@@ -186,6 +186,23 @@ def test_small_and_large_values(dtype, sizes):
     close(state, last, size_last, dtype, "state", STATE, half=False)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("exponent", [100, -60])
+def test_values_far_from_one(dtype, exponent):
+    """Gates that forget little and that grow the state: the exponent that the state is kept with takes no value out of fp32's range."""
+    lens, hq, hkv, d = [640], 2, 2, 64
+    t = make(6, dtype, 640, hq, hkv, d, lens, initial=False)
+    v = (t["v"].float() * 2.0 ** exponent).to(TDT[dtype])
+    gate = t["gate"].clone()
+    gate[320:, 1] = 0.02
+    got, state = seq.msla_recurrence_forward(t["q"], t["k"], v, gate, scale=0.01)
+    args = (f64(t["q"]), f64(t["k"]), f64(v), f64(gate), [(0, 640)])
+    want, last = so.recurrence(*args, None, 0.01)
+    size, size_last = so.recurrence(*[np.abs(a) for a in args[:3]], *args[3:], None, 0.01)
+    close(got, want, size, dtype, "out")
+    close(state, last, size_last, dtype, "state", STATE, half=False)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_heads_inside_wider_rows(dtype):
     """q, k and v as parts of a projected map in msla_linear's order, head-major operands, a shared k, and gradients into such places."""
