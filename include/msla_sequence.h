@@ -27,8 +27,9 @@ extern "C" {
 #endif
 
 /* [token, head, channel] in the storage type: channels next to each other, strides in elements (multiples of 16 bytes; not
- * negative; a token's below 16 MiB, a head's at most 512 MiB, else MSLA_ERR_UNSUPPORTED).  So heads may be part of a wider row: the map that msla_linear projects with w_qkv's row order is
- * q = {p, 3*Ct, 3*d}, k = {p + d, ...}, v = {p + 2*d, ...}.  An output's rows must not overlap each other. */
+ * negative; a token's below 16 MiB, a head's at most 512 MiB, else MSLA_ERR_UNSUPPORTED).  So heads may be part of a wider row: the
+ * map that msla_linear projects with w_qkv's row order is q = {p, 3*Ct, 3*d}, k = {p + d, ...}, v = {p + 2*d, ...}.  An input's strides
+ * may be 0 (one row for all tokens, or all heads); an output's rows must not overlap each other. */
 typedef struct {
     void* data;                 /* read only where the operand is an input */
     int64_t token_stride;
@@ -38,10 +39,10 @@ typedef struct {
 /* What the recurrence runs over.  Rows [0, tokens) of q, k, v, ... are the tokens of `sequences` sequences behind each other:
  * with offsets == NULL all of the same length (tokens a multiple of sequences), else sequence b is the rows
  * [offsets[b], offsets[b + 1]) -- a DEVICE array of sequences + 1 ints in [0, tokens] that does not fall; a sequence may be empty;
- * rows before offsets[0] and from offsets[sequences] on belong to none and are neither read nor written.  (The array is on the device, so it is
- * not checked: entries that fall or lie outside leave results undefined, but nothing outside of the buffers is touched.)
+ * rows before offsets[0] and from offsets[sequences] on belong to none and are neither read nor written.  (The array is on the device,
+ * so it is not checked: entries that fall or lie outside leave results undefined, but nothing outside of the buffers is touched.)
  * heads_q query heads share heads_kv states, heads_q / heads_kv (a whole number) neighbours each.
- * head_dim is 16, 32, 64 or 128, of keys and of values. */
+ * head_dim is 16, 32, 64 or 128, of keys and of values.  tokens below 2^31, sequences * heads_kv below 2^22, heads_q <= 32768. */
 typedef struct {
     int sequences;
     int64_t tokens;
@@ -56,12 +57,13 @@ typedef struct {
  * (the numerator of Eq. (3), over the tokens so far; without the division, whose gradient has no bound -- a norm over the head's
  * channels takes its place).
  *   q [tokens, heads_q, head_dim];  k, v [tokens, heads_kv, head_dim];  out like q
- *   log_gate [tokens, heads_kv] in the storage type (aligned to its element), rows gate_stride elements (below 16 MiB) apart, or NULL: nothing is
- *       forgotten.  At most 0 in earnest; -inf (and anything below -103) forgets all that was.
+ *   log_gate [tokens, heads_kv] in the storage type (aligned to its element), rows gate_stride elements (below 16 MiB) apart, or NULL:
+ *       nothing is forgotten.  At most 0 in earnest; -inf (and anything below -103) forgets all that was.
  *   initial_state, final_state [sequences, heads_kv, head_dim (of k), head_dim (of v)] fp32, either may be NULL; final_state may be
  *       initial_state itself.  A sequence without tokens hands its state on.
- * The state, the sums and the gates' running products are fp32 (or more); an operand of a matrix instruction that is not an input
- * goes in as two or three parts of the storage type.
+ * The state, the sums and the gates' running products are fp32 (or more), a state on the way with up to 2^16 times its value; an
+ * operand of a matrix instruction that is not an input goes in as two or three parts of the storage type.
+ * The workspace hangs on the shape alone, offsets being NULL or not included.
  * A value that is not finite stays within its own sequence and head; there it reaches the tokens behind it and those of its own
  * chunk of 64 tokens before it. */
 msla_status msla_recurrence_workspace_bytes(const msla_recurrence* shape, int backward, msla_dtype dt, size_t* bytes);
@@ -91,7 +93,8 @@ msla_status msla_recurrence_step(const msla_recurrence* shape, msla_heads q, msl
  *     r = x + residual        y = r / sqrt(mean(r^2) + eps) * weight
  *   x, residual, sum, y [rows, channels], contiguous, aligned to an element; weight [channels] in the storage type or NULL (ones);
  *   residual may be NULL (r = x); sum receives r (NULL: not wanted) and may be x or residual itself, y may be x itself where sum is not x.
- * r is fp32 on its way into y; sum is rounded.  channels <= 32768.
+ * r is fp32 on its way into y, and so are its squares (|r| below 1e18 in earnest; a row of zeros with eps = 0 is 0 / 0); sum is rounded.
+ * channels <= 32768, rows below 2^31.
  * msla_norm_quantized writes y in 8 bits instead: y8 [rows, channels] in e4m3 (the finite form: largest value 448), scale [rows] fp32 with
  * y ~ y8 * scale, scale = max |y| of the row / 448 (a row of zeros: scale 0). */
 msla_status msla_norm_forward(const void* x, const void* residual, const void* weight, void* y, void* sum,
@@ -112,7 +115,7 @@ msla_status msla_quantize_rows(const void* x, void* x8, float* scale, int64_t ro
 
 /* y[n, o] = x_scale[n] * w_scale[o] * sum_c x8[n, c] w8[o, c]   (msla_linear of rows that stand in 8 bits)
  *   x8 [rows, c_in], w8 [c_out, c_in] e4m3;  x_scale [rows], w_scale [c_out] fp32 (aligned to 4 bytes);  y [rows, c_out] in dt.
- * c_in, c_out multiples of 16.  Products are exact, sums fp32. */
+ * c_in, c_out multiples of 16 and at most 2^20, rows below 2^31.  Products are exact, sums fp32. */
 msla_status msla_linear_quantized(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows, int c_in,
                                   int c_out, msla_dtype dt, void* stream);
 

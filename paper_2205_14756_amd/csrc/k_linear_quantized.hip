@@ -147,8 +147,8 @@ __global__ void __launch_bounds__(512) linear_quantized_rows_kernel(const unsign
     constexpr int kWaves = 8;
     __shared__ float sums[kWaves][BLOCKS][16][17];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), x = lane & 15, q = lane >> 4;
-    const int o0 = blockIdx.x * 16;
-    const int64_t n0 = (int64_t)blockIdx.y * (16 * BLOCKS);
+    const int tiles_o = c_out / 16, o0 = blockIdx.x % tiles_o * 16;
+    const int64_t n0 = (int64_t)(blockIdx.x / tiles_o) * (16 * BLOCKS);
     const unsigned char* wp = w8 + (int64_t)(o0 + x) * c_in + 16 * q;
     const unsigned char* xp[BLOCKS];
 #pragma unroll
@@ -215,20 +215,28 @@ __global__ void __launch_bounds__(512) linear_quantized_rows_kernel(const unsign
 template <class T>
 hipError_t linear_of(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows, int c_in, int c_out,
                      hipStream_t stream) {
-    const unsigned char *xp = (const unsigned char*)x8, *wp = (const unsigned char*)w8;
-    const int tiles_o = (c_out + 127) / 128;
-    const int64_t tiles = (rows + 127) / 128 * tiles_o;
-    if (tiles > 0x7fffffffL) return hipErrorInvalidValue;
-    if (rows_kernel_wins(rows, c_out)) {
-        const dim3 threads(512);
-        if (rows <= 16) hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 1>), dim3(c_out / 16, 1), threads, 0, stream, xp, x_scale, wp, w_scale, (T*)y, rows, c_in, c_out);
-        else if (rows <= 32) hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 2>), dim3(c_out / 16, 1), threads, 0, stream, xp, x_scale, wp, w_scale, (T*)y, rows, c_in, c_out);
-        else if (rows <= 48) hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 3>), dim3(c_out / 16, 1), threads, 0, stream, xp, x_scale, wp, w_scale, (T*)y, rows, c_in, c_out);
-        else hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 4>), dim3(c_out / 16, (unsigned)((rows + 63) / 64)), threads, 0, stream, xp, x_scale, wp, w_scale, (T*)y, rows, c_in, c_out);
-    } else {
-        hipLaunchKernelGGL((linear_quantized_kernel<T>), dim3((unsigned)tiles), dim3(256), 0, stream, xp, x_scale, wp, w_scale, (T*)y, rows, c_in, c_out, tiles_o);
+    // (a launch has fewer than 2^32 threads: more rows than these, 128 at the most channels, go in several)
+    const int64_t most = (((int64_t)1 << 26) / (c_out / 16) + 1) / 128 * 128 + 128;
+    const unsigned char* wp = (const unsigned char*)w8;
+    for (int64_t from = 0; from < rows; from += most) {
+        const int64_t n = rows - from < most ? rows - from : most;
+        const unsigned char* xp = (const unsigned char*)x8 + from * c_in;
+        T* yp = (T*)y + from * c_out;
+        const float* xs = x_scale + from;
+        if (rows_kernel_wins(n, c_out)) {
+            const dim3 grid((unsigned)((n + 63) / 64 * (c_out / 16))), threads(512);
+            if (n <= 16) hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 1>), grid, threads, 0, stream, xp, xs, wp, w_scale, yp, n, c_in, c_out);
+            else if (n <= 32) hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 2>), grid, threads, 0, stream, xp, xs, wp, w_scale, yp, n, c_in, c_out);
+            else if (n <= 48) hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 3>), grid, threads, 0, stream, xp, xs, wp, w_scale, yp, n, c_in, c_out);
+            else hipLaunchKernelGGL((linear_quantized_rows_kernel<T, 4>), grid, threads, 0, stream, xp, xs, wp, w_scale, yp, n, c_in, c_out);
+        } else {
+            const int tiles_o = (c_out + 127) / 128;
+            hipLaunchKernelGGL((linear_quantized_kernel<T>), dim3((unsigned)((n + 127) / 128 * tiles_o)), dim3(256), 0, stream, xp, xs, wp, w_scale, yp, n, c_in, c_out, tiles_o);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace

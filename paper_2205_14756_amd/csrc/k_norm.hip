@@ -390,14 +390,22 @@ template <class T>
 hipError_t norm_of(const NormCall& c, hipStream_t stream) {
     return with_lanes(lanes_for(c.channels, sizeof(T)), [&](auto lpr, auto per) {
         constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value, kThreads = kLpr > 256 ? kLpr : 256, kRows = kThreads / kLpr;
-        const int64_t blocks = (c.rows + kRows - 1) / kRows;
-        if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
-        const dim3 grid((unsigned)blocks), threads(kThreads);
-        const T *x = (const T*)c.x, *res = (const T*)c.residual, *w = (const T*)c.weight;
-        if (c.plain) hipLaunchKernelGGL((norm_kernel<T, kLpr, kPer, true, true>), grid, threads, 0, stream, x, res, w, c.y, c.scale, (T*)c.sum, c.rows, c.channels, c.eps);
-        else if (c.scale) hipLaunchKernelGGL((norm_kernel<T, kLpr, kPer, true, false>), grid, threads, 0, stream, x, res, w, c.y, c.scale, (T*)c.sum, c.rows, c.channels, c.eps);
-        else hipLaunchKernelGGL((norm_kernel<T, kLpr, kPer, false, false>), grid, threads, 0, stream, x, res, w, c.y, c.scale, (T*)c.sum, c.rows, c.channels, c.eps);
-        return hipGetLastError();
+        // (a launch has fewer than 2^32 threads: more rows than these go in several)
+        constexpr int64_t kMost = ((int64_t)1 << 31) / kThreads * kRows;
+        for (int64_t from = 0; from < c.rows; from += kMost) {
+            const int64_t rows = c.rows - from < kMost ? c.rows - from : kMost, at = from * c.channels;
+            const dim3 grid((unsigned)((rows + kRows - 1) / kRows)), threads(kThreads);
+            const T *x = (const T*)c.x + at, *res = c.residual ? (const T*)c.residual + at : nullptr, *w = (const T*)c.weight;
+            T* sum = c.sum ? (T*)c.sum + at : nullptr;
+            float* scale = c.scale ? c.scale + from : nullptr;
+            void* y = (char*)c.y + at * (int64_t)(c.scale ? 1 : sizeof(T));
+            if (c.plain) hipLaunchKernelGGL((norm_kernel<T, kLpr, kPer, true, true>), grid, threads, 0, stream, x, res, w, y, scale, sum, rows, c.channels, c.eps);
+            else if (c.scale) hipLaunchKernelGGL((norm_kernel<T, kLpr, kPer, true, false>), grid, threads, 0, stream, x, res, w, y, scale, sum, rows, c.channels, c.eps);
+            else hipLaunchKernelGGL((norm_kernel<T, kLpr, kPer, false, false>), grid, threads, 0, stream, x, res, w, y, scale, sum, rows, c.channels, c.eps);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     });
 }
 

@@ -31,6 +31,10 @@ constexpr int64_t kWantGroups = 512;
 // the extra launches sooner, 4 steps 39 (48) against 49 (50).
 constexpr int64_t kUncutSteps = 4, kUncutStepsBackward = 3;
 
+// A launch has fewer than 2^32 threads; the step takes 1024 for a state of 128 x 128, the scan's kernels no more than 512 for one.
+constexpr int64_t kMostStates = 1 << 22;
+constexpr int kMostChannels8 = 1 << 20;
+
 msla_status check_shape(const msla_recurrence* s, msla_dtype dt) {
     if (s == nullptr || !known(dt)) return MSLA_ERR_INVALID_ARG;
     if (s->sequences <= 0 || s->tokens < 0 || s->heads_q <= 0 || s->heads_kv <= 0 || s->head_dim <= 0) return MSLA_ERR_INVALID_ARG;
@@ -38,7 +42,7 @@ msla_status check_shape(const msla_recurrence* s, msla_dtype dt) {
     if (s->offsets == nullptr && s->tokens % s->sequences != 0) return MSLA_ERR_INVALID_ARG;
     if (s->offsets != nullptr && !aligned(s->offsets, 4)) return MSLA_ERR_INVALID_ARG;
     if (s->head_dim != 16 && s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128) return MSLA_ERR_UNSUPPORTED;
-    if (s->heads_q > 32768 || s->tokens > 0x7fffffffLL || (int64_t)s->sequences * s->heads_kv > 0x3fffffffLL) return MSLA_ERR_UNSUPPORTED;
+    if (s->heads_q > 32768 || s->tokens > 0x7fffffffLL || (int64_t)s->sequences * s->heads_kv >= kMostStates) return MSLA_ERR_UNSUPPORTED;
     return MSLA_OK;
 }
 
@@ -300,7 +304,7 @@ msla_status msla_linear_quantized(const void* x8, const float* x_scale, const vo
                                   int c_out, msla_dtype dt, void* stream) {
     if (rows < 0 || c_in <= 0 || c_out <= 0 || !known(dt)) return MSLA_ERR_INVALID_ARG;
     if (!aligned(x8, 16) || !aligned(w8, 16) || !aligned(y, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 4)) return MSLA_ERR_INVALID_ARG;
-    if (c_in % 16 != 0 || c_out % 16 != 0 || rows > 0x7fffffffLL) return MSLA_ERR_UNSUPPORTED;
+    if (c_in % 16 != 0 || c_out % 16 != 0 || c_in > kMostChannels8 || c_out > kMostChannels8 || rows > 0x7fffffffLL) return MSLA_ERR_UNSUPPORTED;
     if (rows == 0) return MSLA_OK;
     if (!x8 || !x_scale || !w8 || !w_scale || !y || y == x8 || y == w8) return MSLA_ERR_INVALID_ARG;
     return status_of(msla::launch_linear_quantized((int)dt, x8, x_scale, w8, w_scale, y, rows, c_in, c_out, (hipStream_t)stream));

@@ -2,7 +2,8 @@
 
 The linear attention of Eq. (3) as a running state over a sequence, the root-mean-square norm with the residual's addition, and
 the projection of rows in 8 bits.  Like ``msla``: argument marshalling only, no CPU fallback, tensors on the current GPU, work on
-its current stream unless one is given.  Buffers that are not passed in are allocated here with torch.
+its current stream unless one is given.  Buffers that are not passed in are allocated here with torch, for the stream that they are
+used on.
 """
 from __future__ import annotations
 
@@ -84,6 +85,14 @@ def _on_gpu(*tensors):
                 here = at
 
 
+def _new(shape, dtype, device, stream):
+    """Memory for a call on ``stream``: of that stream, so that it is not handed on before the call's work is done."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _plain(t, name, shape, dtype):
     if t is not None and not (t.shape == shape and t.dtype == dtype and t.is_contiguous()):
         if not t.is_contiguous():
@@ -128,7 +137,10 @@ def _gate(t, tokens, heads, dtype, name):
         _refuse(f"{name} must be [..., heads_kv]")
     if t.is_contiguous():
         return t.data_ptr(), heads
-    flat = t if t.dim() == 2 else t.view(-1, heads)
+    try:
+        flat = t if t.dim() == 2 else t.view(-1, heads)
+    except RuntimeError:
+        _refuse(f"{name}'s tokens must lie at equal distances")
     if not (heads == 1 or flat.stride(1) == 1):
         _refuse(f"{name}'s heads must lie next to each other")
     return flat.data_ptr(), flat.stride(0) if tokens > 1 else heads
@@ -170,14 +182,14 @@ class _Call:
                             1 if rectify else 0)
         self.state_shape = (sequences, heads_kv, head_dim, head_dim)
 
-    def workspace(self, given, backward, device):
+    def workspace(self, given, backward, device, stream):
         if given is not None:
             if not (given.is_contiguous() and given.dtype == torch.uint8):
                 _refuse("the workspace must be contiguous bytes")
             return given
         size = ctypes.c_size_t(0)
         _check(_lib().msla_recurrence_workspace_bytes(self.shape, backward, self.dt, size), "msla_recurrence_workspace_bytes")
-        return torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None
+        return _new(size.value, torch.uint8, device, stream) if size.value else None
 
 
 def msla_recurrence_workspace_bytes(sequences, tokens, heads_q, heads_kv, head_dim, dtype, packed=False, backward=False) -> int:
@@ -203,13 +215,13 @@ def msla_recurrence_forward(q, k, v, log_gate=None, sequences: Optional[int] = N
     _plain(initial_state, "initial_state", c.state_shape, torch.float32)
     _plain(final_state, "final_state", c.state_shape, torch.float32)
     if out is None:
-        out = q.new_empty(q.shape)
+        out = _new(q.shape, q.dtype, q.device, stream)
     if not (out.dtype == q.dtype):
         _refuse("out must have q's type")
     o, _ = _rows(out, "out", q.shape)
     if final_state is None:
-        final_state = torch.empty(c.state_shape, dtype=torch.float32, device=q.device)
-    ws = c.workspace(workspace, 0, q.device)
+        final_state = _new(c.state_shape, torch.float32, q.device, stream)
+    ws = c.workspace(workspace, 0, q.device, stream)
     _check(_lib().msla_recurrence_forward(c.shape, c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(initial_state), o,
                                           _ptr(final_state), _ptr(ws), 0 if ws is None else ws.numel(), c.dt, _stream(stream)),
            "msla_recurrence_forward")
@@ -232,18 +244,18 @@ def msla_recurrence_backward(q, k, v, d_out, log_gate=None, sequences: Optional[
     grads = []
     for t, like, name in ((d_q, q, "d_q"), (d_k, k, "d_k"), (d_v, v, "d_v")):
         if t is None:
-            t = torch.empty(like.shape, dtype=q.dtype, device=q.device)
+            t = _new(like.shape, q.dtype, q.device, stream)
         if not (t.dtype == q.dtype):
             _refuse(f"{name} must have q's type")
         grads.append((t, _rows(t, name, like.shape)[0]))
     if not (log_gate is not None or d_log_gate is None):
         _refuse("d_log_gate needs a log_gate")
     if d_log_gate is None and log_gate is not None:
-        d_log_gate = torch.empty(log_gate.shape, dtype=q.dtype, device=q.device)
+        d_log_gate = _new(log_gate.shape, q.dtype, q.device, stream)
     dg, dg_stride = _gate(d_log_gate, c.tokens, c.heads_kv, q.dtype, "d_log_gate")
     if d_initial_state is None and initial_state is not None:
-        d_initial_state = torch.empty(c.state_shape, dtype=torch.float32, device=q.device)
-    ws = c.workspace(workspace, 1, q.device)
+        d_initial_state = _new(c.state_shape, torch.float32, q.device, stream)
+    ws = c.workspace(workspace, 1, q.device, stream)
     _check(_lib().msla_recurrence_backward(c.shape, c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(initial_state), do,
                                            _ptr(d_final_state), grads[0][1], grads[1][1], grads[2][1], dg, dg_stride,
                                            _ptr(d_initial_state), _ptr(ws), 0 if ws is None else ws.numel(), c.dt, _stream(stream)),
@@ -263,7 +275,7 @@ def msla_recurrence_step(q, k, v, state, log_gate=None, scale=None, rectify=Fals
     _plain(state, "state", c.state_shape, torch.float32)
     _plain(new_state, "new_state", c.state_shape, torch.float32)
     if out is None:
-        out = q.new_empty(q.shape)
+        out = _new(q.shape, q.dtype, q.device, stream)
     if not (out.dtype == q.dtype):
         _refuse("out must have q's type")
     o, _ = _rows(out, "out", q.shape)
@@ -292,31 +304,31 @@ def msla_norm_forward(x, weight=None, residual=None, eps=1e-6, out=None, sum_out
     _on_gpu(out)
     _plain(out, "out", x.shape, x.dtype)
     if out is None:
-        out = torch.empty_like(x)
+        out = _new(x.shape, x.dtype, x.device, stream)
     if sum_out is None and residual is not None:
-        sum_out = torch.empty_like(x)
+        sum_out = _new(x.shape, x.dtype, x.device, stream)
     _check(_lib().msla_norm_forward(_ptr(x), _ptr(residual), _ptr(weight), _ptr(out), _ptr(sum_out), rows, channels, float(eps),
                                     _DTYPES[x.dtype], _stream(stream)), "msla_norm_forward")
     return out, x if sum_out is None else sum_out
 
 
-def _rows8(x, out8, scale):
+def _rows8(x, out8, scale, stream):
     _on_gpu(out8, scale)
     _plain(out8, "out8", x.shape, torch.float8_e4m3fn)
     _plain(scale, "scale", x.shape[:-1], torch.float32)
     if out8 is None:
-        out8 = x.new_empty(x.shape, dtype=torch.float8_e4m3fn)
+        out8 = _new(x.shape, torch.float8_e4m3fn, x.device, stream)
     if scale is None:
-        scale = x.new_empty(x.shape[:-1], dtype=torch.float32)
+        scale = _new(x.shape[:-1], torch.float32, x.device, stream)
     return out8, scale
 
 
 def msla_norm_quantized(x, weight=None, residual=None, eps=1e-6, out8=None, scale=None, sum_out=None, stream=None):
     """(y8, scale, r): msla_norm_forward with y as e4m3 rows, y ~ y8 * scale[..., None]."""
     rows, channels = _norm_arguments(x, weight, residual, sum_out)
-    out8, scale = _rows8(x, out8, scale)
+    out8, scale = _rows8(x, out8, scale, stream)
     if sum_out is None and residual is not None:
-        sum_out = torch.empty_like(x)
+        sum_out = _new(x.shape, x.dtype, x.device, stream)
     _check(_lib().msla_norm_quantized(_ptr(x), _ptr(residual), _ptr(weight), _ptr(out8), _ptr(scale), _ptr(sum_out), rows, channels,
                                       float(eps), _DTYPES[x.dtype], _stream(stream)), "msla_norm_quantized")
     return out8, scale, x if sum_out is None else sum_out
@@ -325,7 +337,7 @@ def msla_norm_quantized(x, weight=None, residual=None, eps=1e-6, out8=None, scal
 def msla_quantize_rows(x, out8=None, scale=None, stream=None):
     """(x8, scale): rows of x as e4m3, x ~ x8 * scale[..., None]."""
     rows, channels = _norm_arguments(x, None, None, None)
-    out8, scale = _rows8(x, out8, scale)
+    out8, scale = _rows8(x, out8, scale, stream)
     _check(_lib().msla_quantize_rows(_ptr(x), _ptr(out8), _ptr(scale), rows, channels, _DTYPES[x.dtype], _stream(stream)),
            "msla_quantize_rows")
     return out8, scale
@@ -346,11 +358,11 @@ def msla_norm_backward(r, weight, d_y, d_sum=None, eps=1e-6, d_r=None, d_weight=
     _plain(d_r, "d_r", r.shape, r.dtype)
     _plain(d_weight, "d_weight", (channels,), torch.float32)
     if d_r is None:
-        d_r = torch.empty_like(r)
+        d_r = _new(r.shape, r.dtype, r.device, stream)
     if d_weight is None:
-        d_weight = torch.empty(channels, dtype=torch.float32, device=r.device)
+        d_weight = _new(channels, torch.float32, r.device, stream)
     if workspace is None:
-        workspace = torch.empty(msla_norm_backward_workspace_bytes(rows, channels, r.dtype), dtype=torch.uint8, device=r.device)
+        workspace = _new(msla_norm_backward_workspace_bytes(rows, channels, r.dtype), torch.uint8, r.device, stream)
     else:
         if not (workspace.is_contiguous() and workspace.dtype == torch.uint8):
             _refuse("the workspace must be contiguous bytes")
@@ -378,7 +390,7 @@ def msla_linear_quantized(x8, x_scale, w8, w_scale, dtype=torch.bfloat16, out=No
         _refuse(f"{dtype} is not a storage type")
     to = shape[:-1] + (c_out,)
     if out is None:
-        out = x8.new_empty(to, dtype=dtype)
+        out = _new(to, dtype, x8.device, stream)
     else:
         _plain(out, "out", to, dtype)
     rows = x8.numel() // c_in if c_in else 0

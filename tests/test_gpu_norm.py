@@ -205,3 +205,39 @@ def test_the_binding_refuses():
         seq.msla_norm_forward(x, eps=-1.0)
     with pytest.raises(seq.MslaError):
         seq.msla_linear_quantized(x8, s, x8, s)         # four outputs: not a multiple of 16
+
+
+def test_more_rows_than_a_launch_has_threads_for():
+    """Four lanes a row and 2^30 rows and some.  A row of one value is +-1 after the norm, to the bit, whatever the value."""
+    rows = 2 ** 30 + 70
+    x = torch.full((rows, 1), 3.0, dtype=torch.bfloat16, device="cuda")
+    x[::3] = -0.5
+    y, _ = seq.msla_norm_forward(x, eps=0.0)
+    torch.cuda.synchronize()
+    assert bool((y[::3] == -1).all()) and bool((y[1::3] == 1).all()) and bool((y[2::3] == 1).all())
+
+
+def test_more_rows_of_a_projection_than_a_launch_has_threads_for():
+    rows, c = 2 ** 26 + 300, 16
+    x8 = (torch.arange(rows, device="cuda") % 5 - 2).to(torch.float8_e4m3fn)[:, None].expand(rows, c).contiguous()
+    one = torch.ones(rows, dtype=torch.float32, device="cuda")
+    y = seq.msla_linear_quantized(x8, one, torch.ones(c, c, device="cuda").to(torch.float8_e4m3fn), one[:c].contiguous())
+    torch.cuda.synchronize()
+    assert y.shape == (rows, c)
+    assert torch.equal(y[:, 5].float(), 16 * x8[:, 0].float()) and torch.equal(y[-400:].float(), 16 * x8[-400:].float())
+
+
+def test_buffers_of_a_call_on_a_given_stream():
+    """What a call allocates for itself is not handed to the current stream while the given one still works with it."""
+    x, w, g = rnd(70, "f32", 512, 4096), rnd(71, "f32", 4096), rnd(72, "f32", 512, 4096)
+    want = seq.msla_norm_backward(x, w, g)
+    side, big = torch.cuda.Stream(), torch.ones(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            big = big @ big * 0.0
+    got = seq.msla_norm_backward(x, w, g, stream=side)
+    junk = [torch.full((512 * 4096,), 7.0, device="cuda") for _ in range(8)]
+    torch.cuda.synchronize()
+    del junk
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

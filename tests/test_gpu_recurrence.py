@@ -231,6 +231,22 @@ def test_heads_inside_wider_rows(dtype):
                        seq.msla_recurrence_forward(t["q"], shared.contiguous(), t["v"], t["gate"])[0])
 
 
+def test_inputs_that_are_one_row_for_many():
+    """strides of 0 over heads and over tokens give what copies give"""
+    n, h, d = 500, 4, 32
+    q, k, v = (_numbers(90 + i, n, h, d).bfloat16().cuda() for i in range(3))
+    k, q = k[:, :1].expand(n, h, d), q[:1].expand(n, h, d)
+    gate = -_numbers(94, 1, h).abs().bfloat16().cuda().expand(n, h) * 1.0
+    thin = gate[:1].expand(n, h)
+    d_out = _numbers(95, n, h, d).bfloat16().cuda()
+    for a, b in zip(seq.msla_recurrence_forward(q, k, v, thin), seq.msla_recurrence_forward(q.contiguous(), k.contiguous(), v, gate.contiguous())):
+        assert torch.equal(a, b)
+    first = torch.zeros(1, h, d, d, device="cuda")
+    one = seq.msla_recurrence_backward(q, k, v, d_out, thin, initial_state=first)
+    for a, b in zip(one, seq.msla_recurrence_backward(q.contiguous(), k.contiguous(), v, d_out, gate.contiguous(), initial_state=first)):
+        assert torch.equal(a, b)
+
+
 def test_batched_shapes():
     t = make(7, "bf16", 2 * 80, 2, 2, 16, [80, 80])
     a = seq.msla_recurrence_forward(t["q"], t["k"], t["v"], t["gate"], sequences=2)

@@ -50,7 +50,8 @@ BAD_SHAPES = [(dict(sequences=0), INVALID), (dict(sequences=-1), INVALID), (dict
               (dict(heads_q=0), INVALID), (dict(heads_kv=0), INVALID), (dict(heads_q=3), INVALID), (dict(head_dim=0), INVALID),
               (dict(head_dim=48), UNSUPPORTED), (dict(head_dim=256), UNSUPPORTED), (dict(scale=float("inf")), INVALID),
               (dict(scale=float("nan")), INVALID), (dict(rectify=2), INVALID), (dict(offsets=P + 2), INVALID),
-              (dict(heads_q=1 << 16, heads_kv=1), UNSUPPORTED), (dict(tokens=1 << 32), UNSUPPORTED)]
+              (dict(heads_q=1 << 16, heads_kv=1), UNSUPPORTED), (dict(tokens=1 << 32), UNSUPPORTED),
+              (dict(sequences=1 << 21, tokens=1 << 21), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("change,want", BAD_SHAPES)
