@@ -85,12 +85,14 @@ def _on_gpu(*tensors):
                 here = at
 
 
-def _new(shape, dtype, device, stream):
+def _new(like, stream, shape=None, dtype=None):
     """Memory for a call on ``stream``: of that stream, so that it is not handed on before the call's work is done."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _new(like, None, shape, dtype)
+    if shape is None:
+        return torch.empty_like(like) if dtype is None else torch.empty_like(like, dtype=dtype)
+    return like.new_empty(shape, dtype=dtype)
 
 
 def _plain(t, name, shape, dtype):
@@ -182,14 +184,14 @@ class _Call:
                             1 if rectify else 0)
         self.state_shape = (sequences, heads_kv, head_dim, head_dim)
 
-    def workspace(self, given, backward, device, stream):
+    def workspace(self, given, backward, like, stream):
         if given is not None:
             if not (given.is_contiguous() and given.dtype == torch.uint8):
                 _refuse("the workspace must be contiguous bytes")
             return given
         size = ctypes.c_size_t(0)
         _check(_lib().msla_recurrence_workspace_bytes(self.shape, backward, self.dt, size), "msla_recurrence_workspace_bytes")
-        return _new(size.value, torch.uint8, device, stream) if size.value else None
+        return _new(like, stream, size.value, torch.uint8) if size.value else None
 
 
 def msla_recurrence_workspace_bytes(sequences, tokens, heads_q, heads_kv, head_dim, dtype, packed=False, backward=False) -> int:
@@ -215,13 +217,13 @@ def msla_recurrence_forward(q, k, v, log_gate=None, sequences: Optional[int] = N
     _plain(initial_state, "initial_state", c.state_shape, torch.float32)
     _plain(final_state, "final_state", c.state_shape, torch.float32)
     if out is None:
-        out = _new(q.shape, q.dtype, q.device, stream)
+        out = _new(q, stream)
     if not (out.dtype == q.dtype):
         _refuse("out must have q's type")
     o, _ = _rows(out, "out", q.shape)
     if final_state is None:
-        final_state = _new(c.state_shape, torch.float32, q.device, stream)
-    ws = c.workspace(workspace, 0, q.device, stream)
+        final_state = _new(q, stream, c.state_shape, torch.float32)
+    ws = c.workspace(workspace, 0, q, stream)
     _check(_lib().msla_recurrence_forward(c.shape, c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(initial_state), o,
                                           _ptr(final_state), _ptr(ws), 0 if ws is None else ws.numel(), c.dt, _stream(stream)),
            "msla_recurrence_forward")
@@ -244,18 +246,18 @@ def msla_recurrence_backward(q, k, v, d_out, log_gate=None, sequences: Optional[
     grads = []
     for t, like, name in ((d_q, q, "d_q"), (d_k, k, "d_k"), (d_v, v, "d_v")):
         if t is None:
-            t = _new(like.shape, q.dtype, q.device, stream)
+            t = _new(like, stream)
         if not (t.dtype == q.dtype):
             _refuse(f"{name} must have q's type")
         grads.append((t, _rows(t, name, like.shape)[0]))
     if not (log_gate is not None or d_log_gate is None):
         _refuse("d_log_gate needs a log_gate")
     if d_log_gate is None and log_gate is not None:
-        d_log_gate = _new(log_gate.shape, q.dtype, q.device, stream)
+        d_log_gate = _new(log_gate, stream, log_gate.shape)
     dg, dg_stride = _gate(d_log_gate, c.tokens, c.heads_kv, q.dtype, "d_log_gate")
     if d_initial_state is None and initial_state is not None:
-        d_initial_state = _new(c.state_shape, torch.float32, q.device, stream)
-    ws = c.workspace(workspace, 1, q.device, stream)
+        d_initial_state = _new(q, stream, c.state_shape, torch.float32)
+    ws = c.workspace(workspace, 1, q, stream)
     _check(_lib().msla_recurrence_backward(c.shape, c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(initial_state), do,
                                            _ptr(d_final_state), grads[0][1], grads[1][1], grads[2][1], dg, dg_stride,
                                            _ptr(d_initial_state), _ptr(ws), 0 if ws is None else ws.numel(), c.dt, _stream(stream)),
@@ -275,7 +277,7 @@ def msla_recurrence_step(q, k, v, state, log_gate=None, scale=None, rectify=Fals
     _plain(state, "state", c.state_shape, torch.float32)
     _plain(new_state, "new_state", c.state_shape, torch.float32)
     if out is None:
-        out = _new(q.shape, q.dtype, q.device, stream)
+        out = _new(q, stream)
     if not (out.dtype == q.dtype):
         _refuse("out must have q's type")
     o, _ = _rows(out, "out", q.shape)
@@ -304,9 +306,9 @@ def msla_norm_forward(x, weight=None, residual=None, eps=1e-6, out=None, sum_out
     _on_gpu(out)
     _plain(out, "out", x.shape, x.dtype)
     if out is None:
-        out = _new(x.shape, x.dtype, x.device, stream)
+        out = _new(x, stream)
     if sum_out is None and residual is not None:
-        sum_out = _new(x.shape, x.dtype, x.device, stream)
+        sum_out = _new(x, stream)
     _check(_lib().msla_norm_forward(_ptr(x), _ptr(residual), _ptr(weight), _ptr(out), _ptr(sum_out), rows, channels, float(eps),
                                     _DTYPES[x.dtype], _stream(stream)), "msla_norm_forward")
     return out, x if sum_out is None else sum_out
@@ -317,9 +319,9 @@ def _rows8(x, out8, scale, stream):
     _plain(out8, "out8", x.shape, torch.float8_e4m3fn)
     _plain(scale, "scale", x.shape[:-1], torch.float32)
     if out8 is None:
-        out8 = _new(x.shape, torch.float8_e4m3fn, x.device, stream)
+        out8 = _new(x, stream, None, torch.float8_e4m3fn)
     if scale is None:
-        scale = _new(x.shape[:-1], torch.float32, x.device, stream)
+        scale = _new(x, stream, x.shape[:-1], torch.float32)
     return out8, scale
 
 
@@ -328,7 +330,7 @@ def msla_norm_quantized(x, weight=None, residual=None, eps=1e-6, out8=None, scal
     rows, channels = _norm_arguments(x, weight, residual, sum_out)
     out8, scale = _rows8(x, out8, scale, stream)
     if sum_out is None and residual is not None:
-        sum_out = _new(x.shape, x.dtype, x.device, stream)
+        sum_out = _new(x, stream)
     _check(_lib().msla_norm_quantized(_ptr(x), _ptr(residual), _ptr(weight), _ptr(out8), _ptr(scale), _ptr(sum_out), rows, channels,
                                       float(eps), _DTYPES[x.dtype], _stream(stream)), "msla_norm_quantized")
     return out8, scale, x if sum_out is None else sum_out
@@ -358,11 +360,11 @@ def msla_norm_backward(r, weight, d_y, d_sum=None, eps=1e-6, d_r=None, d_weight=
     _plain(d_r, "d_r", r.shape, r.dtype)
     _plain(d_weight, "d_weight", (channels,), torch.float32)
     if d_r is None:
-        d_r = _new(r.shape, r.dtype, r.device, stream)
+        d_r = _new(r, stream)
     if d_weight is None:
-        d_weight = _new(channels, torch.float32, r.device, stream)
+        d_weight = _new(r, stream, channels, torch.float32)
     if workspace is None:
-        workspace = _new(msla_norm_backward_workspace_bytes(rows, channels, r.dtype), torch.uint8, r.device, stream)
+        workspace = _new(r, stream, msla_norm_backward_workspace_bytes(rows, channels, r.dtype), torch.uint8)
     else:
         if not (workspace.is_contiguous() and workspace.dtype == torch.uint8):
             _refuse("the workspace must be contiguous bytes")
@@ -390,7 +392,7 @@ def msla_linear_quantized(x8, x_scale, w8, w_scale, dtype=torch.bfloat16, out=No
         _refuse(f"{dtype} is not a storage type")
     to = shape[:-1] + (c_out,)
     if out is None:
-        out = _new(to, dtype, x8.device, stream)
+        out = _new(x8, stream, to, dtype)
     else:
         _plain(out, "out", to, dtype)
     rows = x8.numel() // c_in if c_in else 0
