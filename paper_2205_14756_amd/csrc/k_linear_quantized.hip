@@ -53,6 +53,8 @@ __device__ __forceinline__ void store8(T* p, const f32x4& a, const f32x4& b) {
 // A workgroup has 128 rows x 128 outputs, a wave 64 x 64.  Tiles lie in LDS as rows of 128 bytes whose 16-byte pieces are XORed with the
 // row's number modulo 8, which gives the eight rows that a read serves together all banks.  Outputs are the rows of the matrix
 // instructions, dealt to pairs of blocks so that a lane ends up with eight neighbours of a row of y.
+// 4096 rows, 4096 -> 8192: 250 us, 1.1 PFLOP/s of the 1.4 that a large bf16 product reaches: bound by issue, the conversions of eight
+// operands for sixteen products of two instructions.  256 x 256 tiles: 8% less here, more where the grid is small.
 template <class T>
 __global__ void __launch_bounds__(256, 2) linear_quantized_kernel(const unsigned char* x8, const float* x_scale, const unsigned char* w8,
                                                                   const float* w_scale, T* y, int64_t rows, int c_in, int c_out, int tiles_o) {
@@ -141,6 +143,7 @@ bool rows_kernel_wins(int64_t rows, int c_out) {
 
 // Few rows: the weights are read once and that is what there is to do, so a workgroup has 16 outputs, its eight waves take 128 bytes of the
 // contraction each in turn, and their sums meet in LDS.  Up to 64 rows a workgroup (BLOCKS of 16), which come out of L2.
+// 48 rows, 4096 -> 4096: 10 us, 17 MB at 1.7 TB/s: the rows come out of L2 to each of 256 workgroups, which is three times the weights' bytes.
 template <class T, int BLOCKS>
 __global__ void __launch_bounds__(512) linear_quantized_rows_kernel(const unsigned char* x8, const float* x_scale, const unsigned char* w8,
                                                                     const float* w_scale, T* y, int64_t rows, int c_in, int c_out) {
