@@ -218,7 +218,7 @@ def msla_recurrence_forward(q, k, v, log_gate=None, sequences: Optional[int] = N
     _plain(final_state, "final_state", c.state_shape, torch.float32)
     if out is None:
         out = _new(q, stream)
-    if not (out.dtype == q.dtype):
+    elif not (out.dtype == q.dtype):
         _refuse("out must have q's type")
     o, _ = _rows(out, "out", q.shape)
     if final_state is None:
@@ -275,10 +275,11 @@ def msla_recurrence_step(q, k, v, state, log_gate=None, scale=None, rectify=Fals
         _refuse("q must be [sequences, heads_q, head_dim]")
     c = _Call(q, k, v, log_gate, q.shape[0], None, scale, rectify)
     _plain(state, "state", c.state_shape, torch.float32)
-    _plain(new_state, "new_state", c.state_shape, torch.float32)
+    if new_state is not state:
+        _plain(new_state, "new_state", c.state_shape, torch.float32)
     if out is None:
         out = _new(q, stream)
-    if not (out.dtype == q.dtype):
+    elif not (out.dtype == q.dtype):
         _refuse("out must have q's type")
     o, _ = _rows(out, "out", q.shape)
     _check(_lib().msla_recurrence_step(c.shape, c.q, c.k, c.v, c.gate, c.gate_stride, _ptr(state), o, _ptr(new_state), c.dt,
@@ -292,10 +293,14 @@ def _norm_arguments(x, weight, residual, total):
         _refuse(f"{x.dtype} is not a storage type")
     if not (x.dim() >= 1 and x.is_contiguous()):
         _refuse("x must be contiguous rows")
-    _plain(weight, "weight", x.shape[-1:], x.dtype)
-    _plain(residual, "residual", x.shape, x.dtype)
-    _plain(total, "sum_out", x.shape, x.dtype)
-    channels = x.shape[-1]
+    shape = x.shape
+    channels = shape[-1]
+    if weight is not None:
+        _plain(weight, "weight", (channels,), x.dtype)
+    if residual is not None:
+        _plain(residual, "residual", shape, x.dtype)
+    if total is not None:
+        _plain(total, "sum_out", shape, x.dtype)
     return x.numel() // channels if channels else 0, channels
 
 
@@ -303,10 +308,11 @@ def msla_norm_forward(x, weight=None, residual=None, eps=1e-6, out=None, sum_out
     """(y, r): r = x + residual, y = r / sqrt(mean(r^2) + eps) * weight over the last axis.  Without a residual r is x itself and is not
     written, unless sum_out is given."""
     rows, channels = _norm_arguments(x, weight, residual, sum_out)
-    _on_gpu(out)
-    _plain(out, "out", x.shape, x.dtype)
     if out is None:
         out = _new(x, stream)
+    else:
+        _on_gpu(out)
+        _plain(out, "out", x.shape, x.dtype)
     if sum_out is None and residual is not None:
         sum_out = _new(x, stream)
     _check(_lib().msla_norm_forward(_ptr(x), _ptr(residual), _ptr(weight), _ptr(out), _ptr(sum_out), rows, channels, float(eps),
@@ -315,13 +321,16 @@ def msla_norm_forward(x, weight=None, residual=None, eps=1e-6, out=None, sum_out
 
 
 def _rows8(x, out8, scale, stream):
-    _on_gpu(out8, scale)
-    _plain(out8, "out8", x.shape, torch.float8_e4m3fn)
-    _plain(scale, "scale", x.shape[:-1], torch.float32)
     if out8 is None:
         out8 = _new(x, stream, None, torch.float8_e4m3fn)
+    else:
+        _on_gpu(out8)
+        _plain(out8, "out8", x.shape, torch.float8_e4m3fn)
     if scale is None:
         scale = _new(x, stream, x.shape[:-1], torch.float32)
+    else:
+        _on_gpu(scale)
+        _plain(scale, "scale", x.shape[:-1], torch.float32)
     return out8, scale
 
 

@@ -231,6 +231,20 @@ def test_heads_inside_wider_rows(dtype):
                        seq.msla_recurrence_forward(t["q"], shared.contiguous(), t["v"], t["gate"])[0])
 
 
+@pytest.mark.parametrize("packed", [True, False])
+def test_no_tokens_at_all(packed):
+    """states are handed on, and their gradients back"""
+    h, d = 2, 64
+    q = torch.empty(0, h, d, dtype=torch.bfloat16, device="cuda")
+    gate = torch.empty(0, h, dtype=torch.bfloat16, device="cuda")
+    first, back = _numbers(96, 3, h, d, d).float().cuda(), _numbers(97, 3, h, d, d).float().cuda()
+    kw = dict(sequences=3, offsets=torch.zeros(4, dtype=torch.int32, device="cuda") if packed else None, initial_state=first)
+    out, last = seq.msla_recurrence_forward(q, q, q, gate, **kw)
+    grads = seq.msla_recurrence_backward(q, q, q, q, gate, d_final_state=back, **kw)
+    assert out.shape == q.shape and torch.equal(last, first)
+    assert torch.equal(grads[4], back) and all(g.numel() == 0 for g in grads[:4])
+
+
 def test_inputs_that_are_one_row_for_many():
     """strides of 0 over heads and over tokens give what copies give"""
     n, h, d = 500, 4, 32
