@@ -75,7 +75,7 @@ msla_status msla_recurrence_forward(const msla_recurrence* shape, msla_heads q, 
 /* The gradient of msla_recurrence_forward: from d_out (like out) and d_final_state (NULL: zero) to d_q, d_k, d_v (like q, k, v; sums
  * over the query heads of a state), d_log_gate [tokens, heads_kv] in the storage type (rows d_gate_stride apart; NULL: not wanted) and
  * d_initial_state (NULL: not wanted).  The rectifier's derivative is 0 at 0.  Nothing of the forward call is needed but its inputs.
- * d_initial_state may not be d_final_state. */
+ * d_initial_state may be neither d_final_state nor initial_state. */
 msla_status msla_recurrence_backward(const msla_recurrence* shape, msla_heads q, msla_heads k, msla_heads v,
                                      const void* log_gate, int64_t gate_stride, const float* initial_state,
                                      msla_heads d_out, const float* d_final_state,

@@ -198,7 +198,7 @@ msla_status msla_recurrence_backward(const msla_recurrence* shape, msla_heads q,
         !aligned(d_initial_state, 16))
         return MSLA_ERR_INVALID_ARG;
     if (d_log_gate != nullptr && log_gate == nullptr) return MSLA_ERR_INVALID_ARG;
-    if (d_initial_state != nullptr && d_initial_state == d_final_state) return MSLA_ERR_INVALID_ARG;
+    if (d_initial_state != nullptr && (d_initial_state == d_final_state || d_initial_state == initial_state)) return MSLA_ERR_INVALID_ARG;
     for (const msla_heads* o : {&d_q, &d_k, &d_v})
         for (const msla_heads* i : {&q, &k, &v, &d_out})
             if (same(*o, *i)) return MSLA_ERR_INVALID_ARG;

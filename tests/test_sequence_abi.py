@@ -116,6 +116,14 @@ def test_outputs_that_overlap_are_refused(lib):
     assert b(x, y, z, n=64) == WORKSPACE
 
 
+def test_the_state_s_gradient_has_a_place_of_its_own(lib):
+    s = shape()
+    for first, d_last in ((8 * P, None), (None, 8 * P), (8 * P, 8 * P)):
+        st = lib.msla_recurrence_backward(ctypes.byref(s), heads(), heads(2 * P), heads(3 * P), None, 0, first, heads(4 * P), d_last, heads(5 * P),
+                                          heads(6 * P), heads(7 * P), None, 0, 8 * P, P, 1 << 40, F16, None)
+        assert st == INVALID
+
+
 def test_step_is_refused(lib):
     f = lambda s, state=P, new=2 * P, dt=F16: lib.msla_recurrence_step(ctypes.byref(s), heads(), heads(2 * P), heads(3 * P), None, 0, state,
                                                                        heads(4 * P), new, dt, None)
