@@ -429,12 +429,15 @@ hipError_t norm_backward_of(const void* sum, const void* weight, const void* d_y
 
 }  // namespace
 
-// Workgroups of the backward pass: what the compute units hold at once, so that their parts of d_weight are few.
+// Workgroups of the backward pass: what the compute units work on at once, so that their parts of d_weight are few, and those no more than one
+// for four rows while there is one a unit.  bf16, us with 256 / 512 (768, 1024) of them: 8192 x 2051 50 / 36 (42, 40), 2048 x 2051 18.7 /
+// 17.2, 1024 x 4096 15.6 / 18.2, 512 x 2048 9.4 / 11.1; of 1024 threads 2048 x 8192 31 / 39 (46, 52), 4096 x 16384 116 / 126.
 int norm_backward_blocks(int64_t rows, int channels, int elem) {
     const Lanes l = lanes_for(channels, elem);
     const int per_block = (l.lpr > 256 ? l.lpr : 256) / l.lpr;
     const int64_t all = (rows + per_block - 1) / per_block;
-    return (int)(all < 512 ? all : 512);
+    const int64_t most = l.lpr > 256 || rows / 4 < 256 ? 256 : (rows / 4 < 512 ? rows / 4 : 512);
+    return (int)(all < most ? all : most);
 }
 
 hipError_t launch_norm(int dt, const NormCall& c, hipStream_t stream) {

@@ -2,7 +2,7 @@
 
 Tolerances: half a step of the result's type, plus fp32 on the way: a sum of squares is off by at most channels * 2^-24 of itself where it
 is summed in a row, and here in pieces of at most 64 values and a tree above them, so 2^-17 covers it, the square root, the
-reciprocal and two products; gradients have two such sums.  d_weight sums rows in runs of at most rows / 512 + 1, then at most 16 of those and 32 of these."""
+reciprocal and two products; gradients have two such sums.  d_weight sums rows in runs of at most rows / 256 + 1, then at most 16 of those and 32 of these."""
 import numpy as np
 import pytest
 import torch
