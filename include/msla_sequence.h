@@ -62,7 +62,7 @@ typedef struct {
  *   initial_state, final_state [sequences, heads_kv, head_dim (of k), head_dim (of v)] fp32, either may be NULL; final_state may be
  *       initial_state itself.  A sequence without tokens hands its state on.
  * The state, the sums and the gates' running products are fp32 (or more), a state on the way with up to 2^16 times its value; an
- * operand of a matrix instruction that is not an input goes in as two or three parts of the storage type.
+ * operand of a matrix instruction that is not an input goes in as parts of the storage type, three in bf16 and two in fp16, which leave fp32's precision.
  * The workspace hangs on the shape alone, offsets being NULL or not included.
  * A value that is not finite stays within its own sequence and head; there it reaches the tokens behind it and those of its own
  * chunk of 64 tokens before it. */

@@ -125,10 +125,8 @@ struct State {
         for (int e = 0; e < Ti::kOp; ++e) v[e] = s[b * Ti::kJoinOp + e / 4][e % 4] * f;
         Ti::template split<kParts<T>>(v, part);
     }
-    // += sum_j b_j (w_j c_j)^T over the chunk; vt: the wave's columns of c over tokens.  ALWAYS or exact: with all of kStateParts (a state that
-    // is handed out), else with those of kParts (one that only goes into outputs, in as many parts).
-    template <bool ALWAYS>
-    __device__ __forceinline__ void add(char* tb, const typename Ti::Vec (&vt)[Ti::kTokenSteps], const float* weight, float unit, bool exact) {
+    // += sum_j b_j (w_j c_j)^T over the chunk; vt: the wave's columns of c over tokens.
+    __device__ __forceinline__ void add(char* tb, const typename Ti::Vec (&vt)[Ti::kTokenSteps], const float* weight, float unit) {
         const int lane = lane_id_again(), x = lane & 15, q = lane >> 4;
 #pragma unroll
         for (int st = 0; st < Ti::kTokenSteps; ++st) {
@@ -145,27 +143,20 @@ struct State {
                     if constexpr (Ti::kNormalise) v[4 * j + r] *= unit;
                 }
             }
-            typename Ti::Vec part[kStateParts<T>];
-            Ti::template split<kStateParts<T>>(v, part);
+            typename Ti::Vec part[kParts<T>];
+            Ti::template split<kParts<T>>(v, part);
 #pragma unroll
             for (int b = 0; b < Ti::kBlocks; b += 2) {
                 typename Ti::Vec more = kt, next = kt;
                 if (b + 1 < Ti::kBlocks) more = Ti::key_operand(tb, b + 1, st, x, q);
                 if (b + 2 < Ti::kBlocks) next = Ti::key_operand(tb, b + 2, st, x, q);
 #pragma unroll
-                for (int p = 0; p < (ALWAYS ? kStateParts<T> : kParts<T>); ++p) {
+                for (int p = 0; p < kParts<T>; ++p) {
                     s[b] = Ti::Tr::mma_vec(s[b], kt, part[p]);
                     if (b + 1 < Ti::kBlocks) s[b + 1] = Ti::Tr::mma_vec(s[b + 1], more, part[p]);
                 }
                 kt = next;
                 __builtin_amdgcn_sched_barrier(0);
-            }
-            if constexpr (!ALWAYS && kStateParts<T> > kParts<T>) {
-                if (exact) {
-#pragma unroll
-                    for (int b = 0; b < Ti::kBlocks; ++b)
-                        s[b] = Ti::Tr::mma_vec(s[b], Ti::key_operand(tb, b, st, x, q), part[kParts<T>]);
-                }
             }
         }
     }
@@ -296,7 +287,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         typename Ti::Vec vt[Ti::kTokenSteps];
 #pragma unroll
         for (int st = 0; st < Ti::kTokenSteps; ++st) vt[st] = Ti::value_operand(tc + mine * Ti::kHeadBytes, slice, st, x, q);
-        state.template add<true>(tb + mine * Ti::kHeadBytes, vt, gt.weight, unit, true);
+        state.add(tb + mine * Ti::kHeadBytes, vt, gt.weight, unit);
         __syncthreads();
     }
     if (head >= p.heads) return;
@@ -676,7 +667,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (MASKED && Tile<T, D>:
             if (decays) factor *= gt.total;
             if constexpr (!Ti::kNormalise) unit = gt.unit;
             if (factor != 1.0f) state.scale(factor);
-            state.template add<false>(hb, vt, gt.weight, unit, hands_out);
+            state.add(hb, vt, gt.weight, unit);
         }
         __syncthreads();
         if constexpr (MASKED) {

@@ -1,0 +1,75 @@
+"""The recurrence where its numbers are hard: sums that are exact in fp32, whatever its operands are split into on the way."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2205_14756_amd import sequence as seq
+
+pytestmark = pytest.mark.gpu
+
+TDT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+DTYPES = ["f32", "f16", "bf16"]
+
+
+def whole(seed, top, *shape):
+    return torch.from_numpy(np.random.default_rng(seed).integers(-top, top + 1, shape)).double()
+
+
+def single(seed, tokens, heads, d):
+    """one channel of every row is 1 or -1, token t's is t mod d: a column sums tokens / d rows"""
+    x = torch.zeros(tokens, heads, d, dtype=torch.float64)
+    t = torch.arange(tokens)
+    x[t, :, t % d] = whole(seed, 1, tokens, heads).mul(2).add(1).sign()
+    return x
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+def test_whole_numbers_are_exact(dtype, d):
+    """Whole numbers up to 255 (8 bits: every type has them), two chunks of 64 tokens, a scale of 2^-9 and no gates: scores stay below
+    128 * 255^2 < 2^23, and so do all sums of them, so fp32 holds every one of them exactly and an output is the exact sum, rounded once."""
+    tokens, heads = 128, 4
+    a, b, one = whole(1, 255, tokens, heads, d), whole(2, 255, tokens, heads, d), single(3, tokens, heads, d)
+    scale = 2.0 ** -9
+    to = lambda x: x.to(TDT[dtype]).cuda()
+    low = torch.ones(tokens, tokens, dtype=torch.float64).tril()
+    scores = torch.einsum("ihc,jhc->hij", a, b) * scale
+
+    def same(got, want, what):
+        want = want.to(TDT[dtype])
+        assert bool(torch.isfinite(want.float()).all())
+        wrong = int((got.cpu() != want).sum())
+        print(f"  {what}: {wrong} of {want.numel()} differ", flush=True)
+        assert wrong == 0, what
+
+    print(f"whole numbers {dtype} d={d}", flush=True)
+    out, state = seq.msla_recurrence_forward(to(a), to(b), to(one), scale=scale)
+    same(out, torch.einsum("hij,jhe->ihe", scores * low, one), "out")
+    assert torch.equal(state[0].cpu().double(), torch.einsum("jhc,jhe->hce", b, one))
+    # scores of d_out and v: of d_q (a: d_out, b: v) over the keys, of d_k (a: v, b: d_out) over the queries
+    back = torch.einsum("ihc,jhc->hij", a, b) * scale
+    d_q, d_k, d_v, *_ = seq.msla_recurrence_backward(to(one), to(one), to(b), to(a), scale=scale)
+    same(d_q, torch.einsum("hij,jhe->ihe", back * low, one), "d_q")
+    same(d_k, torch.einsum("hij,ihe->jhe", back * low, one), "d_k")
+    same(d_v, torch.einsum("hij,ihe->jhe", torch.einsum("ihc,jhc->hij", one, one) * low * scale, a), "d_v")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+def test_a_state_of_whole_numbers_is_read_exactly(dtype, d):
+    """A state of numbers up to 2^20 and queries of one 1 and one -1: differences below 2^21, exact in fp32, rounded once.  The rows behind
+    the state's own tokens are zero, so every token reads the same state."""
+    tokens, heads = 70, 4
+    first = whole(4, 2 ** 20, 1, heads, d, d)
+    q = torch.zeros(tokens, heads, d, dtype=torch.float64)
+    t = torch.arange(tokens)
+    q[t, :, t % d], q[t, :, (t + 1 + t // d) % d] = 1.0, -1.0
+    none = torch.zeros(tokens, heads, d, dtype=TDT[dtype], device="cuda")
+    scale = 2.0 ** -8
+    want = (torch.einsum("ihc,hce->ihe", q, first[0]) * scale).to(TDT[dtype])
+    print(f"state {dtype} d={d}", flush=True)
+    out, state = seq.msla_recurrence_forward(q.to(TDT[dtype]).cuda(), none, none, initial_state=first.float().cuda(), scale=scale)
+    wrong = int((out.cpu() != want).sum())
+    print(f"  out: {wrong} of {want.numel()} differ", flush=True)
+    assert wrong == 0
+    assert torch.equal(state.cpu().double(), first)
