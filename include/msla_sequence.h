@@ -29,7 +29,10 @@ extern "C" {
 /* [token, head, channel] in the storage type: channels next to each other, strides in elements (multiples of 16 bytes; not
  * negative; a token's below 16 MiB, a head's at most 512 MiB, else MSLA_ERR_UNSUPPORTED).  So heads may be part of a wider row: the
  * map that msla_linear projects with w_qkv's row order is q = {p, 3*Ct, 3*d}, k = {p + d, ...}, v = {p + 2*d, ...}.  An input's strides
- * may be 0 (one row for all tokens, or all heads); an output's rows must not overlap each other. */
+ * may be 0 (one row for all tokens, or all heads); an output's rows must not overlap each other.
+ * Where several query heads share a state and head_dim is 16 or 32, the forward and backward calls read n = 64 / head_dim states' rows (heads_kv
+ * of them where those are fewer) of q and of out's gradient at one 32-bit offset: 63 token strides and (n - 1) * heads_q / heads_kv head strides and a
+ * row make at most 2^32 - 16 bytes, else MSLA_ERR_UNSUPPORTED (token-major maps always do). */
 typedef struct {
     void* data;                 /* read only where the operand is an input */
     int64_t token_stride;

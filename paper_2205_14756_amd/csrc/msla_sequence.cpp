@@ -46,9 +46,11 @@ msla_status check_shape(const msla_recurrence* s, msla_dtype dt) {
     return MSLA_OK;
 }
 
+int heads_per_group(const msla_recurrence& s) { return s.head_dim >= 64 ? 1 : 64 / s.head_dim; }       // state heads of a workgroup of the scan
+
 // Segments are as long as leaves kWantGroups workgroups.  One that spans all tokens keeps every sequence whole.
 msla_status plan_of(const msla_recurrence& s, bool backward, RecurrencePlan* plan) {
-    const int per_group = s.head_dim >= 64 ? 1 : 64 / s.head_dim;           // heads of a workgroup
+    const int per_group = heads_per_group(s);
     const int64_t groups = (s.heads_kv + per_group - 1) / per_group;
     const int64_t want = (kWantGroups + groups - 1) / groups;
     int64_t segment = (s.tokens / want + 63) / 64 * 64;
@@ -97,6 +99,15 @@ constexpr int64_t kMostTokenStride = ((int64_t)1 << 24) - 1, kMostHeadStride = (
 bool wide(const msla_heads& h, msla_dtype dt) {
     const int64_t e = (int64_t)elem_size(dt);
     return h.token_stride * e > kMostTokenStride || h.head_stride * e > kMostHeadStride;
+}
+
+// ... and what such an offset reaches in an operand that a workgroup reads for all of its state heads, each with `heads / heads_kv` of the
+// operand's: from the first one's first row to the last one's last, below the offset that stands for "not read" (2^32 - 16).
+bool beyond_reach(const msla_heads& h, const msla_recurrence& s, int heads, msla_dtype dt) {
+    if (s.tokens == 0) return false;
+    const int64_t states = heads_per_group(s) < s.heads_kv ? heads_per_group(s) : s.heads_kv, rows = s.tokens < 64 ? s.tokens : 64;
+    const int64_t last = (rows - 1) * h.token_stride + (states - 1) * (heads / s.heads_kv) * h.head_stride + s.head_dim;
+    return last * (int64_t)elem_size(dt) > 0xfffffff0LL;
 }
 
 // a [tokens, heads, head_dim] operand: 16-byte pieces, no span beyond kMost
@@ -170,7 +181,7 @@ msla_status msla_recurrence_forward(const msla_recurrence* shape, msla_heads q, 
         !apart(out, s, s.heads_q) || !gate_fits(log_gate, gate_stride, s, dt, false) || !aligned(initial_state, 16) ||
         !aligned(final_state, 16) || same(out, q) || same(out, k) || same(out, v))
         return MSLA_ERR_INVALID_ARG;
-    if (wide(q, dt) || wide(k, dt) || wide(v, dt) || wide(out, dt)) return MSLA_ERR_UNSUPPORTED;
+    if (wide(q, dt) || wide(k, dt) || wide(v, dt) || wide(out, dt) || beyond_reach(q, s, s.heads_q, dt)) return MSLA_ERR_UNSUPPORTED;
     RecurrenceCall c = {};
     st = plan_of(s, false, &c.plan);
     if (st != MSLA_OK) return st;
@@ -205,6 +216,7 @@ msla_status msla_recurrence_backward(const msla_recurrence* shape, msla_heads q,
     if (same(d_q, d_k) || same(d_q, d_v) || same(d_k, d_v)) return MSLA_ERR_INVALID_ARG;
     for (const msla_heads* h : {&q, &k, &v, &d_out, &d_q, &d_k, &d_v})
         if (wide(*h, dt)) return MSLA_ERR_UNSUPPORTED;
+    if (beyond_reach(q, s, s.heads_q, dt) || beyond_reach(d_out, s, s.heads_q, dt)) return MSLA_ERR_UNSUPPORTED;
     RecurrenceCall c = {};
     st = plan_of(s, true, &c.plan);
     if (st != MSLA_OK) return st;

@@ -146,7 +146,7 @@ struct Tile {
     static __device__ __forceinline__ long token(const Segment& s, int reverse, long u) { return reverse ? s.hi - 1 - u : s.lo + u; }
 
     // A thread's pieces of a tile: rows row(t) + i * kRowStep, through a buffer resource at the tile's lowest address: one 32-bit offset a
-    // thread and tile, a scalar one a piece.  (The strides' bounds keep their sum below 2^32.)  The thread's number t is made anew for each
+    // thread and tile, a scalar one a piece.  (The host refuses strides whose sum, group of query heads included, does not stay below kNowhere.)  The thread's number t is made anew for each
     // tile, and the offset of it: kept over the loop, they cost registers that are not there, and what is spilled here is waited for among
     // the loads in flight.
     static __device__ __forceinline__ int row(int t) { return t / kPerRow; }

@@ -73,3 +73,25 @@ def test_a_state_of_whole_numbers_is_read_exactly(dtype, d):
     print(f"  out: {wrong} of {want.numel()} differ", flush=True)
     assert wrong == 0
     assert torch.equal(state.cpu().double(), first)
+
+
+@pytest.mark.parametrize("d", [16, 32])
+def test_grouped_heads_as_far_apart_as_they_may_be(d):
+    """Head-major queries and gradients whose last row of a workgroup's last state head ends right below 2^32 - 16 bytes behind the first."""
+    tokens, hkv, group = 150, 64 // d, 4 if d == 16 else 9
+    hq = hkv * group
+    stride = (2 ** 32 - 16 - 2 * d - 63 * 2 * d) // ((64 // d - 1) * group * 2) // 8 * 8
+    n = lambda seed, *s: torch.from_numpy(np.random.default_rng(seed).standard_normal(s)).bfloat16().cuda()
+    q, k, v, d_out = n(1, tokens, hq, d), n(2, tokens, hkv, d), n(3, tokens, hkv, d), n(4, tokens, hq, d)
+
+    def apart(x):
+        room = torch.empty((hq - 1) * stride + tokens * d, dtype=x.dtype, device="cuda")
+        y = room.as_strided(x.shape, (d, stride, 1))
+        y.copy_(x)
+        return y
+
+    fq, fd = apart(q), apart(d_out)
+    for a, b in zip(seq.msla_recurrence_forward(q, k, v), seq.msla_recurrence_forward(fq, k, v, out=torch.empty_like(q))):
+        assert torch.equal(a, b)
+    for a, b in zip(seq.msla_recurrence_backward(q, k, v, d_out)[:3], seq.msla_recurrence_backward(fq, k, v, fd, d_q=torch.empty_like(q))[:3]):
+        assert torch.equal(a, b)
