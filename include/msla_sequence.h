@@ -52,7 +52,7 @@ typedef struct {
     const int32_t* offsets;
     int heads_q, heads_kv, head_dim;
     float scale;                /* of every product of a query and a key; finite */
-    int rectify;                /* 1: q and k are taken as max(q, 0), max(k, 0), as in Eq. (2); 0: as they are */
+    int rectify;                /* 1: q and k are taken as max(q, 0), max(k, 0), as in Eq. (2) (a NaN stays one); 0: as they are */
 } msla_recurrence;
 
 /* For every sequence, state head h and query head of it, with S_{-1} = initial_state (zero where that is NULL):
@@ -77,7 +77,7 @@ msla_status msla_recurrence_forward(const msla_recurrence* shape, msla_heads q, 
 
 /* The gradient of msla_recurrence_forward: from d_out (like out) and d_final_state (NULL: zero) to d_q, d_k, d_v (like q, k, v; sums
  * over the query heads of a state), d_log_gate [tokens, heads_kv] in the storage type (rows d_gate_stride apart; NULL: not wanted) and
- * d_initial_state (NULL: not wanted).  The rectifier's derivative is 0 at 0.  Nothing of the forward call is needed but its inputs.
+ * d_initial_state (NULL: not wanted).  The rectifier's derivative is 0 at 0 and at a NaN.  Nothing of the forward call is needed but its inputs.
  * d_initial_state may be neither d_final_state nor initial_state. */
 msla_status msla_recurrence_backward(const msla_recurrence* shape, msla_heads q, msla_heads k, msla_heads v,
                                      const void* log_gate, int64_t gate_stride, const float* initial_state,

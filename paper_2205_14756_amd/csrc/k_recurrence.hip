@@ -783,7 +783,7 @@ __global__ void __launch_bounds__(kThreads) recurrence_step_kernel(StepArgs p) {
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
         float k = Tr::to_f32(kp[row0 + i * kRowLanes]);
-        if (p.k.relu) k = k > 0.0f ? k : 0.0f;
+        if (p.k.relu) k = k <= 0.0f ? 0.0f : k;       // (a NaN stays one, as in the scan)
 #pragma unroll
         for (int r = 0; r < 4; ++r) s[i][r] = fmaf(k, v[r], keep * s[i][r]);
         if (live) *(f32x4*)(p.fresh + (b * p.heads + h) * (D * D) + (row0 + i * kRowLanes) * D + col) = s[i];
@@ -794,7 +794,7 @@ __global__ void __launch_bounds__(kThreads) recurrence_step_kernel(StepArgs p) {
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             float q = Tr::to_f32(qp[row0 + i * kRowLanes]);
-            if (p.q.relu) q = q > 0.0f ? q : 0.0f;
+            if (p.q.relu) q = q <= 0.0f ? 0.0f : q;
 #pragma unroll
             for (int r = 0; r < 4; ++r) o[r] = fmaf(q, s[i][r], o[r]);
         }

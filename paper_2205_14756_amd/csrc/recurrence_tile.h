@@ -169,20 +169,25 @@ struct Tile {
             r.v[i] = buf_load16(from, row(t) < rows - i * kRowStep ? off : kNowhere, (int)((reverse ? kPieces - 1 - i : i) * step));
     }
 
+    // max(x, 0) of 16 bytes, and a NaN stays one, of either sign.  On the bits: a signed maximum with 0 takes what is negative to 0, NaNs with a sign
+    // among it, and those are what lies above -inf as an unsigned number; 0 less that distance is a NaN again.
+    static __device__ __forceinline__ u32x4 rectified(u32x4 v) {
+        typedef typename std::conditional<sizeof(T) == 2, short, int>::type I;
+        typedef typename std::conditional<sizeof(T) == 2, unsigned short, unsigned>::type U;
+        typedef I Signed __attribute__((ext_vector_type(kVec)));
+        typedef U Unsigned __attribute__((ext_vector_type(kVec)));
+        const Unsigned infinite = (Unsigned)(U)(std::is_same<T, float>::value ? 0xff800000u : (kNormalise ? 0xfc00u : 0xff80u));
+        const Unsigned positive = __builtin_bit_cast(Unsigned, __builtin_elementwise_max(__builtin_bit_cast(Signed, v), (Signed)(I)0));
+        return __builtin_bit_cast(u32x4, positive - __builtin_elementwise_sub_sat(__builtin_bit_cast(Unsigned, v), infinite));
+    }
+
     // into LDS, rectified where asked; returns the largest bit pattern of a finite magnitude (fp16 alone; a value that is not finite may
     // not spoil the other heads' normalisers)
     static __device__ __forceinline__ unsigned store(Regs& r, char* tile, int relu, int t) {
-        typedef short i16x8 __attribute__((ext_vector_type(8)));
-        typedef int i32x4 __attribute__((ext_vector_type(4)));
         unsigned top = 0;
         if (relu) {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                if constexpr (sizeof(T) == 2)
-                    r.v[i] = __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(i16x8, r.v[i]), i16x8{0, 0, 0, 0, 0, 0, 0, 0}));
-                else
-                    r.v[i] = __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(i32x4, r.v[i]), i32x4{0, 0, 0, 0}));
-            }
+            for (int i = 0; i < kPieces; ++i) r.v[i] = rectified(r.v[i]);
         }
         char* at = tile + head_of(t) * kHeadBytes + row(t) * kPitch + t % (D / kVec) * 16;
 #pragma unroll

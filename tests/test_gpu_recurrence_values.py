@@ -95,3 +95,38 @@ def test_grouped_heads_as_far_apart_as_they_may_be(d):
         assert torch.equal(a, b)
     for a, b in zip(seq.msla_recurrence_backward(q, k, v, d_out)[:3], seq.msla_recurrence_backward(fq, k, v, fd, d_q=torch.empty_like(q))[:3]):
         assert torch.equal(a, b)
+
+
+NANS = {"f32": (torch.int32, (0x7FC00000, 0xFFC00000, 0xFF800001)), "f16": (torch.int16, (0x7E00, 0xFE00, 0xFC01)),
+        "bf16": (torch.int16, (0x7FC0, 0xFFC0, 0xFF81))}
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("which", range(3))
+@pytest.mark.parametrize("operand", ["q", "k"])
+def test_a_rectified_nan_stays_one(dtype, which, operand):
+    """NaNs of both signs, in the scan and in the step: what reads one is a NaN, and nothing else is touched."""
+    ints, codes = NANS[dtype]
+    code = codes[which] - (1 << (8 * ints.itemsize)) if codes[which] >> (8 * ints.itemsize - 1) else codes[which]
+    n, h, d, at, head = 150, 3, 64, 100, 1
+    x = {m: torch.from_numpy(np.random.default_rng(i).standard_normal((n, h, d))).to(TDT[dtype]).cuda() for i, m in enumerate("qkv")}
+    x["q"][3, 0, :2], x["k"][3, 0, :2] = float("-inf"), float("-inf")                     # (rectified: 0)
+    first = torch.from_numpy(np.random.default_rng(5).standard_normal((n, h, d, d))).float().cuda()
+    clean, last = seq.msla_recurrence_forward(x["q"], x["k"], x["v"], initial_state=first[:1], rectify=True)
+    one, states = seq.msla_recurrence_step(x["q"], x["k"], x["v"], first, rectify=True, new_state=torch.empty_like(first))
+    assert all(bool(torch.isfinite(t.float()).all()) for t in (clean, last, one, states))
+    x[operand].view(ints)[at, head, 5] = code
+    assert bool(torch.isnan(x[operand][at, head, 5]))
+    got, end = seq.msla_recurrence_forward(x["q"], x["k"], x["v"], initial_state=first[:1], rectify=True)
+    hit = torch.zeros(n, h, dtype=torch.bool, device="cuda")
+    hit[slice(at, at + 1 if operand == "q" else None), head] = True
+    assert bool(torch.isnan(got[hit].float()).all())
+    if dtype != "f16":          # (fp16: a chunk's normaliser hangs on its largest value, which may be another one now)
+        assert torch.equal(got[~hit], clean[~hit])
+    assert bool(torch.isfinite(got[~hit].float()).all())
+    assert bool(torch.isnan(end[0, head, 5]).all()) if operand == "k" else bool(torch.isfinite(end).all())
+    got, after = seq.msla_recurrence_step(x["q"], x["k"], x["v"], first, rectify=True, new_state=torch.empty_like(first))
+    hit = torch.zeros(n, h, dtype=torch.bool, device="cuda")
+    hit[at, head] = True
+    assert bool(torch.isnan(got[hit].float()).all()) and torch.equal(got[~hit], one[~hit])
+    assert bool(torch.isnan(after[at, head, 5]).all()) if operand == "k" else torch.equal(after, states)
