@@ -52,18 +52,37 @@ struct StateArgs {
     float weight_scale;
 };
 
-// bounds on a tile's magnitudes from what the waves left in LDS (fp16 alone)
-template <int WAVES>
-__device__ __forceinline__ float tile_top(const unsigned* top) {
-    unsigned t = top[0];
+// Bounds on the magnitudes of a tile's rows of one head, from what the waves left in LDS (fp16 alone): [wave][head][a, b, c].  A head's own, so that
+// its precision does not hang on the heads that share its workgroup.
+template <class Ti>
+__device__ __forceinline__ float tile_top(const unsigned* top, int head) {
+    unsigned t = top[3 * head];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) t = max(t, top[3 * w]);
+    for (int w = 1; w < Ti::kWaves; ++w) t = max(t, top[3 * (w * Ti::kHeads + head)]);
     return half_bits(t);
 }
 
+// `mine`: of this lane's pieces, which are all of one head (Tile::head_of)
+template <class Ti>
 __device__ __forceinline__ void leave_top(unsigned* top, unsigned mine) {
-    mine = running_max(mine);
-    if (lane_id() == 63) top[(threadIdx.x >> 6) * 3] = mine;
+    const int lane = lane_id();
+    top += 3 * Ti::kHeads * (threadIdx.x >> 6);
+    if constexpr (Ti::kHeads == 1) {
+        mine = running_max(mine);
+        if (lane == 63) *top = mine;
+    } else {
+        // lanes 8 apart have the same head, and so have two (heads of 16) or four (of 32) neighbours
+        constexpr int kLanes = Ti::kPerRow / Ti::kHeads;
+        static_assert(Ti::kPerRow == 8 && (kLanes == 2 || kLanes == 4), "eight pieces a row");
+        mine = max(mine, moved<0x128, 0xf>(mine));              // row_ror 8
+        const u32x2 rows = __builtin_amdgcn_permlane16_swap(mine, mine, false, false);
+        mine = max(rows[0], rows[1]);
+        const u32x2 halves = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
+        mine = max(halves[0], halves[1]);
+        mine = max(mine, moved<0xb1, 0xf>(mine));               // quad_perm 1 0 3 2
+        if constexpr (kLanes == 4) mine = max(mine, moved<0x4e, 0xf>(mine));    // quad_perm 2 3 0 1
+        if (lane < 8 && lane % kLanes == 0) top[3 * (lane / kLanes)] = mine;
+    }
 }
 
 // The state's part of a wave: rows are all channels of the key, columns the wave's 16 output channels.
@@ -213,7 +232,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     char* tb = lds;
     char* tc = tb + Ti::kBytes;
     Gates* gates = (Gates*)(tc + Ti::kBytes);
-    unsigned* tops = (unsigned*)(gates + 2 * Ti::kHeads);           // [2][waves][3]
+    unsigned* tops = (unsigned*)(gates + 2 * Ti::kHeads);           // [2][waves][heads][3]
 
     const Segment seg = find_segment(p.layout, blockIdx.x);
     if (!seg.live || seg.index == (p.reverse ? 0 : seg.count - 1)) return;     // nothing comes after it
@@ -258,11 +277,11 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     int sub = 0, next_sub = 0;
     long first = 0;
     for (int it = 0; it < steps; ++it, first += next_sub == 0 ? kChunk : 0, sub = next_sub) {
-        unsigned* top = tops + (it & 1) * 3 * Ti::kWaves;
+        unsigned* top = tops + (it & 1) * 3 * Ti::kWaves * Ti::kHeads;
         const int t = Ti::thread(wave);
         Ti::store(rb, tb, p.b.relu, t);
         const unsigned mc = Ti::store(rc, tc, p.c.relu, t);
-        if constexpr (Ti::kNormalise) leave_top(top + 2, mc);
+        if constexpr (Ti::kNormalise) leave_top<Ti>(top + 2, mc);
         __syncthreads();
         if (it + 1 < steps) {
             next_sub = sub + 1 == p.gb ? 0 : sub + 1;
@@ -272,7 +291,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         if (sub == 0) gates_of(first + kChunk);
         float fresh = unit, factor = 1.0f;
         if constexpr (Ti::kNormalise) {
-            const float bound = tile_top<Ti::kWaves>(top + 2) * fabsf(p.weight_scale) * gt.grow;
+            const float bound = tile_top<Ti>(top + 2, mine) * fabsf(p.weight_scale) * gt.grow;
             if (bound > 0.0f) fresh = normaliser(bound);
             factor = fresh / unit;
             unit = fresh;
@@ -381,8 +400,8 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (MASKED && Tile<T, D>:
     char* tb = ta + Ti::kBytes;
     char* tc = tb + Ti::kBytes;
     Gates* gates = (Gates*)(tc + Ti::kBytes);
-    unsigned* tops = (unsigned*)(gates + 2 * Ti::kHeads);           // [2][waves][3]
-    float* dots = (float*)(tops + 6 * Ti::kWaves);              // [waves][64]
+    unsigned* tops = (unsigned*)(gates + 2 * Ti::kHeads);           // [2][waves][heads][3]
+    float* dots = (float*)(tops + 6 * Ti::kWaves * Ti::kHeads);              // [waves][64]
     char* scores = (char*)(dots + kChunk * Ti::kWaves);
 
     const Segment seg = find_segment(p.layout, blockIdx.x);
@@ -449,7 +468,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (MASKED && Tile<T, D>:
         const bool new_a = sub == 0 || ga > 1, new_b = sub == 0 || gb > 1;      // (one of ga, gb is 1)
         const bool begins = new_a, ends = gb == 1 || sub == group - 1;            // of an output's sum
         const bool feeds = ga == 1 || sub == group - 1;                           // the state
-        unsigned* top = tops + (it & 1) * 3 * Ti::kWaves;
+        unsigned* top = tops + (it & 1) * 3 * Ti::kWaves * Ti::kHeads;
         unsigned ma = 0, mb = 0, mc = 0;
         const int t = Ti::thread(wave);
         if (new_a) ma = Ti::store(ra, ta, p.a.relu, t);
@@ -458,9 +477,9 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (MASKED && Tile<T, D>:
             mc = Ti::store(rc, tc, p.c.relu, t);
         }
         if constexpr (Ti::kNormalise) {
-            leave_top(top, ma);
-            leave_top(top + 1, mb);
-            leave_top(top + 2, mc);
+            leave_top<Ti>(top, ma);
+            leave_top<Ti>(top + 1, mb);
+            leave_top<Ti>(top + 2, mc);
         }
         __syncthreads();
         // (a lane's number, and the addresses that are made of it, anew for each part: see Tile::load)
@@ -472,10 +491,10 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (MASKED && Tile<T, D>:
         char* hc = tc + mine * Ti::kHeadBytes;
         float fp = 1.0f;
         if constexpr (Ti::kNormalise) {
-            if (new_a) at = tile_top<Ti::kWaves>(top);
+            if (new_a) at = tile_top<Ti>(top, mine);
             if (new_b) {
-                bt = tile_top<Ti::kWaves>(top + 1);
-                ct = tile_top<Ti::kWaves>(top + 2);
+                bt = tile_top<Ti>(top + 1, mine);
+                ct = tile_top<Ti>(top + 2, mine);
             }
             fp = normaliser(fabsf(p.score_scale) * (float)D * at * bt * gt.grow);
         }
@@ -825,7 +844,7 @@ __global__ void __launch_bounds__(kThreads) recurrence_step_kernel(StepArgs p) {
 
 // ------------------------------------------------------------------------------------------------ host side
 template <class T, int D>
-constexpr int tile_lds(int tiles) { return tiles * Tile<T, D>::kBytes + 2 * Tile<T, D>::kHeads * (int)sizeof(Gates) + 6 * Tile<T, D>::kWaves * 4; }
+constexpr int tile_lds(int tiles) { return tiles * Tile<T, D>::kBytes + 2 * Tile<T, D>::kHeads * (int)sizeof(Gates) + 6 * Tile<T, D>::kWaves * Tile<T, D>::kHeads * 4; }
 template <class T, int D>
 constexpr int sweep_lds() { return tile_lds<T, D>(3) + kChunk * Tile<T, D>::kWaves * 4 + Tile<T, D>::kScoreBytes; }
 

@@ -181,8 +181,8 @@ struct Tile {
         return __builtin_bit_cast(u32x4, positive - __builtin_elementwise_sub_sat(__builtin_bit_cast(Unsigned, v), infinite));
     }
 
-    // into LDS, rectified where asked; returns the largest bit pattern of a finite magnitude (fp16 alone; a value that is not finite may
-    // not spoil the other heads' normalisers)
+    // into LDS, rectified where asked; returns the largest bit pattern of a finite magnitude of this lane's pieces (fp16 alone; one that is not
+    // finite bounds nothing, and would take the rest of its head along)
     static __device__ __forceinline__ unsigned store(Regs& r, char* tile, int relu, int t) {
         unsigned top = 0;
         if (relu) {

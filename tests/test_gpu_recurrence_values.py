@@ -3,6 +3,8 @@ import numpy as np
 import pytest
 import torch
 
+import test_gpu_recurrence as base
+from oracle import sequence_oracle as so
 from paper_2205_14756_amd import sequence as seq
 
 pytestmark = pytest.mark.gpu
@@ -130,3 +132,39 @@ def test_a_rectified_nan_stays_one(dtype, which, operand):
     hit[at, head] = True
     assert bool(torch.isnan(got[hit].float()).all()) and torch.equal(got[~hit], one[~hit])
     assert bool(torch.isnan(after[at, head, 5]).all()) if operand == "k" else torch.equal(after, states)
+
+
+# sizes of q, k, v, d_out of every other head and of the heads between: results are not lost in fp16's smallest steps
+HEAD_SIZES = [((100.0, 100.0, 1e-3, 1.0), (1e-2, 1e-2, 300.0, 50.0)), ((1e-2, 1.0, 1e4, 1e-2), (30.0, 30.0, 1e-4, 1.0))]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [16, 32, 64])
+@pytest.mark.parametrize("group", [1, 2])
+@pytest.mark.parametrize("sizes", HEAD_SIZES)
+@pytest.mark.parametrize("tokens", [150, 700])
+def test_heads_of_different_size_side_by_side(dtype, d, group, sizes, tokens):
+    """A head's precision is its own: each within the tolerance of its own terms (base.close), whatever its neighbours' sizes."""
+    hkv, scale = 5, 0.02
+    t = base.make(31, dtype, tokens, hkv * group, hkv, d, [tokens], initial=False)
+    for i, n in enumerate(("q", "k", "v", "d_out")):
+        heads = t[n].shape[1] // hkv
+        size = torch.tensor([sizes[h % 2][i] for h in range(hkv) for _ in range(heads if n in ("q", "d_out") else 1)], device="cuda")
+        t[n] = (t[n].float() * size[:, None]).to(TDT[dtype])
+    args = [base.f64(t[n]) for n in ("q", "k", "v", "gate")] + [[(0, tokens)]]
+    mag = [np.abs(a) for a in args[:3]] + args[3:]
+    print(f"heads of different size {dtype} d={d} group={group} tokens={tokens}", flush=True)
+    out, state = seq.msla_recurrence_forward(t["q"], t["k"], t["v"], t["gate"], scale=scale)
+    want, last = so.recurrence(*args, None, scale)
+    size, size_last = so.recurrence(*mag, None, scale)
+    base.close(out, want, size, dtype, "out")
+    base.close(state, last, size_last, dtype, "state", base.STATE, half=False)
+    got = seq.msla_recurrence_backward(t["q"], t["k"], t["v"], t["d_out"], t["gate"], scale=scale)
+    ref = so.recurrence_backward(*args, None, scale, base.f64(t["d_out"]))
+    m, _ = base.gate_magnitudes(t, [(0, tokens)], scale, False)
+    for i, name in enumerate(("d_q", "d_k", "d_v")):
+        # (some of the large head's d_v, sums of 10^4 * sqrt(d) * scale over the tokens, are above fp16's 65504; a result is an infinity from 65520 on)
+        fits = np.abs(ref[i]) < 65504 * (1 - 2.0 ** -10) if dtype == "f16" else np.ones(ref[i].shape, bool)
+        beyond = np.abs(ref[i]) > 65520 * (1 + 2.0 ** -10) if dtype == "f16" else ~fits
+        assert np.isinf(base.f64(got[i])[beyond]).all()
+        base.close(got[i][torch.from_numpy(fits).cuda()], ref[i][fits], m[i][fits], dtype, name)
