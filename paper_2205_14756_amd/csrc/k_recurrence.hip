@@ -244,7 +244,8 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
 
     State<T, D> state;
     state.clear();
-    float exponent = 0.0f, unit = 1.0f;
+    double exponent = 0.0;          // (a segment may have thousands of chunks, whose equal small exponents add up in fp32 with a drift)
+    float unit = 1.0f;
     typename Ti::Regs rb, rc;
     const int gate_wave = Ti::kWaves - 1 - wave;        // the last waves have the fewest scores to compute
     GateRows<T> gate_rows(p.gate, p.gate_ts, seg, p.reverse, head0 + gate_wave, p.heads);
@@ -298,7 +299,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         }
         if (sub == 0) {
             factor *= gt.total;
-            exponent += gt.exponent;
+            exponent += (double)gt.exponent;
             if constexpr (!Ti::kNormalise) unit = gt.unit;
         }
         if (factor != 1.0f) state.scale(factor);
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     if (head >= p.heads) return;
     const long at = (long)seg.slot * p.heads + head;
     state.write(p.own + at * (D * D), slice, p.rs, Ti::kNormalise ? 1.0f / unit : unit);
-    if (lane == 0 && slice == 0) p.decay[at] = __builtin_amdgcn_exp2f(exponent);
+    if (lane == 0 && slice == 0) p.decay[at] = __builtin_amdgcn_exp2f((float)exponent);
 }
 
 // own[slot] (what a segment adds) becomes the state that the segment starts from, in the order of the scan.  Eight segments are read

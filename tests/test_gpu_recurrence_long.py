@@ -116,3 +116,24 @@ def test_values_far_from_one_over_many_chunks(dtype, exponent, d):
     if hkv == 1:
         t["gate"][::2] *= -0.25         # (some above 0)
     compare(dtype, t, seqs, length, 1, 0.01, [3, 200], list(range(hkv)), backward=False)
+
+
+def test_a_state_that_is_forgotten_slowly():
+    """2^24 tokens that add nothing, and a gate that leaves e^-8.8 of the state in all: 128 segments of 2048 chunks.  A segment's decay is the
+    exponential of its gates' sum (one step of fp32, 2^-23, and half a step of its argument, below 0.1), and the join multiplies (half a step):
+    2^-22 a segment at most, 2^-15 in all."""
+    tokens, h, d = 2 ** 24, 16, 16
+    rate = -141 / 128 * 2.0 ** -21              # (bf16 has it)
+    slots = seq.msla_recurrence_workspace_bytes(1, tokens, h, h, d, torch.bfloat16) / (h * (d * d + 1) * 4)
+    assert slots <= tokens / (64 * 1024) + 2, slots
+    none = torch.zeros(1, 1, d, dtype=torch.bfloat16, device="cuda").expand(tokens, h, d)
+    gate = torch.full((1, h), rate, dtype=torch.bfloat16, device="cuda").expand(tokens, h)
+    assert float(gate[0, 0]) == rate
+    first = torch.randn(1, h, d, d, device="cuda")
+    out = torch.empty(tokens, h, d, dtype=torch.bfloat16, device="cuda")
+    _, last = seq.msla_recurrence_forward(none, none, none, gate, initial_state=first, out=out)
+    want = first.double() * math.exp(tokens * rate)
+    worst = float(((last.double() - want) / want).abs().max())
+    print(f"  {worst:.3g}", flush=True)
+    assert worst <= 2.0 ** -15
+    assert bool((out[::4096] == 0).all())
