@@ -64,7 +64,8 @@ typedef struct {
  *       nothing is forgotten.  At most 0 in earnest; -inf (and anything below -103) forgets all that was.
  *   initial_state, final_state [sequences, heads_kv, head_dim (of k), head_dim (of v)] fp32, either may be NULL; final_state may be
  *       initial_state itself.  A sequence without tokens hands its state on.
- * The state, the sums and the gates' running products are fp32 (or more), a state on the way with up to 2^16 times its value; an
+ * The state, the sums and the gates' running products are fp32 (or more), a state on the way with up to 2^16 times its value (in fp16 with
+ * what takes v to fp16's range, as long as the state stays below 2^100 that way); an
  * operand of a matrix instruction that is not an input goes in as parts of the storage type, three in bf16 and two in fp16, which leave fp32's precision.
  * The workspace hangs on the shape alone, offsets being NULL or not included.
  * A value that is not finite stays within its own sequence and head; there it reaches the tokens behind it and those of its own

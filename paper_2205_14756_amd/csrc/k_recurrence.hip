@@ -245,7 +245,7 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
     State<T, D> state;
     state.clear();
     double exponent = 0.0;          // (a segment may have thousands of chunks, whose equal small exponents add up in fp32 with a drift)
-    float unit = 1.0f;
+    float unit = 1.0f, bound_s = 0.0f;
     typename Ti::Regs rb, rc;
     const int gate_wave = Ti::kWaves - 1 - wave;        // the last waves have the fewest scores to compute
     GateRows<T> gate_rows(p.gate, p.gate_ts, seg, p.reverse, head0 + gate_wave, p.heads);
@@ -290,10 +290,11 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupanc
         }
         const Gates& gt = gates[(first / kChunk & 1) * Ti::kHeads + mine];
         if (sub == 0) gates_of(first + kChunk);
-        float fresh = unit, factor = 1.0f;
+        float factor = 1.0f;
         if constexpr (Ti::kNormalise) {
             const float bound = tile_top<Ti>(top + 2, mine) * fabsf(p.weight_scale) * gt.grow;
-            if (bound > 0.0f) fresh = normaliser(bound);
+            bound_s = (sub == 0 ? bound_s * gt.total : bound_s) + (float)kChunk * 65504.0f * bound;
+            const float fresh = unit_of(bound, bound_s, unit);
             factor = fresh / unit;
             unit = fresh;
         }
@@ -550,13 +551,16 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (MASKED && Tile<T, D>:
                     for (int i = 0; i < 4; ++i) o[i] = Ti::mma(o[i], part[k], va[i]);
                 __builtin_amdgcn_sched_barrier(0);      // (or all steps' operands are read ahead, into registers that are not there)
             }
-            const float all = Ti::kNormalise ? fp / (fs * unit) : 1.0f;
+            const float undo = Ti::kNormalise ? 1.0f / (fs * unit) : 1.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float f = gt.in[16 * i + x];
-                if constexpr (Ti::kNormalise) f *= all;
+                if constexpr (Ti::kNormalise) f *= undo;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[i][r] *= f;
+                for (int r = 0; r < 4; ++r) {
+                    o[i][r] *= f;
+                    if constexpr (Ti::kNormalise) o[i][r] *= fp;        // (f * fp may be above fp32's range where their product with this is not)
+                }
             }
         } else if constexpr (Ti::kNormalise) {
 #pragma unroll
@@ -678,10 +682,10 @@ __global__ void __launch_bounds__((Tile<T, D>::kThreads), (MASKED && Tile<T, D>:
             float factor = 1.0f;
             if constexpr (Ti::kNormalise) {
                 const float bound = ct * fabsf(p.weight_scale) * gt.grow;
-                const float fresh = bound > 0.0f ? normaliser(bound) : unit;
+                bound_s = (new_b && sub > 0 && gb > 1 ? bound_s : bound_s * gt.total) + (float)kChunk * bt * bound;
+                const float fresh = unit_of(bound, bound_s, unit);
                 factor = fresh / unit;
                 unit = fresh;
-                bound_s = (new_b && sub > 0 && gb > 1 ? bound_s : bound_s * gt.total) + (float)kChunk * bt * bound;
             }
             const bool decays = gb == 1 || sub == 0;
             if (decays) factor *= gt.total;

@@ -374,13 +374,19 @@ __device__ __forceinline__ void run_gates(Gates* out, float g, int reverse, floa
     }
 }
 
-// a power of two that takes values up to `bound` to at most 2^15 (fp16's range); 1 where there is no such bound
-__device__ __forceinline__ float normaliser(float bound) {
+// a power of two that takes values up to `bound` to at most 2^top (by default fp16's range); 1 where there is no such bound
+__device__ __forceinline__ float normaliser(float bound, int top = 15) {
     if (!(bound > 0.0f) || !(bound < 3e38f)) return 1.0f;
     int e = (int)(__builtin_bit_cast(unsigned, bound) >> 23) - 126;      // bound < 2^e
-    e = 15 - e;
-    e = e < -100 ? -100 : (e > 100 ? 100 : e);
+    e = top - e;
+    e = e < -120 ? -120 : (e > 100 ? 100 : e);
     return __builtin_bit_cast(float, (unsigned)(e + 127) << 23);
+}
+// What a state of fp16 inputs is multiplied by while it stands in registers: as much as takes what is added next (up to `bound`) to fp16's range,
+// but no more than leaves the state (up to `state`) in fp32's.  `before`: what it is now.
+__device__ __forceinline__ float unit_of(float bound, float state, float before) {
+    const float u = bound > 0.0f ? normaliser(bound) : before;
+    return state * u > 0x1p100f && state < 3e38f ? normaliser(state, 100) : u;
 }
 
 __device__ __forceinline__ float half_bits(unsigned b) { return (float)__builtin_bit_cast(_Float16, (unsigned short)b); }

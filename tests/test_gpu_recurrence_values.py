@@ -168,3 +168,44 @@ def test_heads_of_different_size_side_by_side(dtype, d, group, sizes, tokens):
         beyond = np.abs(ref[i]) > 65520 * (1 + 2.0 ** -10) if dtype == "f16" else ~fits
         assert np.isinf(base.f64(got[i])[beyond]).all()
         base.close(got[i][torch.from_numpy(fits).cuda()], ref[i][fits], m[i][fits], dtype, name)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tokens,group", [(150, 1), (700, 2)])
+@pytest.mark.parametrize("large", [1e30, 1e32])
+def test_small_values_behind_a_large_state(dtype, tokens, group, large):
+    """A state of 1e30 or 1e32 (fp32 has it), values of 1e-4, and a gate that forgets the state at token 100: rows before it see the state times some
+    ten (fp16: an infinity), rows behind it what the values make, and so does the last state.  The gradient likewise from a d_final_state of that size:
+    tokens before 100 know nothing of it.  The short ones run whole, through three chunks, the long ones in segments of one."""
+    hkv, d, reset = 2, 64, 100
+    t = base.make(33, dtype, tokens, hkv * group, hkv, d, [tokens])
+    t["v"] = (t["v"].float() * 1e-4).to(TDT[dtype])
+    t["d_out"] = (t["d_out"].float() * 1e-4).to(TDT[dtype])
+    t["gate"][reset] = -200.0
+    t["first"] *= large
+    t["d_last"] *= large
+    assert (seq.msla_recurrence_workspace_bytes(1, tokens, hkv * group, hkv, d, TDT[dtype]) == 0) == (tokens == 150)
+    spans = [(0, tokens)]
+    args = [base.f64(t[n]) for n in ("q", "k", "v", "gate")] + [spans]
+    mag = [np.abs(a) for a in args[:3]] + args[3:]
+    first, d_last = base.f64(t["first"]), base.f64(t["d_last"])
+    print(f"state of {large} {dtype} tokens={tokens}", flush=True)
+    out, state = seq.msla_recurrence_forward(t["q"], t["k"], t["v"], t["gate"], initial_state=t["first"], scale=1.0)
+    want, last = so.recurrence(*args, first, 1.0)
+    size, size_last = so.recurrence(*mag, np.abs(first), 1.0)
+    base.close(out[reset:], want[reset:], size[reset:], dtype, "out")
+    base.close(state, last, size_last, dtype, "state", base.STATE, half=False)
+    before = base.f64(out[:reset])
+    if dtype == "f16":
+        far = np.abs(want[:reset]) > 2.0 ** 20
+        assert np.isinf(before[far]).all() and not np.isnan(before).any()
+    else:
+        base.close(out[:reset], want[:reset], size[:reset], dtype, "out before")
+    got = seq.msla_recurrence_backward(t["q"], t["k"], t["v"], t["d_out"], t["gate"], d_final_state=t["d_last"], scale=1.0)
+    ref = so.recurrence_backward(*args, None, 1.0, base.f64(t["d_out"]), d_last)
+    m = so.recurrence_backward(*mag, None, 1.0, np.abs(base.f64(t["d_out"])), np.abs(d_last), magnitudes=True)
+    base.close(got[0], ref[0], m[0], dtype, "d_q")
+    for i, name in ((1, "d_k"), (2, "d_v")):
+        base.close(got[i][:reset], ref[i][:reset], m[i][:reset], dtype, name)
+        if dtype != "f16":
+            base.close(got[i][reset:], ref[i][reset:], m[i][reset:], dtype, name + " behind")
