@@ -132,13 +132,14 @@ __global__ void __launch_bounds__(256, 2) linear_quantized_kernel(const unsigned
     }
 }
 
-// Which of the two: by rounds of their workgroups over the 256 compute units.  A round takes, by measurement at 512 .. 8192 channels, 2.7 ns a
-// channel of the contraction here (64 rows, 16 outputs) and 9.8 ns there (128 rows, 128 outputs, one workgroup to a unit): at 4096 channels 11
-// and 40 us.  4096 -> 4096: 64 rows 12 against 43 us, 192 rows 34 against 43, 256 rows 44 against 43; 8192 -> 512: 512 rows 22 against 81.
+// Which of the two: by rounds of their workgroups over the 256 compute units.  By measurement at 512 .. 128000 outputs a round takes, a channel of the
+// contraction, 1.0, 1.45, 1.95 or 2.7 ns here (up to 16, 32, 48, 64 rows, 16 outputs) and 9.8 ns there (128 rows, 128 outputs, one workgroup to a
+// unit).  us here against there, 4096 channels: into 4096 outputs 64 rows 13 against 43, 192 rows 34 against 43, 256 rows 44 against 43; into 16000
+// 48 rows 32 against 43; into 32000 16 rows 33 against 42, 17 rows 36 against 42 (taken for 45), 32 rows 45 against 43, 48 rows 60 against 44; into
+// 128000 16 rows 124 against 135, 48 rows 248 against 140.
 bool rows_kernel_wins(int64_t rows, int c_out) {
-    if (rows <= 48) return true;
     const int64_t here = ((rows + 63) / 64 * (c_out / 16) + 255) / 256, there = ((rows + 127) / 128 * ((c_out + 127) / 128) + 255) / 256;
-    return here * 27 < there * 98;
+    return here * (rows <= 16 ? 100 : (rows <= 32 ? 145 : (rows <= 48 ? 195 : 270))) < there * 980;
 }
 
 // Few rows: the weights are read once and that is what there is to do, so a workgroup has 16 outputs, its eight waves take 128 bytes of the
