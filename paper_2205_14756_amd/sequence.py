@@ -287,20 +287,20 @@ def msla_recurrence_step(q, k, v, state, log_gate=None, scale=None, rectify=Fals
     return out, new_state
 
 
-def _norm_arguments(x, weight, residual, total):
+def _norm_arguments(x, weight, residual, total, names=("x", "residual", "sum_out")):
     _on_gpu(x, weight, residual, total)
     if not (x.dtype in _DTYPES):
         _refuse(f"{x.dtype} is not a storage type")
     if not (x.dim() >= 1 and x.is_contiguous()):
-        _refuse("x must be contiguous rows")
+        _refuse(f"{names[0]} must be contiguous rows")
     shape = x.shape
     channels = shape[-1]
     if weight is not None:
         _plain(weight, "weight", (channels,), x.dtype)
     if residual is not None:
-        _plain(residual, "residual", shape, x.dtype)
+        _plain(residual, names[1], shape, x.dtype)
     if total is not None:
-        _plain(total, "sum_out", shape, x.dtype)
+        _plain(total, names[2], shape, x.dtype)
     return x.numel() // channels if channels else 0, channels
 
 
@@ -364,7 +364,7 @@ def msla_norm_backward_workspace_bytes(rows, channels, dtype) -> int:
 def msla_norm_backward(r, weight, d_y, d_sum=None, eps=1e-6, d_r=None, d_weight=None, workspace=None, stream=None):
     """(d_r, d_weight): the gradient of msla_norm_forward at r (what it returned); d_sum: the gradient that reaches r past the norm.
     d_r is that of x and of residual alike; d_weight is fp32."""
-    rows, channels = _norm_arguments(r, weight, d_y, d_sum)
+    rows, channels = _norm_arguments(r, weight, d_y, d_sum, ("r", "d_y", "d_sum"))
     _on_gpu(d_r, d_weight, workspace)
     _plain(d_r, "d_r", r.shape, r.dtype)
     _plain(d_weight, "d_weight", (channels,), torch.float32)
