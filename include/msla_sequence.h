@@ -45,7 +45,7 @@ typedef struct {
  * rows before offsets[0] and from offsets[sequences] on belong to none and are neither read nor written.  (The array is on the device,
  * so it is not checked: entries that fall or lie outside leave results undefined, but nothing outside of the buffers is touched.)
  * heads_q query heads share heads_kv states, heads_q / heads_kv (a whole number) neighbours each.
- * head_dim is 16, 32, 64 or 128, of keys and of values.  tokens below 2^31, sequences * heads_kv below 2^22, heads_q <= 32768. */
+ * head_dim is 16, 32, 64 or 128, of keys and of values.  tokens below 2^31 - 64, sequences * heads_kv below 2^22, heads_q <= 32768. */
 typedef struct {
     int sequences;
     int64_t tokens;
@@ -65,8 +65,9 @@ typedef struct {
  *   initial_state, final_state [sequences, heads_kv, head_dim (of k), head_dim (of v)] fp32, either may be NULL; final_state may be
  *       initial_state itself.  A sequence without tokens hands its state on.
  * The state, the sums and the gates' running products are fp32 (or more), a state on the way with up to 2^16 times its value (in fp16 with
- * what takes v to fp16's range, as long as the state stays below 2^100 that way); an
- * operand of a matrix instruction that is not an input goes in as parts of the storage type, three in bf16 and two in fp16, which leave fp32's precision.
+ * what takes v to fp16's range, as long as the state stays below 2^100 that way); an operand of a matrix instruction that is not an
+ * input goes in as parts of the storage type, three in bf16 and two in fp16, which leave fp32's precision.  (fp16's range: a score is
+ * held to 2^-39 of the largest that its head's q and k of a chunk of 64 tokens could make, an addend of the state to 2^-39 of the chunk's largest.)
  * The workspace hangs on the shape alone, offsets being NULL or not included.
  * A value that is not finite stays within its own sequence and head; there it reaches the tokens behind it and those of its own
  * chunk of 64 tokens before it. */
@@ -79,6 +80,8 @@ msla_status msla_recurrence_forward(const msla_recurrence* shape, msla_heads q, 
 /* The gradient of msla_recurrence_forward: from d_out (like out) and d_final_state (NULL: zero) to d_q, d_k, d_v (like q, k, v; sums
  * over the query heads of a state), d_log_gate [tokens, heads_kv] in the storage type (rows d_gate_stride apart; NULL: not wanted) and
  * d_initial_state (NULL: not wanted).  The rectifier's derivative is 0 at 0 and at a NaN.  Nothing of the forward call is needed but its inputs.
+ * d_log_gate of a token is the sum of q . d_q - k . d_k from it to a later border of segments, and <d_state, state> there, in fp32 products: its error
+ * goes by those terms' magnitudes, also where a gate that forgets everything makes the sum itself small.
  * d_initial_state may be neither d_final_state nor initial_state. */
 msla_status msla_recurrence_backward(const msla_recurrence* shape, msla_heads q, msla_heads k, msla_heads v,
                                      const void* log_gate, int64_t gate_stride, const float* initial_state,

@@ -1,8 +1,8 @@
 // The 1x1 projection of rows in 8 bits (e4m3): y[n, o] = x_scale[n] w_scale[o] sum_c x8[n, c] w8[o, c].
 //
 // What 8 bits save here is memory; the products run on the fp16 matrix instructions, at the rate that 16x16x32 has for e4m3 as well.  The e4m3
-// form was measured first: its sums keep some 14 bits of their terms' magnitudes (errors of 2^-14.5 of sum |x w| at 16 channels), where fp16
-// operands, which hold every e4m3 value, leave exact products and fp32 sums.  A lane's 16 bytes of a row make two operands, the low and the
+// form was measured first: its sums keep some 14 bits of their terms' magnitudes (a million sums of 32 normal products: errors up to 2^-13.5 of
+// sum |x w|, where fp16 operands, which hold every e4m3 value, leave exact products and fp32 sums, 2^-24.4).  A lane's 16 bytes of a row make two operands, the low and the
 // high eight contraction slots, so both sides are read 16 bytes a lane in memory order.
 #include "msla_device.h"
 #include "msla_sequence_kernels.h"
@@ -53,8 +53,8 @@ __device__ __forceinline__ void store8(T* p, const f32x4& a, const f32x4& b) {
 // A workgroup has 128 rows x 128 outputs, a wave 64 x 64.  Tiles lie in LDS as rows of 128 bytes whose 16-byte pieces are XORed with the
 // row's number modulo 8, which gives the eight rows that a read serves together all banks.  Outputs are the rows of the matrix
 // instructions, dealt to pairs of blocks so that a lane ends up with eight neighbours of a row of y.
-// 4096 rows, 4096 -> 8192: 250 us, 1.1 PFLOP/s of the 1.4 that a large bf16 product reaches: bound by issue, the conversions of eight
-// operands for sixteen products of two instructions.  256 x 256 tiles: 8% less here, more where the grid is small.
+// 4096 rows, 4096 -> 8192: 250 us (after some 80 launches in a row; 300 for the first ones behind an idle GPU), 1.1 PFLOP/s of the 1.4 that a large
+// bf16 product reaches: bound by issue, the conversions of eight operands for sixteen products of two instructions.  256 x 256 tiles: 8% less here, more where the grid is small.
 template <class T>
 __global__ void __launch_bounds__(256, 2) linear_quantized_kernel(const unsigned char* x8, const float* x_scale, const unsigned char* w8,
                                                                   const float* w_scale, T* y, int64_t rows, int c_in, int c_out, int tiles_o) {

@@ -215,7 +215,7 @@ __device__ __forceinline__ float over_column(float v) {
 }
 
 // Passes that do not wait for each other go into one launch, by blockIdx.z: of few tokens none fills the GPU (the gradient of 320 tokens and 8
-// heads of 64: 39 -> 29 us; of 4 x 4096 and 16 of 128: 437 -> 407).  One alone is 2% faster when it need not look which it is.
+// heads of 64: 39 -> 29 us; of 4 x 4096 and 16 of 128: 459 -> 410).  One alone is 2% faster when it need not look which it is.
 template <class A, int N>
 struct Calls {
     A call[N];
@@ -223,7 +223,7 @@ struct Calls {
 };
 
 // What a segment adds to the state, and the product of its gates.  A sweep without scores and outputs: 16384 tokens of 16 heads of 128 in bf16
-// 38 us, 134 MB of keys and values and 38 MB of states at 4.5 TB/s.
+// 34 us, 134 MB of keys and values and 38 MB of states at 5.1 TB/s.
 template <class T, int D, int N>
 __global__ void __launch_bounds__((Tile<T, D>::kThreads), (Tile<T, D>::kOccupancy)) recurrence_state_kernel(Calls<StateArgs, N> calls) {
     const StateArgs& p = calls.mine();
@@ -384,8 +384,10 @@ __device__ __forceinline__ F load_through(BufRsrc r, unsigned off, unsigned scal
 // One of the scan's passes over a segment.  The tiles of the next chunk are on their way while this one's scores, outputs and state are
 // computed; a wave has 16 output channels, so that the state (d rows of them) stays in its registers, and where four or more waves make a
 // head each computes its share of the scores and all meet in LDS.
-// 16384 tokens of 16 heads of 128 in bf16: 87 us (273 MB: 3.1 TB/s), with the masks and dot products 100.  Bound by issue: a wave's chunk is some
-// 570 vector and 97 matrix instructions; the loop with nothing but its loads, LDS traffic and barriers takes 42 us.
+// 16384 tokens of 16 heads of 128 in bf16: 92 us (273 MB: 3.0 TB/s), with the masks and dot products 98.  No one unit is at its limit: of the cycles
+// in which a compute unit holds waves the vector ALU is busy 57 % (some 690 instructions a wave and chunk), the matrix pipe 40 % (119), LDS 37 %; a
+// wave spends 41 % of its time waiting for its turn to issue and 34 % for memory, LDS or a barrier.  The loop with nothing but its loads, LDS traffic
+// and barriers takes 42 us.
 // MASKED: out is masked and measured against m (p.m, p.dots).  GROUP: there are several heads of a, or of (b, c), to a state head.
 template <class T, int D, bool MASKED, bool GROUP, int N>
 __global__ void __launch_bounds__((Tile<T, D>::kThreads), (MASKED && Tile<T, D>::kWide16 ? 2 : Tile<T, D>::kOccupancy)) recurrence_sweep_kernel(Calls<SweepArgs, N> calls) {

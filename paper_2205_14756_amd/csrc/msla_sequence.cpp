@@ -27,8 +27,9 @@ msla_status status_of(hipError_t e) { return e == hipSuccess ? MSLA_OK : MSLA_ER
 constexpr int64_t kWantGroups = 512;
 // Steps of 64 tokens and a head that a workgroup may take in a row before a sequence is cut at all: the pass that sums segments, the one
 // that joins them and their launches cost about what these do.  One sequence, 8 heads of 64 in bf16, us replayed (called one by one), cut against
-// whole: forward, 4 steps 13.7 (22.8) against 14.9 (15.0), 8 steps 14.6 (23.1) against 25.6 (25.8); the gradient, whose three sweeps repay
-// the extra launches sooner, 4 steps 39 (48) against 49 (50).
+// whole: forward, 3 steps 12.9 (15.7) against 11.8 (12.2), 4 steps 13.2 (15.7) against 14.7 (15.2), 5 steps 13.4 (15.8) against 17.5 (18.0), 8 steps
+// 14.1 (15.9) against 25.9 (26.4); the gradient, whose three sweeps repay the extra launches sooner, 2 steps 26.9 (29.0) against 22.9 (24.2), 3 steps
+// 26.8 (29.0) against 29.7 (30.6) but 16 heads of 128 47.1 (49.3) against 38.8 (39.7), 4 steps 28.4 (30.2) against 36.5 (37.6).
 constexpr int64_t kUncutSteps = 4, kUncutStepsBackward = 3;
 
 // A launch has fewer than 2^32 threads; the step takes 1024 for a state of 128 x 128, the scan's kernels no more than 512 for one.
