@@ -6,6 +6,10 @@
  *   msla_norm_*             root-mean-square norm with the addition of a residual, its gradient, and with rows of 8 bits out
  *   msla_quantize_rows      rows of 8 bits out of a map as it is (weights)
  *   msla_linear_quantized   the 1x1 projection of such rows
+ *   msla_selective_scan_*   a scan whose states decay each at their own rate: forward, backward, and one token a sequence
+ *   msla_causal_conv_*      the short causal convolution of each channel in front of it: forward, backward, and one token a sequence
+ *   msla_layer_norm_*       layer norm with the addition of a residual, and its gradient
+ *   msla_quantize_rows_integer, msla_linear_integer   rows in 8-bit integers and their projection
  *
  * General rules: those of msla.h.  Device pointers, 16-byte aligned unless a line below says otherwise; the caller owns every
  * buffer; nothing is allocated; work is enqueued on `stream` and the call returns; every argument is checked on the host before the
@@ -125,6 +129,103 @@ msla_status msla_quantize_rows(const void* x, void* x8, float* scale, int64_t ro
  * c_in, c_out multiples of 16 and at most 2^20, rows below 2^31.  Products are exact, sums fp32. */
 msla_status msla_linear_quantized(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows, int c_in,
                                   int c_out, msla_dtype dt, void* stream);
+
+/* ---- A selective state space layer: the scan, the convolution in front of it, layer norm, and the projection in 8-bit integers. ---- */
+
+/* [token, channel] in the storage type: channels next to each other, rows token_stride elements apart (not negative), aligned to an element.  So
+ * channels may be part of a wider row.  An input's stride may be 0 (one row for all tokens); an output's rows must not overlap each other. */
+typedef struct {
+    void* data;                 /* read only where the operand is an input */
+    int64_t token_stride;
+} msla_rows;
+
+/* What the scan runs over: sequences, tokens and offsets as in msla_recurrence (tokens below 2^31 - 4096).  channels <= 2^20, in `groups` (a divisor) of
+ * neighbours that share b and c; states of a channel: 8, 16, 32 or 64. */
+typedef struct {
+    int sequences;
+    int64_t tokens;
+    const int32_t* offsets;
+    int channels, groups, states;
+    int softplus;               /* 1: a token's step is softplus(delta + delta_bias) = log(1 + exp(.)); 0: delta + delta_bias as it is */
+} msla_selective_scan;
+
+/* For every sequence, channel and state n of it, with t_i the step of token i and g the channel's group:
+ *     h_i[n] = exp(t_i a[n]) h_{i-1}[n] + t_i x_i b_i[g, n]        y_i = sum_n c_i[g, n] h_i[n] + skip x_i        out_i = y_i silu(gate_i)
+ *   x, delta, gate, out [tokens, channels]; gate.data may be NULL (out = y);  b, c [tokens, groups, states] (a row: groups * states next to each other)
+ *   a [channels, states] fp32, negative in earnest (a decay exp(t a) below fp32's normal range is 0);  skip, delta_bias [channels] fp32 or NULL (0)
+ *   initial_state, final_state [sequences, channels, states] fp32, either may be NULL; final_state may be initial_state itself.  A sequence without tokens
+ *       hands its state on.
+ * States, steps and sums are fp32; a, skip, delta_bias and states are aligned to 4 bytes.  The workspace hangs on the shape alone, offsets being NULL
+ * or not included.  A value that is not finite stays within its sequence and channel (one in b or c: its group), and reaches no token before its own. */
+msla_status msla_selective_scan_workspace_bytes(const msla_selective_scan* shape, int backward, msla_dtype dt, size_t* bytes);
+msla_status msla_selective_scan_forward(const msla_selective_scan* shape, msla_rows x, msla_rows delta, const float* a, msla_rows b, msla_rows c,
+                                        const float* skip, const float* delta_bias, msla_rows gate, const float* initial_state, msla_rows out,
+                                        float* final_state, void* workspace, size_t workspace_bytes, msla_dtype dt, void* stream);
+
+/* The gradient of msla_selective_scan_forward: from d_out (like out) and d_final_state (NULL: zero) to d_x, d_delta, d_gate (like x; d_gate where there is a
+ * gate, and only there), d_b, d_c (like b; sums over a group's channels), and in fp32 d_a [channels, states], d_skip, d_delta_bias [channels] (sums over all
+ * tokens; each may be NULL: not wanted) and d_initial_state (NULL: not wanted).  Sums over tokens and channels are taken in a fixed order.  Nothing of
+ * the forward call is needed but its inputs.  d_initial_state may be neither d_final_state nor initial_state. */
+msla_status msla_selective_scan_backward(const msla_selective_scan* shape, msla_rows x, msla_rows delta, const float* a, msla_rows b, msla_rows c,
+                                         const float* skip, const float* delta_bias, msla_rows gate, const float* initial_state, msla_rows d_out,
+                                         const float* d_final_state, msla_rows d_x, msla_rows d_delta, float* d_a, msla_rows d_b, msla_rows d_c,
+                                         float* d_skip, float* d_delta_bias, msla_rows d_gate, float* d_initial_state, void* workspace,
+                                         size_t workspace_bytes, msla_dtype dt, void* stream);
+
+/* One token for each of shape->sequences sequences (shape->tokens equal to it, offsets NULL), without a workspace.  new_state may be state itself (in
+ * place); it may not overlap it otherwise. */
+msla_status msla_selective_scan_step(const msla_selective_scan* shape, msla_rows x, msla_rows delta, const float* a, msla_rows b, msla_rows c,
+                                     const float* skip, const float* delta_bias, msla_rows gate, const float* state, msla_rows out, float* new_state,
+                                     msla_dtype dt, void* stream);
+
+/* What the convolution runs over: sequences, tokens and offsets as in msla_recurrence (tokens below 2^31 - 4096).  channels <= 2^20; width 2, 3 or 4. */
+typedef struct {
+    int sequences;
+    int64_t tokens;
+    const int32_t* offsets;
+    int channels, width;
+    int silu;                   /* 1: out = pre sigmoid(pre); 0: out = pre */
+} msla_causal_conv;
+
+/* For every sequence and channel: pre_i = bias + sum_k weight[k] x_{i - width + 1 + k}, k = 0 .. width - 1
+ *   x, out [tokens, channels];  weight [channels, width], bias [channels] or NULL (0) in the storage type
+ *   initial_state [sequences, width - 1, channels] in the storage type: the rows in front of each sequence's first, oldest first (NULL: zeros);
+ *   final_state the same behind its last (NULL: not wanted; not initial_state itself).  A sequence without tokens hands its state on.
+ * Sums are fp32; states, weight and bias are aligned to an element. */
+msla_status msla_causal_conv_forward(const msla_causal_conv* shape, msla_rows x, const void* weight, const void* bias, const void* initial_state,
+                                     msla_rows out, void* final_state, msla_dtype dt, void* stream);
+
+/* Its gradient: from d_out and d_final_state (NULL: zero) to d_x, d_initial_state (in the storage type; NULL: not wanted), and d_weight [channels, width]
+ * and d_bias [channels] fp32 (either NULL: not wanted), sums over all tokens in a fixed order; workspace: for these two alone.  d_initial_state may be neither
+ * d_final_state nor initial_state. */
+msla_status msla_causal_conv_backward_workspace_bytes(const msla_causal_conv* shape, msla_dtype dt, size_t* bytes);
+msla_status msla_causal_conv_backward(const msla_causal_conv* shape, msla_rows x, const void* weight, const void* bias, const void* initial_state,
+                                      msla_rows d_out, const void* d_final_state, msla_rows d_x, float* d_weight, float* d_bias,
+                                      void* d_initial_state, void* workspace, size_t workspace_bytes, msla_dtype dt, void* stream);
+
+/* One token for each of shape->sequences sequences (shape->tokens equal to it, offsets NULL).  new_state may be state itself (in place). */
+msla_status msla_causal_conv_step(const msla_causal_conv* shape, msla_rows x, const void* weight, const void* bias, const void* state, msla_rows out,
+                                  void* new_state, msla_dtype dt, void* stream);
+
+/* Layer norm of rows, with the residual's addition:
+ *     r = x + residual        y = (r - mean(r)) / sqrt(mean((r - mean(r))^2) + eps) * weight + bias
+ * Operands, overlaps and limits as of msla_norm_forward; weight and bias [channels] in the storage type, either may be NULL (ones; zeros). */
+msla_status msla_layer_norm_forward(const void* x, const void* residual, const void* weight, const void* bias, void* y, void* sum, int64_t rows,
+                                    int channels, float eps, msla_dtype dt, void* stream);
+
+/* Its gradient at r = `sum`, as msla_norm_backward's, with d_bias [channels] fp32 (NULL: not wanted).  workspace: for d_weight and d_bias alone. */
+msla_status msla_layer_norm_backward_workspace_bytes(int64_t rows, int channels, msla_dtype dt, size_t* bytes);
+msla_status msla_layer_norm_backward(const void* sum, const void* weight, const void* d_y, const void* d_sum, void* d_r, float* d_weight, float* d_bias,
+                                     void* workspace, size_t workspace_bytes, int64_t rows, int channels, float eps, msla_dtype dt, void* stream);
+
+/* Rows in 8-bit integers: scale [rows] fp32 = max |x| / 127, x8 [rows, channels] = x / scale to the nearest whole number, ties to even (both quotients as
+ * IEEE rounds them; a row whose scale is 0 or not finite: zeros).  channels <= 32768, rows below 2^31; x is aligned to an element. */
+msla_status msla_quantize_rows_integer(const void* x, void* x8, float* scale, int64_t rows, int channels, msla_dtype dt, void* stream);
+
+/* y[n, o] = x_scale[n] * w_scale[o] * sum_c x8[n, c] w8[o, c]: msla_linear_quantized of 8-bit integers (-128 to 127).  Sums are exact.  c_in, c_out
+ * multiples of 16, c_in below 131072, c_out at most 2^20, rows below 2^31. */
+msla_status msla_linear_integer(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows, int c_in, int c_out,
+                                msla_dtype dt, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,365 @@
+// Layer norm of rows with the residual's addition, its gradient, and rows into 8-bit integers with a scale a row.
+//
+// Bound by memory, like the root-mean-square norm, whose pieces and lanes it has: a row is read once, stays in registers as fp32 through its mean and
+// then the squares of what is left, and is written once.  (Two reductions a row: the squares less the mean's would lose what a mean that is
+// large beside the deviations costs.)
+#include "msla_device.h"
+#include "msla_layer_kernels.h"
+#include "msla_sequence_kernels.h"
+#include "norm_rows.h"
+
+namespace msla {
+namespace {
+
+constexpr float kTop = 127.0f;
+
+// whether channel e of a lane's piece counts: within the row, and not in the piece before as well
+template <int VEC>
+__device__ __forceinline__ bool counts(const Piece<VEC>& pc, int e, int channels) { return pc.live && e >= pc.skip && pc.at + e < channels; }
+
+template <class T, int LPR, int PER>
+__global__ void __launch_bounds__(LPR > 256 ? LPR : 256) layer_norm_kernel(const T* x, const T* residual, const T* weight, const T* bias, T* y, T* sum,
+                                                                           int64_t rows, int channels, float eps) {
+    constexpr int kVec = Traits<T>::kVec, kThreads = LPR > 256 ? LPR : 256, kRows = kThreads / LPR;
+    __shared__ float room[kThreads / 64];
+    const int lane = threadIdx.x % LPR;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR;
+    const bool live = row < rows;
+    const int64_t base = (live ? row : 0) * channels;
+    auto add = [](float a, float b) { return a + b; };
+    float r[PER][kVec];
+    float total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const Piece<kVec> pc(lane + i * LPR, channels);
+        if (live && pc.live) {
+            load_row<T>(x + base, pc.at, channels, r[i]);
+            if (residual != nullptr) {
+                float f[kVec];
+                load_row<T>(residual + base, pc.at, channels, f);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) r[i][e] += f[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) r[i][e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) total += e < pc.skip ? 0.0f : r[i][e];
+    }
+    const float mean = over_row<LPR>(total, room, add) / (float)channels;
+    float squares = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const Piece<kVec> pc(lane + i * LPR, channels);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            const float d = r[i][e] - mean;
+            squares += counts(pc, e, channels) ? d * d : 0.0f;
+        }
+    }
+    squares = over_row<LPR>(squares, room, add);
+    // (only now that the whole row has been read: sum may lie on x or residual, and the last piece shares channels with another lane's)
+    if (sum != nullptr) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const Piece<kVec> pc(lane + i * LPR, channels);
+            if (live && pc.live) store_row<T>(sum + base, pc.at, channels, r[i]);
+        }
+    }
+    const float rstd = 1.0f / sqrtf(squares / (float)channels + eps);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const Piece<kVec> pc(lane + i * LPR, channels);
+        if (!live || !pc.live) continue;
+        float w[kVec], b[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) w[e] = 1.0f, b[e] = 0.0f;
+        if (weight != nullptr) load_row<T>(weight, pc.at, channels, w);
+        if (bias != nullptr) load_row<T>(bias, pc.at, channels, b);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) r[i][e] = fmaf((r[i][e] - mean) * rstd, w[e], b[e]);
+        store_row<T>(y + base, pc.at, channels, r[i]);
+    }
+}
+
+// A workgroup walks over rows; a lane has the same channels of each, so it sums their parts of d_weight and d_bias in registers.  The next row is on
+// its way while this one is reduced.
+template <class T, int LPR, int PER>
+__global__ void __launch_bounds__(LPR > 256 ? LPR : 256) layer_norm_backward_kernel(const T* sum, const T* weight, const T* d_y, const T* d_sum, T* d_r,
+                                                                                    float* parts, int64_t rows, int channels, float eps) {
+    constexpr int kVec = Traits<T>::kVec, kThreads = LPR > 256 ? LPR : 256, kRows = kThreads / LPR;
+    typedef typename Traits<T>::Vec Vec;
+    __shared__ f32x2 room[2][2][kThreads / 64];
+    __shared__ float groups[kRows > 1 ? kThreads * PER * kVec : 1];
+    const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
+    const Vec zero = {};
+    // Rows of up to two pieces a lane stay in registers, and the next one is asked for before this one is reduced; longer ones, and the weight,
+    // are read again (out of L2) for each pass.
+    constexpr bool kHold = LPR < 1024 ? PER <= 2 : PER == 1;
+    float dw[PER][kVec], db[PER][kVec];
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) dw[i][e] = db[i][e] = 0.0f;
+    auto weight_of = [&](int i) {
+        const Piece<kVec> pc(lane + i * LPR, channels);
+        Vec v;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = Traits<T>::from_f32(1.0f);
+        if (weight != nullptr && pc.live) v = load_raw<T>(weight, pc.at, channels);
+        return v;
+    };
+    Vec kept[kHold ? PER : 1];
+    if constexpr (kHold) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) kept[i] = weight_of(i);
+    }
+    struct Row { Vec r[kHold ? PER : 1], g[kHold ? PER : 1], past[kHold ? PER : 1]; };
+    auto read = [&](int64_t row, int i, Vec& r, Vec& g, Vec& past) {
+        const Piece<kVec> pc(lane + i * LPR, channels);
+        r = g = past = zero;
+        if (row < rows && pc.live) {
+            r = load_raw<T>(sum + row * channels, pc.at, channels);
+            g = load_raw<T>(d_y + row * channels, pc.at, channels);
+            if (d_sum != nullptr) past = load_raw<T>(d_sum + row * channels, pc.at, channels);
+        }
+    };
+    auto fetch = [&](Row& to, int64_t row) {
+        if constexpr (kHold) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) read(row, i, to.r[i], to.g[i], to.past[i]);
+        }
+    };
+    auto step = [&](const Row& now, int64_t row, int turn) {
+        auto piece = [&](int i, Vec& r, Vec& g, Vec& past, Vec& w) {
+            if constexpr (kHold) r = now.r[i], g = now.g[i], past = now.past[i], w = kept[i];
+            else read(row, i, r, g, past), w = weight_of(i);
+        };
+        float total = 0.0f, pull = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const Piece<kVec> pc(lane + i * LPR, channels);
+            Vec r, g, past, w;
+            piece(i, r, g, past, w);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                total += e < pc.skip ? 0.0f : Traits<T>::to_f32(r[e]);
+                pull += e < pc.skip ? 0.0f : Traits<T>::to_f32(w[e]) * Traits<T>::to_f32(g[e]);
+            }
+        }
+        sum_row<LPR>(total, pull, room[turn][0]);
+        const float mean = total / (float)channels;
+        pull = pull / (float)channels;
+        float squares = 0.0f, along = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const Piece<kVec> pc(lane + i * LPR, channels);
+            Vec r, g, past, w;
+            piece(i, r, g, past, w);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                const float d = counts(pc, e, channels) ? Traits<T>::to_f32(r[e]) - mean : 0.0f;
+                squares = fmaf(d, d, squares);
+                along = fmaf(d * Traits<T>::to_f32(w[e]), Traits<T>::to_f32(g[e]), along);
+            }
+        }
+        sum_row<LPR>(squares, along, room[turn][1]);
+        const float rstd = 1.0f / sqrtf(squares / (float)channels + eps);
+        const float back = along * rstd * rstd / (float)channels;       // of the deviation, in units of rstd
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const Piece<kVec> pc(lane + i * LPR, channels);
+            Vec r, g, past, w;
+            piece(i, r, g, past, w);
+            if (row >= rows || !pc.live) continue;
+            float d[kVec];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                const float df = Traits<T>::to_f32(r[e]) - mean, gf = Traits<T>::to_f32(g[e]);
+                dw[i][e] = fmaf(gf, df * rstd, dw[i][e]);
+                db[i][e] += gf;
+                d[e] = fmaf(rstd, fmaf(Traits<T>::to_f32(w[e]), gf, -pull) - df * back, Traits<T>::to_f32(past[e]));
+            }
+            if (kHold || pc.skip == 0) {
+                store_row<T>(d_r + row * channels, pc.at, channels, d);
+            } else {
+                // (d_r may be d_y, and what the lane before has stored there was read again here: its own channels alone)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e)
+                    if (e >= pc.skip) d_r[row * channels + pc.at + e] = Traits<T>::from_f32(d[e]);
+            }
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * kRows + group;
+    const int64_t last = rows + group, stride = (int64_t)gridDim.x * kRows;     // (all of a workgroup's rows pass `last` in the same step)
+    Row here, there;
+    fetch(here, row);
+    for (; row < last; row += 2 * stride) {
+        fetch(there, row + stride);
+        step(here, row, 0);
+        if (row + stride >= last) break;
+        fetch(here, row + 2 * stride);
+        step(there, row + stride, 1);
+    }
+    if (parts == nullptr) return;
+    auto leave = [&](float* out, const float (&d)[PER][kVec]) {
+        if constexpr (kRows > 1) {
+            // (by channel: a piece that starts early leaves out what the one before has)
+            constexpr int kWidth = LPR * PER * kVec;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const Piece<kVec> pc(lane + i * LPR, channels);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e)
+                    if (pc.live && e >= pc.skip) groups[group * kWidth + pc.at + e] = d[i][e];
+            }
+            __syncthreads();
+            for (int c = threadIdx.x; c < channels; c += kThreads) {
+                float s = 0.0f;
+#pragma unroll 4
+                for (int k = 0; k < kRows; ++k) s += groups[k * kWidth + c];
+                out[c] = s;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const Piece<kVec> pc(lane + i * LPR, channels);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e)
+                    if (pc.live && e >= pc.skip && pc.at + e < channels) out[pc.at + e] = d[i][e];
+            }
+        }
+    };
+    leave(parts + (int64_t)blockIdx.x * 2 * channels, dw);
+    leave(parts + (int64_t)blockIdx.x * 2 * channels + channels, db);
+}
+
+// Rows into 8-bit integers: scale = max |x| / 127, x8 = x / scale to the nearest whole number, ties to even; both quotients are rounded as IEEE
+// says, so that the same x gives the same integers everywhere.  A row with a NaN has a NaN for its scale, one with an infinity an infinity, and zeros.
+template <class T, int LPR, int PER>
+__global__ void __launch_bounds__(LPR > 256 ? LPR : 256) quantize_integer_kernel(const T* x, signed char* x8, float* scale, int64_t rows, int channels) {
+    constexpr int kVec = Traits<T>::kVec, kThreads = LPR > 256 ? LPR : 256, kRows = kThreads / LPR;
+    __shared__ float room[kThreads / 64];
+    const int lane = threadIdx.x % LPR;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR;
+    const bool live = row < rows;
+    const int64_t base = (live ? row : 0) * channels;
+    float r[PER][kVec], top = 0.0f;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const Piece<kVec> pc(lane + i * LPR, channels);
+        if (live && pc.live) {
+            load_row<T>(x + base, pc.at, channels, r[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) r[i][e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            top = fmaxf(top, fabsf(r[i][e]));
+            odd |= r[i][e] != r[i][e];
+        }
+    }
+    if (odd) top = __builtin_nanf("");
+    // (a NaN anywhere makes the row's scale one: fmaxf would drop it)
+    top = over_row<LPR>(top, room, [](float a, float b) { return a != a || b != b ? __builtin_nanf("") : fmaxf(a, b); });
+    const float s = top / kTop;
+    const bool fine = s > 0.0f && s <= 3.4e38f;
+    if (live && lane == 0) scale[row] = s;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const Piece<kVec> pc(lane + i * LPR, channels);
+        if (!live || !pc.live) continue;
+        unsigned w[kVec / 4];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            const float q = fine ? fminf(fmaxf(rintf(r[i][e] / s), -kTop), kTop) : 0.0f;
+            const unsigned b = (unsigned)(int)q & 255u;
+            w[e / 4] = e % 4 == 0 ? b : w[e / 4] | b << (8 * (e % 4));
+        }
+        signed char* p = x8 + base;
+        if (channels >= kVec) {
+            __builtin_memcpy(__builtin_assume_aligned(p + pc.at, 1), w, kVec);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (e < channels) p[e] = (signed char)(w[e / 4] >> (8 * (e % 4)));
+        }
+    }
+}
+
+// (a launch has fewer than 2^32 threads: more rows than these go in several)
+template <int LPR, class F>
+hipError_t in_launches(int64_t rows, F&& f) {
+    constexpr int kThreads = LPR > 256 ? LPR : 256, kRows = kThreads / LPR;
+    constexpr int64_t kMost = ((int64_t)1 << 31) / kThreads * kRows;
+    for (int64_t from = 0; from < rows; from += kMost) {
+        const int64_t n = rows - from < kMost ? rows - from : kMost;
+        f(from, n, dim3((unsigned)((n + kRows - 1) / kRows)), dim3(kThreads));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <class F>
+hipError_t with_type(int dt, F&& f) {
+    switch (dt) {
+        case 0: return f(float{});
+        case 1: return f(_Float16{});
+        case 2: return f(__bf16{});
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_layer_norm(int dt, const LayerNormCall& c, hipStream_t stream) {
+    return with_type(dt, [&](auto type) {
+        typedef decltype(type) T;
+        return with_lanes(lanes_for(c.channels, sizeof(T)), [&](auto lpr, auto per) {
+            constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value;
+            return in_launches<kLpr>(c.rows, [&](int64_t from, int64_t rows, dim3 grid, dim3 threads) {
+                const int64_t at = from * c.channels;
+                hipLaunchKernelGGL((layer_norm_kernel<T, kLpr, kPer>), grid, threads, 0, stream, (const T*)c.x + at, c.residual ? (const T*)c.residual + at : nullptr,
+                                   (const T*)c.weight, (const T*)c.bias, (T*)c.y + at, c.sum ? (T*)c.sum + at : nullptr, rows, c.channels, c.eps);
+            });
+        });
+    });
+}
+
+hipError_t launch_layer_norm_backward(int dt, const void* sum, const void* weight, const void* d_y, const void* d_sum, void* d_r, float* d_weight,
+                                      float* d_bias, float* parts, int64_t rows, int channels, float eps, hipStream_t stream) {
+    return with_type(dt, [&](auto type) {
+        typedef decltype(type) T;
+        const int blocks = norm_backward_blocks(rows, channels, sizeof(T));
+        const bool sums = d_weight != nullptr || d_bias != nullptr;
+        // (no rows: nothing but sums of zeros)
+        const hipError_t e = blocks == 0 ? hipSuccess : with_lanes(lanes_for(channels, sizeof(T)), [&](auto lpr, auto per) {
+            constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value, kThreads = kLpr > 256 ? kLpr : 256;
+            hipLaunchKernelGGL((layer_norm_backward_kernel<T, kLpr, kPer>), dim3(blocks), dim3(kThreads), 0, stream, (const T*)sum, (const T*)weight,
+                               (const T*)d_y, (const T*)d_sum, (T*)d_r, sums ? parts : nullptr, rows, channels, eps);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess || !sums) return e;
+        return launch_sum_parts(parts, blocks, 2 * (int64_t)channels, PartSums{{d_weight, d_bias, nullptr}, {channels, channels, 0}}, stream);
+    });
+}
+
+hipError_t launch_quantize_integer(int dt, const void* x, void* x8, float* scale, int64_t rows, int channels, hipStream_t stream) {
+    return with_type(dt, [&](auto type) {
+        typedef decltype(type) T;
+        return with_lanes(lanes_for(channels, sizeof(T)), [&](auto lpr, auto per) {
+            constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value;
+            return in_launches<kLpr>(rows, [&](int64_t from, int64_t n, dim3 grid, dim3 threads) {
+                hipLaunchKernelGGL((quantize_integer_kernel<T, kLpr, kPer>), grid, threads, 0, stream, (const T*)x + from * channels,
+                                   (signed char*)x8 + from * channels, scale + from, n, channels);
+            });
+        });
+    });
+}
+
+}  // namespace msla
