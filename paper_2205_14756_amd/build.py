@@ -14,7 +14,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["k_project.hip", "k_aggregate.hip", "k_aggregate_mfma.hip", "k_aggregate_small.hip", "k_aggregate32.hip", "k_apply.hip", "k_small.hip", "k_ffn.hip", "k_ffn_fused.hip", "k_softmax.hip", "k_backward.hip", "k_generic.hip", "k_layout.hip", "msla_static.hip", "msla_api.cpp",
            "k_recurrence.hip", "k_norm.hip", "k_linear_quantized.hip", "msla_sequence.cpp",
            "k_selective.hip", "k_conv.hip", "k_layer_norm.hip", "k_linear_integer.hip", "k_parts.hip", "msla_layer.cpp"]
-HEADERS = ["msla_device.h", "aggregate_sweep.h", "gemm_tile.h", "msla_kernels.h", "recurrence_tile.h", "msla_sequence_kernels.h", "msla_layer_kernels.h", "norm_rows.h", "slots.h", os.path.join("..", "..", "include", "msla.h"),
+HEADERS = ["msla_device.h", "aggregate_sweep.h", "gemm_tile.h", "msla_kernels.h", "recurrence_tile.h", "msla_sequence_kernels.h", "msla_layer_kernels.h", "norm_rows.h", "slots.h", "scan_lanes.h", os.path.join("..", "..", "include", "msla.h"),
            os.path.join("..", "..", "include", "msla_sequence.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -20,6 +20,7 @@
 // lane has), over the waves through LDS, over workgroups through parts in the workspace that a last launch adds up in a fixed order.
 #include "msla_device.h"
 #include "msla_layer_kernels.h"
+#include "scan_lanes.h"
 
 namespace msla {
 namespace {
@@ -38,38 +39,6 @@ __device__ __forceinline__ float softplus_of(float v) {
     return fmaxf(v, 0.0f) + fmaf(__builtin_amdgcn_logf(u), kLn2, (e - (u - 1.0f)) * __builtin_amdgcn_rcpf(u));
 }
 
-template <int CTRL>
-__device__ __forceinline__ float moved(float v) {
-    const int b = __builtin_bit_cast(int, v);
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, CTRL, 0xf, 0xf, true));
-}
-// lane I of every four
-template <int I>
-__device__ __forceinline__ float of_four(float v) { return moved<I * 0x55>(v); }
-// the sum over every four lanes of p[j], to lane j
-__device__ __forceinline__ float deal_four(const float (&p)[4], bool odd, bool upper) {
-    const float r0 = (odd ? p[1] : p[0]) + moved<0xB1>(odd ? p[0] : p[1]);      // (lane ^ 1)
-    const float r1 = (odd ? p[3] : p[2]) + moved<0xB1>(odd ? p[2] : p[3]);
-    return (upper ? r1 : r0) + moved<0x4E>(upper ? r0 : r1);                    // (lane ^ 2)
-}
-// lanes below 32 get a's sum over lane ^ 32, the others b's
-__device__ __forceinline__ float halve32(float a, float b) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
-    const unsigned first = r[0], second = r[1];        // (bit_cast of a vector's element itself reads element 0)
-    return __builtin_bit_cast(float, first) + __builtin_bit_cast(float, second);
-}
-// even rows of 16 lanes get a's sum over lane ^ 16, odd ones b's
-__device__ __forceinline__ float halve16(float a, float b) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
-    const unsigned first = r[0], second = r[1];        // (bit_cast of a vector's element itself reads element 0)
-    return __builtin_bit_cast(float, first) + __builtin_bit_cast(float, second);
-}
-// lanes without the 8 (the 4) get a's sum over lane ^ 8 (lane ^ 4), the others b's
-__device__ __forceinline__ float halve8(float a, float b, bool mine_b) { return (mine_b ? b : a) + moved<0x128>(mine_b ? a : b); }
-__device__ __forceinline__ float halve4(float a, float b, bool mine_b) {
-    return (mine_b ? b : a) + moved<0x1B>(moved<0x141>(mine_b ? a : b));        // (7 - lane within eight, then 3 - lane within four)
-}
-
 // S neighbours of a row that starts anywhere
 template <class T, int S>
 struct Piece {
@@ -82,20 +51,18 @@ struct Piece {
     __device__ __forceinline__ float at(int s) const { return Traits<T>::to_f32(v[s]); }
 };
 
-// What a lane is: its channel, its quarter of the states and its token of every four.
-template <int S>
+// What a lane is: its channel, and its number among the L that share it.  A workgroup has CHANNELS of them, of one group.
+template <int L, int CHANNELS>
 struct Place {
-    int channel, group, quarter;
-    bool live, odd, upper;
+    int channel, group, own;
+    bool live;
     __device__ __forceinline__ Place(const ScanCall& c, int tile) {
-        const int per = c.channels / c.groups, tiles = (per + kScanTile - 1) / kScanTile;
+        const int per = c.channels / c.groups, tiles = (per + CHANNELS - 1) / CHANNELS;
         group = tile / tiles;
-        const int at = tile % tiles * kScanTile + threadIdx.x / 4;
+        const int at = tile % tiles * CHANNELS + threadIdx.x / L;
         live = at < per;
         channel = group * per + (live ? at : per - 1);
-        quarter = threadIdx.x & 3;
-        odd = threadIdx.x & 1;
-        upper = threadIdx.x & 2;
+        own = threadIdx.x % L;
     }
 };
 
@@ -116,129 +83,188 @@ __device__ __forceinline__ void store_own(float* p, const float (&from)[S]) { __
 
 enum Pass { kWhole, kSums, kSumsBoth };
 
-// Four tokens as they are loaded: a lane's own, and its states' b and c of all four.
-template <class T, int S, int PASS>
-struct Block {
-    T x, delta, gate, d_out;
-    Piece<T, S> b[4], c[4];
+// b and c of some tokens in fp32 in LDS, a state's tokens next to each other, so that a lane reads four tokens of a state at once.
+template <class T, int N, int L, bool WITH_C>
+struct Shared {
+    static constexpr int kThreads = kScanSlice * L, kTokens = 4 * L, kRow = kTokens + 4, kQuads = N / 4, kMaps = WITH_C ? 2 : 1;
+    static constexpr int kPieces = kTokens * kQuads * kMaps, kEach = (kPieces + kThreads - 1) / kThreads;
+    typedef float Room[kMaps][N][kRow];
+    Piece<T, 4> piece[kEach];
+    // tokens from t0 to last of a group's rows (zeros behind them)
+    __device__ __forceinline__ void fetch(const ScanCall& call, int group, int t0, int last) {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int e = threadIdx.x + k * kThreads, map = e / (kTokens * kQuads), t = t0 + e / kQuads % kTokens;
+            piece[k].clear();
+            if (e < kPieces && t <= last) piece[k].load(row<T>(map ? call.c : call.b, t) + group * N + e % kQuads * 4);
+        }
+    }
+    __device__ __forceinline__ void park(Room& room) const {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int e = threadIdx.x + k * kThreads, map = e / (kTokens * kQuads), t = e / kQuads % kTokens;
+            if (e >= kPieces) continue;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) room[map][e % kQuads * 4 + n][t] = piece[k].at(n);
+        }
+    }
 };
 
 // kWhole: outputs and the last state.  kSums: a slot's state from zero and the sum of its steps.  kSumsBoth: and what it adds to the gradient of the
 // state in front of it.
-template <class T, int S, int PASS>
-__global__ void __launch_bounds__(kThreads) scan_kernel(ScanCall call, int tiles) {
-    const Slot slot = slot_at(call.slots, blockIdx.x / tiles);
+//
+// L lanes have a channel, with S states each: kScanSlice channels a workgroup, so that a compute unit has two of them, which do not wait at the
+// same time.  Tokens go by in tiles of 4 L.  A tile is loaded with a lane to a channel and four
+// tokens, so that rows are read whole (with the lanes as they share channels, every lane was an access of its own, and those bounded the kernel), what
+// the states need of them goes through LDS, and so do the outputs back, in the steps' places.
+template <class T, int L, int S, int PASS>
+__global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int tiles) {
+    constexpr int N = L * S;
+    typedef Shared<T, N, L, PASS != kSums> Tile;
+    constexpr int kTokens = Tile::kTokens, kRow = Tile::kRow;
+    __shared__ __align__(16) typename Tile::Room room;
+    __shared__ __align__(16) float own[PASS == kSumsBoth ? 3 : 2][kScanSlice][kRow];         // steps (outputs), steps times x, dy
+    const int64_t slot_number = blockIdx.x / tiles;
+    const Slot slot = slot_at(call.slots, (int)slot_number);
     if (!slot.used) return;
-    const Place<S> me(call, blockIdx.x % tiles);
-    constexpr int N = 4 * S;
-    const int64_t state_at = (int64_t)me.channel * N + me.quarter * S, per_state = (int64_t)call.channels * N;
-    const bool gated = call.gate.p != nullptr, soft = call.softplus != 0;
+    // (what a sequence's last slot leaves of a state nobody asks for, nor what its first one adds to the gradient in front of it)
+    if (PASS != kWhole && slot.last && (PASS == kSums || slot.first)) return;
+    const Place<L, kScanSlice> me(call, blockIdx.x % tiles);
+    const int64_t state_at = (int64_t)me.channel * N + me.own * S, per_state = (int64_t)call.channels * N;
     float a[S], h[S];
     load_states(a, call.a + state_at);
 #pragma unroll
     for (int s = 0; s < S; ++s) a[s] = rate_of(a[s]);
-    const float bias = call.bias ? call.bias[me.channel] : 0.0f, skip = call.skip ? call.skip[me.channel] : 0.0f;
 #pragma unroll
     for (int s = 0; s < S; ++s) h[s] = 0.0f;
     if constexpr (PASS == kWhole) {
-        if (call.cut) load_states(h, call.states_at + (int64_t)(blockIdx.x / tiles) * per_state + state_at);
+        if (!slot.first) load_states(h, call.states_at + slot_number * per_state + state_at);
         else if (call.initial) load_states(h, call.initial + slot.sequence * per_state + state_at);
     }
     float along[S], reach[S];           // exp(a * the steps so far), and the sum of that times c dy
 #pragma unroll
     for (int s = 0; s < S; ++s) along[s] = 1.0f, reach[s] = 0.0f;
-    float steps = 0.0f;
     const int last = slot.until - 1;
-    const int shared_at = me.group * N + me.quarter * S;
-    typedef Block<T, S, PASS> B;
-    auto fetch = [&](B& k, int t0) {
-        if (t0 > last) return;
-        const int t = min(t0 + me.quarter, last);
-        k.x = row<T>(call.x, t)[me.channel];
-        k.delta = row<T>(call.delta, t)[me.channel];
-        if constexpr (PASS != kSums)
-            if (gated) k.gate = row<T>(call.gate, t)[me.channel];
-        if constexpr (PASS == kSumsBoth) k.d_out = row<T>(call.d_out, t)[me.channel];
+
+    // a lane's channel as tiles are loaded, and its four tokens of a tile
+    const int per = call.channels / call.groups, first = blockIdx.x % tiles % ((per + kScanSlice - 1) / kScanSlice) * kScanSlice;
+    const int lane = threadIdx.x % kScanSlice, run = threadIdx.x / kScanSlice, mine = 4 * run;
+    const bool live = first + lane < per;
+    const int channel = me.group * per + (live ? first + lane : per - 1);
+    const unsigned at_channel = channel * (unsigned)sizeof(T);
+    const bool gated = call.gate.p != nullptr, soft = call.softplus != 0;
+    const float bias = call.bias ? call.bias[channel] : 0.0f, skip = call.skip ? call.skip[channel] : 0.0f;
+    struct Tokens { T x[4], delta[4], gate[4], d_out[4]; } next;
+    auto fetch = [&](int t0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int ti = min(t0 + i, last);
-            k.b[i].load(row<T>(call.b, ti) + shared_at);
-            if constexpr (PASS != kSums) k.c[i].load(row<T>(call.c, ti) + shared_at);
+            const int t = min(t0 + mine + i, last);
+            auto load = [&](const TokenRows& r) { return *(const T*)((const char*)row<T>(r, t) + at_channel); };
+            next.x[i] = load(call.x);
+            next.delta[i] = load(call.delta);
+            if constexpr (PASS != kSums)
+                if (gated) next.gate[i] = load(call.gate);
+            if constexpr (PASS == kSumsBoth) next.d_out[i] = load(call.d_out);
         }
     };
-    auto advance = [&](B& k, int t0) {
-        const bool in = t0 + me.quarter <= last;
-        if (t0 + 3 > last) {            // (tokens behind the last one: a step of nothing, and nothing that is not finite)
+    Tile tile;
+    float steps = 0.0f;
+    if (slot.from <= last) {
+        tile.fetch(call, me.group, slot.from, last);
+        fetch(slot.from);
+    }
+    for (int t0 = slot.from; t0 <= last; t0 += kTokens) {
+        f32x4 step, add, dy, past, through;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (t0 + i > last) k.b[i].clear(), k.c[i].clear();
-        }
-        const float x = Traits<T>::to_f32(k.x), pre = Traits<T>::to_f32(k.delta) + bias;
-        const float step = in ? (soft ? softplus_of(pre) : pre) : 0.0f, add = in ? step * x : 0.0f;
-        float dy = 0.0f;
-        if constexpr (PASS == kSumsBoth) {
-            dy = Traits<T>::to_f32(k.d_out);
-            if (gated) {
-                const float z = Traits<T>::to_f32(k.gate);
-                dy *= z * sigmoid_of(z);
-            }
-            if (!in) dy = 0.0f;
-        }
-        steps += step;
-        float sums[4];
-        auto token = [&](auto which) {
-            constexpr int i = decltype(which)::value;
-            const float ti = of_four<i>(step), ui = of_four<i>(add);
-            float dyi = 0.0f;
-            if constexpr (PASS == kSumsBoth) dyi = of_four<i>(dy);
-            float y = 0.0f;
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
-                const float keep = exp2_of(ti * a[s]);
-                h[s] = fmaf(keep, h[s], ui * k.b[i].at(s));
-                if constexpr (PASS == kWhole) y = fmaf(k.c[i].at(s), h[s], y);
-                if constexpr (PASS == kSumsBoth) {
-                    along[s] *= keep;
-                    reach[s] = fmaf(along[s] * dyi, k.c[i].at(s), reach[s]);
+        for (int i = 0; i < 4; ++i) {
+            const bool in = t0 + mine + i <= last;          // (tokens behind the last one: a step of nothing, and b and c of zero)
+            const float x = Traits<T>::to_f32(next.x[i]), pre = Traits<T>::to_f32(next.delta[i]) + bias, full = soft ? softplus_of(pre) : pre;
+            step[i] = in ? full : 0.0f;
+            add[i] = in ? full * x : 0.0f;
+            past[i] = skip * x;
+            through[i] = 1.0f;
+            if constexpr (PASS != kSums) {
+                if (gated) {
+                    const float z = Traits<T>::to_f32(next.gate[i]);
+                    through[i] = z * sigmoid_of(z);
                 }
             }
-            sums[i] = y;
-        };
-        static_for<0, 4>(token);
-        if constexpr (PASS == kWhole) {
-            float y = fmaf(skip, x, deal_four(sums, me.odd, me.upper));
-            if (gated) {
-                const float z = Traits<T>::to_f32(k.gate);
-                y *= z * sigmoid_of(z);
-            }
-            if (in && me.live) row_out<T>(call.out, t0 + me.quarter)[me.channel] = Traits<T>::from_f32(y);
+            if constexpr (PASS == kSumsBoth) dy[i] = in ? Traits<T>::to_f32(next.d_out[i]) * through[i] : 0.0f;
+            steps += step[i];
         }
-    };
-    B here, there;
-    fetch(here, slot.from);
-    for (int t = slot.from; t <= last; t += 8) {
-        fetch(there, t + 4);
-        advance(here, t);
-        if (t + 4 > last) break;
-        fetch(here, t + 8);
-        advance(there, t + 4);
+        *(f32x4*)&own[0][lane][mine] = step;
+        *(f32x4*)&own[1][lane][mine] = add;
+        if constexpr (PASS == kSumsBoth) *(f32x4*)&own[2][lane][mine] = dy;
+        tile.park(room);
+        __syncthreads();
+        if (t0 + kTokens <= last) {
+            tile.fetch(call, me.group, t0 + kTokens, last);
+            fetch(t0 + kTokens);
+        }
+        const int channel_at = threadIdx.x / L;
+#pragma unroll
+        for (int block = 0; block < kTokens; block += L) {
+            float sums[L];
+#pragma unroll
+            for (int f = 0; f < L; f += 4) {
+                const f32x4 ti = *(const f32x4*)&own[0][channel_at][block + f], ui = *(const f32x4*)&own[1][channel_at][block + f];
+                f32x4 dyi, b[S], c[S];
+                if constexpr (PASS == kSumsBoth) dyi = *(const f32x4*)&own[2][channel_at][block + f];
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    b[s] = *(const f32x4*)&room[0][me.own * S + s][block + f];
+                    if constexpr (PASS != kSums) c[s] = *(const f32x4*)&room[1][me.own * S + s][block + f];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float y = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < S; ++s) {
+                        const float keep = exp2_of(ti[i] * a[s]);
+                        h[s] = fmaf(keep, h[s], ui[i] * b[s][i]);
+                        if constexpr (PASS == kWhole) y = s == 0 ? c[s][i] * h[s] : fmaf(c[s][i], h[s], y);
+                        if constexpr (PASS == kSumsBoth) {
+                            along[s] *= keep;
+                            reach[s] = fmaf(along[s] * dyi[i], c[s][i], reach[s]);
+                        }
+                    }
+                    sums[f + i] = y;
+                }
+                // (b and c of the next four tokens stay in LDS until these are done: their registers are wanted)
+                if constexpr (S > 1) __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (PASS == kWhole) own[0][channel_at][block + me.own] = deal<L>(sums, me.own);
+        }
+        __syncthreads();
+        if constexpr (PASS == kWhole) {
+            const f32x4 y = *(const f32x4*)&own[0][lane][mine];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (t0 + mine + i <= last && live)
+                    *(T*)((char*)row_out<T>(call.out, t0 + mine + i) + at_channel) = Traits<T>::from_f32((y[i] + past[i]) * through[i]);
+        }
     }
-    if (!me.live) return;
     if constexpr (PASS == kWhole) {
-        if (call.final_state && slot.last) store_states(call.final_state + slot.sequence * per_state + state_at, h);
+        if (call.final_state && slot.last && me.live) store_states(call.final_state + slot.sequence * per_state + state_at, h);
     } else {
-        const int64_t at = (int64_t)(blockIdx.x / tiles) * per_state + state_at;
-        store_states(call.states_at + at, h);
-        if constexpr (PASS == kSumsBoth) store_states(call.d_states_at + at, reach);
-        // (a lane has the steps of its own tokens of every four)
-        steps += moved<0xB1>(steps);
-        steps += moved<0x4E>(steps);
-        if (me.quarter == 0) call.steps_at[(int64_t)(blockIdx.x / tiles) * call.channels + me.channel] = steps;
+        const int64_t at = slot_number * per_state + state_at;
+        if (me.live) {
+            store_states(call.states_at + at, h);
+            if constexpr (PASS == kSumsBoth) store_states(call.d_states_at + at, reach);
+        }
+        // (each has the steps of its own tokens)
+        own[0][lane][run] = steps;
+        __syncthreads();
+        if (run == 0 && live) {
+#pragma unroll
+            for (int r = 1; r < L; ++r) steps += own[0][lane][r];
+            call.steps_at[slot_number * call.channels + channel] = steps;
+        }
     }
 }
 
-// The state that each slot starts from, and (BOTH) the state's gradient behind each slot, in the places of the slots' own sums.  A thread has one state
-// of a sequence; the next slots' sums are on their way while one is joined.
+// The state that each slot but a sequence's first starts from, and (BOTH) the state's gradient behind each but the last, in the places of the slots' own
+// sums.  A thread has one state of a sequence; the next slots' sums are on their way while one is joined.
 template <bool BOTH>
 __global__ void __launch_bounds__(256) scan_join_kernel(ScanCall call, int blocks) {
     const int b = blockIdx.x / blocks;
@@ -246,45 +272,35 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanCall call, int block
     if (at >= per_state) return;
     int lo, hi;
     rows_of_sequence(call.slots, b, lo, hi);
-    // (a sequence without tokens has a slot, too, which hands its state on)
-    const int64_t from = first_slot(call.slots, b), count = max(((int64_t)hi - lo + call.slots.run - 1) / call.slots.run, (int64_t)1);
+    const int64_t from = first_slot(call.slots, b), count = ((int64_t)hi - lo + call.slots.run - 1) / call.slots.run;
+    if (count < 2) return;
     const float a = rate_of(call.a[at]);
     const int64_t channel = at / call.states;
-    float h = call.initial ? call.initial[b * per_state + at] : 0.0f;
     constexpr int kAhead = 8;
-    for (int64_t k0 = 0; k0 < count; k0 += kAhead) {
-        float own[kAhead], steps[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int64_t slot = from + min(k0 + k, count - 1);
-            own[k] = call.states_at[slot * per_state + at];
-            steps[k] = call.steps_at[slot * call.channels + channel];
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            if (k0 + k < count) {
-                call.states_at[(from + k0 + k) * per_state + at] = h;
-                h = fmaf(exp2_of(a * steps[k]), h, own[k]);
-            }
-    }
-    if constexpr (BOTH) {
-        float g = call.d_final ? call.d_final[b * per_state + at] : 0.0f;
-        for (int64_t k0 = 0; k0 < count; k0 += kAhead) {
+    // over slots k = 0 .. count - 2 in the order that `slot_of` gives; v goes to the slot behind each
+    auto join = [&](float* sums, float v, auto slot_of) {
+        float last = 0.0f;
+        for (int64_t k0 = 0; k0 < count - 1; k0 += kAhead) {
             float own[kAhead], steps[kAhead];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
-                const int64_t slot = from + max(count - 1 - k0 - k, (int64_t)0);
-                own[k] = call.d_states_at[slot * per_state + at];
+                const int64_t slot = from + slot_of(min(k0 + k, count - 2));
+                own[k] = sums[slot * per_state + at];
                 steps[k] = call.steps_at[slot * call.channels + channel];
             }
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
-                if (k0 + k < count) {
-                    call.d_states_at[(from + count - 1 - k0 - k) * per_state + at] = g;
-                    g = fmaf(exp2_of(a * steps[k]), g, own[k]);
+                if (k0 + k < count - 1) {
+                    v = fmaf(exp2_of(a * steps[k]), v, own[k]);
+                    // (a slot's place is written when its own sum has been read: one step late)
+                    if (k0 + k > 0) sums[(from + slot_of(k0 + k)) * per_state + at] = last;
+                    last = v;
                 }
         }
-    }
+        sums[(from + slot_of(count - 1)) * per_state + at] = last;
+    };
+    join(call.states_at, call.initial ? call.initial[b * per_state + at] : 0.0f, [](int64_t k) { return k; });
+    if constexpr (BOTH) join(call.d_states_at, call.d_final ? call.d_final[b * per_state + at] : 0.0f, [&](int64_t k) { return count - 1 - k; });
 }
 
 // A slot of the gradient.  K tokens a window, whose states stay in registers (K * S of them).
@@ -304,8 +320,8 @@ __global__ void __launch_bounds__(kThreads) scan_backward_kernel(ScanCall call, 
     const int64_t slot_number = blockIdx.x / tiles;
     const int tile = blockIdx.x % tiles;
     const Slot slot = slot_at(call.slots, (int)slot_number);
-    const Place<S> me(call, tile);
-    const int64_t state_at = (int64_t)me.channel * N + me.quarter * S, per_state = (int64_t)call.channels * N;
+    const Place<4, kScanTile> me(call, tile);
+    const int64_t state_at = (int64_t)me.channel * N + me.own * S, per_state = (int64_t)call.channels * N;
     float* parts = call.parts_at + slot_number * (per_state + 2 * call.channels);
     float d_a[S], carry[S], h[S];
 #pragma unroll
@@ -318,13 +334,10 @@ __global__ void __launch_bounds__(kThreads) scan_backward_kernel(ScanCall call, 
 #pragma unroll
         for (int s = 0; s < S; ++s) a[s] = rate_of(a[s]);
         const float bias = call.bias ? call.bias[me.channel] : 0.0f, skip = call.skip ? call.skip[me.channel] : 0.0f;
-        if (call.cut) {
-            load_states(h, call.states_at + slot_number * per_state + state_at);
-            load_states(carry, call.d_states_at + slot_number * per_state + state_at);
-        } else {
-            if (call.initial) load_states(h, call.initial + slot.sequence * per_state + state_at);
-            if (call.d_final) load_states(carry, call.d_final + slot.sequence * per_state + state_at);
-        }
+        if (!slot.first) load_states(h, call.states_at + slot_number * per_state + state_at);
+        else if (call.initial) load_states(h, call.initial + slot.sequence * per_state + state_at);
+        if (!slot.last) load_states(carry, call.d_states_at + slot_number * per_state + state_at);
+        else if (call.d_final) load_states(carry, call.d_final + slot.sequence * per_state + state_at);
         if (!me.live) {                 // (lanes without a channel read another's values, and must not add even an infinity to sums)
 #pragma unroll
             for (int s = 0; s < S; ++s) carry[s] = h[s] = 0.0f;
@@ -339,7 +352,7 @@ __global__ void __launch_bounds__(kThreads) scan_backward_kernel(ScanCall call, 
         __syncthreads();
         auto of_shared = [&](int which, int t) {
             struct { float v[S]; } r;
-            load_own(r.v, &shared_bc[which][t * N + me.quarter * S]);
+            load_own(r.v, &shared_bc[which][t * N + me.own * S]);
             return r;
         };
         // the state at each window's start
@@ -349,7 +362,7 @@ __global__ void __launch_bounds__(kThreads) scan_backward_kernel(ScanCall call, 
             float step[kBlocks], add[kBlocks];
 #pragma unroll
             for (int q = 0; q < kBlocks; ++q) {
-                const int t = min(slot.from + w * K + 4 * q + me.quarter, last);
+                const int t = min(slot.from + w * K + 4 * q + me.own, last);
                 const float pre = Traits<T>::to_f32(row<T>(call.delta, t)[me.channel]) + bias;
                 step[q] = soft ? softplus_of(pre) : pre;
                 add[q] = step[q] * Traits<T>::to_f32(row<T>(call.x, t)[me.channel]);
@@ -366,7 +379,7 @@ __global__ void __launch_bounds__(kThreads) scan_backward_kernel(ScanCall call, 
         auto fetch = [&](Window<T, S>& to, int w) {
 #pragma unroll
             for (int q = 0; q < kBlocks; ++q) {
-                const int t = min(slot.from + w * K + 4 * q + me.quarter, last);
+                const int t = min(slot.from + w * K + 4 * q + me.own, last);
                 to.x[q] = row<T>(call.x, t)[me.channel];
                 to.delta[q] = row<T>(call.delta, t)[me.channel];
                 to.d_out[q] = row<T>(call.d_out, t)[me.channel];
@@ -379,7 +392,7 @@ __global__ void __launch_bounds__(kThreads) scan_backward_kernel(ScanCall call, 
             float step[kBlocks], add[kBlocks], dy[kBlocks];
 #pragma unroll
             for (int q = 0; q < kBlocks; ++q) {
-                const bool in = w * K + 4 * q + me.quarter < count && me.live;
+                const bool in = w * K + 4 * q + me.own < count && me.live;
                 const float pre = Traits<T>::to_f32(now.delta[q]) + bias, x = Traits<T>::to_f32(now.x[q]);
                 step[q] = in ? (soft ? softplus_of(pre) : pre) : 0.0f;
                 add[q] = in ? step[q] * x : 0.0f;
@@ -408,8 +421,8 @@ __global__ void __launch_bounds__(kThreads) scan_backward_kernel(ScanCall call, 
                 });
                 if (gated) {
                     const float z = Traits<T>::to_f32(now.gate[q]), x = Traits<T>::to_f32(now.x[q]);
-                    const float y = fmaf(skip, x, deal_four(y4, me.odd, me.upper)), g = sigmoid_of(z);
-                    const int t = w * K + 4 * q + me.quarter;
+                    const float y = fmaf(skip, x, deal<4>(y4, me.own)), g = sigmoid_of(z);
+                    const int t = w * K + 4 * q + me.own;
                     if (t < count && me.live)
                         row_out<T>(call.d_gate, slot.from + t)[me.channel] = Traits<T>::from_f32(dy[q] * y * (g * fmaf(z, 1.0f - g, 1.0f)));
                     dy[q] = t < count && me.live ? dy[q] * (z * g) : 0.0f;
@@ -445,14 +458,14 @@ __global__ void __launch_bounds__(kThreads) scan_backward_kernel(ScanCall call, 
                 const bool mine8 = lane & 8, mine4 = lane & 4;
 #pragma unroll
                 for (int p = 0; p < S / 2; ++p) {
-                    const float lower = halve8(both[0][p], both[2][p], mine8), higher = halve8(both[1][p], both[3][p], mine8);
-                    const float v = halve4(lower, higher, mine4);
+                    const float lower = halve8(both[0][p], both[2][p], lane), higher = halve8(both[1][p], both[3][p], lane);
+                    const float v = halve4(lower, higher, lane);
                     const int token = 4 * q + (mine8 ? 2 : 0) + (mine4 ? 1 : 0);
-                    room[threadIdx.x >> 6][token * 2 * N + (lane & 32 ? N : 0) + me.quarter * S + 2 * p + (lane & 16 ? 1 : 0)] = v;
+                    room[threadIdx.x >> 6][token * 2 * N + (lane & 32 ? N : 0) + me.own * S + 2 * p + (lane & 16 ? 1 : 0)] = v;
                 }
-                const float e = deal_four(e4, me.odd, me.upper), along = kLn2 * deal_four(w4, me.odd, me.upper);
+                const float e = deal<4>(e4, me.own), along = kLn2 * deal<4>(w4, me.own);
                 const float x = Traits<T>::to_f32(now.x[q]);
-                const int t = w * K + 4 * q + me.quarter;
+                const int t = w * K + 4 * q + me.own;
                 float d_step = fmaf(x, e, along);
                 if (soft) d_step *= sigmoid_of(Traits<T>::to_f32(now.delta[q]) + bias);
                 if (t < count && me.live) {
@@ -475,13 +488,11 @@ __global__ void __launch_bounds__(kThreads) scan_backward_kernel(ScanCall call, 
         }
         if (slot.first && call.d_initial && me.live) store_states(call.d_initial + slot.sequence * per_state + state_at, carry);
     }
-    d_skip += moved<0xB1>(d_skip);
-    d_skip += moved<0x4E>(d_skip);
-    d_bias += moved<0xB1>(d_bias);
-    d_bias += moved<0x4E>(d_bias);
+    d_skip = sum_over<4>(d_skip);
+    d_bias = sum_over<4>(d_bias);
     if (!me.live) return;
     store_states(parts + state_at, d_a);
-    if (me.quarter == 0) {
+    if (me.own == 0) {
         parts[per_state + me.channel] = d_skip;
         parts[per_state + call.channels + me.channel] = d_bias;
     }
@@ -527,8 +538,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanCall call, int block
         h[s] = fmaf(exp2_of(step * rate_of(a[s])), h[s], step * x * kb.at(s));
         y = fmaf(kc.at(s), h[s], y);
     }
-    y += moved<0xB1>(y);
-    y += moved<0x4E>(y);
+    y = sum_over<4>(y);
     if (!live) return;
     store_states(call.final_state + place, h);
     if (quarter != 0) return;
@@ -540,6 +550,18 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanCall call, int block
     row_out<T>(call.out, b)[channel] = Traits<T>::from_f32(y);
 }
 
+// The lanes that share a channel, and the states of each, of the passes over whole sequences.
+template <class F>
+hipError_t with_lanes(int states, F&& f) {
+    using std::integral_constant;
+    switch (states) {
+        case 8: return f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+        case 16: return f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+        case 32: return f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+        case 64: return f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+    }
+    return hipErrorInvalidValue;
+}
 template <class F>
 hipError_t with_states(int states, F&& f) {
     using std::integral_constant;
@@ -573,17 +595,17 @@ hipError_t join(const ScanCall& c, hipStream_t stream) {
 hipError_t launch_scan_forward(int dt, const ScanCall& c, hipStream_t stream) {
     return with_type(dt, [&](auto type) {
         typedef decltype(type) T;
-        return with_states(c.states, [&](auto s) {
-            constexpr int S = decltype(s)::value;
-            const int tiles = scan_tiles(c.channels, c.groups);
-            const dim3 grid((unsigned)(slot_count(c.slots) * tiles)), threads(kThreads);
+        return with_lanes(c.states, [&](auto l, auto s) {
+            constexpr int L = decltype(l)::value, S = decltype(s)::value;
+            const int tiles = scan_tiles(c.channels, c.groups, kScanSlice);
+            const dim3 grid((unsigned)(slot_count(c.slots) * tiles)), threads(kScanSlice * L);
             if (c.cut) {
-                hipLaunchKernelGGL((scan_kernel<T, S, kSums>), grid, threads, 0, stream, c, tiles);
+                hipLaunchKernelGGL((scan_kernel<T, L, S, kSums>), grid, threads, 0, stream, c, tiles);
                 hipError_t e = hipGetLastError();
                 if (e == hipSuccess) e = join<false>(c, stream);
                 if (e != hipSuccess) return e;
             }
-            hipLaunchKernelGGL((scan_kernel<T, S, kWhole>), grid, threads, 0, stream, c, tiles);
+            hipLaunchKernelGGL((scan_kernel<T, L, S, kWhole>), grid, threads, 0, stream, c, tiles);
             return hipGetLastError();
         });
     });
@@ -594,13 +616,17 @@ hipError_t launch_scan_backward(int dt, const ScanCall& c, hipStream_t stream) {
         typedef decltype(type) T;
         return with_states(c.states, [&](auto s) {
             constexpr int S = decltype(s)::value;
-            const int tiles = scan_tiles(c.channels, c.groups);
+            const int tiles = scan_tiles(c.channels, c.groups, kScanTile);
             const int64_t slots = slot_count(c.slots);
             const dim3 grid((unsigned)(slots * tiles)), threads(kThreads);
             hipError_t e = hipSuccess;
             if (c.cut) {
-                hipLaunchKernelGGL((scan_kernel<T, S, kSumsBoth>), grid, threads, 0, stream, c, tiles);
-                e = hipGetLastError();
+                e = with_lanes(c.states, [&](auto l, auto per) {
+                    constexpr int L = decltype(l)::value;
+                    const int slices = scan_tiles(c.channels, c.groups, kScanSlice);
+                    hipLaunchKernelGGL((scan_kernel<T, L, decltype(per)::value, kSumsBoth>), dim3((unsigned)(slots * slices)), dim3(kScanSlice * L), 0, stream, c, slices);
+                    return hipGetLastError();
+                });
                 if (e == hipSuccess) e = join<true>(c, stream);
                 if (e != hipSuccess) return e;
             }

@@ -21,9 +21,8 @@ constexpr int64_t kMost = (int64_t)1 << 46;             // elements that a buffe
 constexpr int64_t kMostTokens = 0x7fffffffLL - 4096;    // (token numbers, and those of some tokens behind the last, are ints)
 constexpr int kMostChannels = 1 << 20;
 constexpr int64_t kMostGroups = (int64_t)1 << 23;       // workgroups of a launch: fewer than 2^32 threads, 256 to a group
-// Workgroups that a scan should have at least: one for each of an MI355X's 256 compute units.
-constexpr int64_t kWantGroups = 512;
-constexpr int64_t kLeastSlot = 32;
+constexpr int64_t kUnits = 256;                         // compute units of an MI355X
+constexpr int64_t kCutTokens = 96;                      // what a scan's two more launches take, in tokens of one slot
 
 size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -64,25 +63,28 @@ struct ScanPlan {
     size_t states_at, d_states_at, steps_at, parts_at, shared_at, bytes;
 };
 
-// Slots are as long as leaves kWantGroups workgroups, and whole sequences where those are enough.
+// How long slots are.  The gradient's are as long as its states find room in LDS.  The forward pass has workgroups two of which fill a compute unit, and a sequence
+// that is cut does 1.65 times its work and two more launches.  Equal sequences are cut into as many slots as leave every unit two workgroups at most, if
+// that is worth it; packed ones, whose lengths nobody knows here, so that the units have about four (those that are no longer than that run whole).
 msla_status plan_of(const msla_selective_scan& s, bool backward, ScanPlan* p) {
-    const int64_t tiles = msla::scan_tiles(s.channels, s.groups), want = (kWantGroups + tiles - 1) / tiles;
+    const int64_t tiles = msla::scan_tiles(s.channels, s.groups, msla::kScanTile), slices = msla::scan_tiles(s.channels, s.groups, msla::kScanSlice);
+    const int64_t tile = s.states == 8 ? 32 : 64;        // tokens
     const int64_t longest = s.offsets ? s.tokens : s.tokens / s.sequences;
+    auto whole_tiles = [&](int64_t tokens) { return (tokens + tile - 1) / tile * tile; };
     int64_t run;
     if (backward) {
         run = msla::scan_backward_run(s.states);
         p->cut = longest > run;
     } else {
-        run = (s.tokens / want + 3) / 4 * 4;
-        if (run < kLeastSlot) run = kLeastSlot;
-        const bool enough = s.offsets == nullptr && s.sequences >= want;
-        p->cut = longest > run && !enough;
-        if (!p->cut) run = (longest / 4 + 1) * 4;
+        const int64_t each = 2 * kUnits / (s.sequences * slices);
+        run = s.offsets ? whole_tiles(s.tokens * slices / (4 * kUnits) + 1) : whole_tiles(longest / (each > 0 ? each : 1) + 1);
+        p->cut = s.offsets ? longest > run : each >= 2 && longest * 100 > run * 165 + kCutTokens * 100;
+        if (!p->cut) run = whole_tiles(longest + 1);
     }
     p->slots = msla::slots_of(s.offsets, s.sequences, s.tokens, (int)run);
     p->count = msla::slot_count(p->slots);
     const int64_t per_state = (int64_t)s.channels * s.states;
-    if (p->count * tiles >= kMostGroups || (int64_t)s.sequences * ((per_state + 255) / 256) >= kMostGroups) return MSLA_ERR_UNSUPPORTED;
+    if (p->count * slices >= kMostGroups || (int64_t)s.sequences * ((per_state + 255) / 256) >= kMostGroups) return MSLA_ERR_UNSUPPORTED;
     if (backward && (s.tokens * (int64_t)s.groups * s.states * 2 + 255) / 256 >= kMostGroups) return MSLA_ERR_UNSUPPORTED;
     size_t at = 0;
     auto take = [&](size_t floats) {

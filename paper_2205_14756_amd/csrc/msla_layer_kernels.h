@@ -26,8 +26,8 @@ struct ScanCall {
     float *parts_at, *shared_at;
 };
 
-constexpr int kScanTile = 64;       // channels of a workgroup
-inline int scan_tiles(int channels, int groups) { return groups * ((channels / groups + kScanTile - 1) / kScanTile); }
+constexpr int kScanSlice = 32, kScanTile = 64;      // channels of a workgroup: of the passes over whole slots, of the gradient
+inline int scan_tiles(int channels, int groups, int of) { return groups * ((channels / groups + of - 1) / of); }
 // tokens of a slot of the gradient, at most (its states at every window lie in LDS)
 inline int scan_backward_run(int states) { return states <= 16 ? 64 : (states == 32 ? 64 : 32); }
 
