@@ -83,12 +83,14 @@ __device__ __forceinline__ void store_own(float* p, const float (&from)[S]) { __
 
 enum Pass { kWhole, kSums, kSumsBoth };
 
-// b and c of some tokens in fp32 in LDS, a state's tokens next to each other, so that a lane reads four tokens of a state at once.
+// b and c of some tokens in fp32 in LDS, a state's tokens next to each other, so that a lane reads four tokens of a state at once.  The rows of the states that
+// the lanes of a channel read at once follow each other, four words beyond a multiple of the banks.
 template <class T, int N, int L, bool WITH_C>
 struct Shared {
     static constexpr int kThreads = kScanSlice * L, kTokens = 4 * L, kRow = kTokens + 4, kQuads = N / 4, kMaps = WITH_C ? 2 : 1;
     static constexpr int kPieces = kTokens * kQuads * kMaps, kEach = (kPieces + kThreads - 1) / kThreads;
     typedef float Room[kMaps][N][kRow];
+    static __device__ __forceinline__ int row_of(int lane, int s) { return s * L + lane; }     // of state lane * (N / L) + s
     Piece<T, 4> piece[kEach];
     // tokens from t0 to last of a group's rows (zeros behind them)
     __device__ __forceinline__ void fetch(const ScanCall& call, int group, int t0, int last) {
@@ -105,7 +107,10 @@ struct Shared {
             const int e = threadIdx.x + k * kThreads, map = e / (kTokens * kQuads), t = e / kQuads % kTokens;
             if (e >= kPieces) continue;
 #pragma unroll
-            for (int n = 0; n < 4; ++n) room[map][e % kQuads * 4 + n][t] = piece[k].at(n);
+            for (int i = 0; i < 4; ++i) {
+                const int n = e % kQuads * 4 + i;
+                room[map][row_of(n / (N / L), n % (N / L))][t] = piece[k].at(i);
+            }
         }
     }
 };
@@ -212,8 +217,8 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
                 if constexpr (PASS == kSumsBoth) dyi = *(const f32x4*)&own[2][channel_at][block + f];
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
-                    b[s] = *(const f32x4*)&room[0][me.own * S + s][block + f];
-                    if constexpr (PASS != kSums) c[s] = *(const f32x4*)&room[1][me.own * S + s][block + f];
+                    b[s] = *(const f32x4*)&room[0][Tile::row_of(me.own, s)][block + f];
+                    if constexpr (PASS != kSums) c[s] = *(const f32x4*)&room[1][Tile::row_of(me.own, s)][block + f];
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
