@@ -9,6 +9,7 @@ used on.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -471,6 +472,13 @@ def _tokens(t, name, dtype, like=None):
     return _Rows(t.data_ptr(), step if tokens > 1 else channels), tokens
 
 
+def _alike(t, name, dtype, shape):
+    """... of a known shape: most are contiguous, and are recognised by few reads."""
+    if t.is_contiguous() and t.dtype == dtype and t.shape == shape and len(shape) >= 2:
+        return _Rows(t.data_ptr(), shape[-1])
+    return _tokens(t, name, dtype, shape)[0]
+
+
 _NONE = _Rows(None, 0)
 
 
@@ -500,62 +508,71 @@ def _storage(dtype):
 
 class _ScanCall:
     """The arguments that the scan's forward, backward and step share, checked."""
-    __slots__ = ("x", "delta", "a", "b", "c", "skip", "bias", "gate", "shape", "dt", "state_shape")
+    __slots__ = ("x", "delta", "b", "c", "gate", "shape", "dt", "state_shape", "rows")
 
     def __init__(self, x, delta, a, b, c, skip, delta_bias, gate, softplus, sequences, offsets):
-        dtype = x.dtype
+        dtype, self.rows = x.dtype, x.shape
         self.dt = _storage(dtype)
         self.x, tokens = _tokens(x, "x", dtype)
-        channels = x.shape[-1]
-        self.delta, _ = _tokens(delta, "delta", dtype, x.shape)
-        self.gate = _NONE if gate is None else _tokens(gate, "gate", dtype, x.shape)[0]
-        if not (a.dim() == 2 and a.shape[0] == channels):
+        channels = self.rows[-1]
+        self.delta = _alike(delta, "delta", dtype, self.rows)
+        self.gate = _NONE if gate is None else _alike(gate, "gate", dtype, self.rows)
+        of_a = a.shape
+        if not (len(of_a) == 2 and of_a[0] == channels):
             _refuse("a must be [channels, states]")
-        states = a.shape[1]
-        self.a = a
-        _plain(a, "a", (channels, states), torch.float32)
-        _plain(skip, "skip", (channels,), torch.float32)
-        _plain(delta_bias, "delta_bias", (channels,), torch.float32)
-        self.b, groups = self._shared(b, "b", x, states)
-        self.c, _ = self._shared(c, "c", x, states, b.shape)
+        states = of_a[1]
+        _plain(a, "a", of_a, torch.float32)
+        if skip is not None:
+            _plain(skip, "skip", (channels,), torch.float32)
+        if delta_bias is not None:
+            _plain(delta_bias, "delta_bias", (channels,), torch.float32)
+        of_b = b.shape
+        if len(of_b) < 2 or of_b[-1] != states or (of_b[:-1] != self.rows[:-1] and of_b[:-2] != self.rows[:-1]):
+            _refuse("b must be [..., states] or [..., groups, states]")
+        groups = 1 if len(of_b) == len(self.rows) else of_b[-2]
+        self.b = self.shared(b, "b", dtype, of_b, groups * states)
+        self.c = self.shared(c, "c", dtype, of_b, groups * states)
         sequences, at = _sequences(x, sequences, offsets)
         self.shape = _Scan(sequences, tokens, at, channels, groups, states, 1 if softplus else 0)
         self.state_shape = (sequences, channels, states)
-        self.skip, self.bias = skip, delta_bias
 
-    @staticmethod
-    def _shared(t, name, x, states, like=None):
-        """b or c, [..., states] or [..., groups, states] with x's leading axes: (rows, groups)."""
-        shape = t.shape
-        if like is not None and shape != like:
-            _refuse(f"{name} must have the shape {tuple(like)}, not {tuple(shape)}")
-        lead = x.shape[:-1]
-        if not (shape[-1] == states and (shape[:-1] == lead or shape[:-2] == lead)):
-            _refuse(f"{name} must be [..., states] or [..., groups, states]")
-        if shape[:-1] == lead:
-            return _tokens(t, name, x.dtype)[0], 1
-        groups = shape[-2]
-        if not (t.is_contiguous() or groups == 1 or (t.stride(-2) == states and (t.stride(-1) == 1 or states == 1))):
-            _refuse(f"{name}'s groups must lie next to each other")
+    def shared(self, t, name, dtype, shape, width):
+        """b, c or their gradients, of a known shape ([..., states] or [..., groups, states]), as rows of ``width``."""
+        if t.is_contiguous() and t.dtype == dtype and t.shape == shape:
+            return _Rows(t.data_ptr(), width)
+        if t.dtype != dtype:
+            _refuse(f"{name} must be {dtype}, not {t.dtype}")
+        if t.shape != shape:
+            _refuse(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+        if len(shape) == len(self.rows):
+            return _tokens(t, name, dtype)[0]
         if t.is_contiguous():
-            return _tokens(t.view(lead + (groups * states,)), name, x.dtype)[0], groups
+            return _Rows(t.data_ptr(), width)
         strides = t.stride()
-        return _tokens(t.as_strided(lead + (groups * states,), strides[:-2] + strides[-1:]), name, x.dtype)[0], groups
+        if not (shape[-2] == 1 or (strides[-2] == shape[-1] and (strides[-1] == 1 or shape[-1] == 1))):
+            _refuse(f"{name}'s groups must lie next to each other")
+        return _tokens(t.as_strided(shape[:-2] + (width,), strides[:-2] + strides[-1:]), name, dtype)[0]
 
     def workspace(self, given, backward, like, stream):
         if given is not None:
             return _bytes(given)
-        size = ctypes.c_size_t(0)
-        _check(_lib().msla_selective_scan_workspace_bytes(self.shape, backward, self.dt, size), "msla_selective_scan_workspace_bytes")
-        return _new(like, stream, size.value, torch.uint8) if size.value or backward else None
+        s = self.shape
+        size = _scan_bytes(s.sequences, s.tokens, s.offsets is not None, s.channels, s.groups, s.states, backward, self.dt)
+        return _new(like, stream, size, torch.uint8) if size or backward else None
+
+
+@functools.lru_cache(maxsize=256)
+def _scan_bytes(sequences, tokens, packed, channels, groups, states, backward, dt):
+    """(a function of numbers alone, so what it says of the last shapes is kept)"""
+    shape = _Scan(sequences, tokens, 4 if packed else None, channels, groups, states, 0)
+    size = ctypes.c_size_t(0)
+    _check(_lib().msla_selective_scan_workspace_bytes(shape, backward, dt, size), "msla_selective_scan_workspace_bytes")
+    return size.value
 
 
 def msla_selective_scan_workspace_bytes(sequences, tokens, channels, groups, states, dtype, packed=False, backward=False) -> int:
     """Bytes that msla_selective_scan_forward (or _backward) needs; packed: with offsets."""
-    shape = _Scan(sequences, tokens, 4 if packed else None, channels, groups, states, 0)
-    size = ctypes.c_size_t(0)
-    _check(_lib().msla_selective_scan_workspace_bytes(shape, int(backward), _DTYPES[dtype], size), "msla_selective_scan_workspace_bytes")
-    return int(size.value)
+    return _scan_bytes(sequences, tokens, bool(packed), channels, groups, states, int(backward), _DTYPES[dtype])
 
 
 def msla_selective_scan_forward(x, delta, a, b, c, skip=None, delta_bias=None, gate=None, softplus=False, sequences: Optional[int] = None,
@@ -573,7 +590,7 @@ def msla_selective_scan_forward(x, delta, a, b, c, skip=None, delta_bias=None, g
     _plain(final_state, "final_state", k.state_shape, torch.float32)
     if out is None:
         out = _new(x, stream, x.shape)
-    o, _ = _tokens(out, "out", x.dtype, x.shape)
+    o = _alike(out, "out", x.dtype, x.shape)
     if final_state is None:
         final_state = _new(x, stream, k.state_shape, torch.float32)
     ws = k.workspace(workspace, 0, x, stream)
@@ -607,7 +624,7 @@ def msla_selective_scan_backward(x, delta, a, b, c, d_out, skip=None, delta_bias
     f32, channels = torch.float32, x.shape[-1]
     _plain(initial_state, "initial_state", k.state_shape, f32)
     _plain(d_final_state, "d_final_state", k.state_shape, f32)
-    do, _ = _tokens(d_out, "d_out", x.dtype, x.shape)
+    do = _alike(d_out, "d_out", x.dtype, x.shape)
     for t, of, name in ((d_skip, skip, "skip"), (d_delta_bias, delta_bias, "delta_bias"), (d_gate, gate, "gate"),
                         (d_initial_state, initial_state, "initial_state")):
         if t is not None and of is None:
@@ -617,21 +634,21 @@ def msla_selective_scan_backward(x, delta, a, b, c, d_out, skip=None, delta_bias
         if of is None:
             return None, _NONE
         if t is None:
-            t = _new(of, stream, of.shape)
-        return t, _tokens(t, name, x.dtype, of.shape)[0]
+            t = _new(of, stream, k.rows)
+        return t, _alike(t, name, x.dtype, k.rows)
 
     def shared(t, of, name):
         if t is None:
             t = _new(of, stream, of.shape)
-        if t.dtype != x.dtype:
-            _refuse(f"{name} must be {x.dtype}, not {t.dtype}")
-        return t, _ScanCall._shared(t, name, x, a.shape[1], of.shape)[0]
+        return t, k.shared(t, name, x.dtype, of.shape, k.shape.groups * k.shape.states)
 
     def single(t, of, name, shape):
         if of is None:
             return None
+        if t is None:
+            return _new(x, stream, shape, f32)
         _plain(t, name, shape, f32)
-        return _new(x, stream, shape, f32) if t is None else t
+        return t
 
     d_x, rx = rows(d_x, x, "d_x")
     d_delta, rd = rows(d_delta, delta, "d_delta")
@@ -663,7 +680,7 @@ def msla_selective_scan_step(x, delta, a, b, c, state, skip=None, delta_bias=Non
         _plain(new_state, "new_state", k.state_shape, torch.float32)
     if out is None:
         out = _new(x, stream, x.shape)
-    o, _ = _tokens(out, "out", x.dtype, x.shape)
+    o = _alike(out, "out", x.dtype, x.shape)
     _check(_lib().msla_selective_scan_step(k.shape, k.x, k.delta, a.data_ptr(), k.b, k.c, _ptr(skip), _ptr(delta_bias), k.gate, state.data_ptr(), o,
                                            new_state.data_ptr(), k.dt, _stream(stream)), "msla_selective_scan_step")
     return out, new_state
@@ -678,8 +695,9 @@ def _conv_arguments(x, weight, bias, silu, sequences, offsets):
     if not (weight.dim() == 2 and weight.shape[0] == channels):
         _refuse("weight must be [channels, width]")
     width = weight.shape[1]
-    _plain(weight, "weight", (channels, width), dtype)
-    _plain(bias, "bias", (channels,), dtype)
+    _plain(weight, "weight", weight.shape, dtype)
+    if bias is not None:
+        _plain(bias, "bias", (channels,), dtype)
     sequences, at = _sequences(x, sequences, offsets)
     return _Conv(sequences, tokens, at, channels, width, 1 if silu else 0), rows, dt, (sequences, max(width - 1, 0), channels)
 
@@ -697,7 +715,7 @@ def msla_causal_conv_forward(x, weight, bias=None, silu=False, sequences: Option
     _plain(final_state, "final_state", state_shape, x.dtype)
     if out is None:
         out = _new(x, stream, x.shape)
-    o, _ = _tokens(out, "out", x.dtype, x.shape)
+    o = _alike(out, "out", x.dtype, x.shape)
     if final_state is None:
         final_state = _new(x, stream, state_shape)
     _check(_lib().msla_causal_conv_forward(shape, rows, weight.data_ptr(), _ptr(bias), _ptr(initial_state), o, _ptr(final_state), dt, _stream(stream)),
@@ -705,11 +723,16 @@ def msla_causal_conv_forward(x, weight, bias=None, silu=False, sequences: Option
     return out, final_state
 
 
-def msla_causal_conv_backward_workspace_bytes(sequences, tokens, channels, width, dtype, packed=False) -> int:
+@functools.lru_cache(maxsize=256)
+def _conv_bytes(sequences, tokens, packed, channels, width, dt):
     shape = _Conv(sequences, tokens, 4 if packed else None, channels, width, 0)
     size = ctypes.c_size_t(0)
-    _check(_lib().msla_causal_conv_backward_workspace_bytes(shape, _DTYPES[dtype], size), "msla_causal_conv_backward_workspace_bytes")
-    return int(size.value)
+    _check(_lib().msla_causal_conv_backward_workspace_bytes(shape, dt, size), "msla_causal_conv_backward_workspace_bytes")
+    return size.value
+
+
+def msla_causal_conv_backward_workspace_bytes(sequences, tokens, channels, width, dtype, packed=False) -> int:
+    return _conv_bytes(sequences, tokens, bool(packed), channels, width, _DTYPES[dtype])
 
 
 def msla_causal_conv_backward(x, weight, d_out, bias=None, silu=False, sequences: Optional[int] = None, offsets=None, initial_state=None,
@@ -718,7 +741,7 @@ def msla_causal_conv_backward(x, weight, d_out, bias=None, silu=False, sequences
     initial_state is."""
     _on_gpu(x, weight, d_out, bias, offsets, initial_state, d_final_state, d_x, d_weight, d_bias, d_initial_state, workspace)
     shape, rows, dt, state_shape = _conv_arguments(x, weight, bias, silu, sequences, offsets)
-    do, _ = _tokens(d_out, "d_out", x.dtype, x.shape)
+    do = _alike(d_out, "d_out", x.dtype, x.shape)
     _plain(initial_state, "initial_state", state_shape, x.dtype)
     _plain(d_final_state, "d_final_state", state_shape, x.dtype)
     _plain(d_initial_state, "d_initial_state", state_shape, x.dtype)
@@ -729,7 +752,7 @@ def msla_causal_conv_backward(x, weight, d_out, bias=None, silu=False, sequences
             _refuse(f"d_{name} needs a {name}")
     if d_x is None:
         d_x = _new(x, stream, x.shape)
-    dx, _ = _tokens(d_x, "d_x", x.dtype, x.shape)
+    dx = _alike(d_x, "d_x", x.dtype, x.shape)
     if d_weight is None:
         d_weight = _new(x, stream, tuple(weight.shape), torch.float32)
     if d_bias is None and bias is not None:
@@ -737,9 +760,7 @@ def msla_causal_conv_backward(x, weight, d_out, bias=None, silu=False, sequences
     if d_initial_state is None and initial_state is not None:
         d_initial_state = _new(x, stream, state_shape)
     if workspace is None:
-        size = ctypes.c_size_t(0)
-        _check(_lib().msla_causal_conv_backward_workspace_bytes(shape, dt, size), "msla_causal_conv_backward_workspace_bytes")
-        workspace = _new(x, stream, size.value, torch.uint8)
+        workspace = _new(x, stream, _conv_bytes(shape.sequences, shape.tokens, offsets is not None, shape.channels, shape.width, dt), torch.uint8)
     _check(_lib().msla_causal_conv_backward(shape, rows, weight.data_ptr(), _ptr(bias), _ptr(initial_state), do, _ptr(d_final_state), dx, _ptr(d_weight),
                                             _ptr(d_bias), _ptr(d_initial_state), _ptr(_bytes(workspace)), workspace.numel(), dt, _stream(stream)),
            "msla_causal_conv_backward")
@@ -760,7 +781,7 @@ def msla_causal_conv_step(x, weight, state, bias=None, silu=False, out=None, new
         _plain(new_state, "new_state", state_shape, x.dtype)
     if out is None:
         out = _new(x, stream, x.shape)
-    o, _ = _tokens(out, "out", x.dtype, x.shape)
+    o = _alike(out, "out", x.dtype, x.shape)
     _check(_lib().msla_causal_conv_step(shape, rows, weight.data_ptr(), _ptr(bias), state.data_ptr(), o, new_state.data_ptr(), dt, _stream(stream)),
            "msla_causal_conv_step")
     return out, new_state
@@ -784,10 +805,15 @@ def msla_layer_norm_forward(x, weight=None, bias=None, residual=None, eps=1e-5, 
     return out, x if sum_out is None else sum_out
 
 
-def msla_layer_norm_backward_workspace_bytes(rows, channels, dtype) -> int:
+@functools.lru_cache(maxsize=256)
+def _layer_norm_bytes(rows, channels, dt):
     size = ctypes.c_size_t(0)
-    _check(_lib().msla_layer_norm_backward_workspace_bytes(rows, channels, _DTYPES[dtype], size), "msla_layer_norm_backward_workspace_bytes")
-    return int(size.value)
+    _check(_lib().msla_layer_norm_backward_workspace_bytes(rows, channels, dt, size), "msla_layer_norm_backward_workspace_bytes")
+    return size.value
+
+
+def msla_layer_norm_backward_workspace_bytes(rows, channels, dtype) -> int:
+    return _layer_norm_bytes(rows, channels, _DTYPES[dtype])
 
 
 def msla_layer_norm_backward(r, weight, d_y, d_sum=None, eps=1e-5, d_r=None, d_weight=None, d_bias=None, workspace=None, stream=None):
@@ -795,17 +821,20 @@ def msla_layer_norm_backward(r, weight, d_y, d_sum=None, eps=1e-5, d_r=None, d_w
     d_r is that of x and of residual alike; d_weight and d_bias are fp32."""
     rows, channels = _norm_arguments(r, weight, d_y, d_sum, ("r", "d_y", "d_sum"))
     _on_gpu(d_r, d_weight, d_bias, workspace)
-    _plain(d_r, "d_r", r.shape, r.dtype)
-    _plain(d_weight, "d_weight", (channels,), torch.float32)
-    _plain(d_bias, "d_bias", (channels,), torch.float32)
     if d_r is None:
         d_r = _new(r, stream)
+    else:
+        _plain(d_r, "d_r", r.shape, r.dtype)
     if d_weight is None:
         d_weight = _new(r, stream, channels, torch.float32)
+    else:
+        _plain(d_weight, "d_weight", (channels,), torch.float32)
     if d_bias is None:
         d_bias = _new(r, stream, channels, torch.float32)
+    else:
+        _plain(d_bias, "d_bias", (channels,), torch.float32)
     if workspace is None:
-        workspace = _new(r, stream, msla_layer_norm_backward_workspace_bytes(rows, channels, r.dtype), torch.uint8)
+        workspace = _new(r, stream, _layer_norm_bytes(rows, channels, _DTYPES[r.dtype]), torch.uint8)
     _check(_lib().msla_layer_norm_backward(_ptr(r), _ptr(weight), _ptr(d_y), _ptr(d_sum), _ptr(d_r), _ptr(d_weight), _ptr(d_bias),
                                            _ptr(_bytes(workspace)), workspace.numel(), rows, channels, float(eps), _DTYPES[r.dtype], _stream(stream)),
            "msla_layer_norm_backward")
