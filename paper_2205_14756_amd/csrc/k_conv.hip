@@ -21,6 +21,16 @@ __device__ __forceinline__ const T* row(const TokenRows& r, int t) { return (con
 template <class T>
 __device__ __forceinline__ T* row_out(const TokenRows& r, int t) { return (T*)r.p + (int64_t)t * r.ts; }
 
+// VEC neighbours of a row that starts anywhere
+template <class T, int VEC>
+struct Raw {
+    T v[VEC];
+    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(v, __builtin_assume_aligned(p, sizeof(T)), VEC * sizeof(T)); }
+    __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T)), v, VEC * sizeof(T)); }
+    __device__ __forceinline__ float at(int e) const { return Traits<T>::to_f32(v[e]); }
+    __device__ __forceinline__ void set(int e, float f) { v[e] = Traits<T>::from_f32(f); }
+};
+
 // A thread's place: `across` lanes (a power of two, 256 at most) take neighbouring pieces of a row, so that a wave reads whole lines.
 template <int VEC>
 struct Place {
@@ -31,163 +41,230 @@ struct Place {
           slot((int)(blockIdx.x / blocks_across) * (256 / across) + (int)(threadIdx.x / across)) {}
 };
 
-template <class T, int W>
+template <class T, int W, int VEC>
 struct Taps {
-    float w[W][Traits<T>::kVec], bias[Traits<T>::kVec];
+    float w[W][VEC], bias[VEC];
     __device__ __forceinline__ Taps(const ConvCall& c, int at) {
 #pragma unroll
-        for (int e = 0; e < Traits<T>::kVec; ++e) {
-            const bool in = at + e < c.channels;
+        for (int e = 0; e < VEC; ++e) {
 #pragma unroll
-            for (int k = 0; k < W; ++k) w[k][e] = in ? Traits<T>::to_f32(((const T*)c.weight)[(int64_t)(at + e) * W + k]) : 0.0f;
-            bias[e] = in && c.bias ? Traits<T>::to_f32(((const T*)c.bias)[at + e]) : 0.0f;
+            for (int k = 0; k < W; ++k) w[k][e] = Traits<T>::to_f32(((const T*)c.weight)[(int64_t)(at + e) * W + k]);
+            bias[e] = c.bias ? Traits<T>::to_f32(((const T*)c.bias)[at + e]) : 0.0f;
         }
     }
-    __device__ __forceinline__ float pre(const float (&rows)[W][Traits<T>::kVec], int e) const {
+    // of the token in rows[i + W - 1]
+    template <int N>
+    __device__ __forceinline__ float pre(const float (&rows)[N][VEC], int i, int e) const {
         float v = bias[e];
 #pragma unroll
-        for (int k = 0; k < W; ++k) v = fmaf(w[k][e], rows[k][e], v);
+        for (int k = 0; k < W; ++k) v = fmaf(w[k][e], rows[i + k][e], v);
         return v;
     }
 };
 
 // the width - 1 rows in front of token t of a sequence that starts at lo, oldest first, to rows[0 .. W - 2]
-template <class T, int W>
-__device__ __forceinline__ void rows_before(const ConvCall& c, const Slot& s, int t, int at, float (&rows)[W][Traits<T>::kVec]) {
-    constexpr int kVec = Traits<T>::kVec;
+template <class T, int W, int VEC, int N>
+__device__ __forceinline__ void rows_before(const ConvCall& c, const Slot& s, int t, int at, float (&rows)[N][VEC]) {
 #pragma unroll
     for (int k = 0; k < W - 1; ++k) {
         const int i = t - (W - 1) + k;
-        if (i >= s.lo) {
-            load_row<T>(row<T>(c.x, i), at, c.channels, rows[k]);
-        } else if (c.initial) {
-            load_row<T>((const T*)c.initial + ((int64_t)s.sequence * (W - 1) + (W - 1 - (s.lo - i))) * c.channels, at, c.channels, rows[k]);
-        } else {
+        Raw<T, VEC> r = {};
+        if (i >= s.lo) r.load(row<T>(c.x, i) + at);
+        else if (c.initial) r.load((const T*)c.initial + ((int64_t)s.sequence * (W - 1) + (W - 1 - (s.lo - i))) * c.channels + at);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) rows[k][e] = 0.0f;
-        }
+        for (int e = 0; e < VEC; ++e) rows[k][e] = r.at(e);
     }
 }
 
-template <class T, int W>
+constexpr int kAhead = 4;       // tokens of a step: they are asked for a step ahead, and without a branch, so that a step waits for its own alone
+
+template <class T, int W, int VEC>
 __global__ void __launch_bounds__(256) conv_kernel(ConvCall c, int across, int blocks_across, int slots) {
-    constexpr int kVec = Traits<T>::kVec, kAhead = 4;
-    const Place<kVec> me(c.channels, across, blocks_across);
+    const Place<VEC> me(c.channels, across, blocks_across);
     if (!me.piece.live || me.slot >= slots) return;
     const Slot s = slot_at(c.slots, me.slot);
     if (!s.used) return;
     const int at = me.piece.at;
-    const Taps<T, W> taps(c, at);
-    float rows[W][kVec];
-    rows_before<T, W>(c, s, s.from, at, rows);
-    for (int t0 = s.from; t0 < s.until; t0 += kAhead) {
-        typename Traits<T>::Vec raw[kAhead];
+    Raw<T, VEC> next[kAhead];
+    auto fetch = [&](int t0) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) raw[i] = load_raw<T>(row<T>(c.x, min(t0 + i, s.until - 1)), at, c.channels);
+        for (int i = 0; i < kAhead; ++i) next[i].load(row<T>(c.x, min(t0 + i, s.until - 1)) + at);
+    };
+    if (s.from < s.until) fetch(s.from);
+    const Taps<T, W, VEC> taps(c, at);
+    float rows[W - 1 + kAhead][VEC];
+    rows_before<T, W, VEC>(c, s, s.from, at, rows);
+    auto output = [&](int i) {
+        Raw<T, VEC> out;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (t0 + i >= s.until) break;
-            float out[kVec];
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                rows[W - 1][e] = Traits<T>::to_f32(raw[i][e]);
-                const float pre = taps.pre(rows, e);
-                out[e] = c.silu ? pre * sigmoid_of(pre) : pre;
-#pragma unroll
-                for (int k = 0; k < W - 1; ++k) rows[k][e] = rows[k + 1][e];
-            }
-            store_row<T>(row_out<T>(c.out, t0 + i), at, c.channels, out);
+        for (int e = 0; e < VEC; ++e) {
+            const float pre = taps.pre(rows, i, e), open = pre * sigmoid_of(pre);
+            out.set(e, c.silu ? open : pre);
         }
+        return out;
+    };
+    int t0 = s.from;
+    for (; t0 + kAhead <= s.until; t0 += kAhead) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) rows[W - 1 + i][e] = next[i].at(e);
+        fetch(t0 + kAhead);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) output(i).store(row_out<T>(c.out, t0 + i) + at);
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) rows[k][e] = rows[k + kAhead][e];
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead - 1; ++i) {
+        if (t0 + i >= s.until) break;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) rows[W - 1][e] = next[i].at(e);
+        output(0).store(row_out<T>(c.out, t0 + i) + at);
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) rows[k][e] = rows[k + 1][e];
     }
     if (s.last && c.final_state) {
 #pragma unroll
-        for (int k = 0; k < W - 1; ++k) store_row<T>((T*)c.final_state + ((int64_t)s.sequence * (W - 1) + k) * c.channels, at, c.channels, rows[k]);
+        for (int k = 0; k < W - 1; ++k) {
+            Raw<T, VEC> out;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) out.set(e, rows[k][e]);
+            out.store((T*)c.final_state + ((int64_t)s.sequence * (W - 1) + k) * c.channels + at);
+        }
     }
 }
 
-template <class T, int W>
+template <class T, int W, int VEC>
 __global__ void __launch_bounds__(256) conv_backward_kernel(ConvCall c, int across, int blocks_across, int slots) {
-    constexpr int kVec = Traits<T>::kVec, kAhead = 4;
-    const Place<kVec> me(c.channels, across, blocks_across);
+    const Place<VEC> me(c.channels, across, blocks_across);
     if (!me.piece.live || me.slot >= slots) return;
     const Slot s = slot_at(c.slots, me.slot);
     const int at = me.piece.at;
-    float d_w[W][kVec], d_b[kVec];
+    float d_w[W][VEC], d_b[VEC];
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) {
+    for (int e = 0; e < VEC; ++e) {
         d_b[e] = 0.0f;
 #pragma unroll
         for (int k = 0; k < W; ++k) d_w[k][e] = 0.0f;
     }
     if (s.used) {
-        const Taps<T, W> taps(c, at);
-        float rows[W][kVec], d_pre[W][kVec];        // of the last W tokens
-        rows_before<T, W>(c, s, s.from, at, rows);
-#pragma unroll
-        for (int k = 0; k < W; ++k)
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) d_pre[k][e] = 0.0f;
-        const int beyond = s.until + W - 1;
-        for (int t0 = s.from; t0 < beyond; t0 += kAhead) {
-            typename Traits<T>::Vec raw[kAhead], grad[kAhead];
+        Raw<T, VEC> next_x[kAhead], next_g[kAhead];
+        auto fetch = [&](int t0) {
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int t = min(t0 + i, s.hi - 1);
-                if (s.hi > s.lo) {
-                    raw[i] = load_raw<T>(row<T>(c.x, t), at, c.channels);
-                    grad[i] = load_raw<T>(row<T>(c.d_out, t), at, c.channels);
-                } else {
-                    raw[i] = grad[i] = typename Traits<T>::Vec{};
+                next_x[i].load(row<T>(c.x, t) + at);
+                next_g[i].load(row<T>(c.d_out, t) + at);
+            }
+        };
+        // the tokens whose outputs, width - 1 tokens back, are the run's own and know nothing of the state behind the sequence: whole steps of them
+        const int steady = s.from + W - 1, steps = max(0, s.until - steady) / kAhead;
+        if (steps > 0) fetch(steady);
+        const Taps<T, W, VEC> taps(c, at);
+        float rows[W - 1 + kAhead][VEC], d_pre[W - 1 + kAhead][VEC];        // of the last W - 1 tokens, and a step's
+        rows_before<T, W, VEC>(c, s, s.from, at, rows);
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) d_pre[k][e] = 0.0f;
+        // the token in rows[i + W - 1], whose output's gradient is g: d_pre of it, its part of the taps' gradient
+        auto take = [&](int i, const Raw<T, VEC>& g, bool own, bool in) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float pre = taps.pre(rows, i, e), open = sigmoid_of(pre), slope = open * fmaf(pre, 1.0f - open, 1.0f), back = g.at(e);
+                const float d = in ? (c.silu ? back * slope : back) : 0.0f;
+                d_pre[W - 1 + i][e] = d;
+                if (own) {
+                    d_b[e] += d;
+#pragma unroll
+                    for (int k = 0; k < W; ++k) d_w[k][e] = fmaf(d, rows[i + k][e], d_w[k][e]);
                 }
             }
+        };
+        // d_x of the token W - 1 in front of that one
+        auto give = [&](int i, float (&out)[VEC]) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                float v = 0.0f;
+#pragma unroll
+                for (int m = 0; m < W; ++m) v = fmaf(taps.w[W - 1 - m][e], d_pre[i + m][e], v);
+                out[e] = v;
+            }
+        };
+        auto shift = [&](int by) {
+#pragma unroll
+            for (int k = 0; k < W - 1; ++k)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    rows[k][e] = rows[k + by][e];
+                    d_pre[k][e] = d_pre[k + by][e];
+                }
+        };
+        auto edge = [&](int t) {
+            const bool own = t < s.until, in = t < s.hi;
+            const int r = t - (W - 1);
+            Raw<T, VEC> x = {}, g = {};
+            if (in) {
+                x.load(row<T>(c.x, t) + at);
+                g.load(row<T>(c.d_out, t) + at);
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) rows[W - 1][e] = x.at(e);
+            take(0, g, own, in);
+            float out[VEC];
+            give(0, out);
+            shift(1);
+            if (r < s.from && !(s.first && c.d_initial)) return;
+            const int left = r - (s.hi - (W - 1));      // row of the state behind the sequence
+            if (c.d_final && left >= 0) {
+                Raw<T, VEC> f;
+                f.load((const T*)c.d_final + ((int64_t)s.sequence * (W - 1) + left) * c.channels + at);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) out[e] += f.at(e);
+            }
+            Raw<T, VEC> to;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) to.set(e, out[e]);
+            to.store((r >= s.from ? row_out<T>(c.d_x, r) : (T*)c.d_initial + ((int64_t)s.sequence * (W - 1) + (r - s.lo + W - 1)) * c.channels) + at);
+        };
+        const int beyond = s.until + W - 1, first_edge = min(steady, beyond);
+#pragma unroll 1
+        for (int t = s.from; t < first_edge; ++t) edge(t);
+        for (int n = 0; n < steps; ++n) {
+            const int t0 = steady + n * kAhead;
+            Raw<T, VEC> g[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int t = t0 + i, r = t - (W - 1);
-                if (t >= beyond) break;
-                const bool own = t < s.until, in = t < s.hi;
-                float out[kVec];
+                g[i] = next_g[i];
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) {
-                    rows[W - 1][e] = Traits<T>::to_f32(raw[i][e]);
-                    float d = Traits<T>::to_f32(grad[i][e]);
-                    if (c.silu) {
-                        const float pre = taps.pre(rows, e), g = sigmoid_of(pre);
-                        d *= g * fmaf(pre, 1.0f - g, 1.0f);
-                    }
-                    if (!in) d = 0.0f;
-#pragma unroll
-                    for (int k = 0; k < W - 1; ++k) d_pre[k][e] = d_pre[k + 1][e];
-                    d_pre[W - 1][e] = d;
-                    float v = 0.0f;
-#pragma unroll
-                    for (int m = 0; m < W; ++m) v = fmaf(taps.w[W - 1 - m][e], d_pre[m][e], v);
-                    out[e] = v;
-                    if (own) {
-                        d_b[e] += d;
-#pragma unroll
-                        for (int k = 0; k < W; ++k) d_w[k][e] = fmaf(d, rows[k][e], d_w[k][e]);
-                    }
-#pragma unroll
-                    for (int k = 0; k < W - 1; ++k) rows[k][e] = rows[k + 1][e];
-                }
-                if (r < s.from && !(s.first && c.d_initial)) continue;
-                const int left = r - (s.hi - (W - 1));      // row of the state behind the sequence
-                if (c.d_final && left >= 0) {
-                    float f[kVec];
-                    load_row<T>((const T*)c.d_final + ((int64_t)s.sequence * (W - 1) + left) * c.channels, at, c.channels, f);
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e) out[e] += f[e];
-                }
-                if (r >= s.from) store_row<T>(row_out<T>(c.d_x, r), at, c.channels, out);
-                else store_row<T>((T*)c.d_initial + ((int64_t)s.sequence * (W - 1) + (r - s.lo + W - 1)) * c.channels, at, c.channels, out);
+                for (int e = 0; e < VEC; ++e) rows[W - 1 + i][e] = next_x[i].at(e);
             }
+            fetch(t0 + kAhead);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                take(i, g[i], true, true);
+                float out[VEC];
+                give(i, out);
+                Raw<T, VEC> to;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) to.set(e, out[e]);
+                to.store(row_out<T>(c.d_x, t0 + i - (W - 1)) + at);
+            }
+            shift(kAhead);
         }
+#pragma unroll 1
+        for (int t = first_edge + steps * kAhead; t < beyond; ++t) edge(t);
     }
     if (c.parts_at == nullptr) return;
     float* parts = c.parts_at + (int64_t)me.slot * c.channels * (W + 1);
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-        if (e < me.piece.skip || at + e >= c.channels) continue;
+    for (int e = 0; e < VEC; ++e) {
+        if (e < me.piece.skip) continue;
 #pragma unroll
         for (int k = 0; k < W; ++k) parts[(int64_t)(at + e) * W + k] = d_w[k][e];
         parts[(int64_t)c.channels * W + at + e] = d_b[e];
@@ -195,34 +272,40 @@ __global__ void __launch_bounds__(256) conv_backward_kernel(ConvCall c, int acro
 }
 
 // One token for each sequence.  The state may be updated in place: where pieces share channels, each writes its own alone.
-template <class T, int W>
+template <class T, int W, int VEC>
 __global__ void __launch_bounds__(256) conv_step_kernel(ConvCall c, int across, int blocks_across) {
-    constexpr int kVec = Traits<T>::kVec;
-    const Place<kVec> me(c.channels, across, blocks_across);
+    const Place<VEC> me(c.channels, across, blocks_across);
     if (!me.piece.live || me.slot >= c.slots.sequences) return;
     const int at = me.piece.at;
-    const Taps<T, W> taps(c, at);
-    float rows[W][kVec], out[kVec];
-    const int64_t state = (int64_t)me.slot * (W - 1) * c.channels;
+    const Taps<T, W, VEC> taps(c, at);
+    const int64_t state = (int64_t)me.slot * (W - 1) * c.channels + at;
+    Raw<T, VEC> raw[W], out;
+    float rows[W][VEC];
 #pragma unroll
-    for (int k = 0; k < W - 1; ++k) load_row<T>((const T*)c.initial + state + (int64_t)k * c.channels, at, c.channels, rows[k]);
-    load_row<T>(row<T>(c.x, me.slot), at, c.channels, rows[W - 1]);
+    for (int k = 0; k < W - 1; ++k) raw[k].load((const T*)c.initial + state + (int64_t)k * c.channels);
+    raw[W - 1].load(row<T>(c.x, me.slot) + at);
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-        const float pre = taps.pre(rows, e);
-        out[e] = c.silu ? pre * sigmoid_of(pre) : pre;
+    for (int k = 0; k < W; ++k)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) rows[k][e] = raw[k].at(e);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        const float pre = taps.pre(rows, 0, e), open = pre * sigmoid_of(pre);
+        out.set(e, c.silu ? open : pre);
     }
+    T* to = row_out<T>(c.out, me.slot) + at;
+    T* states = (T*)c.final_state + state;
     if (me.piece.skip == 0) {
-        store_row<T>(row_out<T>(c.out, me.slot), at, c.channels, out);
+        out.store(to);
 #pragma unroll
-        for (int k = 0; k < W - 1; ++k) store_row<T>((T*)c.final_state + state + (int64_t)k * c.channels, at, c.channels, rows[k + 1]);
+        for (int k = 0; k < W - 1; ++k) raw[k + 1].store(states + (int64_t)k * c.channels);
     } else {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
+        for (int e = 0; e < VEC; ++e) {
             if (e < me.piece.skip) continue;
-            row_out<T>(c.out, me.slot)[at + e] = Traits<T>::from_f32(out[e]);
+            to[e] = out.v[e];
 #pragma unroll
-            for (int k = 0; k < W - 1; ++k) ((T*)c.final_state)[state + (int64_t)k * c.channels + at + e] = Traits<T>::from_f32(rows[k + 1][e]);
+            for (int k = 0; k < W - 1; ++k) states[(int64_t)k * c.channels + e] = raw[k + 1].v[e];
         }
     }
 }
@@ -246,34 +329,42 @@ hipError_t with_kind(int dt, int width, F&& f) {
     return hipErrorInvalidValue;
 }
 
-struct Grid { int across, blocks_across; };
-Grid grid_of(int channels, int elem) {
-    const int vec = 16 / elem, pieces = (channels + vec - 1) / vec;
-    int across = 1;
-    while (across < pieces && across < 256) across *= 2;
-    return {across, (pieces + across - 1) / across};
+// Pieces of 8 bytes (what a lane keeps for each of its channels, taps and rows, in the gradient those of both, leaves 16-byte ones two or three waves a
+// SIMD); of one element where a row is no longer than that.
+template <class T, class F>
+hipError_t with_pieces(int channels, F&& f) {
+    constexpr int kVec = 8 / sizeof(T);
+    auto launch = [&](auto vec) {
+        const int pieces = (channels + decltype(vec)::value - 1) / decltype(vec)::value;
+        int across = 1;
+        while (across < pieces && across < 256) across *= 2;
+        const int blocks_across = (pieces + across - 1) / across;
+        f(vec, across, blocks_across, [=](int64_t slots) { return dim3((unsigned)((slots + 256 / across - 1) / (256 / across) * blocks_across)); });
+        return hipGetLastError();
+    };
+    if (channels >= kVec) return launch(std::integral_constant<int, kVec>{});
+    return launch(std::integral_constant<int, 1>{});
 }
-unsigned blocks_of(const Grid& g, int64_t slots) { return (unsigned)((slots + 256 / g.across - 1) / (256 / g.across) * g.blocks_across); }
 
 }  // namespace
 
 hipError_t launch_conv_forward(int dt, const ConvCall& c, hipStream_t stream) {
     return with_kind(dt, c.width, [&](auto type, auto w) {
         typedef decltype(type) T;
-        const Grid g = grid_of(c.channels, sizeof(T));
-        const int64_t slots = slot_count(c.slots);
-        hipLaunchKernelGGL((conv_kernel<T, decltype(w)::value>), dim3(blocks_of(g, slots)), dim3(256), 0, stream, c, g.across, g.blocks_across, (int)slots);
-        return hipGetLastError();
+        return with_pieces<T>(c.channels, [&](auto vec, int across, int blocks_across, auto grid) {
+            const int64_t slots = slot_count(c.slots);
+            hipLaunchKernelGGL((conv_kernel<T, decltype(w)::value, decltype(vec)::value>), grid(slots), dim3(256), 0, stream, c, across, blocks_across, (int)slots);
+        });
     });
 }
 
 hipError_t launch_conv_backward(int dt, const ConvCall& c, hipStream_t stream) {
     return with_kind(dt, c.width, [&](auto type, auto w) {
         typedef decltype(type) T;
-        const Grid g = grid_of(c.channels, sizeof(T));
         const int64_t slots = slot_count(c.slots), taps = (int64_t)c.channels * c.width;
-        hipLaunchKernelGGL((conv_backward_kernel<T, decltype(w)::value>), dim3(blocks_of(g, slots)), dim3(256), 0, stream, c, g.across, g.blocks_across, (int)slots);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = with_pieces<T>(c.channels, [&](auto vec, int across, int blocks_across, auto grid) {
+            hipLaunchKernelGGL((conv_backward_kernel<T, decltype(w)::value, decltype(vec)::value>), grid(slots), dim3(256), 0, stream, c, across, blocks_across, (int)slots);
+        });
         if (e != hipSuccess || c.parts_at == nullptr) return e;
         return launch_sum_parts(c.parts_at, slots, taps + c.channels, PartSums{{c.d_weight, c.d_bias, nullptr}, {taps, c.channels, 0}}, stream);
     });
@@ -282,9 +373,9 @@ hipError_t launch_conv_backward(int dt, const ConvCall& c, hipStream_t stream) {
 hipError_t launch_conv_step(int dt, const ConvCall& c, hipStream_t stream) {
     return with_kind(dt, c.width, [&](auto type, auto w) {
         typedef decltype(type) T;
-        const Grid g = grid_of(c.channels, sizeof(T));
-        hipLaunchKernelGGL((conv_step_kernel<T, decltype(w)::value>), dim3(blocks_of(g, c.slots.sequences)), dim3(256), 0, stream, c, g.across, g.blocks_across);
-        return hipGetLastError();
+        return with_pieces<T>(c.channels, [&](auto vec, int across, int blocks_across, auto grid) {
+            hipLaunchKernelGGL((conv_step_kernel<T, decltype(w)::value, decltype(vec)::value>), grid(c.slots.sequences), dim3(256), 0, stream, c, across, blocks_across);
+        });
     });
 }
 

@@ -85,18 +85,41 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) layer_norm_kernel(const
 
 // A workgroup walks over rows; a lane has the same channels of each, so it sums their parts of d_weight and d_bias in registers.  The next row is on
 // its way while this one is reduced.
+// Lanes of a row in the gradient, in whole waves: one piece each up to 256, two up to 512 lanes (which then take two waves a SIMD).
+constexpr int threads_of(int lpr) { return lpr < 192 ? 256 : lpr; }
+template <class F>
+hipError_t with_lanes_back(int channels, int elem, F&& f) {
+    using std::integral_constant;
+    const int pieces = (channels * elem + 15) / 16;
+    integral_constant<int, 1> one;
+    integral_constant<int, 2> two;
+    if (pieces <= 4) return f(integral_constant<int, 4>{}, one);
+    if (pieces <= 16) return f(integral_constant<int, 16>{}, one);
+    if (pieces <= 64) return f(integral_constant<int, 64>{}, one);
+    if (pieces <= 128) return f(integral_constant<int, 128>{}, one);
+    if (pieces <= 192) return f(integral_constant<int, 192>{}, one);
+    if (pieces <= 256) return f(integral_constant<int, 256>{}, one);
+    if (pieces <= 512) return f(integral_constant<int, 256>{}, two);
+    if (pieces <= 1024) return f(integral_constant<int, 512>{}, two);
+    if (pieces <= 2048) return f(integral_constant<int, 1024>{}, two);
+    if (pieces <= 4096) return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+    return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+}
+
 template <class T, int LPR, int PER>
-__global__ void __launch_bounds__(LPR > 256 ? LPR : 256) layer_norm_backward_kernel(const T* sum, const T* weight, const T* d_y, const T* d_sum, T* d_r,
+__global__ void __launch_bounds__(threads_of(LPR)) layer_norm_backward_kernel(const T* sum, const T* weight, const T* d_y, const T* d_sum, T* d_r,
                                                                                     float* parts, int64_t rows, int channels, float eps) {
-    constexpr int kVec = Traits<T>::kVec, kThreads = LPR > 256 ? LPR : 256, kRows = kThreads / LPR;
+    constexpr int kVec = Traits<T>::kVec, kThreads = threads_of(LPR), kRows = kThreads / LPR;
     typedef typename Traits<T>::Vec Vec;
-    __shared__ f32x2 room[2][2][kThreads / 64];
+    __shared__ f32x4 room[2][kThreads / 64];
     __shared__ float groups[kRows > 1 ? kThreads * PER * kVec : 1];
     const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
     const Vec zero = {};
-    // Rows of up to two pieces a lane stay in registers, and the next one is asked for before this one is reduced; longer ones, and the weight,
-    // are read again (out of L2) for each pass.
-    constexpr bool kHold = LPR < 1024 ? PER <= 2 : PER == 1;
+    constexpr int kIn = LPR < 64 ? LPR : 64;
+    auto add = [](float x, float y) { return x + y; };
+    // Rows of up to 1024 pieces stay in registers, and the next one is asked for before this one is reduced; longer ones, and the weight, are
+    // read again (out of L2) for each pass.
+    constexpr bool kHold = LPR < 1024;
     float dw[PER][kVec], db[PER][kVec];
 #pragma unroll
     for (int i = 0; i < PER; ++i)
@@ -131,11 +154,31 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) layer_norm_backward_ker
             for (int i = 0; i < PER; ++i) read(row, i, to.r[i], to.g[i], to.past[i]);
         }
     };
+    // how many channels each wave has of a row, and one over that
+    __shared__ f32x2 sizes[kThreads / 64];
+    float per_wave;
+    {
+        float own = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const Piece<kVec> pc(lane + i * LPR, channels);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) own += counts(pc, e, channels) ? 1.0f : 0.0f;
+        }
+        own = over_lanes<kIn>(own, add);
+        per_wave = own > 0.0f ? 1.0f / own : 0.0f;
+        if constexpr (LPR > 64) {
+            if ((threadIdx.x & 63) == 0) sizes[threadIdx.x >> 6] = f32x2{per_wave, own};
+            __syncthreads();
+        }
+    }
     auto step = [&](const Row& now, int64_t row, int turn) {
         auto piece = [&](int i, Vec& r, Vec& g, Vec& past, Vec& w) {
             if constexpr (kHold) r = now.r[i], g = now.g[i], past = now.past[i], w = kept[i];
             else read(row, i, r, g, past), w = weight_of(i);
         };
+        // Sums of r and of w dy, then of the squares of r's deviations and of their products with w dy: about the mean of what a wave has of the row, so
+        // that one exchange between the waves does.  About the row's mean they are more by the waves' means' own deviations.
         float total = 0.0f, pull = 0.0f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -148,9 +191,9 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) layer_norm_backward_ker
                 pull += e < pc.skip ? 0.0f : Traits<T>::to_f32(w[e]) * Traits<T>::to_f32(g[e]);
             }
         }
-        sum_row<LPR>(total, pull, room[turn][0]);
-        const float mean = total / (float)channels;
-        pull = pull / (float)channels;
+        total = over_lanes<kIn>(total, add);
+        pull = over_lanes<kIn>(pull, add);
+        float mean = total * per_wave;
         float squares = 0.0f, along = 0.0f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -164,7 +207,29 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) layer_norm_backward_ker
                 along = fmaf(d * Traits<T>::to_f32(w[e]), Traits<T>::to_f32(g[e]), along);
             }
         }
-        sum_row<LPR>(squares, along, room[turn][1]);
+        squares = over_lanes<kIn>(squares, add);
+        along = over_lanes<kIn>(along, add);
+        if constexpr (LPR > 64) {
+            constexpr int kWaves = LPR / 64;
+            if ((threadIdx.x & 63) == 0) room[turn][threadIdx.x >> 6] = f32x4{total, pull, squares, along};
+            __syncthreads();
+            total = pull = squares = along = 0.0f;
+            const int first = group * kWaves;       // of the row's waves
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                total += room[turn][first + w][0];
+                pull += room[turn][first + w][1];
+            }
+            mean = total / (float)channels;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const f32x4 v = room[turn][first + w];
+                const float off = sizes[w][0] * v[0] - mean;
+                squares += fmaf(sizes[w][1] * off, off, v[2]);
+                along += fmaf(off, v[1], v[3]);
+            }
+        }
+        pull = pull / (float)channels;
         const float rstd = 1.0f / sqrtf(squares / (float)channels + eps);
         const float back = along * rstd * rstd / (float)channels;       // of the deviation, in units of rstd
 #pragma unroll
@@ -317,6 +382,21 @@ hipError_t with_type(int dt, F&& f) {
 
 }  // namespace
 
+// Workgroups of the gradient: what the compute units work on at once, twelve waves of lanes with one piece and eight of those with two, so that their
+// parts of d_weight and d_bias are few.  us with 4 / 8 / 12 / 16 waves: 16384 x 1024 in bf16 44 / 35 / 32 / 32, 8192 x 1024 in fp32 49 / 34 / 30 / 30, 2048 x 768
+// 18 / 17 / 20 / 17; of two pieces, 8192 x 2051 in fp16, 66 / 50 / 57 / 58.
+int layer_norm_blocks(int64_t rows, int channels, int elem) {
+    int threads = 256, per_block = 1, waves = 12;
+    (void)with_lanes_back(channels, elem, [&](auto lpr, auto per) {
+        threads = threads_of(decltype(lpr)::value);
+        per_block = threads / decltype(lpr)::value;
+        waves = decltype(per)::value > 1 ? 8 : 12;
+        return hipSuccess;
+    });
+    const int64_t all = (rows + per_block - 1) / per_block, most = 256 * (waves * 64 > threads ? waves * 64 / threads : 1);
+    return (int)(all < most ? all : most);
+}
+
 hipError_t launch_layer_norm(int dt, const LayerNormCall& c, hipStream_t stream) {
     return with_type(dt, [&](auto type) {
         typedef decltype(type) T;
@@ -335,12 +415,12 @@ hipError_t launch_layer_norm_backward(int dt, const void* sum, const void* weigh
                                       float* d_bias, float* parts, int64_t rows, int channels, float eps, hipStream_t stream) {
     return with_type(dt, [&](auto type) {
         typedef decltype(type) T;
-        const int blocks = norm_backward_blocks(rows, channels, sizeof(T));
+        const int blocks = layer_norm_blocks(rows, channels, sizeof(T));
         const bool sums = d_weight != nullptr || d_bias != nullptr;
         // (no rows: nothing but sums of zeros)
-        const hipError_t e = blocks == 0 ? hipSuccess : with_lanes(lanes_for(channels, sizeof(T)), [&](auto lpr, auto per) {
-            constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value, kThreads = kLpr > 256 ? kLpr : 256;
-            hipLaunchKernelGGL((layer_norm_backward_kernel<T, kLpr, kPer>), dim3(blocks), dim3(kThreads), 0, stream, (const T*)sum, (const T*)weight,
+        const hipError_t e = blocks == 0 ? hipSuccess : with_lanes_back(channels, sizeof(T), [&](auto lpr, auto per) {
+            constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value;
+            hipLaunchKernelGGL((layer_norm_backward_kernel<T, kLpr, kPer>), dim3(blocks), dim3(threads_of(kLpr)), 0, stream, (const T*)sum, (const T*)weight,
                                (const T*)d_y, (const T*)d_sum, (T*)d_r, sums ? parts : nullptr, rows, channels, eps);
             return hipGetLastError();
         });

@@ -160,13 +160,13 @@ int conv_run(const msla_causal_conv& s, msla_dtype dt, int most, int64_t want) {
     while (run > 4 && s.tokens / run * pieces < 64 * want) run /= 2;
     return run;
 }
-constexpr int kConvRun = 16, kConvRunBackward = 64;
+constexpr int kConvRun = 32, kConvRunBackward = 64;
 constexpr int64_t kConvWaves = 2048;
 
 msla_status conv_slots(const msla_causal_conv& s, msla_dtype dt, bool backward, Slots* slots) {
     *slots = msla::slots_of(s.offsets, s.sequences, s.tokens, conv_run(s, dt, backward ? kConvRunBackward : kConvRun, kConvWaves));
-    // (a workgroup has 256 pieces of rows, or less where a row is no power of two of them)
-    return msla::slot_count(*slots) * (((int64_t)s.channels * (int64_t)elem_size(dt) + 15) / 16 * 2 + 256) / 256 >= kMostGroups ? MSLA_ERR_UNSUPPORTED : MSLA_OK;
+    // (a workgroup has 256 pieces of 16 or 8 bytes, or less where a row is no power of two of them)
+    return msla::slot_count(*slots) * (((int64_t)s.channels * (int64_t)elem_size(dt) + 7) / 8 * 2 + 256) / 256 >= kMostGroups ? MSLA_ERR_UNSUPPORTED : MSLA_OK;
 }
 
 ConvCall call_of(const msla_causal_conv& s, msla_rows x, const void* weight, const void* bias, const void* initial) {
@@ -380,7 +380,7 @@ msla_status msla_layer_norm_forward(const void* x, const void* residual, const v
 msla_status msla_layer_norm_backward_workspace_bytes(int64_t rows, int channels, msla_dtype dt, size_t* bytes) {
     if (bytes == nullptr) return MSLA_ERR_INVALID_ARG;
     const msla_status st = check_rows(rows, channels, 0.0f, dt);
-    if (st == MSLA_OK) *bytes = align_up((size_t)msla::norm_backward_blocks(rows, channels, (int)elem_size(dt)) * channels * 8);
+    if (st == MSLA_OK) *bytes = align_up((size_t)msla::layer_norm_blocks(rows, channels, (int)elem_size(dt)) * channels * 8);
     return st;
 }
 
@@ -395,7 +395,7 @@ msla_status msla_layer_norm_backward(const void* sum, const void* weight, const 
     if (rows > 0 && (sum == nullptr || d_y == nullptr || d_r == nullptr || d_r == sum)) return MSLA_ERR_INVALID_ARG;
     if ((d_weight != nullptr || d_bias != nullptr) && rows > 0) {
         if (workspace == nullptr || !aligned(workspace, 16)) return MSLA_ERR_INVALID_ARG;
-        if (workspace_bytes < (size_t)msla::norm_backward_blocks(rows, channels, (int)e) * channels * 8) return MSLA_ERR_WORKSPACE;
+        if (workspace_bytes < (size_t)msla::layer_norm_blocks(rows, channels, (int)e) * channels * 8) return MSLA_ERR_WORKSPACE;
     }
     return status_of(msla::launch_layer_norm_backward((int)dt, sum, weight, d_y, d_sum, d_r, d_weight, d_bias, (float*)workspace, rows, channels, eps,
                                                       (hipStream_t)stream));

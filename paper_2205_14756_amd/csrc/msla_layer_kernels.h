@@ -55,6 +55,7 @@ struct LayerNormCall {
     float eps;
 };
 hipError_t launch_layer_norm(int dt, const LayerNormCall& c, hipStream_t stream);
+int layer_norm_blocks(int64_t rows, int channels, int elem);       // workgroups of the gradient, and parts of d_weight and d_bias
 hipError_t launch_layer_norm_backward(int dt, const void* sum, const void* weight, const void* d_y, const void* d_sum, void* d_r, float* d_weight,
                                       float* d_bias, float* parts, int64_t rows, int channels, float eps, hipStream_t stream);
 

@@ -54,15 +54,40 @@ __device__ __forceinline__ void store_row(T* p, int at, int channels, const floa
     }
 }
 
+// The join of v over the LANES neighbours (a power of two, 64 at most) that it belongs to, to all of them: pairs, fours, eights, ... by data-parallel
+// moves, a tenth of the latency of a permutation through LDS.
+template <int CTRL>
+__device__ __forceinline__ float moved_by(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <int LANES, class F>
+__device__ __forceinline__ float over_lanes(float v, F&& join) {
+    if constexpr (LANES >= 2) v = join(v, moved_by<0xB1>(v));                       // lane ^ 1
+    if constexpr (LANES >= 4) v = join(v, moved_by<0x4E>(v));                       // lane ^ 2
+    if constexpr (LANES >= 8) v = join(v, moved_by<0x141>(v));                      // 7 - lane: the other four, which are alike
+    if constexpr (LANES >= 16) v = join(v, moved_by<0x128>(v));                     // lane ^ 8
+    if constexpr (LANES >= 32) {
+        const unsigned bits = __builtin_bit_cast(unsigned, v);
+        const auto r = __builtin_amdgcn_permlane16_swap(bits, bits, false, false);
+        const unsigned first = r[0], second = r[1];
+        v = join(__builtin_bit_cast(float, first), __builtin_bit_cast(float, second));
+    }
+    if constexpr (LANES >= 64) {
+        const unsigned bits = __builtin_bit_cast(unsigned, v);
+        const auto r = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+        const unsigned first = r[0], second = r[1];
+        v = join(__builtin_bit_cast(float, first), __builtin_bit_cast(float, second));
+    }
+    return v;
+}
+
 // two sums over the LPR lanes of a row; `room`: two pairs a wave, which take turns, so that one barrier does
 template <int LPR>
 __device__ __forceinline__ void sum_row(float& a, float& b, f32x2* room) {
     constexpr int kIn = LPR < 64 ? LPR : 64;
-#pragma unroll
-    for (int d = 1; d < kIn; d *= 2) {
-        a += __shfl_xor(a, d);
-        b += __shfl_xor(b, d);
-    }
+    auto add = [](float x, float y) { return x + y; };
+    a = over_lanes<kIn>(a, add);
+    b = over_lanes<kIn>(b, add);
     if constexpr (LPR > 64) {
         constexpr int kWaves = LPR / 64;
         if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = f32x2{a, b};
@@ -80,9 +105,7 @@ __device__ __forceinline__ void sum_row(float& a, float& b, f32x2* room) {
 // over the LPR lanes of a row; `room`: a float a wave
 template <int LPR, class F>
 __device__ __forceinline__ float over_row(float v, float* room, F&& join) {
-    constexpr int kIn = LPR < 64 ? LPR : 64;
-#pragma unroll
-    for (int d = 1; d < kIn; d *= 2) v = join(v, __shfl_xor(v, d));
+    v = over_lanes<LPR < 64 ? LPR : 64>(v, join);
     if constexpr (LPR > 64) {
         constexpr int kWaves = LPR / 64;
         const int wave = threadIdx.x >> 6;
