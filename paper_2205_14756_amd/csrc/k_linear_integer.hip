@@ -7,77 +7,89 @@ namespace msla {
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-constexpr int kTileK = 128;         // bytes of the contraction a stage
-
 __device__ __forceinline__ i32x4 mma(i32x4 c, i32x4 a, i32x4 b) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 
-// A workgroup has 128 rows x 128 outputs, a wave 64 x 64.  Tiles lie in LDS as rows of 128 bytes whose 16-byte pieces are XORed with the
-// row's number modulo 8, which gives the eight rows that a read serves together all banks.  Outputs are the rows of the matrix
-// instructions, dealt to pairs of blocks so that a lane ends up with eight neighbours of a row of y.
-template <class T>
+// A workgroup of four waves, two by two, has 32 NB rows x 32 OB outputs, a wave half of each: NB OB products of 16 x 16 for NB + OB operands out of LDS, whose
+// bandwidth is what large tiles are for.  A stage is 64 bytes of the contraction.  Tiles lie in LDS as rows of 64 bytes whose 16-byte pieces are XORed
+// with what the row's number has by 4 and by 16, which gives the sixteen rows that a read serves together all banks: rows of x follow each other, outputs, the rows of the
+// matrix instructions, come in fours, dealt to pairs of blocks so that a lane ends up with eight neighbours of a row of y.
+template <class T, int NB, int OB>
 __global__ void __launch_bounds__(256, 2) linear_integer_kernel(const char* x8, const float* x_scale, const char* w8, const float* w_scale, T* y,
-                                                                int64_t rows, int c_in, int c_out, int tiles_o) {
-    constexpr int kM = 128, kN = 128, kPieces = (kM + kN) * kTileK / 16 / 256;
-    __shared__ __align__(16) char lds[2][(kM + kN) * kTileK];
-    const int64_t n0 = (int64_t)(blockIdx.x / tiles_o) * kM;
-    const int o0 = blockIdx.x % tiles_o * kN;
+                                                                int64_t rows, int c_in, int c_out, int tiles_n, int tiles_o) {
+    constexpr int kM = 32 * NB, kN = 32 * OB, kStage = 64, kPieces = (kM + kN) * kStage / 16 / 256;
+    __shared__ __align__(16) char lds[2][(kM + kN) * kStage];
+    // neighbours on an XCD take tiles of kGroup rows of tiles in turn, so that what they read stays in its L2
+    constexpr int kGroup = 8;
+    const int id = (int)xcd_remap(blockIdx.x, gridDim.x), per_group = kGroup * tiles_o, first_n = id / per_group * kGroup;
+    const int in_group = min(kGroup, tiles_n - first_n), at = id % per_group;
+    const int64_t n0 = (int64_t)(first_n + at % in_group) * kM;
+    const int o0 = at / in_group * kN;
     const int wave = threadIdx.x >> 6, lane = lane_id(), x = lane & 15, q = lane >> 4;
-    const int wn = wave / 2 * 64, wo = wave % 2 * 64;
+    const int wn = wave / 2 * (kM / 2), wo = wave % 2 * (kN / 2);
+    auto swizzle = [](int row) { return (row / 4 + row / 16) % 4 * 16; };
+    // a thread's pieces of a stage: rows behind the last one are read from the last one (and not stored), pieces behind the contraction as zeros
+    const char* from[kPieces];
+    int park_at[kPieces];
+    const int piece = threadIdx.x % 4 * 16;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int row = threadIdx.x / 4 + i * 64;
+        from[i] = (row < kM ? x8 + min(n0 + row, rows - 1) * c_in : w8 + (int64_t)min(o0 + row - kM, c_out - 1) * c_in) + piece;
+        park_at[i] = row * kStage + (piece ^ swizzle(row));
+    }
     i32x4 hold[kPieces];
     auto load = [&](int k0) {
+        const bool in = k0 + piece < c_in;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int p = threadIdx.x + i * 256, row = p / 8, c = k0 + p % 8 * 16;
             hold[i] = i32x4{0, 0, 0, 0};
-            if (row < kM) {
-                if (n0 + row < rows && c < c_in) hold[i] = *(const i32x4*)(x8 + (n0 + row) * c_in + c);
-            } else {
-                if (o0 + row - kM < c_out && c < c_in) hold[i] = *(const i32x4*)(w8 + (int64_t)(o0 + row - kM) * c_in + c);
-            }
+            if (in) hold[i] = *(const i32x4*)(from[i] + k0);
         }
     };
-    auto park = [&](char* at) {
+    i32x4 acc[OB][NB];
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int p = threadIdx.x + i * 256, row = p / 8;
-            *(i32x4*)(at + row * kTileK + ((p % 8) ^ (row & 7)) * 16) = hold[i];
-        }
-    };
-    i32x4 acc[4][4];
+    for (int i = 0; i < OB; ++i)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    int a_at[OB], b_at[NB];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-    const int stages = (c_in + kTileK - 1) / kTileK;
+    for (int i = 0; i < OB; ++i) {
+        const int row = kM + wo + 32 * (i / 2) + 8 * (x >> 2) + 4 * (i & 1) + (x & 3);
+        a_at[i] = row * kStage + (16 * q ^ swizzle(row));
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const int row = wn + 16 * j + x;
+        b_at[j] = row * kStage + (16 * q ^ swizzle(row));
+    }
+    const int stages = (c_in + kStage - 1) / kStage;
     load(0);
     for (int s = 0; s < stages; ++s) {
-        char* at = lds[s & 1];
-        park(at);
+        char* tile = lds[s & 1];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) *(i32x4*)(tile + park_at[i]) = hold[i];
         __syncthreads();
-        if (s + 1 < stages) load((s + 1) * kTileK);
+        if (s + 1 < stages) load((s + 1) * kStage);
+        i32x4 a[OB], b[NB];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i32x4 a[4], b[4];
+        for (int i = 0; i < OB; ++i) a[i] = *(const i32x4*)(tile + a_at[i]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int ro = kM + wo + 32 * (i / 2) + 8 * (x >> 2) + 4 * (i & 1) + (x & 3), rn = wn + 16 * i + x;
-                a[i] = *(const i32x4*)(at + ro * kTileK + ((4 * h + q) ^ (ro & 7)) * 16);
-                b[i] = *(const i32x4*)(at + rn * kTileK + ((4 * h + q) ^ (rn & 7)) * 16);
-            }
+        for (int j = 0; j < NB; ++j) b[j] = *(const i32x4*)(tile + b_at[j]);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < NB; ++j)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = mma(acc[i][j], a[i], b[j]);
-        }
+            for (int i = 0; i < OB; ++i) acc[i][j] = mma(acc[i][j], a[i], b[j]);
+        __builtin_amdgcn_s_setprio(0);
         // (one barrier a stage: the buffer that the next stage fills was last read before this stage's barrier)
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < NB; ++j) {
         const int64_t n = n0 + wn + 16 * j + x;
         if (n >= rows) continue;
         const float sx = x_scale[n];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
+        for (int p = 0; p < OB / 2; ++p) {
             const int o = o0 + wo + 32 * p + 8 * q;
             if (o >= c_out) continue;
             T out[8];
@@ -96,7 +108,7 @@ __global__ void __launch_bounds__(256, 2) linear_integer_kernel(const char* x8, 
 template <class T, int BLOCKS>
 __global__ void __launch_bounds__(512) linear_integer_rows_kernel(const char* x8, const float* x_scale, const char* w8, const float* w_scale, T* y,
                                                                   int64_t rows, int c_in, int c_out) {
-    constexpr int kWaves = 8;
+    constexpr int kWaves = 8, kTileK = 128;
     __shared__ int sums[kWaves][BLOCKS][16][17];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), x = lane & 15, q = lane >> 4;
     const int tiles_o = c_out / 16, o0 = blockIdx.x % tiles_o * 16;
@@ -153,26 +165,58 @@ __global__ void __launch_bounds__(512) linear_integer_rows_kernel(const char* x8
     }
 }
 
+// Which kernel: by rounds of its workgroups over the 256 compute units, each of which takes so many ns a channel of the contraction, and no call less than
+// `least`.  Measured at 4096 channels, us with `rows` of 16 / 32 / 48 / 64, and with tiles of 64 x 64, 64 x 128, 128 x 128, 256 x 128: 16 rows into 4096 outputs 6.3 / 6.8 /
+// 7.4 / 7.9, 18.7, 24, 30, 46; 96 rows 24 / 18.8 / 17.4 / 18.6, 19.3, 24, 31, 48; 128 rows 31 / 24 / 23 / 21, 19.5, 25, 32, 50; 512 rows 114 / 87 / 79 / 74, 25.9, 30, 35,
+// 52; 1024 rows 226 / 171 / 154 / 144, 39.6, 36.3, 39.3, 56; 2048 rows -, 81, 64, 48, 60; 4096 rows into 8192 -, 293, 233, 176, 165; 64 rows into 16000 60 / 46 /
+// 50 / 40, 27.3, 33, 38, 50.
+struct Kind { int rows, outputs; float round, least; };
+constexpr Kind kKinds[] = {{16, 16, 0.95f, 1.54f}, {32, 16, 1.44f, 1.66f}, {48, 16, 1.86f, 2.1f}, {64, 16, 2.44f, 2.6f},
+                           {64, 64, 2.47f, 4.5f}, {64, 128, 4.0f, 5.6f}, {128, 128, 5.5f, 9.0f}, {256, 128, 10.1f, 14.0f}};
+int kind_of(int64_t rows, int c_out) {
+    int best = 0;
+    float least = 0.0f;
+    for (int k = 0; k < 8; ++k) {
+        const Kind& kind = kKinds[k];
+        const int64_t groups = (rows + kind.rows - 1) / kind.rows * ((c_out + kind.outputs - 1) / kind.outputs), rounds = (groups + 255) / 256;
+        const float all = (float)rounds * kind.round, cost = all > kind.least ? all : kind.least;
+        if (k == 0 || cost < least) best = k, least = cost;
+    }
+    return best;
+}
+
 template <class T>
 hipError_t linear_of(const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* y, int64_t rows, int c_in, int c_out,
                      hipStream_t stream) {
-    // (a launch has fewer than 2^32 threads: more rows than these, 128 at the most channels, go in several)
-    const int64_t most = (((int64_t)1 << 26) / (c_out / 16) + 1) / 128 * 128 + 128;
+    // (a launch has fewer than 2^32 threads: more rows than these, 256 at the most channels, go in several)
+    const int64_t most = (((int64_t)1 << 26) / (c_out / 16) + 1) / 256 * 256 + 256;
     const char* wp = (const char*)w8;
     for (int64_t from = 0; from < rows; from += most) {
         const int64_t n = rows - from < most ? rows - from : most;
         const char* xp = (const char*)x8 + from * c_in;
         T* yp = (T*)y + from * c_out;
         const float* xs = x_scale + from;
-        if (n <= 64) {
-            const dim3 grid((unsigned)((n + 63) / 64 * (c_out / 16))), threads(512);
-            if (n <= 16) hipLaunchKernelGGL((linear_integer_rows_kernel<T, 1>), grid, threads, 0, stream, xp, xs, wp, w_scale, yp, n, c_in, c_out);
-            else if (n <= 32) hipLaunchKernelGGL((linear_integer_rows_kernel<T, 2>), grid, threads, 0, stream, xp, xs, wp, w_scale, yp, n, c_in, c_out);
-            else if (n <= 48) hipLaunchKernelGGL((linear_integer_rows_kernel<T, 3>), grid, threads, 0, stream, xp, xs, wp, w_scale, yp, n, c_in, c_out);
-            else hipLaunchKernelGGL((linear_integer_rows_kernel<T, 4>), grid, threads, 0, stream, xp, xs, wp, w_scale, yp, n, c_in, c_out);
-        } else {
-            const int tiles_o = (c_out + 127) / 128;
-            hipLaunchKernelGGL((linear_integer_kernel<T>), dim3((unsigned)((n + 127) / 128 * tiles_o)), dim3(256), 0, stream, xp, xs, wp, w_scale, yp, n, c_in, c_out, tiles_o);
+        auto by_rows = [&](auto blocks) {
+            constexpr int kBlocks = decltype(blocks)::value;
+            hipLaunchKernelGGL((linear_integer_rows_kernel<T, kBlocks>), dim3((unsigned)((n + 16 * kBlocks - 1) / (16 * kBlocks) * (c_out / 16))), dim3(512), 0,
+                               stream, xp, xs, wp, w_scale, yp, n, c_in, c_out);
+        };
+        auto by_tiles = [&](auto nb, auto ob) {
+            constexpr int kM = 32 * decltype(nb)::value, kN = 32 * decltype(ob)::value;
+            const int tiles_n = (int)((n + kM - 1) / kM), tiles_o = (c_out + kN - 1) / kN;
+            hipLaunchKernelGGL((linear_integer_kernel<T, decltype(nb)::value, decltype(ob)::value>), dim3((unsigned)tiles_n * (unsigned)tiles_o), dim3(256), 0,
+                               stream, xp, xs, wp, w_scale, yp, n, c_in, c_out, tiles_n, tiles_o);
+        };
+        using std::integral_constant;
+        switch (kind_of(n, c_out)) {
+            case 0: by_rows(integral_constant<int, 1>{}); break;
+            case 1: by_rows(integral_constant<int, 2>{}); break;
+            case 2: by_rows(integral_constant<int, 3>{}); break;
+            case 3: by_rows(integral_constant<int, 4>{}); break;
+            case 4: by_tiles(integral_constant<int, 2>{}, integral_constant<int, 2>{}); break;
+            case 5: by_tiles(integral_constant<int, 2>{}, integral_constant<int, 4>{}); break;
+            case 6: by_tiles(integral_constant<int, 4>{}, integral_constant<int, 4>{}); break;
+            default: by_tiles(integral_constant<int, 8>{}, integral_constant<int, 4>{});
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
