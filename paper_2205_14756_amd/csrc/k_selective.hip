@@ -25,7 +25,6 @@
 namespace msla {
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -51,15 +50,15 @@ struct Piece {
     __device__ __forceinline__ float at(int s) const { return Traits<T>::to_f32(v[s]); }
 };
 
-// What a lane is: its channel, and its number among the L that share it.  A workgroup has CHANNELS of them, of one group.
-template <int L, int CHANNELS>
+// What a lane is: its channel, and its number among the L that share it.  A workgroup has kScanSlice of them, of one group.
+template <int L>
 struct Place {
     int channel, group, own;
     bool live;
     __device__ __forceinline__ Place(const ScanCall& c, int tile) {
-        const int per = c.channels / c.groups, tiles = (per + CHANNELS - 1) / CHANNELS;
+        const int per = c.channels / c.groups, tiles = (per + kScanSlice - 1) / kScanSlice;
         group = tile / tiles;
-        const int at = tile % tiles * CHANNELS + threadIdx.x / L;
+        const int at = tile % tiles * kScanSlice + threadIdx.x / L;
         live = at < per;
         channel = group * per + (live ? at : per - 1);
         own = threadIdx.x % L;
@@ -75,13 +74,7 @@ template <int S>
 __device__ __forceinline__ void load_states(float (&to)[S], const float* p) { __builtin_memcpy(to, __builtin_assume_aligned(p, 4), S * 4); }
 template <int S>
 __device__ __forceinline__ void store_states(float* p, const float (&from)[S]) { __builtin_memcpy(__builtin_assume_aligned(p, 4), from, S * 4); }
-// ... in LDS, where they lie on multiples of their own size
-template <int S>
-__device__ __forceinline__ void load_own(float (&to)[S], const float* p) { __builtin_memcpy(to, __builtin_assume_aligned(p, S >= 4 ? 16 : 8), S * 4); }
-template <int S>
-__device__ __forceinline__ void store_own(float* p, const float (&from)[S]) { __builtin_memcpy(__builtin_assume_aligned(p, S >= 4 ? 16 : 8), from, S * 4); }
-
-enum Pass { kWhole, kSums, kSumsBoth };
+enum Pass { kWhole, kSums, kMarks, kSumsBoth };
 
 // b and c of some tokens in fp32 in LDS, a state's tokens next to each other, so that a lane reads four tokens of a state at once.  The rows of the states that
 // the lanes of a channel read at once follow each other, four words beyond a multiple of the banks.
@@ -115,8 +108,9 @@ struct Shared {
     }
 };
 
-// kWhole: outputs and the last state.  kSums: a slot's state from zero and the sum of its steps.  kSumsBoth: and what it adds to the gradient of the
-// state in front of it.
+// kWhole: outputs and the last state.  kSums: a slot's state from zero and the sum of its steps.  For the gradient, the state in front of every L tokens
+// (a mark): kMarks, of sequences that are not cut; kSumsBoth, from zero, with the sum of the steps so far, what kSums has, and what the slot adds to the gradient of
+// the state in front of it.
 //
 // L lanes have a channel, with S states each: kScanSlice channels a workgroup, so that a compute unit has two of them, which do not wait at the
 // same time.  Tokens go by in tiles of 4 L.  A tile is loaded with a lane to a channel and four
@@ -125,16 +119,16 @@ struct Shared {
 template <class T, int L, int S, int PASS>
 __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int tiles) {
     constexpr int N = L * S;
-    typedef Shared<T, N, L, PASS != kSums> Tile;
+    constexpr bool kWithC = PASS == kWhole || PASS == kSumsBoth, kFromZero = PASS == kSums || PASS == kSumsBoth, kMark = PASS == kMarks || PASS == kSumsBoth;
+    typedef Shared<T, N, L, kWithC> Tile;
     constexpr int kTokens = Tile::kTokens, kRow = Tile::kRow;
     __shared__ __align__(16) typename Tile::Room room;
     __shared__ __align__(16) float own[PASS == kSumsBoth ? 3 : 2][kScanSlice][kRow];         // steps (outputs), steps times x, dy
     const int64_t slot_number = blockIdx.x / tiles;
     const Slot slot = slot_at(call.slots, (int)slot_number);
     if (!slot.used) return;
-    // (what a sequence's last slot leaves of a state nobody asks for, nor what its first one adds to the gradient in front of it)
-    if (PASS != kWhole && slot.last && (PASS == kSums || slot.first)) return;
-    const Place<L, kScanSlice> me(call, blockIdx.x % tiles);
+    if (PASS == kSums && slot.last) return;         // (what a sequence's last slot leaves of a state nobody asks for)
+    const Place<L> me(call, blockIdx.x % tiles);
     const int64_t state_at = (int64_t)me.channel * N + me.own * S, per_state = (int64_t)call.channels * N;
     float a[S], h[S];
     load_states(a, call.a + state_at);
@@ -142,10 +136,13 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
     for (int s = 0; s < S; ++s) a[s] = rate_of(a[s]);
 #pragma unroll
     for (int s = 0; s < S; ++s) h[s] = 0.0f;
-    if constexpr (PASS == kWhole) {
+    if constexpr (!kFromZero) {
         if (!slot.first) load_states(h, call.states_at + slot_number * per_state + state_at);
         else if (call.initial) load_states(h, call.initial + slot.sequence * per_state + state_at);
     }
+    int64_t mark = 0;
+    if constexpr (kMark) mark = first_slot(call.marks, slot.sequence) + (slot.from - slot.lo) / L;
+    float passed = 0.0f;                // the steps so far (kSumsBoth)
     float along[S], reach[S];           // exp(a * the steps so far), and the sum of that times c dy
 #pragma unroll
     for (int s = 0; s < S; ++s) along[s] = 1.0f, reach[s] = 0.0f;
@@ -167,7 +164,7 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
             auto load = [&](const TokenRows& r) { return *(const T*)((const char*)row<T>(r, t) + at_channel); };
             next.x[i] = load(call.x);
             next.delta[i] = load(call.delta);
-            if constexpr (PASS != kSums)
+            if constexpr (kWithC)
                 if (gated) next.gate[i] = load(call.gate);
             if constexpr (PASS == kSumsBoth) next.d_out[i] = load(call.d_out);
         }
@@ -188,7 +185,7 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
             add[i] = in ? full * x : 0.0f;
             past[i] = skip * x;
             through[i] = 1.0f;
-            if constexpr (PASS != kSums) {
+            if constexpr (kWithC) {
                 if (gated) {
                     const float z = Traits<T>::to_f32(next.gate[i]);
                     through[i] = z * sigmoid_of(z);
@@ -207,18 +204,28 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
             fetch(t0 + kTokens);
         }
         const int channel_at = threadIdx.x / L;
-#pragma unroll
+#pragma unroll (PASS == kWhole ? 4 : 1)
         for (int block = 0; block < kTokens; block += L) {
+            if constexpr (kMark) {
+                if (t0 + block <= last && me.live) {
+                    store_states(call.marks_at + mark * per_state + state_at, h);
+                    if (PASS == kSumsBoth && me.own == 0) call.mark_steps_at[mark * call.channels + me.channel] = passed;
+                }
+                ++mark;
+            }
             float sums[L];
 #pragma unroll
             for (int f = 0; f < L; f += 4) {
                 const f32x4 ti = *(const f32x4*)&own[0][channel_at][block + f], ui = *(const f32x4*)&own[1][channel_at][block + f];
                 f32x4 dyi, b[S], c[S];
-                if constexpr (PASS == kSumsBoth) dyi = *(const f32x4*)&own[2][channel_at][block + f];
+                if constexpr (PASS == kSumsBoth) {
+                    dyi = *(const f32x4*)&own[2][channel_at][block + f];
+                    passed += (ti[0] + ti[1]) + (ti[2] + ti[3]);
+                }
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
                     b[s] = *(const f32x4*)&room[0][Tile::row_of(me.own, s)][block + f];
-                    if constexpr (PASS != kSums) c[s] = *(const f32x4*)&room[1][Tile::row_of(me.own, s)][block + f];
+                    if constexpr (kWithC) c[s] = *(const f32x4*)&room[1][Tile::row_of(me.own, s)][block + f];
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -251,7 +258,7 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
     }
     if constexpr (PASS == kWhole) {
         if (call.final_state && slot.last && me.live) store_states(call.final_state + slot.sequence * per_state + state_at, h);
-    } else {
+    } else if constexpr (kFromZero) {
         const int64_t at = slot_number * per_state + state_at;
         if (me.live) {
             store_states(call.states_at + at, h);
@@ -308,198 +315,240 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanCall call, int block
     if constexpr (BOTH) join(call.d_states_at, call.d_final ? call.d_final[b * per_state + at] : 0.0f, [&](int64_t k) { return count - 1 - k; });
 }
 
-// A slot of the gradient.  K tokens a window, whose states stay in registers (K * S of them).
-template <class T, int S>
-struct Window {
-    static constexpr int kTokens = S <= 4 ? 16 : 64 / S, kBlocks = kTokens / 4;
-    T x[kBlocks], delta[kBlocks], gate[kBlocks], d_out[kBlocks];
-};
-
-template <class T, int S>
-__global__ void __launch_bounds__(kThreads) scan_backward_kernel(ScanCall call, int tiles) {
-    constexpr int N = 4 * S, K = Window<T, S>::kTokens, kBlocks = K / 4, kRun = N <= 32 ? 64 : 32, kWindows = kRun / K, kShared = K * 2 * N;
-    // the states at the windows' starts, a lane's own; b and c of the slot in fp32; a window's sums over the channels of a wave
-    __shared__ __align__(16) float marks[kWindows][kThreads * S];
-    __shared__ __align__(16) float shared_bc[2][kRun * N];
-    __shared__ float sums[2][kWaves][kShared];
+// A slot of the gradient, with the scan's lanes and tiles, the last tile first.  Of every L tokens the states come from their mark, stay in registers, and
+// the state's gradient goes back over them.
+template <class T, int L, int S>
+__global__ void __launch_bounds__(kScanSlice * L) scan_backward_kernel(ScanCall call, int tiles) {
+    constexpr int N = L * S, kThreads = kScanSlice * L, kWaves = kThreads / 64, kSums = L * 2 * N;
+    typedef Shared<T, N, L, true> Tile;
+    constexpr int kTokens = Tile::kTokens, kRow = Tile::kRow;
+    // a window's sums over the channels of a wave: one place, or two that take turns, which save a barrier
+    constexpr int kTurns = S == 1 ? 2 : 1;
+    __shared__ __align__(16) typename Tile::Room room;
+    __shared__ __align__(16) float own[3][kScanSlice][kRow];        // steps (y), steps times x (e), dy (the sum of w a)
+    __shared__ float sums[kTurns][kWaves][kSums];
     const int64_t slot_number = blockIdx.x / tiles;
-    const int tile = blockIdx.x % tiles;
     const Slot slot = slot_at(call.slots, (int)slot_number);
-    const Place<4, kScanTile> me(call, tile);
+    const Place<L> me(call, blockIdx.x % tiles);
     const int64_t state_at = (int64_t)me.channel * N + me.own * S, per_state = (int64_t)call.channels * N;
     float* parts = call.parts_at + slot_number * (per_state + 2 * call.channels);
-    float d_a[S], carry[S], h[S];
+    float d_a[S], carry[S], a[S], start[S];
 #pragma unroll
-    for (int s = 0; s < S; ++s) d_a[s] = carry[s] = h[s] = 0.0f;
+    for (int s = 0; s < S; ++s) d_a[s] = carry[s] = start[s] = 0.0f;
+    load_states(a, call.a + state_at);
+#pragma unroll
+    for (int s = 0; s < S; ++s) a[s] = rate_of(a[s]);
+    // (lanes without a channel read another's values, and must not add even an infinity to sums)
+    if (me.live) {
+        if (!slot.last) {
+            if (slot.used) load_states(carry, call.d_states_at + slot_number * per_state + state_at);
+        } else if (call.d_final) {
+            load_states(carry, call.d_final + slot.sequence * per_state + state_at);
+        }
+        if (call.cut) {             // (marks are of a slot from zero: what it started from comes on top)
+            if (!slot.first) {
+                if (slot.used) load_states(start, call.states_at + slot_number * per_state + state_at);
+            } else if (call.initial) {
+                load_states(start, call.initial + slot.sequence * per_state + state_at);
+            }
+        }
+    }
+    const int last = slot.until - 1;
+
+    // a lane's channel as tiles are loaded, and its four tokens of a tile
+    const int per = call.channels / call.groups, first = blockIdx.x % tiles % ((per + kScanSlice - 1) / kScanSlice) * kScanSlice;
+    const int lane = threadIdx.x % kScanSlice, run = threadIdx.x / kScanSlice, mine = 4 * run;
+    const bool live = first + lane < per;
+    const int channel = me.group * per + (live ? first + lane : per - 1);
+    const unsigned at_channel = channel * (unsigned)sizeof(T);
+    const bool gated = call.gate.p != nullptr, soft = call.softplus != 0;
+    const float bias = call.bias ? call.bias[channel] : 0.0f, skip = call.skip ? call.skip[channel] : 0.0f;
     float d_skip = 0.0f, d_bias = 0.0f;
-    if (slot.used) {
-        const bool gated = call.gate.p != nullptr, soft = call.softplus != 0;
-        float a[S];
-        load_states(a, call.a + state_at);
+    struct Tokens { T x[4], delta[4], gate[4], d_out[4]; } next;
+    Tile tile;
+    auto fetch = [&](int t0) {
+        tile.fetch(call, me.group, t0, last);
 #pragma unroll
-        for (int s = 0; s < S; ++s) a[s] = rate_of(a[s]);
-        const float bias = call.bias ? call.bias[me.channel] : 0.0f, skip = call.skip ? call.skip[me.channel] : 0.0f;
-        if (!slot.first) load_states(h, call.states_at + slot_number * per_state + state_at);
-        else if (call.initial) load_states(h, call.initial + slot.sequence * per_state + state_at);
-        if (!slot.last) load_states(carry, call.d_states_at + slot_number * per_state + state_at);
-        else if (call.d_final) load_states(carry, call.d_final + slot.sequence * per_state + state_at);
-        if (!me.live) {                 // (lanes without a channel read another's values, and must not add even an infinity to sums)
+        for (int i = 0; i < 4; ++i) {
+            const int t = min(t0 + mine + i, last);
+            auto load = [&](const TokenRows& r) { return *(const T*)((const char*)row<T>(r, t) + at_channel); };
+            next.x[i] = load(call.x);
+            next.delta[i] = load(call.delta);
+            if (gated) next.gate[i] = load(call.gate);
+            next.d_out[i] = load(call.d_out);
+        }
+    };
+    const int64_t marks = first_slot(call.marks, slot.sequence);
+    const int channel_at = threadIdx.x / L, wave_lane = threadIdx.x & 63;
+    const int behind = slot.used ? (slot.until - slot.from + kTokens - 1) / kTokens : 0;
+    // the mark of the window in front of the one that is worked on
+    float ahead[S], passed = 0.0f;
+    auto ask = [&](int t) {
+        const int64_t at = marks + (max(t, slot.from) - slot.lo) / L;
+        load_states(ahead, call.marks_at + at * per_state + state_at);
+        if (call.cut) passed = call.mark_steps_at[at * call.channels + me.channel];
+    };
+    if (behind > 0) {
+        fetch(slot.from + (behind - 1) * kTokens);
+        ask(slot.from + (last - slot.from) / L * L);
+    }
+    int turn = 0;
+    for (int n = behind - 1; n >= 0; --n) {
+        const int t0 = slot.from + n * kTokens;
+        const Tokens now = next;
+        f32x4 step, add, dy;
 #pragma unroll
-            for (int s = 0; s < S; ++s) carry[s] = h[s] = 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            const bool in = t0 + mine + i <= last && live;         // (others: a step of nothing, and no gradient)
+            const float x = Traits<T>::to_f32(now.x[i]), pre = Traits<T>::to_f32(now.delta[i]) + bias, full = soft ? softplus_of(pre) : pre;
+            float back = Traits<T>::to_f32(now.d_out[i]);
+            if (gated) {
+                const float z = Traits<T>::to_f32(now.gate[i]);
+                back *= z * sigmoid_of(z);
+            }
+            step[i] = in ? full : 0.0f;
+            add[i] = in ? full * x : 0.0f;
+            dy[i] = in ? back : 0.0f;
         }
-        const int count = slot.until - slot.from, last = slot.until - 1, windows = (count + K - 1) / K;
-        for (int e = threadIdx.x; e < windows * K * N; e += kThreads) {
-            const int t = e / N, n = e % N;
-            const bool in = t < count;          // (zeros behind the last token)
-            shared_bc[0][e] = in ? Traits<T>::to_f32(row<T>(call.b, slot.from + t)[me.group * N + n]) : 0.0f;
-            shared_bc[1][e] = in ? Traits<T>::to_f32(row<T>(call.c, slot.from + t)[me.group * N + n]) : 0.0f;
-        }
+        *(f32x4*)&own[0][lane][mine] = step;
+        *(f32x4*)&own[1][lane][mine] = add;
+        *(f32x4*)&own[2][lane][mine] = dy;
+        tile.park(room);
         __syncthreads();
-        auto of_shared = [&](int which, int t) {
-            struct { float v[S]; } r;
-            load_own(r.v, &shared_bc[which][t * N + me.own * S]);
-            return r;
-        };
-        // the state at each window's start
-        for (int w = 0; w < windows; ++w) {
-            store_own(&marks[w][threadIdx.x * S], h);
-            if (w + 1 == windows) break;
-            float step[kBlocks], add[kBlocks];
+        if (n > 0) fetch(t0 - kTokens);
+#pragma unroll 1
+        for (int base = kTokens - L; base >= 0; base -= L) {
+            const int from = t0 + base;
+            if (from > last) continue;
+            float mark[S];
 #pragma unroll
-            for (int q = 0; q < kBlocks; ++q) {
-                const int t = min(slot.from + w * K + 4 * q + me.own, last);
-                const float pre = Traits<T>::to_f32(row<T>(call.delta, t)[me.channel]) + bias;
-                step[q] = soft ? softplus_of(pre) : pre;
-                add[q] = step[q] * Traits<T>::to_f32(row<T>(call.x, t)[me.channel]);
+            for (int s = 0; s < S; ++s) {
+                mark[s] = call.cut ? fmaf(exp2_of(passed * a[s]), start[s], ahead[s]) : ahead[s];
+                if (!me.live) mark[s] = 0.0f;
             }
-            static_for<0, K>([&](auto which) {
-                constexpr int t = decltype(which)::value, q = t / 4, i = t % 4;
-                const auto b = of_shared(0, w * K + t);
-                const float ti = of_four<i>(step[q]), ui = of_four<i>(add[q]);
+            ask(from - L);
+            float states[L][S], keeps[S == 1 ? L : 1][S], sum[L], sum2[L];
+            float h[S];
 #pragma unroll
-                for (int s = 0; s < S; ++s) h[s] = fmaf(exp2_of(ti * a[s]), h[s], ui * b.v[s]);
-            });
-        }
-        Window<T, S> now, next;
-        auto fetch = [&](Window<T, S>& to, int w) {
+            for (int s = 0; s < S; ++s) h[s] = mark[s];
 #pragma unroll
-            for (int q = 0; q < kBlocks; ++q) {
-                const int t = min(slot.from + w * K + 4 * q + me.own, last);
-                to.x[q] = row<T>(call.x, t)[me.channel];
-                to.delta[q] = row<T>(call.delta, t)[me.channel];
-                to.d_out[q] = row<T>(call.d_out, t)[me.channel];
-                if (gated) to.gate[q] = row<T>(call.gate, t)[me.channel];
-            }
-        };
-        if (windows > 0) fetch(now, windows - 1);
-        for (int w = windows - 1; w >= 0; --w) {
-            if (w > 0) fetch(next, w - 1);
-            float step[kBlocks], add[kBlocks], dy[kBlocks];
+            for (int f = 0; f < L; f += 4) {
+                const f32x4 ti = *(const f32x4*)&own[0][channel_at][base + f], ui = *(const f32x4*)&own[1][channel_at][base + f];
+                f32x4 b[S], c[S];
 #pragma unroll
-            for (int q = 0; q < kBlocks; ++q) {
-                const bool in = w * K + 4 * q + me.own < count && me.live;
-                const float pre = Traits<T>::to_f32(now.delta[q]) + bias, x = Traits<T>::to_f32(now.x[q]);
-                step[q] = in ? (soft ? softplus_of(pre) : pre) : 0.0f;
-                add[q] = in ? step[q] * x : 0.0f;
-                dy[q] = in ? Traits<T>::to_f32(now.d_out[q]) : 0.0f;
-            }
-            float states[K][S];             // behind each token
-            load_own(h, &marks[w][threadIdx.x * S]);
-            float before[S];
-#pragma unroll
-            for (int s = 0; s < S; ++s) before[s] = h[s];
-            static_for<0, kBlocks>([&](auto block) {
-                constexpr int q = decltype(block)::value;
-                float y4[4];
-                static_for<0, 4>([&](auto which) {
-                    constexpr int i = decltype(which)::value, t = 4 * q + i;
-                    const auto b = of_shared(0, w * K + t);
-                    const float ti = of_four<i>(step[q]), ui = of_four<i>(add[q]);
-#pragma unroll
-                    for (int s = 0; s < S; ++s) states[t][s] = h[s] = fmaf(exp2_of(ti * a[s]), h[s], ui * b.v[s]);
-                    y4[i] = 0.0f;
-                    if (gated) {
-                        const auto c = of_shared(1, w * K + t);
-#pragma unroll
-                        for (int s = 0; s < S; ++s) y4[i] = fmaf(c.v[s], h[s], y4[i]);
-                    }
-                });
-                if (gated) {
-                    const float z = Traits<T>::to_f32(now.gate[q]), x = Traits<T>::to_f32(now.x[q]);
-                    const float y = fmaf(skip, x, deal<4>(y4, me.own)), g = sigmoid_of(z);
-                    const int t = w * K + 4 * q + me.own;
-                    if (t < count && me.live)
-                        row_out<T>(call.d_gate, slot.from + t)[me.channel] = Traits<T>::from_f32(dy[q] * y * (g * fmaf(z, 1.0f - g, 1.0f)));
-                    dy[q] = t < count && me.live ? dy[q] * (z * g) : 0.0f;
+                for (int s = 0; s < S; ++s) {
+                    b[s] = *(const f32x4*)&room[0][Tile::row_of(me.own, s)][base + f];
+                    c[s] = *(const f32x4*)&room[1][Tile::row_of(me.own, s)][base + f];
                 }
-            });
-            float(&room)[kWaves][kShared] = sums[w & 1];
-            static_for<0, kBlocks>([&](auto back) {
-                constexpr int q = kBlocks - 1 - decltype(back)::value;
-                float e4[4], w4[4], both[4][S / 2];
-                static_for<0, 4>([&](auto behind) {
-                    constexpr int i = 3 - decltype(behind)::value, t = 4 * q + i;
-                    const auto b = of_shared(0, w * K + t), c = of_shared(1, w * K + t);
-                    const float ti = of_four<i>(step[q]), ui = of_four<i>(add[q]), dyi = of_four<i>(dy[q]);
-                    float e = 0.0f, along = 0.0f, r[S];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float y = 0.0f;
 #pragma unroll
                     for (int s = 0; s < S; ++s) {
-                        const float dh = fmaf(c.v[s], dyi, carry[s]);
-                        r[s] = halve32(dh * ui, dyi * states[t][s]);
-                        e = fmaf(dh, b.v[s], e);
-                        carry[s] = exp2_of(ti * a[s]) * dh;
-                        const float through = carry[s] * (t > 0 ? states[t > 0 ? t - 1 : 0][s] : before[s]);
-                        d_a[s] = fmaf(through, ti, d_a[s]);
-                        along = fmaf(through, a[s], along);
+                        const float keep = exp2_of(ti[i] * a[s]);
+                        if constexpr (S == 1) keeps[f + i][s] = keep;
+                        states[f + i][s] = h[s] = fmaf(keep, h[s], ui[i] * b[s][i]);
+                        y = s == 0 ? c[s][i] * h[s] : fmaf(c[s][i], h[s], y);
                     }
-#pragma unroll
-                    for (int p = 0; p < S / 2; ++p) both[i][p] = halve16(r[2 * p], r[2 * p + 1]);
-                    e4[i] = e;
-                    w4[i] = along;
-                });
-                // sums over the channels of the wave: a lane ends up with those of b or c (its 32), an odd or even state (its 16), one token of the
-                // four (its 8 and 4)
-                const int lane = threadIdx.x & 63;
-                const bool mine8 = lane & 8, mine4 = lane & 4;
-#pragma unroll
-                for (int p = 0; p < S / 2; ++p) {
-                    const float lower = halve8(both[0][p], both[2][p], lane), higher = halve8(both[1][p], both[3][p], lane);
-                    const float v = halve4(lower, higher, lane);
-                    const int token = 4 * q + (mine8 ? 2 : 0) + (mine4 ? 1 : 0);
-                    room[threadIdx.x >> 6][token * 2 * N + (lane & 32 ? N : 0) + me.own * S + 2 * p + (lane & 16 ? 1 : 0)] = v;
+                    sum[f + i] = y;
                 }
-                const float e = deal<4>(e4, me.own), along = kLn2 * deal<4>(w4, me.own);
-                const float x = Traits<T>::to_f32(now.x[q]);
-                const int t = w * K + 4 * q + me.own;
-                float d_step = fmaf(x, e, along);
-                if (soft) d_step *= sigmoid_of(Traits<T>::to_f32(now.delta[q]) + bias);
-                if (t < count && me.live) {
-                    row_out<T>(call.d_x, slot.from + t)[me.channel] = Traits<T>::from_f32(fmaf(step[q], e, skip * dy[q]));
-                    row_out<T>(call.d_delta, slot.from + t)[me.channel] = Traits<T>::from_f32(d_step);
-                    d_skip = fmaf(dy[q], x, d_skip);
-                    d_bias += d_step;
-                }
-            });
-            __syncthreads();
-            // (one barrier a window: the room that the next one fills was last read before this one)
-            const int tokens = min(K, count - w * K);
-            for (int e = threadIdx.x; e < tokens * 2 * N; e += kThreads) {
-                float v = room[0][e];
-#pragma unroll
-                for (int k = 1; k < kWaves; ++k) v += room[k][e];
-                call.shared_at[((int64_t)tile * call.slots.tokens + slot.from + w * K) * (2 * N) + e] = v;
+                if constexpr (S > 1) __builtin_amdgcn_sched_barrier(0);
             }
-            now = next;
+            const float y = gated ? deal<L>(sum, me.own) : 0.0f;
+            float(&place)[kSums] = sums[turn][threadIdx.x >> 6];
+#pragma unroll
+            for (int f = L - 4; f >= 0; f -= 4) {
+                const f32x4 ti = *(const f32x4*)&own[0][channel_at][base + f], ui = *(const f32x4*)&own[1][channel_at][base + f];
+                const f32x4 dyi = *(const f32x4*)&own[2][channel_at][base + f];
+                f32x4 b[S], c[S];
+                float both[4][S];
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    b[s] = *(const f32x4*)&room[0][Tile::row_of(me.own, s)][base + f];
+                    c[s] = *(const f32x4*)&room[1][Tile::row_of(me.own, s)][base + f];
+                }
+#pragma unroll
+                for (int i = 3; i >= 0; --i) {
+                    const int t = f + i;
+                    float e = 0.0f, along = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < S; ++s) {
+                        const float dh = fmaf(c[s][i], dyi[i], carry[s]);
+                        both[i][s] = halve32(dh * ui[i], dyi[i] * states[t][s]);
+                        e = s == 0 ? dh * b[s][i] : fmaf(dh, b[s][i], e);
+                        const float keep = S == 1 ? keeps[S == 1 ? t : 0][s] : exp2_of(ti[i] * a[s]);
+                        carry[s] = keep * dh;
+                        const float through = carry[s] * (t > 0 ? states[t > 0 ? t - 1 : 0][s] : mark[s]);
+                        d_a[s] = fmaf(through, ti[i], d_a[s]);
+                        along = s == 0 ? through * a[s] : fmaf(through, a[s], along);
+                    }
+                    sum[t] = e;
+                    sum2[t] = along;
+                }
+                // sums over the channels of the wave: a lane ends up with those of b or of c (its 32), of one token of two (its 16), or of four (its 8)
+                const int of = (wave_lane & 32 ? N : 0) + me.own * S;
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    const float lower = halve16(both[0][s], both[1][s]), higher = halve16(both[2][s], both[3][s]);
+                    const int odd = wave_lane & 16 ? 1 : 0;
+                    if constexpr (L == 16) {
+                        place[(f + odd) * 2 * N + of + s] = lower;
+                        place[(f + 2 + odd) * 2 * N + of + s] = higher;
+                    } else {
+                        place[(f + odd + (wave_lane & 8 ? 2 : 0)) * 2 * N + of + s] = halve8(lower, higher, wave_lane);
+                    }
+                }
+                if constexpr (S > 1) __builtin_amdgcn_sched_barrier(0);
+            }
+            const float e = deal<L>(sum, me.own), along = deal<L>(sum2, me.own);
+            own[0][channel_at][base + me.own] = y;
+            own[1][channel_at][base + me.own] = e;
+            own[2][channel_at][base + me.own] = along;
+            __syncthreads();
+            const int count = min(L, last - from + 1) * 2 * N;
+            float* to = call.shared_at + ((int64_t)(blockIdx.x % tiles) * call.slots.tokens + from) * (2 * N);
+            for (int k = threadIdx.x; k < count; k += kThreads) {
+                float v = sums[turn][0][k];
+#pragma unroll
+                for (int o = 1; o < kWaves; ++o) v += sums[turn][o][k];
+                to[k] = v;
+            }
+            if constexpr (kTurns == 2) turn ^= 1;
+            else __syncthreads();
         }
-        if (slot.first && call.d_initial && me.live) store_states(call.d_initial + slot.sequence * per_state + state_at, carry);
+        const f32x4 y = *(const f32x4*)&own[0][lane][mine], e = *(const f32x4*)&own[1][lane][mine], along = *(const f32x4*)&own[2][lane][mine];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = t0 + mine + i;
+            if (t > last || !live) continue;
+            const float x = Traits<T>::to_f32(now.x[i]);
+            float d_step = fmaf(x, e[i], kLn2 * along[i]);
+            if (soft) d_step *= sigmoid_of(Traits<T>::to_f32(now.delta[i]) + bias);
+            auto put = [&](const TokenRows& r, float v) { *(T*)((char*)row_out<T>(r, t) + at_channel) = Traits<T>::from_f32(v); };
+            put(call.d_x, fmaf(step[i], e[i], skip * dy[i]));
+            put(call.d_delta, d_step);
+            if (gated) {
+                const float z = Traits<T>::to_f32(now.gate[i]), open = sigmoid_of(z);
+                put(call.d_gate, Traits<T>::to_f32(now.d_out[i]) * fmaf(skip, x, y[i]) * (open * fmaf(z, 1.0f - open, 1.0f)));
+            }
+            d_skip = fmaf(dy[i], x, d_skip);
+            d_bias += d_step;
+        }
     }
-    d_skip = sum_over<4>(d_skip);
-    d_bias = sum_over<4>(d_bias);
-    if (!me.live) return;
-    store_states(parts + state_at, d_a);
-    if (me.own == 0) {
-        parts[per_state + me.channel] = d_skip;
-        parts[per_state + call.channels + me.channel] = d_bias;
+    if (slot.used && slot.first && call.d_initial && me.live) store_states(call.d_initial + slot.sequence * per_state + state_at, carry);
+    if (me.live) store_states(parts + state_at, d_a);
+    // (each has the sums of its own tokens)
+    own[0][lane][run] = d_skip;
+    own[1][lane][run] = d_bias;
+    __syncthreads();
+    if (run == 0 && live) {
+#pragma unroll
+        for (int r = 1; r < L; ++r) {
+            d_skip += own[0][lane][r];
+            d_bias += own[1][lane][r];
+        }
+        parts[per_state + channel] = d_skip;
+        parts[per_state + call.channels + channel] = d_bias;
     }
 }
 
@@ -602,7 +651,7 @@ hipError_t launch_scan_forward(int dt, const ScanCall& c, hipStream_t stream) {
         typedef decltype(type) T;
         return with_lanes(c.states, [&](auto l, auto s) {
             constexpr int L = decltype(l)::value, S = decltype(s)::value;
-            const int tiles = scan_tiles(c.channels, c.groups, kScanSlice);
+            const int tiles = scan_tiles(c.channels, c.groups);
             const dim3 grid((unsigned)(slot_count(c.slots) * tiles)), threads(kScanSlice * L);
             if (c.cut) {
                 hipLaunchKernelGGL((scan_kernel<T, L, S, kSums>), grid, threads, 0, stream, c, tiles);
@@ -619,23 +668,17 @@ hipError_t launch_scan_forward(int dt, const ScanCall& c, hipStream_t stream) {
 hipError_t launch_scan_backward(int dt, const ScanCall& c, hipStream_t stream) {
     return with_type(dt, [&](auto type) {
         typedef decltype(type) T;
-        return with_states(c.states, [&](auto s) {
-            constexpr int S = decltype(s)::value;
-            const int tiles = scan_tiles(c.channels, c.groups, kScanTile);
+        return with_lanes(c.states, [&](auto l, auto s) {
+            constexpr int L = decltype(l)::value, S = decltype(s)::value;
+            const int tiles = scan_tiles(c.channels, c.groups);
             const int64_t slots = slot_count(c.slots);
-            const dim3 grid((unsigned)(slots * tiles)), threads(kThreads);
-            hipError_t e = hipSuccess;
-            if (c.cut) {
-                e = with_lanes(c.states, [&](auto l, auto per) {
-                    constexpr int L = decltype(l)::value;
-                    const int slices = scan_tiles(c.channels, c.groups, kScanSlice);
-                    hipLaunchKernelGGL((scan_kernel<T, L, decltype(per)::value, kSumsBoth>), dim3((unsigned)(slots * slices)), dim3(kScanSlice * L), 0, stream, c, slices);
-                    return hipGetLastError();
-                });
-                if (e == hipSuccess) e = join<true>(c, stream);
-                if (e != hipSuccess) return e;
-            }
-            hipLaunchKernelGGL((scan_backward_kernel<T, S>), grid, threads, 0, stream, c, tiles);
+            const dim3 grid((unsigned)(slots * tiles)), threads(kScanSlice * L);
+            if (c.cut) hipLaunchKernelGGL((scan_kernel<T, L, S, kSumsBoth>), grid, threads, 0, stream, c, tiles);
+            else hipLaunchKernelGGL((scan_kernel<T, L, S, kMarks>), grid, threads, 0, stream, c, tiles);
+            hipError_t e = hipGetLastError();
+            if (e == hipSuccess && c.cut) e = join<true>(c, stream);
+            if (e != hipSuccess) return e;
+            hipLaunchKernelGGL((scan_backward_kernel<T, L, S>), grid, threads, 0, stream, c, tiles);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
             const int64_t shared = (int64_t)c.slots.tokens * c.groups * c.states * 2;

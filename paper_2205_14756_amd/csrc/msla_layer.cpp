@@ -60,31 +60,24 @@ struct ScanPlan {
     Slots slots;
     bool cut;
     int64_t count;                  // slots
-    size_t states_at, d_states_at, steps_at, parts_at, shared_at, bytes;
+    Slots marks;
+    size_t states_at, d_states_at, steps_at, marks_at, mark_steps_at, parts_at, shared_at, bytes;
 };
 
-// How long slots are.  The gradient's are as long as its states find room in LDS.  The forward pass has workgroups two of which fill a compute unit, and a sequence
-// that is cut does 1.65 times its work and two more launches.  Equal sequences are cut into as many slots as leave every unit two workgroups at most, if
-// that is worth it; packed ones, whose lengths nobody knows here, so that the units have about four (those that are no longer than that run whole).
+// How long slots are.  Two workgroups fill a compute unit.  A sequence that is cut does 1.65 times its work, in the gradient 1.2 times, and two (one) more
+// launches.  Equal sequences are cut into as many slots as leave every unit two workgroups at most, if that is worth it; packed ones, whose lengths nobody
+// knows here, so that the units have about four (those that are no longer than that run whole).
 msla_status plan_of(const msla_selective_scan& s, bool backward, ScanPlan* p) {
-    const int64_t tiles = msla::scan_tiles(s.channels, s.groups, msla::kScanTile), slices = msla::scan_tiles(s.channels, s.groups, msla::kScanSlice);
-    const int64_t tile = s.states == 8 ? 32 : 64;        // tokens
-    const int64_t longest = s.offsets ? s.tokens : s.tokens / s.sequences;
+    const int64_t tiles = msla::scan_tiles(s.channels, s.groups), tile = 4 * msla::scan_lanes(s.states);      // (tokens of a tile)
+    const int64_t longest = s.offsets ? s.tokens : s.tokens / s.sequences, each = 2 * kUnits / (s.sequences * tiles);
     auto whole_tiles = [&](int64_t tokens) { return (tokens + tile - 1) / tile * tile; };
-    int64_t run;
-    if (backward) {
-        run = msla::scan_backward_run(s.states);
-        p->cut = longest > run;
-    } else {
-        const int64_t each = 2 * kUnits / (s.sequences * slices);
-        run = s.offsets ? whole_tiles(s.tokens * slices / (4 * kUnits) + 1) : whole_tiles(longest / (each > 0 ? each : 1) + 1);
-        p->cut = s.offsets ? longest > run : each >= 2 && longest * 100 > run * 165 + kCutTokens * 100;
-        if (!p->cut) run = whole_tiles(longest + 1);
-    }
+    int64_t run = s.offsets ? whole_tiles(s.tokens * tiles / (4 * kUnits) + 1) : whole_tiles(longest / (each > 0 ? each : 1) + 1);
+    p->cut = s.offsets ? longest > run : each >= 2 && longest * 100 > run * (backward ? 120 : 165) + kCutTokens * 100;
+    if (!p->cut) run = whole_tiles(longest + 1);
     p->slots = msla::slots_of(s.offsets, s.sequences, s.tokens, (int)run);
     p->count = msla::slot_count(p->slots);
     const int64_t per_state = (int64_t)s.channels * s.states;
-    if (p->count * slices >= kMostGroups || (int64_t)s.sequences * ((per_state + 255) / 256) >= kMostGroups) return MSLA_ERR_UNSUPPORTED;
+    if (p->count * tiles >= kMostGroups || (int64_t)s.sequences * ((per_state + 255) / 256) >= kMostGroups) return MSLA_ERR_UNSUPPORTED;
     if (backward && (s.tokens * (int64_t)s.groups * s.states * 2 + 255) / 256 >= kMostGroups) return MSLA_ERR_UNSUPPORTED;
     size_t at = 0;
     auto take = [&](size_t floats) {
@@ -92,13 +85,17 @@ msla_status plan_of(const msla_selective_scan& s, bool backward, ScanPlan* p) {
         at += align_up(floats * 4);
         return here;
     };
-    p->states_at = p->d_states_at = p->steps_at = p->parts_at = p->shared_at = 0;
+    p->states_at = p->d_states_at = p->steps_at = p->marks_at = p->mark_steps_at = p->parts_at = p->shared_at = 0;
     if (p->cut) {
         p->states_at = take((size_t)p->count * per_state);
         if (backward) p->d_states_at = take((size_t)p->count * per_state);
         p->steps_at = take((size_t)p->count * s.channels);
     }
     if (backward) {
+        p->marks = msla::slots_of(s.offsets, s.sequences, s.tokens, msla::scan_lanes(s.states));
+        const size_t marks = (size_t)msla::slot_count(p->marks);
+        p->marks_at = take(marks * per_state);
+        if (p->cut) p->mark_steps_at = take(marks * s.channels);
         p->parts_at = take((size_t)p->count * (per_state + 2 * s.channels));
         p->shared_at = take((size_t)tiles * s.tokens * 2 * s.states);
     }
@@ -141,6 +138,9 @@ void place(ScanCall* k, const ScanPlan& p, void* workspace) {
     k->states_at = (float*)(ws + p.states_at);
     k->d_states_at = (float*)(ws + p.d_states_at);
     k->steps_at = (float*)(ws + p.steps_at);
+    k->marks = p.marks;
+    k->marks_at = (float*)(ws + p.marks_at);
+    k->mark_steps_at = (float*)(ws + p.mark_steps_at);
     k->parts_at = (float*)(ws + p.parts_at);
     k->shared_at = (float*)(ws + p.shared_at);
 }

@@ -22,14 +22,16 @@ struct ScanCall {
     float *final_state, *d_a, *d_skip, *d_bias, *d_initial;
     // workspace: a slot's own state and, behind the join, the one that it starts from; the sum of its steps; the same for the state's gradient
     float *states_at, *steps_at, *d_states_at;
+    // the gradient's marks: the states in front of every scan_lanes() tokens of a sequence (of a slot from zero, with the steps so far, where it is cut)
+    Slots marks;
+    float *marks_at, *mark_steps_at;
     // parts of the sums over tokens (a slot's, [channels, states + 2]) and over channels (a tile's, [tokens, 2 * states])
     float *parts_at, *shared_at;
 };
 
-constexpr int kScanSlice = 32, kScanTile = 64;      // channels of a workgroup: of the passes over whole slots, of the gradient
-inline int scan_tiles(int channels, int groups, int of) { return groups * ((channels / groups + of - 1) / of); }
-// tokens of a slot of the gradient, at most (its states at every window lie in LDS)
-inline int scan_backward_run(int states) { return states <= 16 ? 64 : (states == 32 ? 64 : 32); }
+constexpr int kScanSlice = 32;      // channels of a workgroup
+inline int scan_tiles(int channels, int groups) { return groups * ((channels / groups + kScanSlice - 1) / kScanSlice); }
+inline int scan_lanes(int states) { return states == 8 ? 8 : 16; }     // that share a channel; tokens from mark to mark of the gradient, a quarter of a tile's
 
 hipError_t launch_scan_forward(int dt, const ScanCall& c, hipStream_t stream);
 hipError_t launch_scan_backward(int dt, const ScanCall& c, hipStream_t stream);

@@ -9,9 +9,6 @@ template <int CTRL>
 __device__ __forceinline__ float moved(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
-// (lane I of every four)
-template <int I>
-__device__ __forceinline__ float of_four(float v) { return moved<I * 0x55>(v); }
 // the value of lane ^ 1, ^ 2, ^ 4, ^ 8
 __device__ __forceinline__ float across1(float v) { return moved<0xB1>(v); }
 __device__ __forceinline__ float across2(float v) { return moved<0x4E>(v); }
@@ -97,14 +94,10 @@ __device__ __forceinline__ float halve16(float a, float b) {
     const unsigned first = r[0], second = r[1];
     return __builtin_bit_cast(float, first) + __builtin_bit_cast(float, second);
 }
-// lanes without the 8 (the 4) get a's sum over lane ^ 8 (lane ^ 4), the others b's
+// lanes without the 8 get a's sum over lane ^ 8, the others b's
 __device__ __forceinline__ float halve8(float a, float b, int lane) {
     const bool mine_b = lane & 8;
     return (mine_b ? b : a) + across8(mine_b ? a : b);
-}
-__device__ __forceinline__ float halve4(float a, float b, int lane) {
-    const bool mine_b = lane & 4;
-    return (mine_b ? b : a) + across4(mine_b ? a : b);
 }
 
 }  // namespace
