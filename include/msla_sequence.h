@@ -151,7 +151,7 @@ typedef struct {
 
 /* For every sequence, channel and state n of it, with t_i the step of token i and g the channel's group:
  *     h_i[n] = exp(t_i a[n]) h_{i-1}[n] + t_i x_i b_i[g, n]        y_i = sum_n c_i[g, n] h_i[n] + skip x_i        out_i = y_i silu(gate_i)
- *   x, delta, gate, out [tokens, channels]; gate.data may be NULL (out = y);  b, c [tokens, groups, states] (a row: groups * states next to each other)
+ *   x, delta, gate, out [tokens, channels], rows less than 16 MiB apart (else MSLA_ERR_UNSUPPORTED); gate.data may be NULL (out = y);  b, c [tokens, groups, states] (a row: groups * states next to each other)
  *   a [channels, states] fp32, negative in earnest (a decay exp(t a) below fp32's normal range is 0);  skip, delta_bias [channels] fp32 or NULL (0)
  *   initial_state, final_state [sequences, channels, states] fp32, either may be NULL; final_state may be initial_state itself.  A sequence without tokens
  *       hands its state on.

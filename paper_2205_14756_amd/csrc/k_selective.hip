@@ -70,6 +70,21 @@ __device__ __forceinline__ const T* row(const TokenRows& r, int t) { return (con
 template <class T>
 __device__ __forceinline__ T* row_out(const TokenRows& r, int t) { return (T*)r.p + (int64_t)t * r.ts; }
 
+// A lane's tokens of a tile, `mine` + i: from the tile's row i, which is the same for the workgroup, by an offset that stays (rows are less than 16 MiB
+// apart, and 60 of them less than 1 GiB).
+template <class T>
+struct Column {
+    const TokenRows rows;
+    const unsigned here, off;
+    __device__ __forceinline__ Column(const TokenRows& r, int channel, int mine)
+        : rows(r), here(channel * (unsigned)sizeof(T)), off(here + (unsigned)(mine * (int)r.ts) * (unsigned)sizeof(T)) {}
+    // (what lies behind the last token is read from the tile's own row instead)
+    __device__ __forceinline__ T load(int t0, int i, int last, bool in) const {
+        return *(const T*)((const char*)row<T>(rows, min(t0 + i, last)) + (in ? off : here));
+    }
+    __device__ __forceinline__ void store(int t0, int i, float v) const { *(T*)((char*)row_out<T>(rows, t0 + i) + off) = Traits<T>::from_f32(v); }
+};
+
 template <int S>
 __device__ __forceinline__ void load_states(float (&to)[S], const float* p) { __builtin_memcpy(to, __builtin_assume_aligned(p, 4), S * 4); }
 template <int S>
@@ -153,20 +168,20 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
     const int lane = threadIdx.x % kScanSlice, run = threadIdx.x / kScanSlice, mine = 4 * run;
     const bool live = first + lane < per;
     const int channel = me.group * per + (live ? first + lane : per - 1);
-    const unsigned at_channel = channel * (unsigned)sizeof(T);
     const bool gated = call.gate.p != nullptr, soft = call.softplus != 0;
     const float bias = call.bias ? call.bias[channel] : 0.0f, skip = call.skip ? call.skip[channel] : 0.0f;
+    const Column<T> xs(call.x, channel, mine), deltas(call.delta, channel, mine), gates(call.gate, channel, mine), d_outs(call.d_out, channel, mine),
+        outs(call.out, channel, mine);
     struct Tokens { T x[4], delta[4], gate[4], d_out[4]; } next;
     auto fetch = [&](int t0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = min(t0 + mine + i, last);
-            auto load = [&](const TokenRows& r) { return *(const T*)((const char*)row<T>(r, t) + at_channel); };
-            next.x[i] = load(call.x);
-            next.delta[i] = load(call.delta);
+            const bool in = t0 + mine + i <= last;
+            next.x[i] = xs.load(t0, i, last, in);
+            next.delta[i] = deltas.load(t0, i, last, in);
             if constexpr (kWithC)
-                if (gated) next.gate[i] = load(call.gate);
-            if constexpr (PASS == kSumsBoth) next.d_out[i] = load(call.d_out);
+                if (gated) next.gate[i] = gates.load(t0, i, last, in);
+            if constexpr (PASS == kSumsBoth) next.d_out[i] = d_outs.load(t0, i, last, in);
         }
     };
     Tile tile;
@@ -204,7 +219,7 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
             fetch(t0 + kTokens);
         }
         const int channel_at = threadIdx.x / L;
-#pragma unroll (PASS == kWhole ? 4 : 1)
+#pragma unroll PASS == kWhole ? 4 : 1
         for (int block = 0; block < kTokens; block += L) {
             if constexpr (kMark) {
                 if (t0 + block <= last && me.live) {
@@ -252,8 +267,7 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
             const f32x4 y = *(const f32x4*)&own[0][lane][mine];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (t0 + mine + i <= last && live)
-                    *(T*)((char*)row_out<T>(call.out, t0 + mine + i) + at_channel) = Traits<T>::from_f32((y[i] + past[i]) * through[i]);
+                if (t0 + mine + i <= last && live) outs.store(t0, i, (y[i] + past[i]) * through[i]);
         }
     }
     if constexpr (PASS == kWhole) {
@@ -324,6 +338,7 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_backward_kernel(ScanCall 
     constexpr int kTokens = Tile::kTokens, kRow = Tile::kRow;
     // a window's sums over the channels of a wave: one place, or two that take turns, which save a barrier
     constexpr int kTurns = S == 1 ? 2 : 1;
+    constexpr bool kTileAhead = S < 4;          // (four states a lane leave no registers for it)
     __shared__ __align__(16) typename Tile::Room room;
     __shared__ __align__(16) float own[3][kScanSlice][kRow];        // steps (y), steps times x (e), dy (the sum of w a)
     __shared__ float sums[kTurns][kWaves][kSums];
@@ -360,22 +375,22 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_backward_kernel(ScanCall 
     const int lane = threadIdx.x % kScanSlice, run = threadIdx.x / kScanSlice, mine = 4 * run;
     const bool live = first + lane < per;
     const int channel = me.group * per + (live ? first + lane : per - 1);
-    const unsigned at_channel = channel * (unsigned)sizeof(T);
     const bool gated = call.gate.p != nullptr, soft = call.softplus != 0;
     const float bias = call.bias ? call.bias[channel] : 0.0f, skip = call.skip ? call.skip[channel] : 0.0f;
     float d_skip = 0.0f, d_bias = 0.0f;
+    const Column<T> xs(call.x, channel, mine), deltas(call.delta, channel, mine), gates(call.gate, channel, mine), d_outs(call.d_out, channel, mine),
+        d_xs(call.d_x, channel, mine), d_deltas(call.d_delta, channel, mine), d_gates(call.d_gate, channel, mine);
     struct Tokens { T x[4], delta[4], gate[4], d_out[4]; } next;
     Tile tile;
     auto fetch = [&](int t0) {
         tile.fetch(call, me.group, t0, last);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = min(t0 + mine + i, last);
-            auto load = [&](const TokenRows& r) { return *(const T*)((const char*)row<T>(r, t) + at_channel); };
-            next.x[i] = load(call.x);
-            next.delta[i] = load(call.delta);
-            if (gated) next.gate[i] = load(call.gate);
-            next.d_out[i] = load(call.d_out);
+            const bool in = t0 + mine + i <= last;
+            next.x[i] = xs.load(t0, i, last, in);
+            next.delta[i] = deltas.load(t0, i, last, in);
+            if (gated) next.gate[i] = gates.load(t0, i, last, in);
+            next.d_out[i] = d_outs.load(t0, i, last, in);
         }
     };
     const int64_t marks = first_slot(call.marks, slot.sequence);
@@ -389,12 +404,13 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_backward_kernel(ScanCall 
         if (call.cut) passed = call.mark_steps_at[at * call.channels + me.channel];
     };
     if (behind > 0) {
-        fetch(slot.from + (behind - 1) * kTokens);
+        if constexpr (kTileAhead) fetch(slot.from + (behind - 1) * kTokens);
         ask(slot.from + (last - slot.from) / L * L);
     }
     int turn = 0;
     for (int n = behind - 1; n >= 0; --n) {
         const int t0 = slot.from + n * kTokens;
+        if constexpr (!kTileAhead) fetch(t0);
         const Tokens now = next;
         f32x4 step, add, dy;
 #pragma unroll
@@ -415,7 +431,7 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_backward_kernel(ScanCall 
         *(f32x4*)&own[2][lane][mine] = dy;
         tile.park(room);
         __syncthreads();
-        if (n > 0) fetch(t0 - kTokens);
+        if (kTileAhead && n > 0) fetch(t0 - kTokens);
 #pragma unroll 1
         for (int base = kTokens - L; base >= 0; base -= L) {
             const int from = t0 + base;
@@ -519,17 +535,15 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_backward_kernel(ScanCall 
         const f32x4 y = *(const f32x4*)&own[0][lane][mine], e = *(const f32x4*)&own[1][lane][mine], along = *(const f32x4*)&own[2][lane][mine];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = t0 + mine + i;
-            if (t > last || !live) continue;
+            if (t0 + mine + i > last || !live) continue;
             const float x = Traits<T>::to_f32(now.x[i]);
             float d_step = fmaf(x, e[i], kLn2 * along[i]);
             if (soft) d_step *= sigmoid_of(Traits<T>::to_f32(now.delta[i]) + bias);
-            auto put = [&](const TokenRows& r, float v) { *(T*)((char*)row_out<T>(r, t) + at_channel) = Traits<T>::from_f32(v); };
-            put(call.d_x, fmaf(step[i], e[i], skip * dy[i]));
-            put(call.d_delta, d_step);
+            d_xs.store(t0, i, fmaf(step[i], e[i], skip * dy[i]));
+            d_deltas.store(t0, i, d_step);
             if (gated) {
                 const float z = Traits<T>::to_f32(now.gate[i]), open = sigmoid_of(z);
-                put(call.d_gate, Traits<T>::to_f32(now.d_out[i]) * fmaf(skip, x, y[i]) * (open * fmaf(z, 1.0f - open, 1.0f)));
+                d_gates.store(t0, i, Traits<T>::to_f32(now.d_out[i]) * fmaf(skip, x, y[i]) * (open * fmaf(z, 1.0f - open, 1.0f)));
             }
             d_skip = fmaf(dy[i], x, d_skip);
             d_bias += d_step;

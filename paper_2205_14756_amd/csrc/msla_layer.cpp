@@ -39,6 +39,9 @@ msla_status check_sequences(int sequences, int64_t tokens, const int32_t* offset
 }
 
 // rows of `width` elements; where they are written they lie apart
+// (further apart than a lane's 32-bit offset reaches over a scan's tile of 64 tokens)
+bool wide(const msla_rows& r, int64_t tokens, msla_dtype dt) { return tokens > 1 && r.token_stride * (int64_t)elem_size(dt) >= (int64_t)1 << 24; }
+
 bool fits(const msla_rows& r, int64_t tokens, int64_t width, msla_dtype dt, bool written) {
     if (tokens == 0) return true;
     if (r.data == nullptr || !aligned(r.data, elem_size(dt)) || r.token_stride < 0 || r.token_stride > kMost / tokens) return false;
@@ -212,6 +215,8 @@ msla_status msla_selective_scan_forward(const msla_selective_scan* shape, msla_r
         return MSLA_ERR_INVALID_ARG;
     for (const msla_rows* i : {&x, &delta, &gate})
         if (same(out, *i)) return MSLA_ERR_INVALID_ARG;
+    for (const msla_rows* r : {&x, &delta, &gate, &out})
+        if (wide(*r, s.tokens, dt)) return MSLA_ERR_UNSUPPORTED;
     ScanPlan plan;
     st = plan_of(s, false, &plan);
     if (st != MSLA_OK) return st;
@@ -248,6 +253,8 @@ msla_status msla_selective_scan_backward(const msla_selective_scan* shape, msla_
         for (int other = 0; other < o; ++other)
             if (same(*outs[o], *outs[other])) return MSLA_ERR_INVALID_ARG;
     }
+    for (const msla_rows* r : {&x, &delta, &gate, &d_out, &d_x, &d_delta, &d_gate})
+        if (wide(*r, s.tokens, dt)) return MSLA_ERR_UNSUPPORTED;
     ScanPlan plan;
     st = plan_of(s, true, &plan);
     if (st != MSLA_OK) return st;
