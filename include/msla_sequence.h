@@ -218,8 +218,8 @@ msla_status msla_layer_norm_backward_workspace_bytes(int64_t rows, int channels,
 msla_status msla_layer_norm_backward(const void* sum, const void* weight, const void* d_y, const void* d_sum, void* d_r, float* d_weight, float* d_bias,
                                      void* workspace, size_t workspace_bytes, int64_t rows, int channels, float eps, msla_dtype dt, void* stream);
 
-/* Rows in 8-bit integers: scale [rows] fp32 = max |x| / 127, x8 [rows, channels] = x / scale to the nearest whole number, ties to even (both quotients as
- * IEEE rounds them; a row whose scale is 0 or not finite: zeros).  channels <= 32768, rows below 2^31; x is aligned to an element. */
+/* Rows in 8-bit integers: scale [rows] fp32 = max |x| * (1 / 127 in fp32), x8 [rows, channels] = x / scale to the nearest whole number, ties to even
+ * (product and quotient as IEEE rounds them; a row whose scale is 0 or not finite: zeros).  channels <= 32768, rows below 2^31; x is aligned to an element. */
 msla_status msla_quantize_rows_integer(const void* x, void* x8, float* scale, int64_t rows, int channels, msla_dtype dt, void* stream);
 
 /* y[n, o] = x_scale[n] * w_scale[o] * sum_c x8[n, c] w8[o, c]: msla_linear_quantized of 8-bit integers (-128 to 127).  Sums are exact.  c_in, c_out

@@ -301,8 +301,8 @@ __global__ void __launch_bounds__(threads_of(LPR)) layer_norm_backward_kernel(co
     leave(parts + (int64_t)blockIdx.x * 2 * channels + channels, db);
 }
 
-// Rows into 8-bit integers: scale = max |x| / 127, x8 = x / scale to the nearest whole number, ties to even; both quotients are rounded as IEEE
-// says, so that the same x gives the same integers everywhere.  A row with a NaN has a NaN for its scale, one with an infinity an infinity, and zeros.
+// Rows into 8-bit integers: scale = max |x| times fp32's 1 / 127, x8 = x / scale to the nearest whole number, ties to even; product and quotient are rounded
+// as IEEE says, so that the same x gives the same integers everywhere.  A row with a NaN has a NaN for its scale, one with an infinity an infinity, and zeros.
 template <class T, int LPR, int PER>
 __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) quantize_integer_kernel(const T* x, signed char* x8, float* scale, int64_t rows, int channels) {
     constexpr int kVec = Traits<T>::kVec, kThreads = LPR > 256 ? LPR : 256, kRows = kThreads / LPR;
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) quantize_integer_kernel
     if (odd) top = __builtin_nanf("");
     // (a NaN anywhere makes the row's scale one: fmaxf would drop it)
     top = over_row<LPR>(top, room, [](float a, float b) { return a != a || b != b ? __builtin_nanf("") : fmaxf(a, b); });
-    const float s = top / kTop;
+    const float s = top * (1.0f / kTop);
     const bool fine = s > 0.0f && s <= 3.4e38f;
     if (live && lane == 0) scale[row] = s;
 #pragma unroll

@@ -152,7 +152,8 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
 #pragma unroll
     for (int s = 0; s < S; ++s) h[s] = 0.0f;
     if constexpr (!kFromZero) {
-        if (!slot.first) load_states(h, call.states_at + slot_number * per_state + state_at);
+        // (only a whole sequence reads its initial state here: of one that is cut, the last slot may write the final state over it meanwhile)
+        if (!slot.first || !slot.last) load_states(h, call.states_at + slot_number * per_state + state_at);
         else if (call.initial) load_states(h, call.initial + slot.sequence * per_state + state_at);
     }
     int64_t mark = 0;
@@ -289,8 +290,7 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int
     }
 }
 
-// The state that each slot but a sequence's first starts from, and (BOTH) the state's gradient behind each but the last, in the places of the slots' own
-// sums.  A thread has one state of a sequence; the next slots' sums are on their way while one is joined.
+// The state that each slot of a sequence that is cut starts from, and (BOTH) the state's gradient behind each, in the places of the slots' own sums.  A thread has one state of a sequence; the next slots' sums are on their way while one is joined.
 template <bool BOTH>
 __global__ void __launch_bounds__(256) scan_join_kernel(ScanCall call, int blocks) {
     const int b = blockIdx.x / blocks;
@@ -303,9 +303,8 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanCall call, int block
     const float a = rate_of(call.a[at]);
     const int64_t channel = at / call.states;
     constexpr int kAhead = 8;
-    // over slots k = 0 .. count - 2 in the order that `slot_of` gives; v goes to the slot behind each
+    // over slots in the order that `slot_of` gives; v goes to the first, and on
     auto join = [&](float* sums, float v, auto slot_of) {
-        float last = 0.0f;
         for (int64_t k0 = 0; k0 < count - 1; k0 += kAhead) {
             float own[kAhead], steps[kAhead];
 #pragma unroll
@@ -317,13 +316,11 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanCall call, int block
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
                 if (k0 + k < count - 1) {
+                    sums[(from + slot_of(k0 + k)) * per_state + at] = v;
                     v = fmaf(exp2_of(a * steps[k]), v, own[k]);
-                    // (a slot's place is written when its own sum has been read: one step late)
-                    if (k0 + k > 0) sums[(from + slot_of(k0 + k)) * per_state + at] = last;
-                    last = v;
                 }
         }
-        sums[(from + slot_of(count - 1)) * per_state + at] = last;
+        sums[(from + slot_of(count - 1)) * per_state + at] = v;
     };
     join(call.states_at, call.initial ? call.initial[b * per_state + at] : 0.0f, [](int64_t k) { return k; });
     if constexpr (BOTH) join(call.d_states_at, call.d_final ? call.d_final[b * per_state + at] : 0.0f, [&](int64_t k) { return count - 1 - k; });
@@ -347,25 +344,20 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_backward_kernel(ScanCall 
     const Place<L> me(call, blockIdx.x % tiles);
     const int64_t state_at = (int64_t)me.channel * N + me.own * S, per_state = (int64_t)call.channels * N;
     float* parts = call.parts_at + slot_number * (per_state + 2 * call.channels);
-    float d_a[S], carry[S], a[S], start[S];
+    float d_a[S], of_tile[S], carry[S], a[S], start[S];      // (of_tile: d_a of a tile's tokens, so that long sequences add up tiles and not tokens)
 #pragma unroll
-    for (int s = 0; s < S; ++s) d_a[s] = carry[s] = start[s] = 0.0f;
+    for (int s = 0; s < S; ++s) d_a[s] = of_tile[s] = carry[s] = start[s] = 0.0f;
     load_states(a, call.a + state_at);
 #pragma unroll
     for (int s = 0; s < S; ++s) a[s] = rate_of(a[s]);
     // (lanes without a channel read another's values, and must not add even an infinity to sums)
-    if (me.live) {
-        if (!slot.last) {
-            if (slot.used) load_states(carry, call.d_states_at + slot_number * per_state + state_at);
-        } else if (call.d_final) {
-            load_states(carry, call.d_final + slot.sequence * per_state + state_at);
-        }
+    if (me.live && slot.used) {
+        const bool whole = slot.first && slot.last;
+        if (!whole) load_states(carry, call.d_states_at + slot_number * per_state + state_at);
+        else if (call.d_final) load_states(carry, call.d_final + slot.sequence * per_state + state_at);
         if (call.cut) {             // (marks are of a slot from zero: what it started from comes on top)
-            if (!slot.first) {
-                if (slot.used) load_states(start, call.states_at + slot_number * per_state + state_at);
-            } else if (call.initial) {
-                load_states(start, call.initial + slot.sequence * per_state + state_at);
-            }
+            if (!whole) load_states(start, call.states_at + slot_number * per_state + state_at);
+            else if (call.initial) load_states(start, call.initial + slot.sequence * per_state + state_at);
         }
     }
     const int last = slot.until - 1;
@@ -495,7 +487,7 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_backward_kernel(ScanCall 
                         const float keep = S == 1 ? keeps[S == 1 ? t : 0][s] : exp2_of(ti[i] * a[s]);
                         carry[s] = keep * dh;
                         const float through = carry[s] * (t > 0 ? states[t > 0 ? t - 1 : 0][s] : mark[s]);
-                        d_a[s] = fmaf(through, ti[i], d_a[s]);
+                        of_tile[s] = fmaf(through, ti[i], of_tile[s]);
                         along = s == 0 ? through * a[s] : fmaf(through, a[s], along);
                     }
                     sum[t] = e;
@@ -531,6 +523,11 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_backward_kernel(ScanCall 
             }
             if constexpr (kTurns == 2) turn ^= 1;
             else __syncthreads();
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            d_a[s] += of_tile[s];
+            of_tile[s] = 0.0f;
         }
         const f32x4 y = *(const f32x4*)&own[0][lane][mine], e = *(const f32x4*)&own[1][lane][mine], along = *(const f32x4*)&own[2][lane][mine];
 #pragma unroll

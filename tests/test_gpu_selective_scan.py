@@ -207,6 +207,19 @@ def test_the_state_in_place_and_a_sequence_in_pieces():
     torch.testing.assert_close(torch.cat(outs).float(), whole.float(), rtol=2.0 ** -7, atol=way * float(whole.abs().max()))
 
 
+@pytest.mark.parametrize("lens", [[2000], [900, 0, 3, 700]])
+def test_the_state_in_place_where_sequences_are_cut(lens):
+    """many slots to a sequence, more workgroups than run at once: the last may end before the first begins"""
+    t = make(14, "bf16", sum(lens), 2048, 1, 16, len(lens))
+    offs = torch.tensor(offsets_of(lens), dtype=torch.int32, device="cuda")
+    assert seq.msla_selective_scan_workspace_bytes(len(lens), sum(lens), 2048, 1, 16, torch.bfloat16, packed=True) > 0
+    want, state = seq.msla_selective_scan_forward(*args_of(t), offsets=offs, initial_state=t["first"], **rest_of(t, True))
+    for _ in range(3):
+        s = t["first"].clone()
+        got, _ = seq.msla_selective_scan_forward(*args_of(t), offsets=offs, initial_state=s, final_state=s, **rest_of(t, True))
+        assert torch.equal(got, want) and torch.equal(s, state)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("states", [8, 16, 32, 64])
 @pytest.mark.parametrize("sequences,channels,groups", [(1, 1, 1), (3, 100, 2), (150, 64, 1)])
