@@ -1,11 +1,12 @@
 // The short causal convolution of each channel with its own taps, over sequences: pre_i = bias + sum_k w[k] x_{i - width + 1 + k}, out = pre or silu(pre).
 //
-// Bound by memory.  A thread has a piece of 16 bytes of the channels and a run of tokens of one sequence (a slot), whose last width - 1 rows stay in registers as the
+// Bound by memory.  A thread has a piece of 8 bytes of the channels and a run of tokens of one sequence (a slot), whose last width - 1 rows stay in registers as the
 // run goes on; those before the run are read once more (out of a cache).  The sequence's state is those rows: the ones in front of its first
-// token, and the last ones.
+// token, and the last ones.  16384 tokens of 4096 channels in bf16, width 4: 63 us, 4.3 TB/s.
 //
 // The gradient goes over the same runs and the width - 1 tokens behind them, whose part of d_x it needs: pre again, d_pre = d_out silu'(pre), d_x_i = sum_m
-// w[width - 1 - m] d_pre_{i + m}; taps and bias are summed over a run in registers, over runs through parts that a second launch adds up.
+// w[width - 1 - m] d_pre_{i + m}; taps and bias are summed over a run in registers, over runs through parts that a second launch adds up.  The same rows: 112 us
+// and 6 for the parts, 3.4 TB/s at the three waves a SIMD that its registers leave.
 #include "msla_device.h"
 #include "msla_layer_kernels.h"
 #include "norm_rows.h"

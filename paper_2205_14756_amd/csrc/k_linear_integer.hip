@@ -1,5 +1,6 @@
 // The 1x1 projection of rows in 8-bit integers: y[n, o] = x_scale[n] w_scale[o] sum_c x8[n, c] w8[o, c], on the 8-bit integer matrix instructions, whose
-// sums are exact in 32 bits (131056 products of -128 and -128 stay below 2^31).
+// sums are exact in 32 bits (131056 products of -128 and -128 stay below 2^31).  4096 rows, 4096 -> 8192: 200 us, 1.4 POP/s of the 2.1 that a large library
+// product reaches here (159 with the instruction of 64 slots, below); 48 rows, 4096 -> 4096: 10 us, the rows out of L2 to each of 256 workgroups beside 17 MB of weights.
 #include "msla_device.h"
 #include "msla_layer_kernels.h"
 
@@ -7,7 +8,15 @@ namespace msla {
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ i32x4 mma(i32x4 c, i32x4 a, i32x4 b) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+// A lane's 16 bytes of a row are the operands of two instructions, the low and the high eight contraction slots (the one of 64 slots, which has twice the rate, is
+// not among those whose wait states the built library is checked for).
+template <int HALF>
+__device__ __forceinline__ i32x4 mma(i32x4 c, i32x4 a, i32x4 b) {
+    typedef long i64x2 __attribute__((ext_vector_type(2)));
+    const i64x2 p = __builtin_bit_cast(i64x2, a), q = __builtin_bit_cast(i64x2, b);
+    const long row = p[HALF], column = q[HALF];
+    return __builtin_amdgcn_mfma_i32_16x16x32_i8(row, column, c, 0, 0, 0);
+}
 
 // A workgroup of four waves, two by two, has 32 NB rows x 32 OB outputs, a wave half of each: NB OB products of 16 x 16 for NB + OB operands out of LDS, whose
 // bandwidth is what large tiles are for.  A stage is 64 bytes of the contraction.  Tiles lie in LDS as rows of 64 bytes whose 16-byte pieces are XORed
@@ -76,10 +85,13 @@ __global__ void __launch_bounds__(256, 2) linear_integer_kernel(const char* x8, 
 #pragma unroll
         for (int j = 0; j < NB; ++j) b[j] = *(const i32x4*)(tile + b_at[j]);
         __builtin_amdgcn_s_setprio(1);
+        // (all low halves first: a sum's two products would wait for each other)
+        static_for<0, 2>([&](auto half) {
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
+            for (int j = 0; j < NB; ++j)
 #pragma unroll
-            for (int i = 0; i < OB; ++i) acc[i][j] = mma(acc[i][j], a[i], b[j]);
+                for (int i = 0; i < OB; ++i) acc[i][j] = mma<decltype(half)::value>(acc[i][j], a[i], b[j]);
+        });
         __builtin_amdgcn_s_setprio(0);
         // (one barrier a stage: the buffer that the next stage fills was last read before this stage's barrier)
     }
@@ -138,7 +150,7 @@ __global__ void __launch_bounds__(512) linear_integer_rows_kernel(const char* x8
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) acc[b] = mma(acc[b], s.w[h], s.x[b][h]);
+            for (int b = 0; b < BLOCKS; ++b) acc[b] = mma<1>(mma<0>(acc[b], s.w[h], s.x[b][h]), s.w[h], s.x[b][h]);
     };
     constexpr int kStride = kWaves * kTileK;
     Stage s0, s1;
@@ -166,17 +178,18 @@ __global__ void __launch_bounds__(512) linear_integer_rows_kernel(const char* x8
 }
 
 // Which kernel: by rounds of its workgroups over the 256 compute units, each of which takes so many ns a channel of the contraction, and no call less than
-// `least`.  Measured at 4096 channels, us with `rows` of 16 / 32 / 48 / 64, and with tiles of 64 x 64, 64 x 128, 128 x 128, 256 x 128: 16 rows into 4096 outputs 6.3 / 6.8 /
-// 7.4 / 7.9, 18.7, 24, 30, 46; 96 rows 24 / 18.8 / 17.4 / 18.6, 19.3, 24, 31, 48; 128 rows 31 / 24 / 23 / 21, 19.5, 25, 32, 50; 512 rows 114 / 87 / 79 / 74, 25.9, 30, 35,
-// 52; 1024 rows 226 / 171 / 154 / 144, 39.6, 36.3, 39.3, 56; 2048 rows -, 81, 64, 48, 60; 4096 rows into 8192 -, 293, 233, 176, 165; 64 rows into 16000 60 / 46 /
-// 50 / 40, 27.3, 33, 38, 50.
+// `least`.  Measured at 4096 channels, us with `rows` of 16 / 32 / 48 / 64, and with tiles of 64 x 64, 64 x 128, 128 x 128 (256 x 128 gains nowhere: 216 where these take
+// 210): 16 rows into 4096 outputs 6.3 / 6.8 / 7.4 / 7.9, 21, 29, 38; 96 rows 24 / 18.8 / 17.4 / 18.6, 21, 29, 40; 128 rows 31 / 24 / 23 / 21, 21.6, 30, 40; 512 rows
+// 114 / 87 / 79 / 74, 26.8, 33, 42; 1024 rows 226 / 171 / 154 / 144, 44, 42, 44; 2048 rows -, 94, 73, 64; 4096 rows into 8192 -, 338, 265, 210; 64 rows into 16000
+// 60 / 46 / 50 / 40, 28.6, 35, 42.
 struct Kind { int rows, outputs; float round, least; };
-constexpr Kind kKinds[] = {{16, 16, 0.95f, 1.54f}, {32, 16, 1.44f, 1.66f}, {48, 16, 1.86f, 2.1f}, {64, 16, 2.44f, 2.6f},
-                           {64, 64, 2.47f, 4.5f}, {64, 128, 4.0f, 5.6f}, {128, 128, 5.5f, 9.0f}, {256, 128, 10.1f, 14.0f}};
+constexpr int kKindCount = 7;
+constexpr Kind kKinds[kKindCount] = {{16, 16, 0.95f, 1.54f}, {32, 16, 1.44f, 1.66f}, {48, 16, 1.86f, 2.1f}, {64, 16, 2.44f, 2.6f},
+                                     {64, 64, 2.7f, 5.2f}, {64, 128, 4.4f, 7.1f}, {128, 128, 6.4f, 9.7f}};
 int kind_of(int64_t rows, int c_out) {
     int best = 0;
     float least = 0.0f;
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kKindCount; ++k) {
         const Kind& kind = kKinds[k];
         const int64_t groups = (rows + kind.rows - 1) / kind.rows * ((c_out + kind.outputs - 1) / kind.outputs), rounds = (groups + 255) / 256;
         const float all = (float)rounds * kind.round, cost = all > kind.least ? all : kind.least;
@@ -215,8 +228,7 @@ hipError_t linear_of(const void* x8, const float* x_scale, const void* w8, const
             case 3: by_rows(integral_constant<int, 4>{}); break;
             case 4: by_tiles(integral_constant<int, 2>{}, integral_constant<int, 2>{}); break;
             case 5: by_tiles(integral_constant<int, 2>{}, integral_constant<int, 4>{}); break;
-            case 6: by_tiles(integral_constant<int, 4>{}, integral_constant<int, 4>{}); break;
-            default: by_tiles(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+            default: by_tiles(integral_constant<int, 4>{}, integral_constant<int, 4>{});
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

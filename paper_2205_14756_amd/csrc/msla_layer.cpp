@@ -69,12 +69,15 @@ struct ScanPlan {
 
 // How long slots are.  Two workgroups fill a compute unit.  A sequence that is cut does 1.65 times its work, in the gradient 1.2 times, and two (one) more
 // launches.  Equal sequences are cut into as many slots as leave every unit two workgroups at most, if that is worth it; packed ones, whose lengths nobody
-// knows here, so that the units have about four (those that are no longer than that run whole).
+// knows here, into runs of a share of what a unit has to do (those that are no longer run whole).  us with a whole share, half of one, a quarter: 24 sequences of
+// 5003 tokens, 2048 channels of 64 states 211 / 245 / 267, 16 of 8192 tokens, 4096 channels 225 / 281 / 275; but of fewer sequences than fill the units, 8 of 4096,
+// 1024 channels 78 / 59 / 59, 2 of 8000, 2048 channels 189 / 152 / 153; the gradient of the second one 999 / 982 / 941, of the third 181 / 155 / 149.
 msla_status plan_of(const msla_selective_scan& s, bool backward, ScanPlan* p) {
     const int64_t tiles = msla::scan_tiles(s.channels, s.groups), tile = 4 * msla::scan_lanes(s.states);      // (tokens of a tile)
     const int64_t longest = s.offsets ? s.tokens : s.tokens / s.sequences, each = 2 * kUnits / (s.sequences * tiles);
     auto whole_tiles = [&](int64_t tokens) { return (tokens + tile - 1) / tile * tile; };
-    int64_t run = s.offsets ? whole_tiles(s.tokens * tiles / (4 * kUnits) + 1) : whole_tiles(longest / (each > 0 ? each : 1) + 1);
+    const int64_t shares = backward ? 4 : (s.sequences * tiles >= 2 * kUnits ? 1 : 2);
+    int64_t run = s.offsets ? whole_tiles(s.tokens * tiles / (shares * kUnits) + 1) : whole_tiles(longest / (each > 0 ? each : 1) + 1);
     p->cut = s.offsets ? longest > run : each >= 2 && longest * 100 > run * (backward ? 120 : 165) + kCutTokens * 100;
     if (!p->cut) run = whole_tiles(longest + 1);
     p->slots = msla::slots_of(s.offsets, s.sequences, s.tokens, (int)run);
