@@ -546,7 +546,8 @@ __global__ void __launch_bounds__(kScanSlice * L) scan_backward_kernel(ScanCall 
     }
     if (slot.used && slot.first && call.d_initial && me.live) store_states(call.d_initial + slot.sequence * per_state + state_at, carry);
     if (me.live) store_states(parts + state_at, d_a);
-    // (each has the sums of its own tokens)
+    // (each has the sums of its own tokens; the places that they go to hold the last tile's y and e, which other waves may be reading still)
+    __syncthreads();
     own[0][lane][run] = d_skip;
     own[1][lane][run] = d_bias;
     __syncthreads();
