@@ -88,10 +88,10 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) layer_norm_kernel(const
 // its way while this one is reduced.
 // Lanes of a row in the gradient, in whole waves: one piece each up to 256, two up to 512 lanes (which then take two waves a SIMD).
 constexpr int threads_of(int lpr) { return lpr < 192 ? 256 : lpr; }
-template <class F>
-hipError_t with_lanes_back(int channels, int elem, F&& f) {
+template <int ELEM, class F>
+hipError_t with_lanes_back(int channels, F&& f) {
     using std::integral_constant;
-    const int pieces = (channels * elem + 15) / 16;
+    const int pieces = (channels * ELEM + 15) / 16;
     integral_constant<int, 1> one;
     integral_constant<int, 2> two;
     if (pieces <= 4) return f(integral_constant<int, 4>{}, one);
@@ -103,8 +103,9 @@ hipError_t with_lanes_back(int channels, int elem, F&& f) {
     if (pieces <= 512) return f(integral_constant<int, 256>{}, two);
     if (pieces <= 1024) return f(integral_constant<int, 512>{}, two);
     if (pieces <= 2048) return f(integral_constant<int, 1024>{}, two);
-    if (pieces <= 4096) return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
-    return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+    if constexpr (ELEM == 4)
+        if (pieces > 4096) return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+    return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
 }
 
 template <class T, int LPR, int PER>
@@ -388,12 +389,13 @@ hipError_t with_type(int dt, F&& f) {
 // 18 / 17 / 20 / 17; of two pieces, 8192 x 2051 in fp16, 66 / 50 / 57 / 58.
 int layer_norm_blocks(int64_t rows, int channels, int elem) {
     int threads = 256, per_block = 1, waves = 12;
-    (void)with_lanes_back(channels, elem, [&](auto lpr, auto per) {
+    auto take = [&](auto lpr, auto per) {
         threads = threads_of(decltype(lpr)::value);
         per_block = threads / decltype(lpr)::value;
         waves = decltype(per)::value > 1 ? 8 : 12;
         return hipSuccess;
-    });
+    };
+    (void)(elem == 4 ? with_lanes_back<4>(channels, take) : with_lanes_back<2>(channels, take));
     const int64_t all = (rows + per_block - 1) / per_block, most = 256 * (waves * 64 > threads ? waves * 64 / threads : 1);
     return (int)(all < most ? all : most);
 }
@@ -401,7 +403,7 @@ int layer_norm_blocks(int64_t rows, int channels, int elem) {
 hipError_t launch_layer_norm(int dt, const LayerNormCall& c, hipStream_t stream) {
     return with_type(dt, [&](auto type) {
         typedef decltype(type) T;
-        return with_lanes(lanes_for(c.channels, sizeof(T)), [&](auto lpr, auto per) {
+        return with_lanes<sizeof(T)>(lanes_for(c.channels, sizeof(T)), [&](auto lpr, auto per) {
             constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value;
             return in_launches<kLpr>(c.rows, [&](int64_t from, int64_t rows, dim3 grid, dim3 threads) {
                 const int64_t at = from * c.channels;
@@ -419,7 +421,7 @@ hipError_t launch_layer_norm_backward(int dt, const void* sum, const void* weigh
         const int blocks = layer_norm_blocks(rows, channels, sizeof(T));
         const bool sums = d_weight != nullptr || d_bias != nullptr;
         // (no rows: nothing but sums of zeros)
-        const hipError_t e = blocks == 0 ? hipSuccess : with_lanes_back(channels, sizeof(T), [&](auto lpr, auto per) {
+        const hipError_t e = blocks == 0 ? hipSuccess : with_lanes_back<sizeof(T)>(channels, [&](auto lpr, auto per) {
             constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value;
             hipLaunchKernelGGL((layer_norm_backward_kernel<T, kLpr, kPer>), dim3(blocks), dim3(threads_of(kLpr)), 0, stream, (const T*)sum, (const T*)weight,
                                (const T*)d_y, (const T*)d_sum, (T*)d_r, sums ? parts : nullptr, rows, channels, eps);
@@ -433,7 +435,7 @@ hipError_t launch_layer_norm_backward(int dt, const void* sum, const void* weigh
 hipError_t launch_quantize_integer(int dt, const void* x, void* x8, float* scale, int64_t rows, int channels, hipStream_t stream) {
     return with_type(dt, [&](auto type) {
         typedef decltype(type) T;
-        return with_lanes(lanes_for(channels, sizeof(T)), [&](auto lpr, auto per) {
+        return with_lanes<sizeof(T)>(lanes_for(channels, sizeof(T)), [&](auto lpr, auto per) {
             constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value;
             return in_launches<kLpr>(rows, [&](int64_t from, int64_t n, dim3 grid, dim3 threads) {
                 hipLaunchKernelGGL((quantize_integer_kernel<T, kLpr, kPer>), grid, threads, 0, stream, (const T*)x + from * channels,

@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(1024) norm_weight_kernel(const float* partials
 
 template <class T>
 hipError_t norm_of(const NormCall& c, hipStream_t stream) {
-    return with_lanes(lanes_for(c.channels, sizeof(T)), [&](auto lpr, auto per) {
+    return with_lanes<sizeof(T)>(lanes_for(c.channels, sizeof(T)), [&](auto lpr, auto per) {
         constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value, kThreads = kLpr > 256 ? kLpr : 256, kRows = kThreads / kLpr;
         // (a launch has fewer than 2^32 threads: more rows than these go in several)
         constexpr int64_t kMost = ((int64_t)1 << 31) / kThreads * kRows;
@@ -299,7 +299,7 @@ hipError_t norm_backward_of(const void* sum, const void* weight, const void* d_y
                             int64_t rows, int channels, float eps, hipStream_t stream) {
     const int blocks = norm_backward_blocks(rows, channels, sizeof(T));
     // (no rows: nothing but a d_weight of zeros)
-    hipError_t e = blocks == 0 ? hipSuccess : with_lanes(lanes_for(channels, sizeof(T)), [&](auto lpr, auto per) {
+    hipError_t e = blocks == 0 ? hipSuccess : with_lanes<sizeof(T)>(lanes_for(channels, sizeof(T)), [&](auto lpr, auto per) {
         constexpr int kLpr = decltype(lpr)::value, kPer = decltype(per)::value, kThreads = kLpr > 256 ? kLpr : 256;
         hipLaunchKernelGGL((norm_backward_kernel<T, kLpr, kPer>), dim3(blocks), dim3(kThreads), 0, stream, (const T*)sum, (const T*)weight,
                            (const T*)d_y, (const T*)d_sum, (T*)d_r, d_weight ? partials : nullptr, rows, channels, eps);

@@ -602,7 +602,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanCall call, int block
         h[s] = fmaf(exp2_of(step * rate_of(a[s])), h[s], step * x * kb.at(s));
         y = fmaf(kc.at(s), h[s], y);
     }
-    y = sum_over<4>(y);
+    y = sum_of_four(y);
     if (!live) return;
     store_states(call.final_state + place, h);
     if (quarter != 0) return;

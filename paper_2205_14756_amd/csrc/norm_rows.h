@@ -130,7 +130,8 @@ inline Lanes lanes_for(int channels, int elem) {
     return {1024, pieces <= 1024 ? 1 : (pieces <= 2048 ? 2 : (pieces <= 4096 ? 4 : 8))};
 }
 
-template <class F>
+// (ELEM: bytes of an element; 32768 channels of 2 are half of the longest row)
+template <int ELEM, class F>
 hipError_t with_lanes(Lanes l, F&& f) {
     using std::integral_constant;
     auto per2 = [&](auto lpr) { return l.per == 1 ? f(lpr, integral_constant<int, 1>{}) : f(lpr, integral_constant<int, 2>{}); };
@@ -142,8 +143,9 @@ hipError_t with_lanes(Lanes l, F&& f) {
     }
     if (l.per == 1) return f(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
     if (l.per == 2) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-    if (l.per == 4) return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
-    return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+    if constexpr (ELEM == 4)
+        if (l.per == 8) return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+    return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
 }
 
 }  // namespace

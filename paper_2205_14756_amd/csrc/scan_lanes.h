@@ -1,4 +1,4 @@
-// Lanes that share a channel of the selective scan: 4, 8 or 16 neighbours of a wave, each with some of its states.
+// Lanes that share a channel of the selective scan: 8 or 16 neighbours of a wave (4 of a step for single tokens), each with some of its states.
 #pragma once
 #include "msla_device.h"
 
@@ -9,10 +9,9 @@ template <int CTRL>
 __device__ __forceinline__ float moved(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
-// the value of lane ^ 1, ^ 2, ^ 4, ^ 8
+// the value of lane ^ 1, ^ 2, ^ 8
 __device__ __forceinline__ float across1(float v) { return moved<0xB1>(v); }
 __device__ __forceinline__ float across2(float v) { return moved<0x4E>(v); }
-__device__ __forceinline__ float across4(float v) { return moved<0x1B>(moved<0x141>(v)); }      // 7 - lane within eight, then 3 - lane within four
 __device__ __forceinline__ float across8(float v) { return moved<0x128>(v); }
 
 // The sum of p[j] over the L lanes that share a channel, to lane j of them: each step leaves half of the numbers, of twice as many lanes.
@@ -72,13 +71,10 @@ __device__ __forceinline__ float deal<16>(const float (&p)[16], int lane) {
     return deal<8>(q, lane);
 }
 
-// the sum of v over the L lanes that share a channel, to all of them
-template <int L>
-__device__ __forceinline__ float sum_over(float v) {
+// the sum of v over four neighbours, to all of them
+__device__ __forceinline__ float sum_of_four(float v) {
     v += across1(v);
     v += across2(v);
-    if constexpr (L >= 8) v += across4(v);
-    if constexpr (L >= 16) v += across8(v);
     return v;
 }
 
