@@ -140,7 +140,10 @@ typedef struct {
 } msla_rows;
 
 /* What the scan runs over: sequences, tokens and offsets as in msla_recurrence (tokens below 2^31 - 4096).  channels <= 2^20, in `groups` (a divisor) of
- * neighbours that share b and c; states of a channel: 8, 16, 32 or 64. */
+ * neighbours that share b and c; states of a channel: 8, 16, 32 or 64.
+ * A launch has fewer than 2^23 workgroups, which takes what else there is of everything: (sequences + tokens / 64) * groups * (channels of a group / 32, rounded up), with
+ * 8 states tokens / 32, below 2^23; sequences * (channels * states / 256, rounded up) below 2^23; in the gradient tokens * groups * states below 2^30; for single
+ * tokens sequences * (channels / 64, rounded up) below 2^23 alone.  These are taken; what is beyond may be refused with MSLA_ERR_UNSUPPORTED. */
 typedef struct {
     int sequences;
     int64_t tokens;
@@ -178,7 +181,8 @@ msla_status msla_selective_scan_step(const msla_selective_scan* shape, msla_rows
                                      const float* skip, const float* delta_bias, msla_rows gate, const float* state, msla_rows out, float* new_state,
                                      msla_dtype dt, void* stream);
 
-/* What the convolution runs over: sequences, tokens and offsets as in msla_recurrence (tokens below 2^31 - 4096).  channels <= 2^20; width 2, 3 or 4. */
+/* What the convolution runs over: sequences, tokens and offsets as in msla_recurrence (tokens below 2^31 - 4096).  channels <= 2^20; width 2, 3 or 4.
+ * (sequences + tokens / 32) * (bytes of a row / 1024 + 2) below 2^23 is taken; what is beyond may be refused with MSLA_ERR_UNSUPPORTED (a launch's workgroups). */
 typedef struct {
     int sequences;
     int64_t tokens;
