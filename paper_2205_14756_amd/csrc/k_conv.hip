@@ -5,8 +5,8 @@
 // token, and the last ones.  16384 tokens of 4096 channels in bf16, width 4: 63 us, 4.3 TB/s.
 //
 // The gradient goes over the same runs and the width - 1 tokens behind them, whose part of d_x it needs: pre again, d_pre = d_out silu'(pre), d_x_i = sum_m
-// w[width - 1 - m] d_pre_{i + m}; taps and bias are summed over a run in registers, over runs through parts that a second launch adds up.  The same rows: 112 us
-// and 6 for the parts, 3.4 TB/s at the three waves a SIMD that its registers leave.
+// w[width - 1 - m] d_pre_{i + m}; taps and bias are summed over a run in registers, over runs through parts that a second launch adds up.  The same rows: 114 us
+// and 6 for the parts, 3.4 TB/s at the three waves a SIMD that its 161 registers leave.  (Three in fp16 as well; two of width 3 in bf16, which takes 170; four of the others.)
 #include "msla_device.h"
 #include "msla_layer_kernels.h"
 #include "norm_rows.h"

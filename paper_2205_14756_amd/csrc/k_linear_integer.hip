@@ -1,6 +1,6 @@
 // The 1x1 projection of rows in 8-bit integers: y[n, o] = x_scale[n] w_scale[o] sum_c x8[n, c] w8[o, c], on the 8-bit integer matrix instructions, whose
-// sums are exact in 32 bits (131056 products of -128 and -128 stay below 2^31).  4096 rows, 4096 -> 8192: 200 us, 1.4 POP/s of the 2.1 that a large library
-// product reaches here (159 with the instruction of 64 slots, below); 48 rows, 4096 -> 4096: 10 us, the rows out of L2 to each of 256 workgroups beside 17 MB of weights.
+// sums are exact in 32 bits (131056 products of -128 and -128 stay below 2^31).  4096 rows, 4096 -> 8192: 195 us, 1.4 POP/s of the 2.1 that a large library
+// product reaches here (159 with the instruction of 64 slots, below); 48 rows, 4096 -> 4096: 11 us, the rows out of L2 to each of 256 workgroups beside 17 MB of weights.
 #include "msla_device.h"
 #include "msla_layer_kernels.h"
 

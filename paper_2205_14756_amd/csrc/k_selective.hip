@@ -2,8 +2,8 @@
 //     t_i,c = softplus(delta_i,c + bias_c)        h_i[c, n] = exp(t_i,c a[c, n]) h_{i-1}[c, n] + t_i,c x_i,c b_i[n]
 //     y_i,c = sum_n c_i[n] h_i[c, n] + skip_c x_i,c                out = y silu(gate)
 // The decays differ for every channel and state, so no product of matrices is in it: a state and token is an exponential, two products and two
-// multiply-adds on the vector units, and their issue bounds it (the exponential costs two slots), not memory.  8192 tokens of 4096 channels of 16 states in bf16: 176 us,
-// 1.5 TB/s; the vector units are busy for 81% of the cycles, with 9.2 instructions a state and token, 5 of them the recurrence's own.
+// multiply-adds on the vector units, and their issue bounds it (the exponential costs two slots), not memory.  8192 tokens of 4096 channels of 16 states in bf16: 172 us,
+// 1.6 TB/s; the vector units are busy for 0.9 of the cycles, with 9.6 instructions a state and token, 5 of them the recurrence's own.
 //
 // Sixteen lanes have a channel (eight where it has 8 states) and its states in registers.  Sums over the states of as many tokens as there are lanes are exchanged so that
 // each lane ends up with one token's.  Sequences are cut into slots where channels alone do not fill the GPU: a pass over each slot from a state of zero, a join
@@ -15,7 +15,7 @@
 // runs over slots as well.  A pass forward leaves the state at every 16 tokens (a mark); where sequences are cut it also sums exp(a * the steps up to i) c_i dy_i, which is
 // what a slot adds to dh in front of it.  The pass back makes 16 tokens' states again from their mark, keeps them in registers, and goes back over them.  Sums
 // over channels go over the lanes of a wave by exchanging halves, over the waves through LDS, over workgroups through parts in the workspace that a last
-// launch adds up in a fixed order.  The same tokens and channels: 745 us, of which the pass back 580 (vector units busy for 77%, 31 instructions a state and token).
+// launch adds up in a fixed order.  The same tokens and channels: 751 us, of which the pass back 597 (vector units busy for 0.75 of the cycles, 29 instructions a state and token).
 #include "msla_device.h"
 #include "msla_layer_kernels.h"
 #include "scan_lanes.h"
@@ -48,7 +48,8 @@ struct Piece {
     __device__ __forceinline__ float at(int s) const { return Traits<T>::to_f32(v[s]); }
 };
 
-// What a lane is: its channel, and its number among the L that share it.  A workgroup has kScanSlice of them, of one group.
+// What a lane is: its channel, and its number among the L that share it.  A workgroup has kScanSlice of them, of one group (whose b and c it keeps in LDS), so groups
+// of fewer channels, or of some more than a multiple, leave lanes without work: groups of 4 seven of eight.
 template <int L>
 struct Place {
     int channel, group, own;
@@ -126,9 +127,9 @@ struct Shared {
 // the state in front of it.
 //
 // L lanes have a channel, with S states each: kScanSlice channels a workgroup, so that a compute unit has two of them, which do not wait at the
-// same time.  Tokens go by in tiles of 4 L.  A tile is loaded with a lane to a channel and four
-// tokens, so that rows are read whole (with the lanes as they share channels, every lane was an access of its own, and those bounded the kernel), what
-// the states need of them goes through LDS, and so do the outputs back, in the steps' places.
+// same time (where a lane has no more than 128 registers: fp32 with 64 states takes 130, kSumsBoth with 64 states 134 to 142, and of those a unit has one).
+// Tokens go by in tiles of 4 L.  A tile is loaded with a lane to a channel and four tokens, so that rows are read whole (with the lanes as they share channels, every
+// lane was an access of its own, and those bounded the kernel), what the states need of them goes through LDS, and so do the outputs back, in the steps' places.
 template <class T, int L, int S, int PASS>
 __global__ void __launch_bounds__(kScanSlice * L) scan_kernel(ScanCall call, int tiles) {
     constexpr int N = L * S;

@@ -20,7 +20,7 @@ constexpr size_t kAlign = 256;
 constexpr int64_t kMost = (int64_t)1 << 46;             // elements that a buffer may span
 constexpr int64_t kMostTokens = 0x7fffffffLL - 4096;    // (token numbers, and those of some tokens behind the last, are ints)
 constexpr int kMostChannels = 1 << 20;
-constexpr int64_t kMostGroups = (int64_t)1 << 23;       // workgroups of a launch: fewer than 2^32 threads, 256 to a group
+constexpr int64_t kMostGroups = (int64_t)1 << 23;       // workgroups of a launch: fewer than 2^32 threads, at most 512 to a group
 constexpr int64_t kUnits = 256;                         // compute units of an MI355X
 constexpr int64_t kCutTokens = 96;                      // what a scan's two more launches take, in tokens of one slot
 
@@ -38,10 +38,10 @@ msla_status check_sequences(int sequences, int64_t tokens, const int32_t* offset
     return tokens > kMostTokens ? MSLA_ERR_UNSUPPORTED : MSLA_OK;
 }
 
-// rows of `width` elements; where they are written they lie apart
-// (further apart than a lane's 32-bit offset reaches over a scan's tile of 64 tokens)
+// further apart than a lane's 32-bit offset reaches over a scan's tile of 64 tokens
 bool wide(const msla_rows& r, int64_t tokens, msla_dtype dt) { return tokens > 1 && r.token_stride * (int64_t)elem_size(dt) >= (int64_t)1 << 24; }
 
+// rows of `width` elements; where they are written they lie apart
 bool fits(const msla_rows& r, int64_t tokens, int64_t width, msla_dtype dt, bool written) {
     if (tokens == 0) return true;
     if (r.data == nullptr || !aligned(r.data, elem_size(dt)) || r.token_stride < 0 || r.token_stride > kMost / tokens) return false;
@@ -67,7 +67,8 @@ struct ScanPlan {
     size_t states_at, d_states_at, steps_at, marks_at, mark_steps_at, parts_at, shared_at, bytes;
 };
 
-// How long slots are.  Two workgroups fill a compute unit.  A sequence that is cut does 1.65 times its work, in the gradient 1.2 times, and two (one) more
+// How long slots are.  Two workgroups fill a compute unit (one of fp32 with 64 states and one of the gradient's pass back, whose registers leave no more: the
+// same plan serves them, a unit's two in turn).  A sequence that is cut does 1.65 times its work, in the gradient 1.2 times, and two (one) more
 // launches.  Equal sequences are cut into as many slots as leave every unit two workgroups at most, if that is worth it; packed ones, whose lengths nobody
 // knows here, into runs of a share of what a unit has to do (those that are no longer run whole).  us with a whole share, half of one, a quarter: 24 sequences of
 // 5003 tokens, 2048 channels of 64 states 211 / 245 / 267, 16 of 8192 tokens, 4096 channels 225 / 281 / 275; but of fewer sequences than fill the units, 8 of 4096,

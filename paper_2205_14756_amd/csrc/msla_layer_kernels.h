@@ -29,7 +29,7 @@ struct ScanCall {
     float *parts_at, *shared_at;
 };
 
-constexpr int kScanSlice = 32;      // channels of a workgroup
+constexpr int kScanSlice = 32;      // channels of a workgroup, of one group
 inline int scan_tiles(int channels, int groups) { return groups * ((channels / groups + kScanSlice - 1) / kScanSlice); }
 inline int scan_lanes(int states) { return states == 8 ? 8 : 16; }     // that share a channel; tokens from mark to mark of the gradient, a quarter of a tile's
 

@@ -842,7 +842,8 @@ def msla_layer_norm_backward(r, weight, d_y, d_sum=None, eps=1e-5, d_r=None, d_w
 
 
 def msla_quantize_rows_integer(x, out8=None, scale=None, stream=None):
-    """(x8, scale): rows of x in 8-bit integers, x ~ x8 * scale[..., None], scale = max |x| / 127."""
+    """(x8, scale): rows of x in 8-bit integers, x ~ x8 * scale[..., None].  scale is the fp32 product of max |x| and fp32's 1 / 127 (which is not always the
+    quotient's rounding), x8 is x / scale to the nearest whole number, ties to even; a row whose scale is 0 or not finite has zeros."""
     rows, channels = _norm_arguments(x, None, None, None)
     if out8 is None:
         out8 = _new(x, stream, None, torch.int8)
